@@ -685,6 +685,167 @@ int ft_plain_copy(void *dst, const void *src, uint64_t bytes, uint32_t workgroup
 int ft_plain_read(const void *src, uint64_t bytes, uint32_t workgroups, void *hip_stream);
 int ft_plain_fill(void *dst, uint64_t bytes, uint32_t word, uint32_t workgroups, void *hip_stream);
 
+/* ------------------------------------------- operators on memory of the pool */
+
+/*
+ * What functions that serve language models keep in the pool is read and written there: a key/value
+ * cache in pages that requests take as they grow, and low-rank adapters that come and go with their
+ * tenants. Each call below queues its kernels on hip_stream, of the pool's device, and returns; nothing is
+ * allocated, nothing waited for, so the calls may be captured into a graph. Tensors are device memory of the
+ * caller's, which has to stay until the stream has passed the work; so have the pool's allocations
+ * (no FT_EBUSY protects them). Strides count elements; the innermost dimension of every tensor is
+ * contiguous; no alignment beyond an element's is needed. What a call finds wrong with its arguments is
+ * FT_EINVAL, a cache or an adapter that is not inside one live allocation FT_ERANGE, and then nothing is
+ * launched. Lengths, tables, masks and the like lie in device memory, where no call can look at them:
+ * whatever they hold, no kernel leaves the tensors it was given.
+ */
+
+/* element types of tensors */
+enum { FT_BF16 = 0, FT_FP16 = 1 };
+
+/* Keys and values of `pages` pages of page_tokens tokens: element (page, token, head, d) of either lies at
+ * page * page_stride + token * token_stride + head * head_stride + d behind the pool offset k or v. A token's
+ * slot is page * page_tokens + token. */
+typedef struct ft_kv_cache {
+  ft_off_t k, v;       /* multiples of 2 */
+  uint32_t type;       /* FT_BF16 or FT_FP16 */
+  uint32_t pages;      /* pages * page_tokens < 2^31 */
+  uint32_t page_tokens;
+  uint32_t heads;      /* key heads */
+  uint32_t dim;        /* of a head: a multiple of 8, at most 256 */
+  uint32_t _pad;       /* ignored */
+  uint64_t page_stride, token_stride, head_stride; /* >= dim where there is more than one; < 2^40 */
+} ft_kv_cache;         /* 64 bytes */
+
+/* Who has which pages. Entry b of row r of the table is the page of tokens [b * page_tokens, (b + 1) * page_tokens) of
+ * request r; entries behind a request's last page mean nothing. Free pages are a stack: free_pages[0 .. state[0]). */
+typedef struct ft_kv_tables {
+  const int32_t *lens;  /* device, requests: cached tokens of each */
+  int32_t *table;       /* device, requests x blocks */
+  int32_t *free_pages;  /* device, pages entries */
+  const int32_t *state; /* device, 4: pages on the stack; the other three are not read */
+  uint32_t requests, blocks, pages, page_tokens;
+} ft_kv_tables;         /* 48 bytes */
+
+/*
+ * Pages and slots of the tokens that a step adds. Rows [starts[r], starts[r + 1]) of the step's `tokens` rows (starts:
+ * device, requests + 1 entries that do not descend) belong to request r; keep (device, `tokens` bytes, or NULL:
+ * all) says which of them are cached, in their order behind the cached ones. A request takes the pages it
+ * lacks from the top of the stack, requests in ascending order, pages in a request too; if they are not
+ * all there, or its table row is too short, it takes none and keeps its length: it is refused. (Once one
+ * has been refused for want of pages, so are all behind it that lack any.)
+ *   slots      device, tokens entries: the slot of every row, -1 for rows not kept, of refused requests, or of no request
+ *   lens_out   device, requests entries: the lengths after the step
+ *   state_out  device, 4 entries: pages left on the stack, pages that were missing, refused requests, 0
+ * lens and state stay as they are, so a step that was refused can be tried again; lens_out and state_out may not be
+ * the same memory. Sums are exact whole numbers.
+ */
+int ft_kv_grow(ft_pool *p, const ft_kv_tables *t, const int32_t *starts, const uint8_t *keep, uint32_t tokens, int64_t *slots,
+               int32_t *lens_out, int32_t *state_out, void *hip_stream);
+
+/*
+ * The pages of all requests r with done[r] != 0 (device, requests bytes) go back on the stack, requests in ascending order,
+ * a request's pages too; their lengths become 0. state_out: pages on the stack, 0, 0, 0. lens_out and state_out as above.
+ * The table keeps its entries. Pages that do not fit the stack's `pages` entries are lost.
+ */
+int ft_kv_release(ft_pool *p, const ft_kv_tables *t, const uint8_t *done, int32_t *lens_out, int32_t *state_out, void *hip_stream);
+
+/*
+ * Keys and values of `tokens` rows to their slots: cache[slots[t]] = k[t], v[t] for every slot inside the cache; other
+ * rows (slot -1) are skipped and not read. k, v: device, tokens x heads x dim of the cache's type. Two rows
+ * with one slot leave either's elements.
+ */
+int ft_kv_append(ft_pool *p, const ft_kv_cache *c, const void *k, const void *v, uint64_t k_token_stride, uint64_t k_head_stride,
+                 uint64_t v_token_stride, uint64_t v_head_stride, const int64_t *slots, uint32_t tokens, void *hip_stream);
+
+/* Arguments of ft_tree_attention: device pointers but for the numbers. */
+typedef struct ft_tree_call {
+  const void *q;         /* tokens x heads x dim */
+  const void *k, *v;     /* tokens x the cache's heads x dim: the drafted tokens' own, which are not in the cache */
+  void *out;             /* tokens x heads x dim */
+  float *lse;            /* tokens x heads, or NULL */
+  const int32_t *starts; /* requests + 1 entries: rows [starts[r], starts[r + 1]) are request r's drafted tokens */
+  const int32_t *lens;   /* requests: cached tokens */
+  const int32_t *table;  /* requests x blocks: their pages */
+  const uint64_t *mask;  /* tokens x mask_words: bit j of a row: the token sees its request's j-th drafted one. NULL: it sees those up to itself */
+  uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  uint64_t v_token_stride, v_head_stride, out_token_stride, out_head_stride;
+  uint32_t requests, tokens;
+  uint32_t drafts;       /* the most drafted tokens of one request; those beyond are not answered */
+  uint32_t heads;        /* query heads, a multiple of the cache's: head h reads key head h / (heads / cache heads) */
+  uint32_t blocks;
+  uint32_t mask_words;   /* 64 * mask_words >= drafts where there is a mask */
+  float scale;           /* of the products, finite */
+  uint32_t _pad;         /* ignored */
+  void *workspace;       /* ft_tree_workspace bytes, 16-byte aligned, of this call alone while it runs; contents do not matter */
+  uint64_t workspace_bytes;
+} ft_tree_call;          /* 184 bytes */
+
+/*
+ * Attention of the drafted tokens of all requests over their cached tokens, all of which each of them sees, and over each
+ * other as the mask says:
+ *   out[t, h] = sum over s of softmax over s (scale * q[t, h] . key[s]) value[s],   lse[t, h] = log of the sum of exp
+ * A row that sees nothing is 0, its lse -infinity. What a row does not see does not reach it, NaN and
+ * infinities included; neither does what lies in a page behind a request's last token. One token a request is
+ * plain decoding; without a mask any number of rows may be a prompt's next piece.
+ * Types: products are exact, sums, softmax and lse 32 bits, weights are rounded to the tensors' type for
+ * their product with the values, and the result once.
+ */
+int ft_tree_attention(ft_pool *p, const ft_kv_cache *c, const ft_tree_call *call, void *hip_stream);
+/* Bytes of workspace that ft_tree_attention asks for (host only; of the call its numbers are read, no pointers). */
+int ft_tree_workspace(ft_pool *p, const ft_kv_cache *c, const ft_tree_call *call, uint64_t *bytes_out);
+
+/* A low-rank adapter in the pool: A is rank x width_in, B width_out x rank, both without gaps. */
+typedef struct ft_adapter {
+  ft_off_t a, b;     /* multiples of 2 */
+  uint32_t rank;     /* 1 .. 256 */
+  float scale;       /* finite */
+} ft_adapter;        /* 24 bytes */
+
+/* The same as the kernels read it: device addresses. */
+typedef struct ft_adapter_record {
+  uint64_t a, b;
+  uint32_t rank;
+  float scale;
+} ft_adapter_record; /* 24 bytes */
+
+/*
+ * Host only: resolves `count` adapters to the records that the caller hands to the device (host arrays). They hold as
+ * long as the adapters' allocations live. FT_ERANGE if a factor is not inside one live allocation.
+ */
+int ft_adapters_resolve(ft_pool *p, const ft_adapter *adapters, uint32_t count, uint32_t width_in, uint32_t width_out,
+                        ft_adapter_record *records_out);
+
+/*
+ * Which rows belong to which adapter: ids (device, rows entries) is a row's adapter, anything outside [0, count) none.
+ * One grouping serves every projection of a step. groups: device, ft_adapters_group_bytes bytes, 16-byte aligned.
+ */
+int ft_adapters_group_bytes(uint32_t rows, uint32_t count, uint64_t *bytes_out);
+int ft_adapters_group(ft_pool *p, const int32_t *ids, uint32_t rows, uint32_t count, void *groups, uint64_t groups_bytes, void *hip_stream);
+
+/* Arguments of ft_adapters_apply: device pointers but for the numbers. */
+typedef struct ft_adapters_call {
+  const ft_adapter_record *records; /* count records of one pair of widths */
+  const void *groups;               /* of ft_adapters_group for the same rows and count */
+  const void *x;                    /* rows x width_in */
+  const void *base;                 /* rows x width_out: the shared projection's result, or NULL: 0 */
+  void *out;                        /* rows x width_out; may be base itself */
+  uint64_t x_stride, base_stride, out_stride; /* of a row: >= its width, < 2^40 */
+  uint32_t rows, count, type;
+  uint32_t width_in, width_out;
+  uint32_t max_rank;                /* of the records; of a larger one's factors the rows behind it are left out */
+  void *workspace;                  /* ft_adapters_workspace bytes, 16-byte aligned, as for ft_tree_attention */
+  uint64_t workspace_bytes;
+} ft_adapters_call;                 /* 104 bytes */
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share:
+ *   out[t] = base[t] + scale * B (A x[t])  of the adapter of row t;  out[t] = base[t] where it has none.
+ * Products are exact, sums 32 bits; A x[t] is kept in twice 16 bits, and the result rounded once.
+ */
+int ft_adapters_apply(ft_pool *p, const ft_adapters_call *call, void *hip_stream);
+int ft_adapters_workspace(ft_pool *p, const ft_adapters_call *call, uint64_t *bytes_out);
+
 const char *ft_strerror(int rc);
 /* Text of the last failing HIP call on this pool ("" if none). */
 const char *ft_last_hip_error(ft_pool *p);

@@ -20,7 +20,9 @@ EXPORTS = ["ft_pool_create", "ft_pool_grow", "ft_pool_shrink", "ft_pool_usage", 
            "ft_pool_ptr", "ft_store_create", "ft_store_put", "ft_store_get", "ft_store_done", "ft_store_advance", "ft_store_sync", "ft_store_stats", "ft_store_destroy", "ft_host_window_add", "ft_pageable_window_add", "ft_set_stage_threads", "ft_reserve_rings", "ft_submit_transfers", "ft_submit_static", "ft_submit_merge", "ft_job_reweight", "ft_set_batch",
            "ft_job_arrival", "ft_job_batches", "ft_slo_weights", "ft_wait", "ft_job_done", "ft_timing_epoch", "ft_job_release",
            "ft_job_stats", "ft_job_schedule", "ft_job_log", "ft_job_log_jobs", "ft_job_progress", "ft_job_log_workgroups", "ft_job_log_units", "ft_set_tuning", "ft_plan_schedule", "ft_plan_tickets",
-           "ft_plain_copy", "ft_plain_read", "ft_plain_fill", "ft_strerror", "ft_last_hip_error"]
+           "ft_plain_copy", "ft_plain_read", "ft_plain_fill", "ft_strerror", "ft_last_hip_error",
+           "ft_kv_grow", "ft_kv_release", "ft_kv_append", "ft_tree_attention", "ft_tree_workspace",
+           "ft_adapters_resolve", "ft_adapters_group_bytes", "ft_adapters_group", "ft_adapters_apply", "ft_adapters_workspace"]
 
 
 class FtError(Exception):
@@ -42,6 +44,37 @@ class StoreStats(C.Structure):
 
 class JobStats(C.Structure):
     _fields_ = [("cls", ClassStats * FT_NCLASS), ("host_submit_us", C.c_double)]
+
+
+class KvCacheRecord(C.Structure):
+    _fields_ = [("k", C.c_uint64), ("v", C.c_uint64), ("type", C.c_uint32), ("pages", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("heads", C.c_uint32), ("dim", C.c_uint32), ("_pad", C.c_uint32),
+                ("page_stride", C.c_uint64), ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class KvTables(C.Structure):
+    _fields_ = [("lens", C.c_void_p), ("table", C.c_void_p), ("free_pages", C.c_void_p), ("state", C.c_void_p),
+                ("requests", C.c_uint32), ("blocks", C.c_uint32), ("pages", C.c_uint32), ("page_tokens", C.c_uint32)]
+
+
+class TreeCall(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "starts", "lens", "table", "mask")] + \
+               [(n, C.c_uint64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                          "v_token_stride", "v_head_stride", "out_token_stride", "out_head_stride")] + \
+               [(n, C.c_uint32) for n in ("requests", "tokens", "drafts", "heads", "blocks", "mask_words")] + \
+               [("scale", C.c_float), ("_pad", C.c_uint32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class AdapterRecord(C.Structure):
+    """ft_adapter (a and b pool offsets) and ft_adapter_record (device addresses): the same layout."""
+    _fields_ = [("a", C.c_uint64), ("b", C.c_uint64), ("rank", C.c_uint32), ("scale", C.c_float)]
+
+
+class AdaptersCall(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("records", "groups", "x", "base", "out")] + \
+               [(n, C.c_uint64) for n in ("x_stride", "base_stride", "out_stride")] + \
+               [(n, C.c_uint32) for n in ("rows", "count", "type", "width_in", "width_out", "max_rank")] + \
+               [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
 def _load():
@@ -113,6 +146,16 @@ def _load():
         "ft_plain_copy": (i32, [vp, vp, u64, u32, vp]),
         "ft_plain_read": (i32, [vp, u64, u32, vp]),
         "ft_plain_fill": (i32, [vp, u64, u32, u32, vp]),
+        "ft_kv_grow": (i32, [vp, vp, vp, vp, u32, vp, vp, vp, vp]),
+        "ft_kv_release": (i32, [vp, vp, vp, vp, vp, vp]),
+        "ft_kv_append": (i32, [vp, vp, vp, vp, u64, u64, u64, u64, vp, u32, vp]),
+        "ft_tree_attention": (i32, [vp, vp, vp, vp]),
+        "ft_tree_workspace": (i32, [vp, vp, vp, P(u64)]),
+        "ft_adapters_resolve": (i32, [vp, vp, u32, u32, u32, vp]),
+        "ft_adapters_group_bytes": (i32, [u32, u32, P(u64)]),
+        "ft_adapters_group": (i32, [vp, vp, u32, u32, vp, u64, vp]),
+        "ft_adapters_apply": (i32, [vp, vp, vp]),
+        "ft_adapters_workspace": (i32, [vp, vp, P(u64)]),
         "ft_strerror": (C.c_char_p, [i32]),
         "ft_last_hip_error": (C.c_char_p, [vp]),
     }
@@ -542,3 +585,55 @@ def plain_read(src_ptr, nbytes, workgroups=0, stream=0):
 
 def plain_fill(dst_ptr, nbytes, word, workgroups=0, stream=0):
     _check(_lib.ft_plain_fill(dst_ptr, nbytes, word, workgroups, stream))
+
+
+# ---- operators on memory of the pool: device pointers and the records above ------------------------
+
+def kv_grow(pool, tables, starts, keep, tokens, slots, lens_out, state_out, stream=0):
+    _check(_lib.ft_kv_grow(pool, C.byref(tables), starts, keep, tokens, slots, lens_out, state_out, stream), pool)
+
+
+def kv_release(pool, tables, done, lens_out, state_out, stream=0):
+    _check(_lib.ft_kv_release(pool, C.byref(tables), done, lens_out, state_out, stream), pool)
+
+
+def kv_append(pool, cache, k, v, k_strides, v_strides, slots, tokens, stream=0):
+    _check(_lib.ft_kv_append(pool, C.byref(cache), k, v, *k_strides, *v_strides, slots, tokens, stream), pool)
+
+
+def tree_workspace(pool, cache, call):
+    n = C.c_uint64()
+    _check(_lib.ft_tree_workspace(pool, C.byref(cache), C.byref(call), C.byref(n)), pool)
+    return n.value
+
+
+def tree_attention(pool, cache, call, stream=0):
+    _check(_lib.ft_tree_attention(pool, C.byref(cache), C.byref(call), stream), pool)
+
+
+def adapters_resolve(pool, adapters, width_in, width_out):
+    """[(a offset, b offset, rank, scale)] -> the records as bytes, for the device."""
+    n = len(adapters)
+    given, out = (AdapterRecord * max(n, 1))(*adapters), (AdapterRecord * max(n, 1))()
+    _check(_lib.ft_adapters_resolve(pool, given, n, width_in, width_out, out), pool)
+    return bytes(out)[:n * C.sizeof(AdapterRecord)]
+
+
+def adapters_group_bytes(rows, count):
+    n = C.c_uint64()
+    _check(_lib.ft_adapters_group_bytes(rows, count, C.byref(n)))
+    return n.value
+
+
+def adapters_group(pool, ids, rows, count, groups, groups_bytes, stream=0):
+    _check(_lib.ft_adapters_group(pool, ids, rows, count, groups, groups_bytes, stream), pool)
+
+
+def adapters_workspace(pool, call):
+    n = C.c_uint64()
+    _check(_lib.ft_adapters_workspace(pool, C.byref(call), C.byref(n)), pool)
+    return n.value
+
+
+def adapters_apply(pool, call, stream=0):
+    _check(_lib.ft_adapters_apply(pool, C.byref(call), stream), pool)

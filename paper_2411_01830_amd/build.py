@@ -7,7 +7,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfaastube.so")
-SOURCES = ["ft_pool.cpp", "ft_plan.cpp", "ft_api.cpp", "ft_open.cpp", "ft_policy.cpp", "ft_store.cpp", "ft_paths.cpp", "ft_kernels.hip", "ft_pieces.hip", "ft_static.hip"]
+SOURCES = ["ft_pool.cpp", "ft_plan.cpp", "ft_api.cpp", "ft_open.cpp", "ft_policy.cpp", "ft_store.cpp", "ft_paths.cpp", "ft_kernels.hip", "ft_pieces.hip", "ft_static.hip",
+           "ft_operators.cpp", "ft_kv.hip", "ft_tree.hip", "ft_adapters.hip"]
 # packed fp32 code generation is switched off for every translation unit
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-unused-result",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -84,7 +85,7 @@ def build(verbose=False):
     for src in SOURCES:
         obj = os.path.join(out_dir, os.path.splitext(src)[0] + ".o")
         cmd = [hipcc(), "-x", "hip", *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
-        if src in ("ft_kernels.hip", "ft_pieces.hip"):
+        if src in ("ft_kernels.hip", "ft_pieces.hip", "ft_kv.hip", "ft_tree.hip", "ft_adapters.hip"):
             cmd.insert(-4, "-Rpass-analysis=kernel-resource-usage")
         if verbose:
             print(" ".join(cmd), flush=True)
@@ -96,7 +97,7 @@ def build(verbose=False):
             per_class = check_registers(res.stderr)
             if verbose:
                 print("registers per lane (host->pool, pool->host, pool->pool, pool->pool by wavefronts):", per_class, flush=True)
-        elif src == "ft_pieces.hip":
+        elif src in ("ft_pieces.hip", "ft_kv.hip", "ft_tree.hip", "ft_adapters.hip"):
             kernel_registers(res.stderr)
         else:
             sys.stderr.write(res.stderr)

@@ -1,0 +1,614 @@
+"""The operators on pool memory against plain 64-bit implementations.
+
+Bounds come from the types alone. u is the unit roundoff of the tensors' type (bfloat16 2^-8, float16 2^-11): a result is
+rounded once, and attention's weights once more for their product with the values; sums and softmax have 24 bits."""
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2411_01830_amd import binding as ft
+
+pytestmark = pytest.mark.gpu
+
+SLAB = 4096
+BF16, FP16 = torch.bfloat16, torch.float16
+U = {BF16: 2.0 ** -8, FP16: 2.0 ** -11}
+TINY = {BF16: 0.0, FP16: 2.0 ** -25}   # half the smallest float16
+
+
+def ops():
+    from paper_2411_01830_amd import operators
+    return operators
+
+
+class Memory:
+    """A pool over one device tensor, filled with the bytes of NaN."""
+
+    def __init__(self, nbytes, fill=0xFF):
+        n = (nbytes + SLAB - 1) // SLAB * SLAB + SLAB
+        self.mem = torch.empty(n, dtype=torch.uint8, device="cuda")
+        if fill is not None:
+            self.mem.fill_(fill)
+        self.pool = ft.pool_create(self.mem.data_ptr(), n, SLAB, 0)
+
+    def alloc(self, nbytes):
+        return ft.slab_alloc(self.pool, nbytes)
+
+    def view(self, off, dtype, n):
+        return self.mem[off:off + 2 * n].view(dtype)
+
+    def __del__(self):
+        torch.cuda.synchronize()
+        ft.pool_destroy(self.pool)
+
+
+def gpu(values, dtype=torch.int32):
+    return torch.tensor(values, dtype=dtype, device="cuda")
+
+
+# ---- pages and slots ------------------------------------------------------------------------------
+
+def grow_oracle(lens, starts, tokens, table, free, top, page, keep):
+    """The definition, request by request; table is changed in place."""
+    slots, after, refused, asked, taken = [-1] * tokens, list(lens), 0, 0, 0
+    for r, n in enumerate(lens):
+        mine = [t for t in range(starts[r], starts[r + 1]) if keep is None or keep[t]]
+        have, want = -(-n // page), -(-(n + len(mine)) // page)
+        if want > len(table[r]) or n < 0:
+            refused += 1
+            continue
+        first, asked = asked, asked + want - have
+        if want > have and asked > top:
+            refused += 1
+            continue
+        if want > have:
+            taken = asked
+        for j in range(have, want):
+            table[r][j] = free[top - 1 - first - (j - have)]
+        for j, t in enumerate(mine):
+            slots[t] = table[r][(n + j) // page] * page + (n + j) % page
+        after[r] = n + len(mine)
+    return slots, after, [top - taken, max(asked - top, 0), refused, 0]
+
+
+GROW = [
+    # requests, new tokens up to, cached up to, page, share kept (None: no flags), share of the pages there, blocks missing
+    (1, 1, 0, 16, None, 1.0, 0), (1, 1, 40, 16, None, 1.0, 0), (1, 5000, 3, 16, None, 1.0, 0), (5, 0, 70, 16, None, 1.0, 0),
+    (64, 16, 300, 16, 0.3, 1.0, 0), (64, 16, 300, 16, 0.0, 1.0, 0), (37, 200, 100, 1, 0.6, 1.0, 0), (200, 9, 100, 7, None, 0.4, 0),
+    (200, 30, 100, 24, 0.5, 0.0, 0), (1023, 5, 50, 8, 0.5, 1.0, 0), (1024, 5, 50, 8, None, 0.7, 0), (2500, 40, 90, 16, 0.4, 0.9, 0),
+    (1025, 130, 10, 64, None, 1.0, 0), (300, 70, 90, 16, None, 1.0, 2), (90, 1500, 3000, 32, None, 1.0, 0), (3, 4000, 10, 128, 0.5, 1.0, 0),
+]
+
+
+@pytest.mark.parametrize("case", GROW, ids=lambda c: "-".join(map(str, c)))
+def test_pages_and_slots_of_a_step(case):
+    requests, new, cached, page, kept, there, lacking = case
+    rng = random.Random(str(case))
+    lens = [rng.randint(0, cached) for _ in range(requests)]
+    news = [rng.choice([0, new, rng.randint(0, new)]) for _ in range(requests)]
+    starts = [3]                                     # rows before and behind the requests' belong to nobody
+    for n in news:
+        starts.append(starts[-1] + n)
+    tokens = starts[-1] + 5
+    keep = None if kept is None else [int(rng.random() < kept) for _ in range(tokens)]
+    blocks = max(1, -(-max(a + b for a, b in zip(lens, news)) // page) - lacking)
+    have = [min(blocks, -(-n // page)) for n in lens]
+    need = sum(-(-(a + b) // page) for a, b in zip(lens, news))
+    order = list(range(need + 3))
+    rng.shuffle(order)
+    table, at = [], 0
+    for h in have:
+        table.append(order[at:at + h] + [-7] * (blocks - h))
+        at += h
+    top = int((len(order) - at) * there)
+    free = order[at:at + top] + [-9] * (len(order) - top)
+    given = gpu(table), gpu(free), gpu([top, 11, 12, 13])
+    m = Memory(SLAB)
+    args = (m.pool, gpu(lens), gpu(starts), tokens, given[0], given[1], given[2], page)
+    flags = None if keep is None else gpu(keep, torch.uint8 if rng.random() < 0.5 else torch.bool)
+    slots, after, state = ops().kv_grow(*args, keep=flags)
+    want = grow_oracle(lens, starts, tokens, table, free, top, page, keep)
+    assert state.tolist() == want[2]
+    assert after.tolist() == want[1]
+    assert slots.tolist() == want[0]
+    assert given[0].tolist() == table
+    assert given[1].tolist() == free and given[2].tolist() == [top, 11, 12, 13]
+    again = ops().kv_grow(*args, keep=flags)          # nothing that it read has changed
+    assert all(torch.equal(a, b) for a, b in zip(again, (slots, after, state)))
+
+
+def test_lengths_that_no_request_can_have_are_refused():
+    m = Memory(SLAB)
+    lens = gpu([-5, 2 ** 31 - 1, 17, 2 ** 31 - 40])
+    table = torch.full((4, 3), 1, dtype=torch.int32, device="cuda")
+    slots, after, state = ops().kv_grow(m.pool, lens, gpu([0, 2, 4, 6, 8]), 8, table, gpu([5, 6, 7]), gpu([3, 0, 0, 0]), 16)
+    assert after.tolist() == [-5, 2 ** 31 - 1, 19, 2 ** 31 - 40]
+    assert slots.tolist() == [-1] * 4 + [17, 18] + [-1] * 2 and state.tolist() == [3, 0, 3, 0]
+
+
+def test_starts_that_descend_or_leave_the_rows_write_inside_the_slots_only():
+    m = Memory(SLAB)
+    slots, after, state = ops().kv_grow(m.pool, gpu([0, 0, 0]), gpu([-4, 9, 2, 50]), 6, torch.zeros(3, 4, dtype=torch.int32, device="cuda"),
+                                        gpu([3, 4, 5]), gpu([900, 0, 0, 0]), 16)
+    assert after.tolist() == [6, 0, 4] and state.tolist() == [1, 0, 0, 0] and slots.shape[0] == 6
+
+
+@pytest.mark.parametrize("requests,cached,page,share", [(1, 0, 16, 1.0), (1, 5000, 1, 1.0), (256, 900, 16, 0.25), (1500, 70, 7, 0.5), (40, 9000, 24, 1.0)])
+def test_pages_given_back(requests, cached, page, share):
+    rng = random.Random(requests)
+    lens = [rng.randint(0, cached) for _ in range(requests)]
+    done = [int(rng.random() < share) for _ in lens]
+    blocks = max(1, -(-max(lens) // page)) + 1
+    order = list(range(sum(-(-n // page) for n in lens) + 4))
+    rng.shuffle(order)
+    free, table = order[:4] + [-9] * (len(order) - 4), []
+    at = 4
+    for n in lens:
+        h = -(-n // page)
+        table.append(order[at:at + h] + [-1] * (blocks - h))
+        at += h
+    m = Memory(SLAB)
+    stack = gpu(free)
+    after, state = ops().kv_release(m.pool, gpu(done, torch.uint8), gpu(lens), gpu(table), stack, gpu([4, 1, 1, 1]), page)
+    top = 4
+    for r, n in enumerate(lens):
+        if done[r]:
+            h = -(-n // page)
+            free[top:top + h] = table[r][:h]
+            top += h
+            lens[r] = 0
+    assert after.tolist() == lens and state.tolist() == [top, 0, 0, 0] and stack.tolist() == free
+
+
+def test_a_stack_that_is_too_short_keeps_its_size():
+    m = Memory(SLAB)
+    stack = gpu([1, 2, -9])
+    after, state = ops().kv_release(m.pool, gpu([1, 1], torch.uint8), gpu([40, 20]), gpu([[5, 6, 7], [8, 9, 4]]), stack, gpu([2, 0, 0, 0]), 16)
+    assert after.tolist() == [0, 0] and state.tolist() == [3, 0, 0, 0] and stack.tolist() == [1, 2, 5]
+
+
+# ---- a cache --------------------------------------------------------------------------------------
+
+def make_cache(pages, page, heads, dim, dtype, order="token", gap=0):
+    """A cache of NaN; keys and values as [page, token, head, dim] views."""
+    if order == "token":
+        shape, turn = (pages, page, heads, dim + gap), False
+    else:
+        shape, turn = (pages, heads, page, dim + gap), True
+    n = math.prod(shape)
+    m = Memory(4 * n + 4 * SLAB)
+    at = [m.alloc(2 * n), m.alloc(2 * n)]
+    views = [m.view(a, dtype, n).view(shape)[..., :dim] for a in at]
+    views = [v.transpose(1, 2) if turn else v for v in views]
+    return m, ops().KvCache(m.pool, at[0], at[1], pages, page, heads, dim, dtype, views[0].stride()[:3]), views[0], views[1]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("tokens,page,heads,dim,order,gap", [(1, 16, 8, 128, "token", 0), (1000, 16, 8, 128, "token", 0), (77, 1, 3, 8, "token", 1),
+                                                             (130, 7, 5, 80, "head", 0), (4099, 32, 8, 64, "head", 3), (50, 24, 1, 256, "token", 0)])
+def test_appended_tokens(tokens, page, heads, dim, order, gap, dtype):
+    m, cache, kc, vc = make_cache(-(-tokens // page) + 4, page, heads, dim, dtype, order, gap)
+    before = m.mem.clone()
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    wide = torch.randn(tokens, heads, 2, dim + 1, device="cuda", generator=g).to(dtype)
+    k, v = wide[:, :, 0, :dim], wide[:, :, 1, 1:]
+    slots = torch.randperm((kc.shape[0]) * page, device="cuda", generator=g)[:tokens]
+    drop = torch.rand(tokens, device="cuda", generator=g) < 0.3
+    slots = torch.where(drop, torch.where(slots % 2 == 0, -1, kc.shape[0] * page + slots), slots)   # behind the cache: skipped as well
+    wide[drop] = float("inf")
+    ops().kv_append(cache, k, v, slots)
+    got = m.mem.clone()
+    m.mem.copy_(before)
+    t = torch.nonzero(~drop)[:, 0]
+    kc[slots[t] // page, slots[t] % page] = k[t]
+    vc[slots[t] // page, slots[t] % page] = v[t]
+    assert torch.equal(got, m.mem)
+
+
+# ---- attention ------------------------------------------------------------------------------------
+
+def tree_bits(n, rng):
+    rows = []
+    for i in range(n):
+        rows.append((rows[rng.randrange(max(0, i - 8), i)] if i else 0) | 1 << i)
+    return rows
+
+
+class Tree:
+    """A call's tensors, with NaN and infinities wherever no row looks, and its answer in 64 bits with a bound for every element."""
+
+    def __init__(self, lens, news, heads, group, dim, page, dtype, order="token", mask="tree", seed=0, lead=0, gap=0, views=False, loud=1.0):
+        rng = random.Random(seed)
+        g = torch.Generator().manual_seed(seed)
+        randn = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+        self.lens, self.news, self.heads, self.group, self.dtype, self.dim = lens, news, heads, group, dtype, dim
+        blocks = max(1, -(-max(lens) // page)) + 1
+        need = sum(-(-n // page) for n in lens)
+        self.m, self.cache, kc, vc = make_cache(need + 2, page, heads, dim, dtype, order, gap)
+        ids = list(range(need + 2))
+        rng.shuffle(ids)
+        table, at = [], 0
+        self.keys, self.values = [], []
+        for n in lens:
+            h = -(-n // page)
+            table.append(ids[at:at + h] + [rng.choice([-1, 2 ** 31 - 1, 0])] * (blocks - h))
+            k, v = randn(n, heads, dim).to(dtype), randn(n, heads, dim).to(dtype)
+            t = torch.arange(n)
+            where = torch.tensor(table[-1], dtype=torch.int64)[t // page].cuda(), (t % page).cuda()
+            kc[where], vc[where] = k.cuda(), v.cuda()
+            self.keys.append(k)
+            self.values.append(v)
+            at += h
+        starts = [lead]
+        for n in news:
+            starts.append(starts[-1] + n)
+        total = starts[-1] + lead
+        words = max(1, -(-max(news) // 64))
+        bits = []
+        for n in news:
+            if mask == "tree":
+                bits += tree_bits(n, rng)
+            elif mask == "any":       # anything at all, rows that see nothing among them
+                bits += [rng.getrandbits(n) if rng.random() < 0.8 else 0 for _ in range(n)] if n else []
+            else:
+                bits += [(2 << i) - 1 for i in range(n)]
+        self.bits = [0] * lead + bits + [0] * lead
+        self.starts, self.total = starts, total
+        q, k, v = randn(total, heads * group, dim).mul(loud).to(dtype), randn(total, heads, dim).to(dtype), randn(total, heads, dim).to(dtype)
+        self.q, self.k, self.v = q, k, v
+        # a drafted token that nobody sees holds NaN and infinities
+        for r, n in enumerate(news):
+            seen = 0
+            for b in bits[starts[r] - lead:starts[r] - lead + n]:
+                seen |= b
+            for j in range(n):
+                if not seen >> j & 1:
+                    k[starts[r] + j], v[starts[r] + j] = float("nan"), float("inf")
+        if views:      # rows apart, heads apart, tokens last: strides that nothing is aligned to
+            wide = torch.full((total, 3, heads, dim + 3), float("nan"), dtype=dtype)
+            wide[:, 0, :, 1:dim + 1], wide[:, 2, :, 2:dim + 2] = k, v
+            wide = wide.cuda()
+            gk, gv = wide[:, 0, :, 1:dim + 1], wide[:, 2, :, 2:dim + 2]
+            gq = torch.full((heads * group, total, dim + 1), float("nan"), dtype=dtype)
+            gq[:, :, :dim] = q.transpose(0, 1)
+            gq = gq.cuda()[:, :, :dim].transpose(0, 1)
+        else:
+            gq, gk, gv = q.cuda(), k.cuda(), v.cuda()
+        full = (1 << 64) - 1
+        signed = lambda b: b - (1 << 64) if b >> 63 else b  # noqa: E731
+        # bits behind a request's last drafted token mean nothing
+        noise = [rng.getrandbits(64 * words) for _ in range(total)]
+        row_of = [r for r, n in enumerate(news) for _ in range(n)]
+        said = list(self.bits)
+        for t in range(lead, total - lead):
+            n = news[row_of[t - lead]]
+            said[t] |= noise[t] >> n << n & ((1 << 64 * words) - 1)
+        packed = [[signed(b >> 64 * w & full) for w in range(words)] for b in said]
+        self.mask = None if mask is None else gpu(packed, torch.int64)
+        if self.mask is not None and words == 1 and rng.random() < 0.5:
+            self.mask = self.mask[:, 0].contiguous()
+        self.args = (gq, gk, gv, gpu(starts), gpu(lens), gpu(table), max(max(news), 1))
+        self.scale = dim ** -0.5
+
+    def call(self, **more):
+        return ops().tree_attention(self.cache, *self.args, mask=self.mask, scale=self.scale, lse=True, **more)
+
+    def check(self, out, lse):
+        u, tiny = U[self.dtype], TINY[self.dtype]
+        out, lse = out.double().cpu(), lse.double().cpu()
+        for r, (n, m) in enumerate(zip(self.lens, self.news)):
+            if m == 0:
+                continue
+            t0 = self.starts[r]
+            sees = torch.tensor([[self.bits[t0 + i] >> j & 1 for j in range(m)] for i in range(m)], dtype=torch.bool)
+            sees = torch.cat([torch.ones(m, n, dtype=torch.bool), sees], 1)
+            for h in range(self.heads):
+                k = torch.cat([self.keys[r][:, h], self.k[t0:t0 + m, h]]).double()
+                v = torch.cat([self.values[r][:, h], self.v[t0:t0 + m, h]]).double()
+                seen_k, seen_v = torch.where(sees.any(0)[:, None], k, 0), torch.where(sees.any(0)[:, None], v, 0)
+                for g in range(h * self.group, (h + 1) * self.group):
+                    q = self.q[t0:t0 + m, g].double()
+                    s = torch.where(sees, q @ seen_k.t() * self.scale, -math.inf)
+                    top = s.max(1, keepdim=True).values
+                    top = torch.where(top.isinf(), 0.0, top)
+                    p = (s - top).exp()
+                    z = p.sum(1, keepdim=True)
+                    w = p / torch.where(z == 0, 1.0, z)
+                    want, mass = w @ seen_v, w @ seen_v.abs()
+                    # a score is a sum of dim products in 24 bits, scaled and carried to powers of two: its error is a weight's relative one
+                    score = torch.where(sees, q.abs() @ seen_k.abs().t() * self.scale, 0).max(1, keepdim=True).values
+                    delta = (self.dim + 8) * 2.0 ** -24 * score + 2.0 ** -19
+                    keys = sees.sum(1, keepdim=True)
+                    bound = u * want.abs() + (1.01 * u + 2 * delta) * mass + tiny * (1 + keys * seen_v.abs().max(0).values[None]) + keys * 2.0 ** -24 * mass
+                    off = (out[t0:t0 + m, g] - want).abs()
+                    assert (off <= bound).all(), (r, g, float((off - bound).max()), float(off.max()))
+                    wz = (z.log() + top)[:, 0]
+                    got = lse[t0:t0 + m, g]
+                    empty = z[:, 0] == 0
+                    assert torch.equal(got.isinf(), empty), (r, g)
+                    assert (out[t0:t0 + m, g][empty] == 0).all()
+                    off = (got - wz).abs()[~empty]
+                    assert (off <= (delta[:, 0] + 2.0 ** -22 * wz.abs() + 2.0 ** -20 + keys[:, 0] * 2.0 ** -24)[~empty]).all(), (r, g, off.max())
+
+
+TREES = {
+    "one": dict(lens=[2000], news=[1], heads=8, group=4, dim=128, page=16, mask=None),
+    "one, nothing cached": dict(lens=[0], news=[1], heads=2, group=1, dim=64, page=16, mask=None),
+    "one cached": dict(lens=[1], news=[1], heads=1, group=1, dim=128, page=1, mask=None),
+    "tokens": dict(lens=[0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 700, 1500], news=[1] * 16, heads=2, group=4, dim=128, page=16, mask=None),
+    "trees": dict(lens=[5, 300, 64, 1111], news=[16, 9, 12, 16], heads=2, group=4, dim=128, page=16),
+    "trees of 64": dict(lens=[900, 33], news=[64, 64], heads=2, group=8, dim=128, page=64),
+    "two words": dict(lens=[90, 0, 500], news=[65, 3, 128], heads=1, group=5, dim=64, page=16),
+    "many words": dict(lens=[40], news=[300], heads=2, group=1, dim=64, page=16, mask="any"),
+    "prompt": dict(lens=[100, 0, 37], news=[333, 200, 1], heads=2, group=3, dim=128, page=16, mask=None),
+    "rows that see nothing": dict(lens=[0, 0, 40, 0], news=[7, 1, 20, 33], heads=2, group=2, dim=64, page=8, mask="any"),
+    "empty requests": dict(lens=[50, 60, 0, 70, 80], news=[0, 4, 0, 0, 2], heads=2, group=2, dim=128, page=16, lead=3),
+    "pages of 1": dict(lens=[333, 70], news=[5, 30], heads=2, group=2, dim=128, page=1),
+    "pages of 7": dict(lens=[333, 70, 6, 7, 8], news=[5, 30, 1, 2, 3], heads=2, group=2, dim=128, page=7),
+    "pages of 24": dict(lens=[333, 24, 25], news=[5, 30, 17], heads=2, group=7, dim=96, page=24),
+    "pages of 48": dict(lens=[333, 48, 49, 1000], news=[5, 30, 17, 2], heads=2, group=4, dim=128, page=48),
+    "pages of 128": dict(lens=[333, 128, 1000], news=[5, 30, 17], heads=4, group=4, dim=64, page=128),
+    "dim 8": dict(lens=[100, 9], news=[5, 20], heads=2, group=3, dim=8, page=16),
+    "dim 40": dict(lens=[100, 9], news=[5, 20], heads=2, group=3, dim=40, page=16),
+    "dim 80": dict(lens=[100, 900], news=[5, 20], heads=3, group=4, dim=80, page=16),
+    "dim 120": dict(lens=[100, 900], news=[5, 40], heads=2, group=4, dim=120, page=8),
+    "dim 136": dict(lens=[100, 300], news=[5, 20], heads=2, group=4, dim=136, page=16),
+    "dim 200": dict(lens=[100, 300], news=[1, 20], heads=2, group=4, dim=200, page=16),
+    "dim 256": dict(lens=[100, 300, 0], news=[1, 40, 20], heads=2, group=4, dim=256, page=16),
+    "wide group": dict(lens=[200], news=[3], heads=1, group=71, dim=64, page=16),
+    "views": dict(lens=[300, 20], news=[16, 40], heads=3, group=4, dim=128, page=16, views=True, gap=5),
+    "odd views": dict(lens=[300, 20, 0], news=[16, 1, 70], heads=3, group=2, dim=72, page=3, views=True, gap=1, mask=None),
+    "heads first": dict(lens=[300, 20], news=[16, 40], heads=3, group=4, dim=128, page=16, order="head"),
+    "loud": dict(lens=[700, 30], news=[16, 3], heads=2, group=4, dim=128, page=16, loud=20.0),
+    "long": dict(lens=[20000, 3], news=[2, 1], heads=1, group=4, dim=128, page=16),
+    "many": dict(lens=[(37 * i) % 190 for i in range(300)], news=[(i * 5) % 4 for i in range(300)], heads=1, group=2, dim=64, page=16),
+    "very many": dict(lens=[(7 * i) % 30 for i in range(1100)], news=[1] * 1100, heads=1, group=1, dim=8, page=16, mask=None),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("name", TREES)
+def test_attention_of_drafted_tokens(name, dtype):
+    print("attention", name, dtype, flush=True)
+    t = Tree(dtype=dtype, seed=len(name), **TREES[name])
+    out, lse = t.call()
+    t.check(out, lse)
+    again = t.call()
+    assert torch.equal(out[t.starts[0]:t.starts[-1]], again[0][t.starts[0]:t.starts[-1]]), "the same call twice"
+
+
+def test_attention_without_lse_into_a_tensor_of_the_callers():
+    t = Tree(lens=[100, 40], news=[9, 33], heads=2, group=3, dim=80, page=16, dtype=BF16)
+    want, lse = t.call()
+    t.check(want, lse)
+    room = torch.full((t.total, 2 * 3 * 2, 80 + 3), 7.0, dtype=BF16, device="cuda")
+    out = room[:, 1::2, 2:82]
+    got = ops().tree_attention(t.cache, *t.args, mask=t.mask, out=out)
+    assert got is out and torch.equal(got, want)
+    assert (room[:, ::2] == 7).all() and (room[:, :, :2] == 7).all() and (room[:, :, 82:] == 7).all()
+
+
+def test_a_value_that_some_rows_see_reaches_those_alone():
+    """NaN and infinities in a drafted token's value: what its ancestors and siblings answer is as if it were not there."""
+    t = Tree(lens=[70, 0], news=[20, 40], heads=2, group=4, dim=128, page=16, dtype=BF16)
+    q, k, v = t.args[:3]
+    want, _ = t.call()
+    for at, value, put in ((5, float("nan"), 3), (20 + 33, float("inf"), 100), (20 + 7, -float("inf"), 64)):
+        bad_v = v.clone()
+        bad_v[at, 1, put] = value
+        got, _ = ops().tree_attention(t.cache, q, k, bad_v, *t.args[3:], mask=t.mask, lse=True)
+        r0, r1 = (0, 20) if at < 20 else (20, 60)
+        for i in range(t.total):
+            sees = r0 <= i < r1 and t.bits[i] >> (at - r0) & 1
+            row = got[i].float().clone()
+            if sees:
+                hit = row[4:, put]
+                assert not torch.isfinite(hit).any(), (at, i, hit)
+                if not math.isnan(value):
+                    assert (hit == value).all()
+                row[4:, put] = want[i].float()[4:, put]
+            assert torch.equal(row, want[i].float()), (at, i)
+
+
+def test_a_key_that_some_rows_see_reaches_those_alone():
+    t = Tree(lens=[70], news=[30], heads=2, group=4, dim=64, page=16, dtype=FP16)
+    q, k, v = t.args[:3]
+    want, _ = t.call()
+    bad_k = k.clone()
+    bad_k[4, 0, 9] = float("nan")
+    got, lse = ops().tree_attention(t.cache, q, bad_k, v, *t.args[3:], mask=t.mask, lse=True)
+    for i in range(30):
+        if t.bits[i] >> 4 & 1:
+            assert torch.isnan(got[i, :4]).all() and torch.isnan(lse[i, :4]).all()
+            assert torch.equal(got[i, 4:], want[i, 4:])
+        else:
+            assert torch.equal(got[i], want[i])
+
+
+def test_a_cache_whose_offsets_pass_32_bits():
+    """Three pages more than 2^31 elements apart."""
+    page, heads, dim, stride = 16, 2, 64, (1 << 31) + 64
+    n = 2 * stride + page * heads * dim
+    m = Memory(2 * (2 * n) + 4 * SLAB, fill=None)
+    at = [m.alloc(2 * n), m.alloc(2 * n)]
+    cache = ops().KvCache(m.pool, at[0], at[1], 3, page, heads, dim, BF16, (stride, heads * dim, dim))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    kv = torch.randn(2, 48, heads, dim, device="cuda", generator=g).to(BF16)
+    slots = torch.randperm(48, device="cuda", generator=g)
+    ops().kv_append(cache, kv[0], kv[1], slots)
+    q, new = torch.randn(1, 4, dim, device="cuda", generator=g).to(BF16), torch.randn(2, 1, heads, dim, device="cuda", generator=g).to(BF16)
+    out = ops().tree_attention(cache, q, new[0], new[1], gpu([0, 1]), gpu([48]), gpu([[0, 1, 2]]), 1)
+    near, small, kc, vc = make_cache(3, page, heads, dim, BF16)
+    ops().kv_append(small, kv[0], kv[1], slots)
+    want = ops().tree_attention(small, q, new[0], new[1], gpu([0, 1]), gpu([48]), gpu([[0, 1, 2]]), 1)
+    assert torch.isfinite(want).all() and torch.equal(out, want)
+
+
+def test_lengths_and_tables_that_are_wrong_stay_inside_the_cache():
+    t = Tree(lens=[100, 40, 30], news=[3, 4, 5], heads=2, group=2, dim=64, page=16, dtype=BF16)
+    want, _ = t.call()
+    q, k, v, starts, lens, table, drafts = t.args
+    bad = table.clone()
+    bad[0] = gpu([-1, 2 ** 31 - 1, -2 ** 31] * 8)[:bad.shape[1]]
+    wrong = gpu([2 ** 31 - 1, -3, 30])
+    got = ops().tree_attention(t.cache, q, k, v, starts, wrong, bad, drafts, mask=t.mask)
+    assert torch.equal(got[7:], want[7:])                # the third request is as it was
+
+
+# ---- adapters -------------------------------------------------------------------------------------
+
+class Adapt:
+    def __init__(self, ids, ranks, width_in, width_out, dtype, seed=0, base=True, views=False):
+        g = torch.Generator().manual_seed(seed)
+        randn = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+        self.ids, self.dtype, rows = ids, dtype, len(ids)
+        self.m = Memory(sum(2 * r * (width_in + width_out) + 2 * SLAB for r in ranks) + SLAB)
+        self.factors, given = [], []
+        for i, r in enumerate(ranks):
+            a, b, s = (randn(r, width_in) * width_in ** -0.5).to(dtype), (randn(width_out, r)).to(dtype), 0.5 + i % 3
+            at = self.m.alloc(2 * r * width_in), self.m.alloc(2 * r * width_out)
+            self.m.view(at[0], dtype, r * width_in).copy_(a.flatten())
+            self.m.view(at[1], dtype, r * width_out).copy_(b.flatten())
+            self.factors.append((a.double(), b.double(), s))
+            given.append((at[0], at[1], r, s))
+        self.adapters = ops().Adapters(self.m.pool, given, width_in, width_out, dtype)
+        self.x, self.base = randn(rows, width_in).to(dtype), randn(rows, width_out).to(dtype) if base else None
+        if views:
+            self.gx = torch.full((rows, width_in + 5), float("nan"), dtype=dtype, device="cuda")[:, 1:width_in + 1]
+            self.gb = torch.full((rows, width_out + 3), float("nan"), dtype=dtype, device="cuda")[:, 2:width_out + 2]
+            self.gx.copy_(self.x)
+            self.gb.copy_(self.base)
+        else:
+            self.gx, self.gb = self.x.cuda(), self.base.cuda() if base else None
+        self.gids = gpu(ids)
+
+    def call(self, **more):
+        return ops().adapters_apply(self.adapters, ops().adapter_groups(self.adapters, self.gids), self.gx, self.gb, **more)
+
+    def check(self, out):
+        u, tiny = U[self.dtype], TINY[self.dtype]
+        want = self.base.double() if self.base is not None else torch.zeros(out.shape, dtype=torch.float64)
+        slack = torch.zeros_like(want)
+        ids = torch.tensor(self.ids)
+        for i, (a, b, s) in enumerate(self.factors):
+            rows = torch.nonzero(ids == i)[:, 0]
+            x = self.x[rows].double()
+            h, mass = x @ a.t() * s, x.abs() @ a.abs().t() * s
+            want[rows] += h @ b.t()
+            # A x: width_in products in 24 bits, then twice the type's bits; B: rank products in 24 bits
+            eh = (a.shape[1] + 8) * 2.0 ** -24 * mass + 2 * u * u * h.abs() + 2 * tiny
+            slack[rows] += eh @ b.abs().t() + (a.shape[0] + 8) * 2.0 ** -23 * (h.abs() @ b.abs().t())
+        bound = u * want.abs() + 1.01 * slack + tiny + 2.0 ** -23 * want.abs()
+        off = (out.double().cpu() - want).abs()
+        assert (off <= bound).all(), float((off - bound).max())
+
+
+def runs(rows, adapters, run, none, seed=0):
+    rng, out = random.Random(seed), []
+    while len(out) < rows:
+        out += [rng.choice([-1, adapters, 2 ** 31 - 1]) if rng.random() < none else rng.randrange(adapters)] * rng.randint(1, run)
+    return out[:rows]
+
+
+ADAPT = {
+    "one row": dict(ids=[0], ranks=[16], width_in=512, width_out=512),
+    "one row without": dict(ids=[-1], ranks=[16], width_in=512, width_out=512),
+    "one element": dict(ids=[0, 0], ranks=[1], width_in=1, width_out=1),
+    "tokens": dict(ids=runs(64, 32, 1, 0.1), ranks=[8, 16, 32, 64] * 8, width_in=1024, width_out=768),
+    "odd widths": dict(ids=runs(37, 5, 3, 0.2), ranks=[8, 3, 17, 12, 1], width_in=333, width_out=517),
+    "odd ranks": dict(ids=runs(90, 6, 3, 0.0), ranks=[1, 7, 9, 31, 33, 100], width_in=264, width_out=200),
+    "large ranks": dict(ids=runs(70, 3, 20, 0.0), ranks=[128, 256, 255], width_in=512, width_out=320),
+    "all of one": dict(ids=[2] * 300, ranks=[8, 8, 64], width_in=640, width_out=1000),
+    "none": dict(ids=[-1] * 50, ranks=[8, 8], width_in=64, width_out=100),
+    "prompts": dict(ids=runs(2000, 4, 500, 0.1), ranks=[16, 32, 64, 8], width_in=1024, width_out=1536),
+    "prompts, odd": dict(ids=runs(1777, 4, 300, 0.1), ranks=[12, 20, 64, 5], width_in=777, width_out=1031),
+    "narrow": dict(ids=runs(500, 9, 4, 0.1), ranks=[4] * 9, width_in=8, width_out=24),
+    "wide": dict(ids=runs(20, 3, 2, 0.0), ranks=[16, 8, 64], width_in=8192, width_out=9000),
+    "many adapters": dict(ids=runs(700, 300, 1, 0.3), ranks=[4, 8] * 150, width_in=128, width_out=128),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("name", ADAPT)
+def test_adapters_of_many_requests(name, dtype):
+    print("adapters", name, dtype, flush=True)
+    a = Adapt(dtype=dtype, seed=len(name), **ADAPT[name])
+    out = a.call()
+    a.check(out)
+    assert torch.equal(out, a.call()), "the same call twice"
+
+
+def test_adapters_without_a_base_in_place_and_on_views():
+    for kind in ("none", "in place", "views"):
+        a = Adapt(runs(100, 7, 3, 0.2), [8, 16, 5, 64, 8, 24, 32], 300, 500, BF16, base=kind != "none", views=kind == "views")
+        if kind == "in place":
+            kept = a.gb.clone()
+            out = a.call(out=a.gb)
+            assert out is a.gb and not torch.equal(kept, out)
+        elif kind == "views":
+            room = torch.full((100, 520), 3.0, dtype=BF16, device="cuda")
+            out = a.call(out=room[:, 7:507])
+            assert (room[:, :7] == 3).all() and (room[:, 507:] == 3).all()
+        else:
+            out = a.call()
+        a.check(out)
+
+
+def test_what_one_row_holds_does_not_reach_another():
+    """NaN in a row's input stays with that row."""
+    ids = runs(80, 4, 5, 0.1)
+    a = Adapt(ids, [16, 8, 64, 24], 512, 256, BF16)
+    want = a.call()
+    a.gx[11] = float("nan")
+    got = a.call()
+    has = 0 <= ids[11] < 4
+    assert torch.isnan(got[11]).all() == has
+    rows = [i for i in range(80) if i != 11]
+    assert torch.equal(got[rows], want[rows])
+
+
+# ---- streams, graphs, the step as a whole -----------------------------------------------------------
+
+def test_operators_on_a_stream_of_their_own():
+    t = Tree(lens=[500, 40], news=[9, 33], heads=2, group=3, dim=128, page=16, dtype=BF16)
+    a = Adapt(runs(64, 5, 2, 0.1), [8, 16, 32, 64, 8], 512, 512, BF16)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got, lse = t.call()
+        out = a.call()
+    s.synchronize()
+    t.check(got, lse)
+    a.check(out)
+
+
+def test_operators_captured_in_a_graph():
+    """Every replay, with eager work in between, gives what the eager call gives for the inputs of the moment."""
+    t = Tree(lens=[500, 40, 0], news=[9, 33, 2], heads=2, group=4, dim=128, page=16, dtype=BF16)
+    a = Adapt(runs(64, 5, 2, 0.1), [8, 16, 32, 64, 8], 512, 512, BF16)
+    m = Memory(SLAB)
+    table = torch.full((3, 40), -1, dtype=torch.int32, device="cuda")
+    table[:, :] = torch.arange(120, device="cuda", dtype=torch.int32).view(3, 40)
+    grow = (m.pool, gpu([500, 40, 0]), gpu([0, 9, 42, 44]), 44, table, torch.arange(200, 300, device="cuda", dtype=torch.int32), gpu([100, 0, 0, 0]), 16)
+    for f in (t.call, a.call, lambda: ops().kv_grow(*grow)):
+        f()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attn = t.call()
+        adapted = a.call()
+        grown = ops().kv_grow(*grow)
+    for i in range(4):
+        t.args[0].mul_(0.9)
+        a.gx.mul_(1.1)
+        grow[1].add_(1)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (*attn, adapted, *grown)]
+        want = [*t.call(), a.call(), *ops().kv_grow(*grow)]
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y), i
+        torch.empty(1 << 20, device="cuda").fill_(float("nan"))
