@@ -93,7 +93,8 @@ bool good_strides(std::initializer_list<uint64_t> strides) {
 bool good_numbers(const ft_kv_cache &c, const ft_tree_call &t) {
   if (t.drafts == 0 || t.requests > 1u << 24 || t.tokens >= 1u << 31 || t.drafts >= 1u << 31 || t.heads == 0 || t.heads % c.heads != 0) return false;
   if (t.heads > 1u << 16 || t.blocks > 1u << 31 || !std::isfinite(t.scale)) return false;
-  return (uint64_t)t.drafts * (t.heads / c.heads) < 1ull << 31;
+  const uint64_t drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
+  return drafts * (t.heads / c.heads) < 1u << 20 && (uint64_t)t.requests * c.heads < 1ull << 31;  // (what a launch's grid takes)
 }
 
 bool good_numbers(const ft_adapters_call &a) {

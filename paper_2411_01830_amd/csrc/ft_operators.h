@@ -21,7 +21,9 @@ struct Divisor {
       shift = s - 1;
     }
   }
-  __host__ __device__ uint32_t of(uint32_t n) const { return d == 1 ? n : (uint32_t)(((uint64_t)n * m) >> 32) >> shift; }
+  __host__ __device__ uint32_t of(uint32_t n) const { return d == 1 ? n : above_one(n); }
+  __host__ __device__ uint32_t above_one(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> 32) >> shift; }  // where d > 1
+  __host__ __device__ uint32_t rest(uint32_t n) const { return n - of(n) * d; }
 };
 
 // A cache with its pool offsets resolved.

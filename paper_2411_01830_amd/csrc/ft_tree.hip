@@ -1,4 +1,12 @@
 // Attention of drafted tokens over a paged cache and over each other.
+//
+// The rows of a request that read one key head - its drafted tokens times the query heads of that key head - are a matrix Q. 32 keys at
+// a time, S^T = K Q^T and O^T += V^T P^T by the matrix instruction, with the running maximum and sum of a softmax in
+// between. Both products have the rows of Q as columns, so a lane deals with the same row throughout: its scores, its maximum, its sum and
+// its part of O, and the weights P^T leave the first product in the registers that the second one reads them from - the 32 keys of a
+// step are numbered so that lane group g (of four, 16 lanes each) holds keys 4g .. 4g+3 and 16+4g .. 16+4g+3 in both. Keys are read as
+// the instruction wants them, 16 bytes a lane; of values a lane reads a piece of 8 rows and turns it round by byte permutes,
+// so nothing but the waves' sums goes through shared memory.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"
@@ -8,108 +16,654 @@ namespace ft {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kStep = 32;     // keys
+// How far, in powers of two, a score may pass the maximum that weights are relative to before sums are brought to a new one: weights
+// stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
+constexpr float kSlack = 8.0f;
 
 struct Tree {
   KvView c;
   ft_tree_call t;
+  uint32_t group;        // query heads of a key head
+  Divisor by_group;
+  uint32_t workers, least;  // workgroups, and steps that each takes at least
+  float scale;           // |scale| log2 e
+  uint32_t keep, flip;   // of two queries: nothing where the scale is zero; the sign bits where it is negative
+  uint64_t *prefix;      // requests + 2: steps of the requests before, of all; steps a worker
+  float *sums;           // partial results, see Partial
 };
 
-// A workgroup per token and query head, 256 keys at a time.
-template <class T>
-__global__ __launch_bounds__(256) void ft_tree_kernel(Tree a) {
+__device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+
+__device__ inline uint64_t from_lane(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32 | (uint32_t)__shfl((int)(uint32_t)v, lane);
+}
+
+// over the four lanes that have a row in common
+__device__ inline float row_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float row_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// read through the scalar cache where the index is the same for all lanes: a vector load's answer would have to wait for all keys and
+// values that were asked for before it
+typedef const __attribute__((address_space(4))) int32_t *Constants;
+__device__ inline Constants constants(const int32_t *p) { return reinterpret_cast<Constants>(reinterpret_cast<uintptr_t>(p)); }
+
+struct Request {
+  int start, n, len;  // drafted tokens from `start`, cached ones
+};
+
+__device__ inline Request request(const Tree &a, uint32_t r) {
+  const int tokens = (int)a.t.tokens;
+  const Constants starts = constants(a.t.starts);
+  int s = starts[r], e = starts[r + 1], len = constants(a.t.lens)[r];
+  s = s < 0 ? 0 : s > tokens ? tokens : s;
+  e = e < s ? s : e > tokens ? tokens : e;
+  const uint64_t room = (uint64_t)a.t.blocks * a.c.page_tokens.d;
+  len = len < 0 ? 0 : (uint64_t)len > room ? (int)room : len;
+  const int n = e - s;
+  return {s, n > (int)a.t.drafts ? (int)a.t.drafts : n, len};
+}
+
+__device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len + (kStep - 1)) >> 5) + (uint32_t)((q.n + (kStep - 1)) >> 5); }
+
+// Work of a request: for each key head and each tile of `rows` rows all of its steps.
+__device__ inline uint64_t work_of(const Tree &a, uint32_t r, uint32_t rows) {
+  const Request q = request(a, r);
+  const uint32_t tiles = ((uint32_t)q.n * a.group + rows - 1) / rows;
+  return (uint64_t)a.c.heads * tiles * steps_of(q);
+}
+
+// A worker's sums of a segment that it has a part of: [16 rows][4 elements x 64 lanes of every product], then a row's maximum and sum.
+template <int DT>
+struct Partial {
+  static constexpr uint32_t kTile = 16 * DT + 32;  // floats of 16 rows
+};
+
+// The elements of one row that a lane holds: O[E (4 g + i) + j] in acc[j][i].
+template <class T, int DT>
+__device__ inline void write_row(const Tree &a, const Floats4 (&acc)[DT / 16], float l, float m, const Request &q, uint32_t row, uint32_t kv_head, int g) {
+  constexpr int E = DT / 16;
+  const uint32_t token = a.by_group.of(row), head = kv_head * a.group + (row - token * a.group);
+  if ((int)token >= q.n) return;
+  const uint64_t t = (uint64_t)(q.start + (int)token);
+  uint16_t *out = static_cast<uint16_t *>(a.t.out) + t * a.t.out_token_stride + head * a.t.out_head_stride + 4 * E * g;
+  const float by = l == 0 ? 0 : 1 / l;
+  uint32_t w[2 * E];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < E; j += 2) w[(i * E + j) / 2] = T::pack(acc[j][i] * by, acc[j + 1][i] * by);
+#pragma unroll
+  for (int x = 0; x < 2 * E; x += 4)  // 8 elements; the head's size is a multiple of that
+    if (4 * E * g + 2 * x < (int)a.c.dim) *reinterpret_cast<Loose4 *>(out + 2 * x) = Loose4{{w[x], w[x + 1], w[x + 2], w[x + 3]}};
+  if (g == 0 && a.t.lse != nullptr) a.t.lse[t * a.t.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Two bytes of each of eight rows, as the matrix instruction wants them.
+template <int W>
+__device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t bytes) {
+  Words4 out;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) out[x] = __builtin_amdgcn_perm(v[2 * x + 1][word], v[2 * x][word], bytes);
+  return out;
+}
+
+// NR: tiles of 16 rows a wavefront has. WR: wavefronts that have different rows; 4 / WR share the keys among them.
+// PAGED: the head has DT elements and a page a multiple of 16 tokens, so 16 keys are read from one base address that is the same for all
+// lanes; without it every lane finds the row of one key, and hands it on to those that read it.
+template <class T, int DT, int NR, int WR, bool PAGED>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 256 ? 2 : 1, NR * DT < 256 ? 2 : 1))) void ft_tree_kernel(Tree a) {
+  constexpr int E = DT / 16, KS = DT / 32, WK = 4 / WR, RT = 16 * NR, ROWS = RT * WR;
   const ft_tree_call &t = a.t;
   const KvView &c = a.c;
-  __shared__ float q[256], p[256], part[4];
-  __shared__ int64_t rows[256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int token = blockIdx.x, head = blockIdx.y, kv_head = head / (t.heads / c.heads);
-  int lo = 0, hi = (int)t.requests;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (t.starts[mid] <= token) lo = mid;
-    else hi = mid;
+  const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
+  const int wave = (int)uniform((uint32_t)(tid >> 6)), wr = wave / WK, wk = wave % WK;
+  __shared__ uint64_t scan[256];
+  __shared__ uint64_t found[3];  // the request that this worker begins in, steps of it that others have, steps that this one has
+  __shared__ float stat[4][2][RT];
+  constexpr int kJoin = WK > 1 ? WR * (WK - 1) * NR * E * 256 : 1;
+  __shared__ float join[kJoin];
+
+  // The workers next to each other go to the same die: they read the same pages for other rows.
+  const uint32_t per_die = gridDim.x / 8;
+  const uint32_t worker = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
+  {
+    const uint32_t each = (t.requests + 255) / 256, r0 = tid * each, r1 = r0 + each < t.requests ? r0 + each : t.requests;
+    uint64_t mine = 0;
+    for (uint32_t r = r0; r < r1; ++r) mine += work_of(a, r, ROWS);
+    scan[tid] = mine;
+    __syncthreads();
+    uint64_t sum = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint64_t q = __shfl_up(sum, d);
+      if (lane >= d) sum += q;
+    }
+    __syncthreads();
+    scan[tid] = sum;
+    __syncthreads();
+    uint64_t all = 0, before = sum - mine;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += scan[w * 64 + 63];
+      all += scan[w * 64 + 63];
+    }
+    uint64_t per = (all + a.workers - 1) / a.workers;
+    if (per < a.least) per = a.least;
+    const uint64_t begin = per * worker;
+    if (begin >= before && begin < before + mine)
+      for (uint32_t r = r0; r < r1; ++r) {
+        const uint64_t w = work_of(a, r, ROWS);
+        if (begin < before + w) {
+          found[0] = r;
+          found[1] = begin - before;
+          break;
+        }
+        before += w;
+      }
+    if (tid == 0) found[2] = begin < all ? (all - begin < per ? all - begin : per) : 0;
+    if (worker == 0) {
+      uint64_t at = sum - mine;
+      for (int w = 0; w < wave; ++w) at += scan[w * 64 + 63];
+      for (uint32_t r = r0; r < r1; ++r) {
+        a.prefix[r] = at;
+        at += work_of(a, r, ROWS);
+      }
+      if (tid == 0) a.prefix[t.requests] = per;
+    }
+    __syncthreads();
   }
-  while (lo > 0 && t.starts[lo] > token) --lo;
-  const int start = t.starts[lo], end = t.starts[lo + 1] < (int)t.tokens ? t.starts[lo + 1] : (int)t.tokens;
-  if (start < 0 || token < start || token >= end || token - start >= (int)t.drafts) return;
-  int len = t.lens[lo];
-  const int64_t room = (int64_t)t.blocks * c.page_tokens.d;
-  if (len < 0) len = 0;
-  if (len > room) len = (int)room;
-  const int drafts = end - start;
-  const int keys = len + drafts;
-  const uint16_t *qp = static_cast<const uint16_t *>(t.q) + token * t.q_token_stride + head * t.q_head_stride;
-  if (tid < (int)c.dim) q[tid] = T::to_float(qp[tid]);
-  float m = -INFINITY, l = 0, acc = 0;
-  for (int s0 = 0; s0 < keys; s0 += 256) {
-    const int s = s0 + tid;
-    bool sees = s < keys;
-    const uint16_t *kp = nullptr;
-    int64_t v_row = -1;
-    if (s < len) {
-      const uint32_t block = c.page_tokens.of((uint32_t)s);
-      uint32_t page = (uint32_t)t.table[(uint64_t)lo * t.blocks + block];
-      page = page < c.pages ? page : 0;
-      const uint64_t at = page * c.page_stride + (s - block * c.page_tokens.d) * c.token_stride + kv_head * c.head_stride;
-      kp = reinterpret_cast<const uint16_t *>(c.k) + at;
-      v_row = (int64_t)at;
-    } else if (sees) {
-      const int j = s - len;
-      sees = t.mask != nullptr ? (uint32_t)(j >> 6) < t.mask_words && (t.mask[(uint64_t)token * t.mask_words + (j >> 6)] >> (j & 63) & 1) != 0 : j <= token - start;
-      kp = static_cast<const uint16_t *>(t.k) + (start + j) * t.k_token_stride + kv_head * t.k_head_stride;
-      v_row = (int64_t)((start + j) * t.v_token_stride + kv_head * t.v_head_stride);
-    }
-    __syncthreads();
-    float score = -INFINITY;
-    if (sees) {
-      float x = 0;
-      for (uint32_t d = 0; d < c.dim; ++d) x += q[d] * T::to_float(kp[d]);
-      score = x * (t.scale * kLog2e);
-    }
-    float top = score;
-    bool nan = score != score;
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) part[wave] = top;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, part[w]);
-    const float now = fmaxf(m, top), from = now == -INFINITY ? 0 : now;
-    const float shrink = exp2f(m - from);
-    const float weight = sees ? (nan ? score : exp2f(score - from)) : 0;
-    float sum = weight;
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    __syncthreads();
-    if (lane == 0) part[wave] = sum;
-    p[tid] = weight;
-    rows[tid] = sees ? v_row : -1;
-    __syncthreads();
-    l = l * shrink + part[0] + part[1] + part[2] + part[3];
-    acc *= shrink;
-    m = now;
-    if (tid < (int)c.dim) {
-      const int n = keys - s0 < 256 ? keys - s0 : 256;
-      for (int j = 0; j < n; ++j) {
-        if (rows[j] < 0) continue;
-        const uint16_t *vp = s0 + j < len ? reinterpret_cast<const uint16_t *>(c.v) : static_cast<const uint16_t *>(t.v);
-        acc += p[j] * T::to_float(vp[rows[j] + tid]);
+  // a lane's place in 16 keys' rows, and in 4 values' (PAGED: less than 2^31)
+  const uint32_t key_off = (n16 * (uint32_t)c.token_stride + 8 * g) * 2, value_off = (4 * g * (uint32_t)c.token_stride + E * n16) * 2;
+  uint32_t left = uniform((uint32_t)found[2]), r = uniform((uint32_t)found[0]);
+  uint64_t at = uniform(found[1]);
+
+  for (; left != 0; ++r, at = 0) {
+    const Request q = request(a, r);
+    const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
+    if (tiles == 0) continue;
+    const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
+    const uint64_t segments = (uint64_t)c.heads * tiles;
+    const Constants table = constants(t.table + (uint64_t)r * t.blocks);
+    for (uint64_t seg = at / steps; seg < segments && left != 0; ++seg) {
+      const uint32_t first = (uint32_t)(at > seg * steps ? at - seg * steps : 0);
+      const uint32_t last = steps - first < left ? steps : first + left;
+      left -= last - first;
+      const uint32_t head = (uint32_t)(seg / tiles), tile = (uint32_t)(seg - (uint64_t)head * tiles);
+      const uint32_t row0 = tile * ROWS + wr * RT;
+      const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
+      const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
+      const char *vd = static_cast<const char *>(t.v) + 2 * (q.start * t.v_token_stride + head * t.v_head_stride);
+
+      Words4 qf[NR][KS];
+      int token[NR];
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) {
+        uint32_t row = row0 + nr * 16 + n16;
+        const uint32_t most = (uint32_t)q.n * a.group - 1;
+        row = row < most ? row : most;  // rows behind the last one are answered and not written
+        const uint32_t tok = a.by_group.of(row);
+        token[nr] = (int)tok;
+        const uint16_t *p = static_cast<const uint16_t *>(t.q) + (q.start + (int)tok) * t.q_token_stride + (head * a.group + (row - tok * a.group)) * t.q_head_stride;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int d = ks * 32 + 8 * g;
+          Words4 w{0, 0, 0, 0};
+          if (PAGED || d < (int)c.dim) w = load16(p + d);
+          qf[nr][ks] = (w & a.keep) ^ a.flip;
+        }
+      }
+      Floats4 acc[NR][E];
+      float m[NR], l[NR];
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) {
+        m[nr] = -INFINITY;
+        l[nr] = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[nr][j] = Floats4{0, 0, 0, 0};
+      }
+
+      Words4 kf[2][KS];
+      uint32_t vf[8][E / 2];
+
+      // Where a key's row lies, from the head's first one, in elements. PAGED: of the first of 16 keys in one page; otherwise lane l % 32 of a
+      // step finds key l % 32. Keys behind the last cached one give that one's page.
+      const uint32_t end_key = q.len > 0 ? (uint32_t)q.len - 1 : 0;
+      const auto lane_page = [&](uint32_t st) -> uint32_t {
+        const uint32_t key = st * kStep + (lane & 31);
+        return (uint32_t)table[c.page_tokens.of(key < end_key ? key : end_key)];
+      };
+      const auto lane_row = [&](uint32_t st, uint32_t page) -> uint64_t {
+        uint32_t key = st * kStep + (lane & 31);
+        key = key < end_key ? key : end_key;
+        return (page < c.pages ? page : 0) * c.page_stride + c.page_tokens.rest(key) * c.token_stride;
+      };
+      const auto pages_of = [&](uint32_t st, uint32_t (&ids)[2]) {
+        if constexpr (PAGED) {
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const uint32_t key = st * kStep + kk * 16;
+            ids[kk] = (uint32_t)table[uniform(c.page_tokens.above_one(key < end_key ? key : end_key))];
+          }
+        } else {
+          ids[0] = lane_page(st);
+        }
+      };
+      const auto keys_at = [&](int kk, Global base, uint32_t off) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if (PAGED || ks * 32 + 8 * g < (int)c.dim) kf[kk][ks] = load16(base + off + ks * 64);
+          else kf[kk][ks] = Words4{0, 0, 0, 0};
+        }
+      };
+      // a lane's piece of a row: E elements, of which E is 4, 8 or 16 and the head's size a multiple of 8
+      const auto values_at = [&](int e, Global base, uint32_t off) {
+        if constexpr (E == 4) {
+          typedef const __attribute__((address_space(1))) Loose2 *P;
+          const bool has = PAGED || E * n16 < (int)c.dim;
+          vf[e][0] = has ? ((P)(base + off))->w[0] : 0;
+          vf[e][1] = has ? ((P)(base + off))->w[1] : 0;
+        } else {
+#pragma unroll
+          for (int x = 0; x < E / 8; ++x) {
+            Words4 w{0, 0, 0, 0};
+            if (PAGED || E * n16 + 8 * x < (int)c.dim) w = load16(base + off + 16 * x);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
+          }
+        }
+      };
+      // steps of 32 cached keys
+      const auto page_row = [&](uint32_t key, uint32_t page) -> uint64_t {
+        return 2 * ((page < c.pages ? page : 0) * c.page_stride + (key - c.page_tokens.above_one(key) * c.page_tokens.d) * c.token_stride);
+      };
+      const auto load_keys = [&](uint32_t st, const uint32_t (&ids)[2]) {
+        if constexpr (PAGED) {
+          uint32_t off = key_off;
+          asm volatile("" : "+v"(off));  // (32 bits beside a base in scalar registers: the sum of both would take two registers a row)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            Global base = global(kc) + page_row(st * kStep + kk * 16, ids[kk]);
+            asm volatile("" : "+s"(base));
+            keys_at(kk, base, off);
+          }
+        } else {
+          const uint64_t row = lane_row(st, ids[0]);
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) keys_at(kk, global(kc) + 2 * from_lane(row, kk * 16 + n16), 16 * g);
+        }
+      };
+      const auto load_values = [&](uint32_t st, const uint32_t (&ids)[2]) {
+        if constexpr (PAGED) {
+          uint32_t off = value_off;
+          asm volatile("" : "+v"(off));
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const Global first_of_four = global(vc) + page_row(st * kStep + kk * 16, ids[kk]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              Global base = first_of_four + 2 * e * c.token_stride;
+              asm volatile("" : "+s"(base));
+              values_at(kk * 4 + e, base, off);
+            }
+          }
+        } else {
+          const uint64_t row = lane_row(st, ids[0]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) values_at(e, global(vc) + 2 * from_lane(row, (e >> 2) * 16 + 4 * g + (e & 3)), 2 * E * n16);
+        }
+      };
+      // the last cached keys where they are no whole step, and steps of drafted ones
+      const auto load_edge_keys = [&](uint32_t st) {
+        Global p[2];
+        if (st < cached) {
+          const uint64_t row = lane_row(st, lane_page(st));
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) p[kk] = global(kc) + 2 * from_lane(row, kk * 16 + n16);
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const int j = (int)(st - cached) * kStep + kk * 16 + n16;
+            p[kk] = global(kd) + 2 * ((j < q.n ? j : q.n - 1) * t.k_token_stride);
+          }
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) keys_at(kk, p[kk], 16 * g);
+      };
+      const auto load_edge_values = [&](uint32_t st) {
+        Global p[8];
+        if (st < cached) {
+          const uint64_t row = lane_row(st, lane_page(st));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = global(vc) + 2 * from_lane(row, (e >> 2) * 16 + 4 * g + (e & 3));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int j = (int)(st - cached) * kStep + (e >> 2) * 16 + 4 * g + (e & 3);
+            p[e] = global(vd) + 2 * ((j < q.n ? j : q.n - 1) * t.v_token_stride);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) values_at(e, p[e], 2 * E * n16);
+      };
+      // which of such a step's keys a row sees
+      const auto sees_of = [&](int nr, uint32_t st) -> uint32_t {
+        const bool drafted = st >= cached;
+        const uint32_t js = st - cached, valid = drafted ? (uint32_t)q.n - js * kStep : (uint32_t)q.len - st * kStep;
+        uint32_t w = ~0u;
+        if (drafted) {
+          if (t.mask != nullptr) {
+            w = reinterpret_cast<const uint32_t *>(t.mask)[(uint64_t)(q.start + token[nr]) * 2 * t.mask_words + js];
+          } else {
+            const int d = token[nr] - (int)(js * kStep);
+            w = d < 0 ? 0 : d >= 31 ? ~0u : (2u << d) - 1;
+          }
+        }
+        return valid < 32 ? w & ((1u << valid) - 1) : w;
+      };
+
+      Floats4 s[NR][2];
+      const auto scores = [&] {
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            s[nr][kk] = Floats4{0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[nr][kk] = T::mfma(kf[kk][ks], qf[nr][ks], s[nr][kk]);
+          }
+      };
+      Words4 p[NR];
+      const auto weights = [&] {
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+          float x[8], w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3] * a.scale;
+          const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+          if (__any(top > m[nr] + kSlack)) {
+            const float now = fmaxf(m[nr], row_max(top));
+            const float shrink = now == -INFINITY ? 1 : __builtin_amdgcn_exp2f(m[nr] - now);
+            m[nr] = now;
+            l[nr] *= shrink;
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[nr][j] *= shrink;
+          }
+          const float from = m[nr] == -INFINITY ? 0 : m[nr];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(x[i] - from);
+          l[nr] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+          p[nr] = Words4{T::pack(w[0], w[1]), T::pack(w[2], w[3]), T::pack(w[4], w[5]), T::pack(w[6], w[7])};
+        }
+      };
+      const auto outputs = [&] {
+#pragma unroll
+        for (int j = 0; j < E; j += 2) {
+          const Words4 lo = turned(vf, j / 2, 0x05040100), hi = turned(vf, j / 2, 0x07060302);
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+            acc[nr][j] = T::mfma(lo, p[nr], acc[nr][j]);
+            acc[nr][j + 1] = T::mfma(hi, p[nr], acc[nr][j + 1]);
+          }
+        }
+      };
+
+      // Whole steps of cached keys. A step's keys are on their way while the one before weighs its values, its values from there on, and the
+      // pages of the one behind it are asked for first of all.
+      const uint32_t steps_whole = (uint32_t)q.len >> 5, whole = last < steps_whole ? last : steps_whole;
+      uint32_t st = first + wk;
+      if (st < whole) {
+        uint32_t ids[2], ahead[2];
+        pages_of(st, ids);
+        pages_of(st + WK, ahead);
+        load_keys(st, ids);
+        load_values(st, ids);
+        for (; st + WK < whole; st += WK) {  // (the last step apart: loads under a condition would be waited for as if they were not there)
+          ids[0] = ahead[0];
+          ids[1] = ahead[1];
+          scores();
+          load_keys(st + WK, ids);
+          __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
+          pages_of(st + 2 * WK, ahead);
+          weights();
+          outputs();
+          load_values(st + WK, ids);
+        }
+        scores();
+        weights();
+        outputs();
+        st += WK;
+      }
+      // the others
+      const uint32_t edge = st;
+      uint32_t bad = 0;
+      for (; st < last; st += WK) {
+        load_edge_keys(st);
+        load_edge_values(st);
+        scores();
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+          const uint32_t sees = sees_of(nr, st);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] = sees >> ((i >> 2) * 16 + 4 * g + (i & 3)) & 1 ? s[nr][i >> 2][i & 3] : -INFINITY;
+        }
+        weights();
+        // A drafted value that is not finite must reach those rows alone that see it: it is left out of the product, where it would
+        // meet weights of zero too.
+        if (st >= cached)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int x = 0; x < E / 2; ++x) {
+              const uint32_t lo = (vf[e][x] & T::kExponent) == T::kExponent ? 0xffffu : 0, hi = (vf[e][x] >> 16 & T::kExponent) == T::kExponent ? 0xffff0000u : 0;
+              bad |= lo | hi;
+              vf[e][x] &= ~(lo | hi);
+            }
+        outputs();
+      }
+      // What has been left out, by the same product on ones: how many infinities of either sign, and NaN, a row sees of every element.
+      if (__any(bad != 0))
+        for (st = edge; st < last; st += WK) {
+          if (st < cached) continue;
+          for (int kind = 0; kind < 3; ++kind) {
+            load_edge_values(st);
+            const auto one = [&](uint32_t v) {
+              const bool is = kind == 2 ? (v & 0x7fff) > T::kExponent : v == (T::kExponent | (uint32_t)kind << 15);
+              return is ? T::kOne : 0u;
+            };
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+              for (int x = 0; x < E / 2; ++x) vf[e][x] = one(vf[e][x] & 0xffff) | one(vf[e][x] >> 16) << 16;
+            const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+              const uint32_t sees = sees_of(nr, st);
+              Words4 seen;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const uint32_t two = sees >> ((x >> 1) * 16 + 4 * g + (x & 1) * 2);
+                seen[x] = (two & 1 ? T::kOne : 0) | (two & 2 ? T::kOne << 16 : 0);
+              }
+#pragma unroll
+              for (int j = 0; j < E; ++j) {
+                const Floats4 count = T::mfma(turned(vf, j / 2, j & 1 ? 0x07060302 : 0x05040100), seen, Floats4{0, 0, 0, 0});
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (count[i] != 0) acc[nr][j][i] += value;
+                __builtin_amdgcn_sched_barrier(0);  // (rare: what it takes is registers, not time)
+              }
+            }
+          }
+        }
+
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) l[nr] = row_sum(l[nr]);
+      if constexpr (WK > 1) {
+        __syncthreads();  // what the segment before has left here has been read
+        if (g == 0)
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+            stat[wave][0][nr * 16 + n16] = m[nr];
+            stat[wave][1][nr * 16 + n16] = l[nr];
+          }
+        __syncthreads();
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+          float now = -INFINITY, sum = 0;
+          for (int w = 0; w < WK; ++w) now = fmaxf(now, stat[wr * WK + w][0][nr * 16 + n16]);
+          const float from = now == -INFINITY ? 0 : now;
+          for (int w = 0; w < WK; ++w) sum += stat[wr * WK + w][1][nr * 16 + n16] * __builtin_amdgcn_exp2f(stat[wr * WK + w][0][nr * 16 + n16] - from);
+          const float shrink = __builtin_amdgcn_exp2f(m[nr] - from);
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            acc[nr][j] *= shrink;
+            if (wk != 0) reinterpret_cast<Floats4 *>(join)[(((wr * (WK - 1) + wk - 1) * NR + nr) * E + j) * 64 + lane] = acc[nr][j];
+          }
+          m[nr] = now;
+          l[nr] = sum;
+        }
+        __syncthreads();
+        if (wk == 0)
+          for (int w = 0; w < WK - 1; ++w)
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+              for (int j = 0; j < E; ++j) acc[nr][j] += reinterpret_cast<Floats4 *>(join)[(((wr * (WK - 1) + w) * NR + nr) * E + j) * 64 + lane];
+      }
+      if (wk == 0) {
+        if (first == 0 && last == steps) {
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
+        } else {
+          // a worker has at most two segments that it shares: the one it begins in, which others have begun, and the one it ends in
+          float *sums = a.sums + ((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * (WR * NR * Partial<DT>::kTile) + wr * NR * Partial<DT>::kTile;
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) reinterpret_cast<Floats4 *>(sums + nr * Partial<DT>::kTile)[j * 64 + lane] = acc[nr][j];
+            if (g == 0) {
+              sums[nr * Partial<DT>::kTile + 16 * DT + n16] = m[nr];
+              sums[nr * Partial<DT>::kTile + 16 * DT + 16 + n16] = l[nr];
+            }
+          }
+        }
       }
     }
   }
-  if (tid < (int)c.dim)
-    static_cast<uint16_t *>(t.out)[token * t.out_token_stride + head * t.out_head_stride + tid] = T::from_float(l == 0 ? 0 : acc / l);
-  if (tid == 0 && t.lse != nullptr) t.lse[(uint64_t)token * t.heads + head] = l == 0 ? -INFINITY : (m + log2f(l)) / kLog2e;
+}
+
+// The sums of segments that several workers share: a wavefront for every 16 rows.
+template <class T, int DT, int NR, int WR>
+__global__ __launch_bounds__(64) void ft_tree_join_kernel(Tree a) {
+  constexpr int E = DT / 16, ROWS = 16 * NR * WR;
+  const int lane = threadIdx.x, n16 = lane & 15, g = lane >> 4;
+  const uint32_t r = blockIdx.x / a.c.heads, head = blockIdx.x - r * a.c.heads;
+  const uint32_t tile = blockIdx.y / (NR * WR), part = blockIdx.y - tile * (NR * WR);
+  const Request q = request(a, r);
+  const uint32_t tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
+  if (tile >= tiles || tile * ROWS + part * 16 >= (uint32_t)q.n * a.group) return;
+  const uint32_t steps = steps_of(q);
+  const uint64_t per = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)head * tiles + tile) * steps;
+  const uint32_t w0 = (uint32_t)(begin / per), w1 = (uint32_t)((begin + steps - 1) / per);
+  if (w0 == w1) return;
+  const auto at = [&](uint32_t w) { return a.sums + (((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * (WR * NR) + part) * Partial<DT>::kTile; };
+  float now = -INFINITY, l = 0;
+  for (uint32_t w = w0; w <= w1; ++w) now = fmaxf(now, at(w)[16 * DT + n16]);
+  const float from = now == -INFINITY ? 0 : now;
+  Floats4 acc[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc[j] = Floats4{0, 0, 0, 0};
+  for (uint32_t w = w0; w <= w1; ++w) {
+    const float *sums = at(w);
+    const float shrink = __builtin_amdgcn_exp2f(sums[16 * DT + n16] - from);
+    l += sums[16 * DT + 16 + n16] * shrink;
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] += reinterpret_cast<const Floats4 *>(sums)[j * 64 + lane] * shrink;
+  }
+  write_row<T, DT>(a, acc, l, now, q, tile * ROWS + part * 16 + n16, head, g);
+}
+
+struct Shape {
+  int dt, nr, wr;
+};
+
+// Heads are padded to 64, 128 or 256 elements. Up to 16 rows a tile of them is one wavefront's, and four share the keys; then two such
+// tiles; then wavefronts with other rows, which read the same keys.
+Shape shape_of(uint32_t dim, uint64_t rows) {
+  const int dt = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+  if (rows <= 16) return {dt, 1, 1};
+  if (dt == 256) return {dt, 1, 4};
+  if (rows <= 32) return {dt, 2, 1};
+  if (rows <= 64) return {dt, 2, 2};
+  return {dt, 2, 4};
+}
+
+uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(s.nr == 2 || s.dt == 256 ? cu_count : 2 * cu_count) / 8 * 8 + 8; }
+
+uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
+
+template <class T, int DT, int NR, int WR>
+hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) {
+  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const uint64_t tiles = (rows + 16 * NR * WR - 1) / (16 * NR * WR) * NR * WR;
+  hipLaunchKernelGGL((ft_tree_join_kernel<T, DT, NR, WR>), dim3(a.t.requests * a.c.heads, (uint32_t)tiles), dim3(64), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <class T, int DT>
+hipError_t launch_rows(const Tree &a, const Shape &s, bool paged, uint64_t rows, hipStream_t stream) {
+  if (s.nr == 1 && s.wr == 1) return launch<T, DT, 1, 1>(a, paged, rows, stream);
+  if constexpr (DT == 256) return launch<T, DT, 1, 4>(a, paged, rows, stream);
+  else if (s.wr == 1) return launch<T, DT, 2, 1>(a, paged, rows, stream);
+  else if (s.wr == 2) return launch<T, DT, 2, 2>(a, paged, rows, stream);
+  else return launch<T, DT, 2, 4>(a, paged, rows, stream);
+}
+
+template <class T>
+hipError_t launch_dim(const Tree &a, const Shape &s, bool paged, uint64_t rows, hipStream_t stream) {
+  return s.dt == 64 ? launch_rows<T, 64>(a, s, paged, rows, stream) : s.dt == 128 ? launch_rows<T, 128>(a, s, paged, rows, stream)
+                                                                                 : launch_rows<T, 256>(a, s, paged, rows, stream);
+}
+
+uint64_t rows_of(const ft_tree_call &t, uint32_t heads) {
+  const uint64_t n = t.drafts < t.tokens ? t.drafts : t.tokens;
+  return n * (t.heads / heads);
 }
 
 }  // namespace
 
-uint64_t tree_workspace(const ft_kv_cache &, const ft_tree_call &, int) { return 0; }
+uint64_t tree_workspace(const ft_kv_cache &c, const ft_tree_call &t, int cu_count) {
+  const Shape s = shape_of(c.dim, rows_of(t, c.heads));
+  return up16(((uint64_t)t.requests + 2) * 8) + (uint64_t)workers_of(s, cu_count) * 2 * s.nr * s.wr * (16 * s.dt + 32) * 4;
+}
 
-hipError_t launch_tree(const KvView &c, const ft_tree_call &call, int, hipStream_t stream) {
-  const Tree a{c, call};
-  const dim3 grid(call.tokens, call.heads);
-  if (c.type == FT_BF16) hipLaunchKernelGGL(ft_tree_kernel<Bf16>, grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(ft_tree_kernel<Fp16>, grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
+hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hipStream_t stream) {
+  const uint64_t rows = rows_of(t, c.heads);
+  const Shape s = shape_of(c.dim, rows);
+  Tree a{c, t};
+  a.t.drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
+  a.group = t.heads / c.heads;
+  a.by_group = Divisor(a.group);
+  a.workers = workers_of(s, cu_count);
+  a.least = 2 * (4 / s.wr);
+  a.scale = t.scale == 0 ? 1 : (t.scale < 0 ? -t.scale : t.scale) * kLog2e;
+  a.keep = t.scale == 0 ? 0 : ~0u;
+  a.flip = t.scale < 0 ? 0x80008000u : 0;
+  a.prefix = static_cast<uint64_t *>(t.workspace);
+  a.sums = reinterpret_cast<float *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
+  // 16 keys lie within 2 GiB of each other
+  const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && c.token_stride < 1u << 25;
+  return c.type == FT_BF16 ? launch_dim<Bf16>(a, s, paged, rows, stream) : launch_dim<Fp16>(a, s, paged, rows, stream);
 }
 
 }  // namespace ft
