@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
   const KvView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
   const int wave = (int)uniform((uint32_t)(tid >> 6)), wr = wave / WK, wk = wave % WK;
-  __shared__ uint64_t scan[256];
+  __shared__ uint64_t scan[4];
   __shared__ uint64_t found[3];  // the request that this worker begins in, steps of it that others have, steps that this one has
   __shared__ float stat[4][2][RT];
   constexpr int kJoin = WK > 1 ? WR * (WK - 1) * NR * E * 256 : 1;
@@ -136,51 +136,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
   const uint32_t per_die = gridDim.x / 8;
   const uint32_t worker = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
   {
-    const uint32_t each = (t.requests + 255) / 256, r0 = tid * each, r1 = r0 + each < t.requests ? r0 + each : t.requests;
-    uint64_t mine = 0;
-    for (uint32_t r = r0; r < r1; ++r) mine += work_of(a, r, ROWS);
-    scan[tid] = mine;
-    __syncthreads();
-    uint64_t sum = mine;
+    // Every workgroup sums up the requests' work for itself: a thread has a few that are neighbours.
+    const uint32_t each = (t.requests + 255) / 256, r0 = tid * each < t.requests ? tid * each : t.requests, r1 = r0 + each < t.requests ? r0 + each : t.requests;
+    uint64_t mine = 0, sum;
+    for (uint32_t i = r0; i < r1; ++i) mine += work_of(a, i, ROWS);
+    sum = mine;
     for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t q = __shfl_up(sum, d);
-      if (lane >= d) sum += q;
+      const uint64_t other = __shfl_up(sum, d);
+      if (lane >= d) sum += other;
     }
-    __syncthreads();
-    scan[tid] = sum;
+    if (lane == 63) scan[wave] = sum;
     __syncthreads();
     uint64_t all = 0, before = sum - mine;
     for (int w = 0; w < 4; ++w) {
-      if (w < wave) before += scan[w * 64 + 63];
-      all += scan[w * 64 + 63];
+      if (w < wave) before += scan[w];
+      all += scan[w];
     }
     uint64_t per = (all + a.workers - 1) / a.workers;
     if (per < a.least) per = a.least;
     const uint64_t begin = per * worker;
-    if (begin >= before && begin < before + mine)
-      for (uint32_t r = r0; r < r1; ++r) {
-        const uint64_t w = work_of(a, r, ROWS);
-        if (begin < before + w) {
-          found[0] = r;
-          found[1] = begin - before;
-          break;
-        }
-        before += w;
-      }
-    if (tid == 0) found[2] = begin < all ? (all - begin < per ? all - begin : per) : 0;
     if (worker == 0) {
-      uint64_t at = sum - mine;
-      for (int w = 0; w < wave; ++w) at += scan[w * 64 + 63];
-      for (uint32_t r = r0; r < r1; ++r) {
-        a.prefix[r] = at;
-        at += work_of(a, r, ROWS);
+      uint64_t sofar = before;
+      for (uint32_t i = r0; i < r1; ++i) {
+        a.prefix[i] = sofar;
+        sofar += r1 - r0 == 1 ? mine : work_of(a, i, ROWS);
       }
       if (tid == 0) a.prefix[t.requests] = per;
     }
+    if (begin >= all) return;
+    if (begin >= before && begin < before + mine) {
+      uint32_t i = r0;
+      if (r1 - r0 > 1)
+        for (;; ++i) {
+          const uint64_t w = work_of(a, i, ROWS);
+          if (begin < before + w) break;
+          before += w;
+        }
+      found[0] = i;
+      found[1] = begin - before;
+      found[2] = all - begin < per ? all - begin : per;
+    }
     __syncthreads();
   }
-  // a lane's place in 16 keys' rows, and in 4 values' (PAGED: less than 2^31)
-  const uint32_t key_off = (n16 * (uint32_t)c.token_stride + 8 * g) * 2, value_off = (4 * g * (uint32_t)c.token_stride + E * n16) * 2;
+  // What the loop over keys goes by, each in a register of its own (as parts of the argument's words they would come and go with those). PAGED only.
+  uint32_t row_bytes = 2 * (uint32_t)c.token_stride, k_bytes = 2 * (uint32_t)t.k_token_stride, v_bytes = 2 * (uint32_t)t.v_token_stride;
+  uint32_t pages = c.pages, page_d = c.page_tokens.d, page_m = c.page_tokens.m, page_shift = c.page_tokens.shift;
+  uint64_t page_bytes = 2 * c.page_stride;
+  float scale = a.scale;
+  asm volatile("" : "+s"(row_bytes), "+s"(k_bytes), "+s"(v_bytes), "+s"(pages), "+s"(page_d), "+s"(page_m), "+s"(page_shift), "+s"(page_bytes), "+s"(scale));
   uint32_t left = uniform((uint32_t)found[2]), r = uniform((uint32_t)found[0]);
   uint64_t at = uniform(found[1]);
 
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
       const uint32_t first = (uint32_t)(at > seg * steps ? at - seg * steps : 0);
       const uint32_t last = steps - first < left ? steps : first + left;
       left -= last - first;
-      const uint32_t head = (uint32_t)(seg / tiles), tile = (uint32_t)(seg - (uint64_t)head * tiles);
+      const uint32_t head = uniform((uint32_t)(seg / tiles)), tile = uniform((uint32_t)(seg - (uint64_t)head * tiles));
       const uint32_t row0 = tile * ROWS + wr * RT;
       const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
       const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
@@ -232,127 +235,105 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
       Words4 kf[2][KS];
       uint32_t vf[8][E / 2];
 
-      // Where a key's row lies, from the head's first one, in elements. PAGED: of the first of 16 keys in one page; otherwise lane l % 32 of a
-      // step finds key l % 32. Keys behind the last cached one give that one's page.
+      // A step's rows. PAGED: 16 cached keys have a page in common, whose number is read two steps ahead; rows behind the last
+      // key, in that page still, are read and not looked at. Otherwise lane l % 32 finds key l % 32, behind the last one that one again. So
+      // it is with drafted keys. (No branches here: loads under a condition, of either outcome, would be waited for as if they were not there.)
       const uint32_t end_key = q.len > 0 ? (uint32_t)q.len - 1 : 0;
-      const auto lane_page = [&](uint32_t st) -> uint32_t {
-        const uint32_t key = st * kStep + (lane & 31);
-        return (uint32_t)table[c.page_tokens.of(key < end_key ? key : end_key)];
-      };
-      const auto lane_row = [&](uint32_t st, uint32_t page) -> uint64_t {
-        uint32_t key = st * kStep + (lane & 31);
-        key = key < end_key ? key : end_key;
-        return (page < c.pages ? page : 0) * c.page_stride + c.page_tokens.rest(key) * c.token_stride;
-      };
       const auto pages_of = [&](uint32_t st, uint32_t (&ids)[2]) {
+        if (st >= cached) return;
         if constexpr (PAGED) {
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk) {
             const uint32_t key = st * kStep + kk * 16;
-            ids[kk] = (uint32_t)table[uniform(c.page_tokens.above_one(key < end_key ? key : end_key))];
+            ids[kk] = (uint32_t)table[uniform(__umulhi(key < end_key ? key : end_key, page_m) >> page_shift)];
           }
         } else {
-          ids[0] = lane_page(st);
+          const uint32_t key = st * kStep + (lane & 31);
+          ids[0] = (uint32_t)table[c.page_tokens.of(key < end_key ? key : end_key)];
         }
       };
-      const auto keys_at = [&](int kk, Global base, uint32_t off) {
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if (PAGED || ks * 32 + 8 * g < (int)c.dim) kf[kk][ks] = load16(base + off + ks * 64);
-          else kf[kk][ks] = Words4{0, 0, 0, 0};
-        }
+      // Lane l % 32's row as an offset in bytes from the head's first one (without PAGED), of cached and of drafted keys.
+      const auto lane_row = [&](uint32_t st, uint32_t page, uint64_t draft_stride) -> uint64_t {
+        uint32_t key = st * kStep + (lane & 31), draft = key - cached * kStep;
+        key = key < end_key ? key : end_key;
+        draft = draft < (uint32_t)q.n ? draft : (uint32_t)q.n - 1;
+        const uint64_t in_cache = (page < c.pages ? page : 0) * c.page_stride + c.page_tokens.rest(key) * c.token_stride;
+        return 2 * (st < cached ? in_cache : draft * draft_stride);
       };
-      // a lane's piece of a row: E elements, of which E is 4, 8 or 16 and the head's size a multiple of 8
-      const auto values_at = [&](int e, Global base, uint32_t off) {
-        if constexpr (E == 4) {
-          typedef const __attribute__((address_space(1))) Loose2 *P;
-          const bool has = PAGED || E * n16 < (int)c.dim;
-          vf[e][0] = has ? ((P)(base + off))->w[0] : 0;
-          vf[e][1] = has ? ((P)(base + off))->w[1] : 0;
-        } else {
-#pragma unroll
-          for (int x = 0; x < E / 8; ++x) {
-            Words4 w{0, 0, 0, 0};
-            if (PAGED || E * n16 + 8 * x < (int)c.dim) w = load16(base + off + 16 * x);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
-          }
-        }
+      // PAGED: where 16 keys of a step begin, in bytes from the head's first one, and how many rows there are behind that one.
+      struct Half {
+        uint64_t row;
+        uint32_t behind;
       };
-      // steps of 32 cached keys
-      const auto page_row = [&](uint32_t key, uint32_t page) -> uint64_t {
-        return 2 * ((page < c.pages ? page : 0) * c.page_stride + (key - c.page_tokens.above_one(key) * c.page_tokens.d) * c.token_stride);
+      const auto half = [&](uint32_t st, int kk, uint32_t page, uint32_t draft_stride) -> Half {
+        const uint32_t key = st * kStep + kk * 16, end = (uint32_t)q.n - 1;
+        const uint32_t draft = key - cached * kStep < end ? key - cached * kStep : end;
+        const bool in_cache = st < cached;
+        page = in_cache && page < pages ? page : 0;
+        const uint32_t row = in_cache ? key - (__umulhi(key, page_m) >> page_shift) * page_d : draft;
+        return {page * page_bytes + (uint64_t)row * (in_cache ? row_bytes : draft_stride), in_cache ? 15 : end - draft};
       };
       const auto load_keys = [&](uint32_t st, const uint32_t (&ids)[2]) {
-        if constexpr (PAGED) {
-          uint32_t off = key_off;
-          asm volatile("" : "+v"(off));  // (32 bits beside a base in scalar registers: the sum of both would take two registers a row)
+        const uint64_t row = PAGED ? 0 : lane_row(st, ids[0], t.k_token_stride);
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            Global base = global(kc) + page_row(st * kStep + kk * 16, ids[kk]);
-            asm volatile("" : "+s"(base));
-            keys_at(kk, base, off);
+        for (int kk = 0; kk < 2; ++kk) {
+          Global base = global(st < cached ? kc : kd);
+          uint32_t off = 16 * g;
+          if constexpr (PAGED) {
+            const Half h = half(st, kk, ids[kk], k_bytes);
+            base += h.row;
+            off += __umul24((uint32_t)n16 < h.behind ? n16 : h.behind, st < cached ? row_bytes : k_bytes);
+            asm volatile("" : "+s"(base), "+v"(off));  // (32 bits beside a base in scalar registers: the sum of both would take two registers a row)
+          } else {
+            base += from_lane(row, kk * 16 + n16);
           }
-        } else {
-          const uint64_t row = lane_row(st, ids[0]);
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) keys_at(kk, global(kc) + 2 * from_lane(row, kk * 16 + n16), 16 * g);
+          for (int ks = 0; ks < KS; ++ks) {
+            if (PAGED || ks * 32 + 8 * g < (int)c.dim) kf[kk][ks] = load16(base + off + ks * 64);
+            else kf[kk][ks] = Words4{0, 0, 0, 0};
+          }
         }
       };
       const auto load_values = [&](uint32_t st, const uint32_t (&ids)[2]) {
-        if constexpr (PAGED) {
-          uint32_t off = value_off;
-          asm volatile("" : "+v"(off));
+        const uint64_t row = PAGED ? 0 : lane_row(st, ids[0], t.v_token_stride);
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            const Global first_of_four = global(vc) + page_row(st * kStep + kk * 16, ids[kk]);
+        for (int kk = 0; kk < 2; ++kk) {
+          Global half_base = global(st < cached ? vc : vd);
+          Half h{0, 0};
+          if constexpr (PAGED) {
+            h = half(st, kk, ids[kk], v_bytes);
+            half_base += h.row;
+          }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              Global base = first_of_four + 2 * e * c.token_stride;
-              asm volatile("" : "+s"(base));
-              values_at(kk * 4 + e, base, off);
+          for (int i = 0; i < 4; ++i) {
+            const int e = 4 * kk + i;
+            Global base = half_base;
+            uint32_t off = 2 * E * n16;
+            if constexpr (PAGED) {
+              off += __umul24((uint32_t)(4 * g + i) < h.behind ? 4 * g + i : h.behind, st < cached ? row_bytes : v_bytes);
+              asm volatile("" : "+s"(base), "+v"(off));
+            } else {
+              base += from_lane(row, kk * 16 + 4 * g + i);
+            }
+            // a lane's piece of a row: E elements, of which E is 4, 8 or 16 and the head's size a multiple of 8
+            if constexpr (E == 4) {
+              typedef const __attribute__((address_space(1))) Loose2 *P;
+              const bool has = PAGED || E * n16 < (int)c.dim;
+              vf[e][0] = has ? ((P)(base + off))->w[0] : 0;
+              vf[e][1] = has ? ((P)(base + off))->w[1] : 0;
+            } else {
+#pragma unroll
+              for (int x = 0; x < E / 8; ++x) {
+                Words4 w{0, 0, 0, 0};
+                if (PAGED || E * n16 + 8 * x < (int)c.dim) w = load16(base + off + 16 * x);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
+              }
             }
           }
-        } else {
-          const uint64_t row = lane_row(st, ids[0]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) values_at(e, global(vc) + 2 * from_lane(row, (e >> 2) * 16 + 4 * g + (e & 3)), 2 * E * n16);
         }
       };
-      // the last cached keys where they are no whole step, and steps of drafted ones
-      const auto load_edge_keys = [&](uint32_t st) {
-        Global p[2];
-        if (st < cached) {
-          const uint64_t row = lane_row(st, lane_page(st));
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) p[kk] = global(kc) + 2 * from_lane(row, kk * 16 + n16);
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            const int j = (int)(st - cached) * kStep + kk * 16 + n16;
-            p[kk] = global(kd) + 2 * ((j < q.n ? j : q.n - 1) * t.k_token_stride);
-          }
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) keys_at(kk, p[kk], 16 * g);
-      };
-      const auto load_edge_values = [&](uint32_t st) {
-        Global p[8];
-        if (st < cached) {
-          const uint64_t row = lane_row(st, lane_page(st));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = global(vc) + 2 * from_lane(row, (e >> 2) * 16 + 4 * g + (e & 3));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int j = (int)(st - cached) * kStep + (e >> 2) * 16 + 4 * g + (e & 3);
-            p[e] = global(vd) + 2 * ((j < q.n ? j : q.n - 1) * t.v_token_stride);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) values_at(e, p[e], 2 * E * n16);
-      };
-      // which of such a step's keys a row sees
+      // which of a step's keys a row sees
       const auto sees_of = [&](int nr, uint32_t st) -> uint32_t {
         const bool drafted = st >= cached;
         const uint32_t js = st - cached, valid = drafted ? (uint32_t)q.n - js * kStep : (uint32_t)q.len - st * kStep;
@@ -385,7 +366,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
         for (int nr = 0; nr < NR; ++nr) {
           float x[8], w[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3] * a.scale;
+          for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3] * scale;
           const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
           if (__any(top > m[nr] + kSlack)) {
             const float now = fmaxf(m[nr], row_max(top));
@@ -414,65 +395,83 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
         }
       };
 
-      // Whole steps of cached keys. A step's keys are on their way while the one before weighs its values, its values from there on, and the
-      // pages of the one behind it are asked for first of all.
-      const uint32_t steps_whole = (uint32_t)q.len >> 5, whole = last < steps_whole ? last : steps_whole;
-      uint32_t st = first + wk;
-      if (st < whole) {
-        uint32_t ids[2], ahead[2];
-        pages_of(st, ids);
-        pages_of(st + WK, ahead);
-        load_keys(st, ids);
-        load_values(st, ids);
-        for (; st + WK < whole; st += WK) {  // (the last step apart: loads under a condition would be waited for as if they were not there)
-          ids[0] = ahead[0];
-          ids[1] = ahead[1];
-          scores();
-          load_keys(st + WK, ids);
-          __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
-          pages_of(st + 2 * WK, ahead);
-          weights();
-          outputs();
-          load_values(st + WK, ids);
-        }
-        scores();
-        weights();
-        outputs();
-        st += WK;
-      }
-      // the others
-      const uint32_t edge = st;
+      // Steps in which not everything is seen: the last cached keys where they are no whole step, and drafted ones. What a row does not see
+      // has a weight of zero, and its value, which may be anything, must not be met by it where it is not finite: such values
+      // are left out of the product. Where a row may see one it is added afterwards.
       uint32_t bad = 0;
-      for (; st < last; st += WK) {
-        load_edge_keys(st);
-        load_edge_values(st);
-        scores();
+      const auto edge = [&](uint32_t st) {
+        if ((st + 1) * kStep <= (uint32_t)q.len) return;
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
           const uint32_t sees = sees_of(nr, st);
 #pragma unroll
           for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] = sees >> ((i >> 2) * 16 + 4 * g + (i & 3)) & 1 ? s[nr][i >> 2][i & 3] : -INFINITY;
         }
-        weights();
-        // A drafted value that is not finite must reach those rows alone that see it: it is left out of the product, where it would
-        // meet weights of zero too.
-        if (st >= cached)
+      };
+      const auto edge_values = [&](uint32_t st) {
+        if ((st + 1) * kStep <= (uint32_t)q.len) return;
+        // an exponent of all ones carries into the sign's place
+        const auto odd = [](uint32_t v) { return ((v & T::kExponent * 0x10001u) + T::kLowest * 0x10001u) & 0x80008000u; };
+        uint32_t any = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int x = 0; x < E / 2; ++x) {
-              const uint32_t lo = (vf[e][x] & T::kExponent) == T::kExponent ? 0xffffu : 0, hi = (vf[e][x] >> 16 & T::kExponent) == T::kExponent ? 0xffff0000u : 0;
-              bad |= lo | hi;
-              vf[e][x] &= ~(lo | hi);
-            }
-        outputs();
+          for (int x = 0; x < E / 2; ++x) any |= odd(vf[e][x]);
+        if (!__any(any != 0)) return;
+        const int valid = st >= cached ? q.n - (int)(st - cached) * kStep : q.len - (int)(st * kStep);
+        uint32_t seen = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t may = (e >> 2) * 16 + 4 * g + (e & 3) < valid ? ~0u : 0;
+#pragma unroll
+          for (int x = 0; x < E / 2; ++x) {
+            const uint32_t bit = odd(vf[e][x]) >> 15;
+            seen |= bit & may;
+            vf[e][x] &= ~((bit << 16) - bit);
+          }
+        }
+        bad |= uniform((uint32_t)(__any(seen != 0) ? 1 : 0));
+      };
+
+      // A step's keys are on their way while the one before weighs its values, its values from there on, and the pages of the one behind it
+      // are asked for first of all. The last step asks for its own rows once more, which are near by then: were there a
+      // condition on these loads, what is asked for before them would be waited for together with them.
+      uint32_t st = first + wk;
+      if (st < last) {
+        uint32_t ids[2] = {0, 0}, ahead[2] = {0, 0};
+        pages_of(st, ids);
+        if (st + WK < last) pages_of(st + WK, ahead);
+        load_keys(st, ids);
+        __builtin_amdgcn_sched_barrier(0);  // (loads are waited for in their order: in the loop keys come first)
+        load_values(st, ids);
+        bool more;
+        do {
+          more = st + WK < last;
+          const uint32_t next = more ? st + WK : st;
+          if (more) {
+            ids[0] = ahead[0];
+            ids[1] = ahead[1];
+          }
+          scores();
+          load_keys(next, ids);
+          __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
+          if (next + WK < last) pages_of(next + WK, ahead);
+          edge(st);
+          weights();
+          edge_values(st);
+          outputs();
+          load_values(next, ids);
+          st = next;
+        } while (more);
       }
       // What has been left out, by the same product on ones: how many infinities of either sign, and NaN, a row sees of every element.
-      if (__any(bad != 0))
-        for (st = edge; st < last; st += WK) {
-          if (st < cached) continue;
+      if (bad)
+        for (st = first + wk; st < last; st += WK) {
+          if ((st + 1) * kStep <= (uint32_t)q.len) continue;
           for (int kind = 0; kind < 3; ++kind) {
-            load_edge_values(st);
+            uint32_t ids[2] = {0, 0};
+            pages_of(st, ids);
+            load_values(st, ids);
             const auto one = [&](uint32_t v) {
               const bool is = kind == 2 ? (v & 0x7fff) > T::kExponent : v == (T::kExponent | (uint32_t)kind << 15);
               return is ? T::kOne : 0u;
@@ -559,11 +558,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
   }
 }
 
-// The sums of segments that several workers share: a wavefront for every 16 rows.
+// The sums of segments that several workers share, 16 rows to a workgroup, whose wavefronts take every fourth worker's each.
 template <class T, int DT, int NR, int WR>
-__global__ __launch_bounds__(64) void ft_tree_join_kernel(Tree a) {
+__global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree a) {
   constexpr int E = DT / 16, ROWS = 16 * NR * WR;
-  const int lane = threadIdx.x, n16 = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  __shared__ float top[16][16], total[4][16];
+  __shared__ Floats4 join[3][E][64];
   const uint32_t r = blockIdx.x / a.c.heads, head = blockIdx.x - r * a.c.heads;
   const uint32_t tile = blockIdx.y / (NR * WR), part = blockIdx.y - tile * (NR * WR);
   const Request q = request(a, r);
@@ -574,19 +575,33 @@ __global__ __launch_bounds__(64) void ft_tree_join_kernel(Tree a) {
   const uint32_t w0 = (uint32_t)(begin / per), w1 = (uint32_t)((begin + steps - 1) / per);
   if (w0 == w1) return;
   const auto at = [&](uint32_t w) { return a.sums + (((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * (WR * NR) + part) * Partial<DT>::kTile; };
-  float now = -INFINITY, l = 0;
-  for (uint32_t w = w0; w <= w1; ++w) now = fmaxf(now, at(w)[16 * DT + n16]);
+  float now = -INFINITY;
+  for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) now = fmaxf(now, at(w)[16 * DT + n16]);
+  top[threadIdx.x >> 4][n16] = now;
+  __syncthreads();
+  for (int i = 0; i < 16; ++i) now = fmaxf(now, top[i][n16]);
   const float from = now == -INFINITY ? 0 : now;
+  float l = 0;
   Floats4 acc[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) acc[j] = Floats4{0, 0, 0, 0};
-  for (uint32_t w = w0; w <= w1; ++w) {
+  for (uint32_t w = w0 + wave; w <= w1; w += 4) {
     const float *sums = at(w);
     const float shrink = __builtin_amdgcn_exp2f(sums[16 * DT + n16] - from);
     l += sums[16 * DT + 16 + n16] * shrink;
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[j] += reinterpret_cast<const Floats4 *>(sums)[j * 64 + lane] * shrink;
   }
+  if (g == 0) total[wave][n16] = l;
+  if (wave != 0)
+#pragma unroll
+    for (int j = 0; j < E; ++j) join[wave - 1][j][lane] = acc[j];
+  __syncthreads();
+  if (wave != 0) return;
+  l = ((total[0][n16] + total[1][n16]) + total[2][n16]) + total[3][n16];
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] += join[w][j][lane];
   write_row<T, DT>(a, acc, l, now, q, tile * ROWS + part * 16 + n16, head, g);
 }
 
@@ -605,7 +620,7 @@ Shape shape_of(uint32_t dim, uint64_t rows) {
   return {dt, 2, 4};
 }
 
-uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(s.nr == 2 || s.dt == 256 ? cu_count : 2 * cu_count) / 8 * 8 + 8; }
+uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(s.nr * s.dt >= 256 ? cu_count : 2 * cu_count) / 8 * 8 + 8; }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
@@ -616,7 +631,7 @@ hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint64_t tiles = (rows + 16 * NR * WR - 1) / (16 * NR * WR) * NR * WR;
-  hipLaunchKernelGGL((ft_tree_join_kernel<T, DT, NR, WR>), dim3(a.t.requests * a.c.heads, (uint32_t)tiles), dim3(64), 0, stream, a);
+  hipLaunchKernelGGL((ft_tree_join_kernel<T, DT, NR, WR>), dim3(a.t.requests * a.c.heads, (uint32_t)tiles), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -661,8 +676,8 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.flip = t.scale < 0 ? 0x80008000u : 0;
   a.prefix = static_cast<uint64_t *>(t.workspace);
   a.sums = reinterpret_cast<float *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
-  // 16 keys lie within 2 GiB of each other
-  const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && c.token_stride < 1u << 25;
+  // strides of 24 bits in bytes
+  const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && (c.token_stride | t.k_token_stride | t.v_token_stride) < 1u << 23;
   return c.type == FT_BF16 ? launch_dim<Bf16>(a, s, paged, rows, stream) : launch_dim<Fp16>(a, s, paged, rows, stream);
 }
 

@@ -36,7 +36,7 @@ struct Bf16 {
     typedef __bf16 V __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((F{lo, hi}), V));
   }
-  static constexpr uint32_t kExponent = 0x7f80, kOne = 0x3f80;  // an exponent of all ones: infinite or NaN
+  static constexpr uint32_t kExponent = 0x7f80, kLowest = 0x0080, kOne = 0x3f80;  // an exponent of all ones (infinite or NaN), its lowest bit
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef __bf16 V __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
@@ -51,7 +51,7 @@ struct Fp16 {
     typedef _Float16 V __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((F{lo, hi}), V));
   }
-  static constexpr uint32_t kExponent = 0x7c00, kOne = 0x3c00;
+  static constexpr uint32_t kExponent = 0x7c00, kLowest = 0x0400, kOne = 0x3c00;
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef _Float16 V __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
