@@ -18,6 +18,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;     // keys
+constexpr uint32_t kSegment = 6;  // what a segment costs beside its steps, in steps
 // How far, in powers of two, a score may pass the maximum that weights are relative to before sums are brought to a new one: weights
 // stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
 constexpr float kSlack = 8.0f;
@@ -56,6 +57,9 @@ __device__ inline float row_sum(float v) {
 typedef const __attribute__((address_space(4))) int32_t *Constants;
 __device__ inline Constants constants(const int32_t *p) { return reinterpret_cast<Constants>(reinterpret_cast<uintptr_t>(p)); }
 
+// n / d; both are nearly always small, and a division of 64 bits is long
+__device__ inline uint64_t quotient(uint64_t n, uint32_t d) { return n >> 32 == 0 ? (uint32_t)n / d : n / d; }
+
 struct Request {
   int start, n, len;  // drafted tokens from `start`, cached ones
 };
@@ -74,11 +78,11 @@ __device__ inline Request request(const Tree &a, uint32_t r) {
 
 __device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len + (kStep - 1)) >> 5) + (uint32_t)((q.n + (kStep - 1)) >> 5); }
 
-// Work of a request: for each key head and each tile of `rows` rows all of its steps.
+// Work of a request: for each key head and each tile of `rows` rows, which is a segment, what it costs to begin with and all of its steps.
 __device__ inline uint64_t work_of(const Tree &a, uint32_t r, uint32_t rows) {
   const Request q = request(a, r);
   const uint32_t tiles = ((uint32_t)q.n * a.group + rows - 1) / rows;
-  return (uint64_t)a.c.heads * tiles * steps_of(q);
+  return (uint64_t)a.c.heads * tiles * (steps_of(q) + kSegment);
 }
 
 // A worker's sums of a segment that it has a part of: [16 rows][4 elements x 64 lanes of every product], then a row's maximum and sum.
@@ -116,28 +120,25 @@ __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t by
   return out;
 }
 
-// NR: tiles of 16 rows a wavefront has. WR: wavefronts that have different rows; 4 / WR share the keys among them.
+// NR: tiles of 16 rows a wavefront has. WR: wavefronts of a worker, which have different rows and read the same keys.
 // PAGED: the head has DT elements and a page a multiple of 16 tokens, so 16 keys are read from one base address that is the same for all
 // lanes; without it every lane finds the row of one key, and hands it on to those that read it.
 template <class T, int DT, int NR, int WR, bool PAGED>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 256 ? 2 : 1, NR * DT < 256 ? 2 : 1))) void ft_tree_kernel(Tree a) {
-  constexpr int E = DT / 16, KS = DT / 32, WK = 4 / WR, RT = 16 * NR, ROWS = RT * WR;
+__global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT < 256 ? 2 : 1, NR * DT < 256 ? 2 : 1))) void ft_tree_kernel(Tree a) {
+  constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
   const ft_tree_call &t = a.t;
   const KvView &c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
-  const int wave = (int)uniform((uint32_t)(tid >> 6)), wr = wave / WK, wk = wave % WK;
-  __shared__ uint64_t scan[4];
-  __shared__ uint64_t found[3];  // the request that this worker begins in, steps of it that others have, steps that this one has
-  __shared__ float stat[4][2][RT];
-  constexpr int kJoin = WK > 1 ? WR * (WK - 1) * NR * E * 256 : 1;
-  __shared__ float join[kJoin];
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+  const int wr = (int)uniform((uint32_t)threadIdx.x >> 6);
 
   // The workers next to each other go to the same die: they read the same pages for other rows.
   const uint32_t per_die = gridDim.x / 8;
   const uint32_t worker = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
+  // Every wavefront sums up the requests' work for itself, a lane a few that are neighbours, and finds where it begins.
+  uint32_t r;
+  uint64_t at, left;
   {
-    // Every workgroup sums up the requests' work for itself: a thread has a few that are neighbours.
-    const uint32_t each = (t.requests + 255) / 256, r0 = tid * each < t.requests ? tid * each : t.requests, r1 = r0 + each < t.requests ? r0 + each : t.requests;
+    const uint32_t each = (t.requests + 63) / 64, r0 = lane * each < t.requests ? lane * each : t.requests, r1 = r0 + each < t.requests ? r0 + each : t.requests;
     uint64_t mine = 0, sum;
     for (uint32_t i = r0; i < r1; ++i) mine += work_of(a, i, ROWS);
     sum = mine;
@@ -145,38 +146,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
       const uint64_t other = __shfl_up(sum, d);
       if (lane >= d) sum += other;
     }
-    if (lane == 63) scan[wave] = sum;
-    __syncthreads();
-    uint64_t all = 0, before = sum - mine;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) before += scan[w];
-      all += scan[w];
-    }
-    uint64_t per = (all + a.workers - 1) / a.workers;
+    const uint64_t all = from_lane(sum, 63), before = sum - mine;
+    uint64_t per = quotient(all + a.workers - 1, a.workers);
     if (per < a.least) per = a.least;
     const uint64_t begin = per * worker;
-    if (worker == 0) {
+    if (worker == 0 && wr == 0) {
       uint64_t sofar = before;
       for (uint32_t i = r0; i < r1; ++i) {
         a.prefix[i] = sofar;
         sofar += r1 - r0 == 1 ? mine : work_of(a, i, ROWS);
       }
-      if (tid == 0) a.prefix[t.requests] = per;
+      if (lane == 0) a.prefix[t.requests] = per;
     }
     if (begin >= all) return;
-    if (begin >= before && begin < before + mine) {
-      uint32_t i = r0;
-      if (r1 - r0 > 1)
-        for (;; ++i) {
-          const uint64_t w = work_of(a, i, ROWS);
-          if (begin < before + w) break;
-          before += w;
-        }
-      found[0] = i;
-      found[1] = begin - before;
-      found[2] = all - begin < per ? all - begin : per;
-    }
-    __syncthreads();
+    left = uniform(all - begin < per ? all - begin : per);
+    uint32_t i = r0;
+    uint64_t sofar = before;
+    const bool here = begin >= before && begin < before + mine;
+    if (here && r1 - r0 > 1)
+      for (;; ++i) {
+        const uint64_t w = work_of(a, i, ROWS);
+        if (begin < sofar + w) break;
+        sofar += w;
+      }
+    const int finder = __builtin_ctzll(__ballot(here));
+    r = uniform((uint32_t)__shfl((int)i, finder));
+    at = uniform(from_lane(begin - sofar, finder));
   }
   // What the loop over keys goes by, each in a register of its own (as parts of the argument's words they would come and go with those). PAGED only.
   uint32_t row_bytes = 2 * (uint32_t)c.token_stride, k_bytes = 2 * (uint32_t)t.k_token_stride, v_bytes = 2 * (uint32_t)t.v_token_stride;
@@ -184,21 +179,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
   uint64_t page_bytes = 2 * c.page_stride;
   float scale = a.scale;
   asm volatile("" : "+s"(row_bytes), "+s"(k_bytes), "+s"(v_bytes), "+s"(pages), "+s"(page_d), "+s"(page_m), "+s"(page_shift), "+s"(page_bytes), "+s"(scale));
-  uint32_t left = uniform((uint32_t)found[2]), r = uniform((uint32_t)found[0]);
-  uint64_t at = uniform(found[1]);
 
   for (; left != 0; ++r, at = 0) {
     const Request q = request(a, r);
-    const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
+    const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS, cost = steps + kSegment;
     if (tiles == 0) continue;
     const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
     const uint64_t segments = (uint64_t)c.heads * tiles;
     const Constants table = constants(t.table + (uint64_t)r * t.blocks);
-    for (uint64_t seg = at / steps; seg < segments && left != 0; ++seg) {
-      const uint32_t first = (uint32_t)(at > seg * steps ? at - seg * steps : 0);
-      const uint32_t last = steps - first < left ? steps : first + left;
-      left -= last - first;
-      const uint32_t head = uniform((uint32_t)(seg / tiles)), tile = uniform((uint32_t)(seg - (uint64_t)head * tiles));
+    uint64_t seg = quotient(at, cost);
+    for (at -= seg * cost; seg < segments && left != 0; ++seg, at = 0) {
+      // this worker's part of the segment's cost, and of its steps
+      const uint32_t from = (uint32_t)at, to = cost - from < left ? cost : from + (uint32_t)left;
+      left -= to - from;
+      const uint32_t first = from < kSegment ? 0 : from - kSegment, last = to < kSegment ? 0 : to - kSegment;
+      if (first == last) continue;
+      const uint32_t head = uniform((uint32_t)quotient(seg, tiles)), tile = uniform((uint32_t)(seg - (uint64_t)head * tiles));
       const uint32_t row0 = tile * ROWS + wr * RT;
       const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
       const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
@@ -436,18 +432,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
       // A step's keys are on their way while the one before weighs its values, its values from there on, and the pages of the one behind it
       // are asked for first of all. The last step asks for its own rows once more, which are near by then: were there a
       // condition on these loads, what is asked for before them would be waited for together with them.
-      uint32_t st = first + wk;
-      if (st < last) {
+      uint32_t st = first;
+      {
         uint32_t ids[2] = {0, 0}, ahead[2] = {0, 0};
         pages_of(st, ids);
-        if (st + WK < last) pages_of(st + WK, ahead);
+        if (st + 1 < last) pages_of(st + 1, ahead);
         load_keys(st, ids);
         __builtin_amdgcn_sched_barrier(0);  // (loads are waited for in their order: in the loop keys come first)
         load_values(st, ids);
         bool more;
         do {
-          more = st + WK < last;
-          const uint32_t next = more ? st + WK : st;
+          more = st + 1 < last;
+          const uint32_t next = more ? st + 1 : st;
           if (more) {
             ids[0] = ahead[0];
             ids[1] = ahead[1];
@@ -455,7 +451,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
           scores();
           load_keys(next, ids);
           __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
-          if (next + WK < last) pages_of(next + WK, ahead);
+          if (next + 1 < last) pages_of(next + 1, ahead);
           edge(st);
           weights();
           edge_values(st);
@@ -466,7 +462,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
       }
       // What has been left out, by the same product on ones: how many infinities of either sign, and NaN, a row sees of every element.
       if (bad)
-        for (st = first + wk; st < last; st += WK) {
+        for (st = first; st < last; ++st) {
           if ((st + 1) * kStep <= (uint32_t)q.len) continue;
           for (int kind = 0; kind < 3; ++kind) {
             uint32_t ids[2] = {0, 0};
@@ -504,39 +500,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR * DT < 2
 
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) l[nr] = row_sum(l[nr]);
-      if constexpr (WK > 1) {
-        __syncthreads();  // what the segment before has left here has been read
-        if (g == 0)
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            stat[wave][0][nr * 16 + n16] = m[nr];
-            stat[wave][1][nr * 16 + n16] = l[nr];
-          }
-        __syncthreads();
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-          float now = -INFINITY, sum = 0;
-          for (int w = 0; w < WK; ++w) now = fmaxf(now, stat[wr * WK + w][0][nr * 16 + n16]);
-          const float from = now == -INFINITY ? 0 : now;
-          for (int w = 0; w < WK; ++w) sum += stat[wr * WK + w][1][nr * 16 + n16] * __builtin_amdgcn_exp2f(stat[wr * WK + w][0][nr * 16 + n16] - from);
-          const float shrink = __builtin_amdgcn_exp2f(m[nr] - from);
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            acc[nr][j] *= shrink;
-            if (wk != 0) reinterpret_cast<Floats4 *>(join)[(((wr * (WK - 1) + wk - 1) * NR + nr) * E + j) * 64 + lane] = acc[nr][j];
-          }
-          m[nr] = now;
-          l[nr] = sum;
-        }
-        __syncthreads();
-        if (wk == 0)
-          for (int w = 0; w < WK - 1; ++w)
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-              for (int j = 0; j < E; ++j) acc[nr][j] += reinterpret_cast<Floats4 *>(join)[(((wr * (WK - 1) + w) * NR + nr) * E + j) * 64 + lane];
-      }
-      if (wk == 0) {
+      {
         if (first == 0 && last == steps) {
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
@@ -571,7 +535,7 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree a) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
   if (tile >= tiles || tile * ROWS + part * 16 >= (uint32_t)q.n * a.group) return;
   const uint32_t steps = steps_of(q);
-  const uint64_t per = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)head * tiles + tile) * steps;
+  const uint64_t per = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)head * tiles + tile) * (steps + kSegment) + kSegment;
   const uint32_t w0 = (uint32_t)(begin / per), w1 = (uint32_t)((begin + steps - 1) / per);
   if (w0 == w1) return;
   const auto at = [&](uint32_t w) { return a.sums + (((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * (WR * NR) + part) * Partial<DT>::kTile; };
@@ -609,8 +573,8 @@ struct Shape {
   int dt, nr, wr;
 };
 
-// Heads are padded to 64, 128 or 256 elements. Up to 16 rows a tile of them is one wavefront's, and four share the keys; then two such
-// tiles; then wavefronts with other rows, which read the same keys.
+// Heads are padded to 64, 128 or 256 elements. A wavefront has up to 32 rows (16 where heads are large), beyond that workers are several
+// wavefronts.
 Shape shape_of(uint32_t dim, uint64_t rows) {
   const int dt = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
   if (rows <= 16) return {dt, 1, 1};
@@ -620,14 +584,15 @@ Shape shape_of(uint32_t dim, uint64_t rows) {
   return {dt, 2, 4};
 }
 
-uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(s.nr * s.dt >= 256 ? cu_count : 2 * cu_count) / 8 * 8 + 8; }
+// As many as the chip holds, a multiple of its dies: two wavefronts, or one of more registers, to each of a compute unit's four parts.
+uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(cu_count * (s.nr * s.dt >= 256 ? 4 : 8) / s.wr + 7) / 8 * 8; }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
 template <class T, int DT, int NR, int WR>
 hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(256), 0, stream, a);
+  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(64 * WR), 0, stream, a);
+  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(64 * WR), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint64_t tiles = (rows + 16 * NR * WR - 1) / (16 * NR * WR) * NR * WR;
@@ -670,7 +635,7 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
   a.workers = workers_of(s, cu_count);
-  a.least = 2 * (4 / s.wr);
+  a.least = kSegment + 2;
   a.scale = t.scale == 0 ? 1 : (t.scale < 0 ? -t.scale : t.scale) * kLog2e;
   a.keep = t.scale == 0 ? 0 : ~0u;
   a.flip = t.scale < 0 ? 0x80008000u : 0;
