@@ -18,7 +18,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;     // keys
-constexpr uint32_t kSegment = 6;  // what a segment costs beside its steps, in steps
+constexpr uint32_t kSegment = 3;  // what a segment costs beside its steps, in steps
 // How far, in powers of two, a score may pass the maximum that weights are relative to before sums are brought to a new one: weights
 // stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
 constexpr float kSlack = 8.0f;
@@ -27,11 +27,11 @@ struct Tree {
   KvView c;
   ft_tree_call t;
   uint32_t group;        // query heads of a key head
+  uint32_t together;     // key heads that a worker reads, a wavefront (or WR of them) each
   Divisor by_group;
   uint32_t workers, least;  // workgroups, and steps that each takes at least
-  float scale;           // |scale| log2 e
-  uint32_t keep, flip;   // of two queries: nothing where the scale is zero; the sign bits where it is negative
-  uint64_t *prefix;      // requests + 2: steps of the requests before, of all; steps a worker
+  float scale;           // of products, times log2 e
+  uint64_t *prefix;      // requests + 1: work of the requests before; the workers' rate
   float *sums;           // partial results, see Partial
 };
 
@@ -57,14 +57,41 @@ __device__ inline float row_sum(float v) {
 typedef const __attribute__((address_space(4))) int32_t *Constants;
 __device__ inline Constants constants(const int32_t *p) { return reinterpret_cast<Constants>(reinterpret_cast<uintptr_t>(p)); }
 
+// Workers' ranges: worker w has units [begin_of(w), begin_of(w + 1)), `rate` of them on average in 48.16 bits. All are as long but for
+// one, so that no die has less to read than another.
+__device__ inline uint64_t rate_of(uint64_t all, uint32_t workers, uint32_t least) {
+  const uint64_t rate = ((all << 16) + workers - 1) / workers;
+  return rate < (uint64_t)least << 16 ? (uint64_t)least << 16 : rate;
+}
+__device__ inline uint64_t begin_of(uint32_t worker, uint64_t rate) { return worker * rate >> 16; }
+__device__ inline uint32_t worker_of(uint64_t unit, uint64_t rate) { return (uint32_t)(((unit + 1 << 16) - 1) / rate); }
+
 // n / d; both are nearly always small, and a division of 64 bits is long
 __device__ inline uint64_t quotient(uint64_t n, uint32_t d) { return n >> 32 == 0 ? (uint32_t)n / d : n / d; }
+
+// A kernel's argument where it lies. What is read through it is read where it is used: the compiler would have all of it in scalar
+// registers from the start, which are too few.
+typedef const __attribute__((address_space(4))) Tree *Argument;
+__device__ inline Argument argument() {
+  Argument a = reinterpret_cast<Argument>(reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr()));
+  asm volatile("" : "+s"(a));
+  return a;
+}
+template <class D>
+__device__ inline Divisor divisor(const D &d) {
+  Divisor out;
+  out.d = d.d;
+  out.m = d.m;
+  out.shift = d.shift;
+  return out;
+}
 
 struct Request {
   int start, n, len;  // drafted tokens from `start`, cached ones
 };
 
-__device__ inline Request request(const Tree &a, uint32_t r) {
+template <class A>
+__device__ inline Request request(const A &a, uint32_t r) {
   const int tokens = (int)a.t.tokens;
   const Constants starts = constants(a.t.starts);
   int s = starts[r], e = starts[r + 1], len = constants(a.t.lens)[r];
@@ -78,11 +105,12 @@ __device__ inline Request request(const Tree &a, uint32_t r) {
 
 __device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len + (kStep - 1)) >> 5) + (uint32_t)((q.n + (kStep - 1)) >> 5); }
 
-// Work of a request: for each key head and each tile of `rows` rows, which is a segment, what it costs to begin with and all of its steps.
-__device__ inline uint64_t work_of(const Tree &a, uint32_t r, uint32_t rows) {
-  const Request q = request(a, r);
+// Work of a request: for each few key heads that are read together and each tile of `rows` rows, which are a segment, what it costs to begin with
+// and all of its steps.
+template <class A>
+__device__ inline uint64_t work_of(const A &a, const Request &q, uint32_t rows) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + rows - 1) / rows;
-  return (uint64_t)a.c.heads * tiles * (steps_of(q) + kSegment);
+  return (uint64_t)(a.c.heads / a.together) * tiles * (steps_of(q) + kSegment);
 }
 
 // A worker's sums of a segment that it has a part of: [16 rows][4 elements x 64 lanes of every product], then a row's maximum and sum.
@@ -92,10 +120,10 @@ struct Partial {
 };
 
 // The elements of one row that a lane holds: O[E (4 g + i) + j] in acc[j][i].
-template <class T, int DT>
-__device__ inline void write_row(const Tree &a, const Floats4 (&acc)[DT / 16], float l, float m, const Request &q, uint32_t row, uint32_t kv_head, int g) {
+template <class T, int DT, class A>
+__device__ inline void write_row(const A &a, const Floats4 (&acc)[DT / 16], float l, float m, const Request &q, uint32_t row, uint32_t kv_head, int g) {
   constexpr int E = DT / 16;
-  const uint32_t token = a.by_group.of(row), head = kv_head * a.group + (row - token * a.group);
+  const uint32_t token = divisor(a.by_group).of(row), head = kv_head * a.group + (row - token * a.group);
   if ((int)token >= q.n) return;
   const uint64_t t = (uint64_t)(q.start + (int)token);
   uint16_t *out = static_cast<uint16_t *>(a.t.out) + t * a.t.out_token_stride + head * a.t.out_head_stride + 4 * E * g;
@@ -111,6 +139,9 @@ __device__ inline void write_row(const Tree &a, const Floats4 (&acc)[DT / 16], f
   if (g == 0 && a.t.lse != nullptr) a.t.lse[t * a.t.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Wavefronts to each of a compute unit's four parts: what their registers leave room for.
+constexpr int waves(int dt, int nr, bool paged) { return dt <= 128 && nr * dt <= (paged ? 256 : 128) ? 2 : 1; }
+
 // Two bytes of each of eight rows, as the matrix instruction wants them.
 template <int W>
 __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t bytes) {
@@ -120,16 +151,16 @@ __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t by
   return out;
 }
 
-// NR: tiles of 16 rows a wavefront has. WR: wavefronts of a worker, which have different rows and read the same keys.
+// NR: tiles of 16 rows a wavefront has. WR: wavefronts that have different rows and read the same keys. A worker is that many for each of
+// the key heads that it reads, side by side in step: where a token's heads lie next to each other, as they mostly do, memory is read
+// in longer pieces than one head's.
 // PAGED: the head has DT elements and a page a multiple of 16 tokens, so 16 keys are read from one base address that is the same for all
 // lanes; without it every lane finds the row of one key, and hands it on to those that read it.
 template <class T, int DT, int NR, int WR, bool PAGED>
-__global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT < 256 ? 2 : 1, NR * DT < 256 ? 2 : 1))) void ft_tree_kernel(Tree a) {
+__global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED), waves(DT, NR, PAGED)))) void ft_tree_kernel(Tree) {
   constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
-  const ft_tree_call &t = a.t;
-  const KvView &c = a.c;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
-  const int wr = (int)uniform((uint32_t)threadIdx.x >> 6);
+  const uint32_t wave = uniform((uint32_t)threadIdx.x >> 6), wr = wave % WR;
 
   // The workers next to each other go to the same die: they read the same pages for other rows.
   const uint32_t per_die = gridDim.x / 8;
@@ -137,56 +168,62 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
   // Every wavefront sums up the requests' work for itself, a lane a few that are neighbours, and finds where it begins.
   uint32_t r;
   uint64_t at, left;
+  Request q;
   {
-    const uint32_t each = (t.requests + 63) / 64, r0 = lane * each < t.requests ? lane * each : t.requests, r1 = r0 + each < t.requests ? r0 + each : t.requests;
+    const auto &a = *argument();
+    const uint32_t requests = a.t.requests, each = (requests + 63) / 64, r0 = lane * each < requests ? lane * each : requests;
+    const uint32_t r1 = r0 + each < requests ? r0 + each : requests;
     uint64_t mine = 0, sum;
-    for (uint32_t i = r0; i < r1; ++i) mine += work_of(a, i, ROWS);
+    Request one{0, 0, 0};
+    for (uint32_t i = r0; i < r1; ++i) {
+      one = request(a, i);
+      mine += work_of(a, one, ROWS);
+    }
     sum = mine;
     for (int d = 1; d < 64; d <<= 1) {
       const uint64_t other = __shfl_up(sum, d);
       if (lane >= d) sum += other;
     }
-    const uint64_t all = from_lane(sum, 63), before = sum - mine;
-    uint64_t per = quotient(all + a.workers - 1, a.workers);
-    if (per < a.least) per = a.least;
-    const uint64_t begin = per * worker;
-    if (worker == 0 && wr == 0) {
+    const uint64_t all = from_lane(sum, 63), before = sum - mine, rate = rate_of(all, a.workers, a.least);
+    if (worker == 0 && wave == 0) {
       uint64_t sofar = before;
       for (uint32_t i = r0; i < r1; ++i) {
         a.prefix[i] = sofar;
-        sofar += r1 - r0 == 1 ? mine : work_of(a, i, ROWS);
+        sofar += r1 - r0 == 1 ? mine : work_of(a, request(a, i), ROWS);
       }
-      if (lane == 0) a.prefix[t.requests] = per;
+      if (lane == 0) a.prefix[requests] = rate;
     }
+    const uint64_t begin = begin_of(worker, rate), end = begin_of(worker + 1, rate);
     if (begin >= all) return;
-    left = uniform(all - begin < per ? all - begin : per);
+    left = uniform((end < all ? end : all) - begin);
     uint32_t i = r0;
     uint64_t sofar = before;
     const bool here = begin >= before && begin < before + mine;
     if (here && r1 - r0 > 1)
       for (;; ++i) {
-        const uint64_t w = work_of(a, i, ROWS);
+        one = request(a, i);
+        const uint64_t w = work_of(a, one, ROWS);
         if (begin < sofar + w) break;
         sofar += w;
       }
     const int finder = __builtin_ctzll(__ballot(here));
     r = uniform((uint32_t)__shfl((int)i, finder));
     at = uniform(from_lane(begin - sofar, finder));
+    q = {(int)uniform((uint32_t)__shfl(one.start, finder)), (int)uniform((uint32_t)__shfl(one.n, finder)), (int)uniform((uint32_t)__shfl(one.len, finder))};
   }
   // What the loop over keys goes by, each in a register of its own (as parts of the argument's words they would come and go with those). PAGED only.
-  uint32_t row_bytes = 2 * (uint32_t)c.token_stride, k_bytes = 2 * (uint32_t)t.k_token_stride, v_bytes = 2 * (uint32_t)t.v_token_stride;
-  uint32_t pages = c.pages, page_d = c.page_tokens.d, page_m = c.page_tokens.m, page_shift = c.page_tokens.shift;
-  uint64_t page_bytes = 2 * c.page_stride;
-  float scale = a.scale;
+  const Argument all = argument();
+  uint32_t row_bytes = 2 * (uint32_t)all->c.token_stride, k_bytes = 2 * (uint32_t)all->t.k_token_stride, v_bytes = 2 * (uint32_t)all->t.v_token_stride;
+  uint32_t pages = all->c.pages, page_d = all->c.page_tokens.d, page_m = all->c.page_tokens.m, page_shift = all->c.page_tokens.shift;
+  uint64_t page_bytes = 2 * all->c.page_stride;
+  float scale = all->scale;
   asm volatile("" : "+s"(row_bytes), "+s"(k_bytes), "+s"(v_bytes), "+s"(pages), "+s"(page_d), "+s"(page_m), "+s"(page_shift), "+s"(page_bytes), "+s"(scale));
 
-  for (; left != 0; ++r, at = 0) {
-    const Request q = request(a, r);
-    const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS, cost = steps + kSegment;
-    if (tiles == 0) continue;
+  for (;;) {
+    const uint32_t together = argument()->together, heads = argument()->c.heads, group = argument()->group;
+    const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * group + ROWS - 1) / ROWS, cost = steps + kSegment;
     const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
-    const uint64_t segments = (uint64_t)c.heads * tiles;
-    const Constants table = constants(t.table + (uint64_t)r * t.blocks);
+    const uint64_t segments = (uint64_t)(heads / together) * tiles;
     uint64_t seg = quotient(at, cost);
     for (at -= seg * cost; seg < segments && left != 0; ++seg, at = 0) {
       // this worker's part of the segment's cost, and of its steps
@@ -194,28 +231,32 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
       left -= to - from;
       const uint32_t first = from < kSegment ? 0 : from - kSegment, last = to < kSegment ? 0 : to - kSegment;
       if (first == last) continue;
-      const uint32_t head = uniform((uint32_t)quotient(seg, tiles)), tile = uniform((uint32_t)(seg - (uint64_t)head * tiles));
+      const auto &a = *argument();
+      const auto &t = a.t;
+      const auto &c = a.c;
+      const Constants table = constants(t.table + (uint64_t)r * t.blocks);
+      const uint32_t heads_before = uniform((uint32_t)quotient(seg, tiles)), tile = uniform((uint32_t)(seg - (uint64_t)heads_before * tiles));
+      const uint32_t head = heads_before * together + wave / WR;
       const uint32_t row0 = tile * ROWS + wr * RT;
       const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
       const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
       const char *vd = static_cast<const char *>(t.v) + 2 * (q.start * t.v_token_stride + head * t.v_head_stride);
 
       Words4 qf[NR][KS];
-      int token[NR];
+      // rows behind the last one are answered as that one is, and not written
+      const auto row_of = [&](int nr) -> uint32_t {
+        const uint32_t row = row0 + nr * 16 + n16, most = (uint32_t)q.n * group - 1;
+        return row < most ? row : most;
+      };
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) {
-        uint32_t row = row0 + nr * 16 + n16;
-        const uint32_t most = (uint32_t)q.n * a.group - 1;
-        row = row < most ? row : most;  // rows behind the last one are answered and not written
-        const uint32_t tok = a.by_group.of(row);
-        token[nr] = (int)tok;
-        const uint16_t *p = static_cast<const uint16_t *>(t.q) + (q.start + (int)tok) * t.q_token_stride + (head * a.group + (row - tok * a.group)) * t.q_head_stride;
+        const uint32_t row = row_of(nr), tok = divisor(a.by_group).of(row);
+        const uint16_t *p = static_cast<const uint16_t *>(t.q) + (q.start + (int)tok) * t.q_token_stride + (head * group + (row - tok * group)) * t.q_head_stride;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const int d = ks * 32 + 8 * g;
-          Words4 w{0, 0, 0, 0};
-          if (PAGED || d < (int)c.dim) w = load16(p + d);
-          qf[nr][ks] = (w & a.keep) ^ a.flip;
+          if (PAGED || d < (int)c.dim) qf[nr][ks] = load16(p + d);
+          else qf[nr][ks] = Words4{0, 0, 0, 0};
         }
       }
       Floats4 acc[NR][E];
@@ -245,7 +286,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
           }
         } else {
           const uint32_t key = st * kStep + (lane & 31);
-          ids[0] = (uint32_t)table[c.page_tokens.of(key < end_key ? key : end_key)];
+          ids[0] = (uint32_t)table[divisor(c.page_tokens).of(key < end_key ? key : end_key)];
         }
       };
       // Lane l % 32's row as an offset in bytes from the head's first one (without PAGED), of cached and of drafted keys.
@@ -253,7 +294,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
         uint32_t key = st * kStep + (lane & 31), draft = key - cached * kStep;
         key = key < end_key ? key : end_key;
         draft = draft < (uint32_t)q.n ? draft : (uint32_t)q.n - 1;
-        const uint64_t in_cache = (page < c.pages ? page : 0) * c.page_stride + c.page_tokens.rest(key) * c.token_stride;
+        const uint64_t in_cache = (page < c.pages ? page : 0) * c.page_stride + divisor(c.page_tokens).rest(key) * c.token_stride;
         return 2 * (st < cached ? in_cache : draft * draft_stride);
       };
       // PAGED: where 16 keys of a step begin, in bytes from the head's first one, and how many rows there are behind that one.
@@ -335,10 +376,11 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
         const uint32_t js = st - cached, valid = drafted ? (uint32_t)q.n - js * kStep : (uint32_t)q.len - st * kStep;
         uint32_t w = ~0u;
         if (drafted) {
+          const int token = (int)divisor(a.by_group).of(row_of(nr));
           if (t.mask != nullptr) {
-            w = reinterpret_cast<const uint32_t *>(t.mask)[(uint64_t)(q.start + token[nr]) * 2 * t.mask_words + js];
+            w = reinterpret_cast<const uint32_t *>(t.mask)[(uint64_t)(q.start + token) * 2 * t.mask_words + js];
           } else {
-            const int d = token[nr] - (int)(js * kStep);
+            const int d = token - (int)(js * kStep);
             w = d < 0 ? 0 : d >= 31 ? ~0u : (2u << d) - 1;
           }
         }
@@ -362,7 +404,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
         for (int nr = 0; nr < NR; ++nr) {
           float x[8], w[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3] * scale;
+          for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3];
           const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
           if (__any(top > m[nr] + kSlack)) {
             const float now = fmaxf(m[nr], row_max(top));
@@ -452,6 +494,10 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
           load_keys(next, ids);
           __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
           if (next + 1 < last) pages_of(next + 1, ahead);
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] *= scale;
           edge(st);
           weights();
           edge_values(st);
@@ -506,7 +552,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
           for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
         } else {
           // a worker has at most two segments that it shares: the one it begins in, which others have begun, and the one it ends in
-          float *sums = a.sums + ((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * (WR * NR * Partial<DT>::kTile) + wr * NR * Partial<DT>::kTile;
+          float *sums = a.sums + (((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * together * WR + wave) * (NR * Partial<DT>::kTile);
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
@@ -519,12 +565,19 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(NR * DT
         }
       }
     }
+    if (left == 0) return;
+    at = 0;
+    do {
+      if (++r >= argument()->t.requests) return;
+      q = request(*argument(), r);
+    } while (q.n == 0);
   }
 }
 
 // The sums of segments that several workers share, 16 rows to a workgroup, whose wavefronts take every fourth worker's each.
 template <class T, int DT, int NR, int WR>
-__global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree a) {
+__global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
+  const auto &a = *argument();
   constexpr int E = DT / 16, ROWS = 16 * NR * WR;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
   __shared__ float top[16][16], total[4][16];
@@ -535,10 +588,10 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree a) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
   if (tile >= tiles || tile * ROWS + part * 16 >= (uint32_t)q.n * a.group) return;
   const uint32_t steps = steps_of(q);
-  const uint64_t per = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)head * tiles + tile) * (steps + kSegment) + kSegment;
-  const uint32_t w0 = (uint32_t)(begin / per), w1 = (uint32_t)((begin + steps - 1) / per);
+  const uint64_t rate = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)(head / a.together) * tiles + tile) * (steps + kSegment) + kSegment;
+  const uint32_t w0 = worker_of(begin, rate), w1 = worker_of(begin + steps - 1, rate);
   if (w0 == w1) return;
-  const auto at = [&](uint32_t w) { return a.sums + (((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * (WR * NR) + part) * Partial<DT>::kTile; };
+  const auto at = [&](uint32_t w) { return a.sums + ((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.together + head % a.together) * (WR * NR) + part) * Partial<DT>::kTile; };
   float now = -INFINITY;
   for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) now = fmaxf(now, at(w)[16 * DT + n16]);
   top[threadIdx.x >> 4][n16] = now;
@@ -584,15 +637,24 @@ Shape shape_of(uint32_t dim, uint64_t rows) {
   return {dt, 2, 4};
 }
 
-// As many as the chip holds, a multiple of its dies: two wavefronts, or one of more registers, to each of a compute unit's four parts.
-uint32_t workers_of(const Shape &s, int cu_count) { return (uint32_t)(cu_count * (s.nr * s.dt >= 256 ? 4 : 8) / s.wr + 7) / 8 * 8; }
+// Key heads that a worker reads: as many as divide all of them and leave room on a compute unit.
+uint32_t together_of(const Shape &s, bool paged, uint32_t heads) {
+  uint32_t n = (uint32_t)(4 * waves(s.dt, s.nr, paged) / s.wr);
+  while (heads % n != 0) n /= 2;
+  return n;
+}
+
+// As many as the chip holds, a multiple of its dies.
+uint32_t workers_of(const Shape &s, bool paged, uint32_t together, int cu_count) {
+  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged) / (s.wr * (int)together) + 7) / 8 * 8;
+}
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
 template <class T, int DT, int NR, int WR>
 hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(64 * WR), 0, stream, a);
-  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(64 * WR), 0, stream, a);
+  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(64 * WR * a.together), 0, stream, a);
+  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(64 * WR * a.together), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint64_t tiles = (rows + 16 * NR * WR - 1) / (16 * NR * WR) * NR * WR;
@@ -624,7 +686,7 @@ uint64_t rows_of(const ft_tree_call &t, uint32_t heads) {
 
 uint64_t tree_workspace(const ft_kv_cache &c, const ft_tree_call &t, int cu_count) {
   const Shape s = shape_of(c.dim, rows_of(t, c.heads));
-  return up16(((uint64_t)t.requests + 2) * 8) + (uint64_t)workers_of(s, cu_count) * 2 * s.nr * s.wr * (16 * s.dt + 32) * 4;
+  return up16(((uint64_t)t.requests + 2) * 8) + ((uint64_t)cu_count * 4 * waves(s.dt, s.nr, true) + 64) * 2 * s.nr * (16 * s.dt + 32) * 4;
 }
 
 hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hipStream_t stream) {
@@ -632,17 +694,16 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   const Shape s = shape_of(c.dim, rows);
   Tree a{c, t};
   a.t.drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
-  a.group = t.heads / c.heads;
-  a.by_group = Divisor(a.group);
-  a.workers = workers_of(s, cu_count);
-  a.least = kSegment + 2;
-  a.scale = t.scale == 0 ? 1 : (t.scale < 0 ? -t.scale : t.scale) * kLog2e;
-  a.keep = t.scale == 0 ? 0 : ~0u;
-  a.flip = t.scale < 0 ? 0x80008000u : 0;
-  a.prefix = static_cast<uint64_t *>(t.workspace);
-  a.sums = reinterpret_cast<float *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
   // strides of 24 bits in bytes
   const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && (c.token_stride | t.k_token_stride | t.v_token_stride) < 1u << 23;
+  a.together = together_of(s, paged, c.heads);
+  a.workers = workers_of(s, paged, a.together, cu_count);
+  a.group = t.heads / c.heads;
+  a.by_group = Divisor(a.group);
+  a.least = kSegment + 2;
+  a.scale = t.scale * kLog2e;
+  a.prefix = static_cast<uint64_t *>(t.workspace);
+  a.sums = reinterpret_cast<float *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
   return c.type == FT_BF16 ? launch_dim<Bf16>(a, s, paged, rows, stream) : launch_dim<Fp16>(a, s, paged, rows, stream);
 }
 
