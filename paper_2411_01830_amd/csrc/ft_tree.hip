@@ -28,15 +28,24 @@ struct Tree {
   ft_tree_call t;
   uint32_t group;        // query heads of a key head
   uint32_t together;     // key heads that a worker reads, a wavefront (or WR of them) each
+  uint32_t cluster;      // workgroups of a worker, which have different rows
   Divisor by_group;
   uint32_t workers, least;  // workgroups, and steps that each takes at least
   float scale;           // of products, times log2 e
   uint64_t *prefix;      // requests + 1: work of the requests before; the workers' rate
+  uint32_t *flags;       // of every wavefront, whether it has left out values that are not finite
   float *sums;           // partial results, see Partial
 };
 
 __device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ inline uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+
+// A barrier for shared memory alone: loads from global memory stay on their way.
+__device__ inline void fence() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 __device__ inline uint64_t from_lane(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32 | (uint32_t)__shfl((int)(uint32_t)v, lane);
@@ -110,7 +119,7 @@ __device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len
 template <class A>
 __device__ inline uint64_t work_of(const A &a, const Request &q, uint32_t rows) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + rows - 1) / rows;
-  return (uint64_t)(a.c.heads / a.together) * tiles * (steps_of(q) + kSegment);
+  return (uint64_t)(a.c.heads / a.together) * ((tiles + a.cluster - 1) / a.cluster) * (steps_of(q) + kSegment);
 }
 
 // A worker's sums of a segment that it has a part of: [16 rows][4 elements x 64 lanes of every product], then a row's maximum and sum.
@@ -140,7 +149,7 @@ __device__ inline void write_row(const A &a, const Floats4 (&acc)[DT / 16], floa
 }
 
 // Wavefronts to each of a compute unit's four parts: what their registers leave room for.
-constexpr int waves(int dt, int nr, bool paged) { return dt <= 128 && nr * dt <= (paged ? 256 : 128) ? 2 : 1; }
+constexpr int waves(int dt, int nr, bool paged, bool shared) { return dt <= 128 && nr * dt <= (paged || shared ? 256 : 128) ? 2 : 1; }
 
 // Two bytes of each of eight rows, as the matrix instruction wants them.
 template <int W>
@@ -156,15 +165,21 @@ __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t by
 // in longer pieces than one head's.
 // PAGED: the head has DT elements and a page a multiple of 16 tokens, so 16 keys are read from one base address that is the same for all
 // lanes; without it every lane finds the row of one key, and hands it on to those that read it.
-template <class T, int DT, int NR, int WR, bool PAGED>
-__global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED), waves(DT, NR, PAGED)))) void ft_tree_kernel(Tree) {
+// SHARED: keys and values go through shared memory, which the WR wavefronts of a workgroup fill together; several workgroups, a cluster, have
+// the rows beyond those and are next to each other on one die, where the second finds in the cache what the first has read.
+template <class T, int DT, int NR, int WR, bool PAGED, bool SHARED>
+__global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARED)) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED, SHARED), waves(DT, NR, PAGED, SHARED)))) void ft_tree_kernel(Tree) {
   constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
+  // SHARED: 16-byte pieces of a row, those of a step that a thread has, steps that are on their way besides the one in shared memory
+  constexpr int CH = DT / 8, N = SHARED ? CH / (2 * WR) : 1, DEPTH = SHARED ? (NR == 1 ? 4 : 2) / N : 1, NI = SHARED && !PAGED ? N : 2;
+  static_assert(!SHARED || (N >= 1 && N * 2 * WR == CH));
+  __shared__ Words4 tile_lds[SHARED ? 2 : 1][2][SHARED ? 32 * CH : 1];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const uint32_t wave = uniform((uint32_t)threadIdx.x >> 6), wr = wave % WR;
 
   // The workers next to each other go to the same die: they read the same pages for other rows.
   const uint32_t per_die = gridDim.x / 8;
-  const uint32_t worker = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
+  const uint32_t place = (blockIdx.x % 8) * per_die + blockIdx.x / 8, worker = place / argument()->cluster, member = place - worker * argument()->cluster;
   // Every wavefront sums up the requests' work for itself, a lane a few that are neighbours, and finds where it begins.
   uint32_t r;
   uint64_t at, left;
@@ -185,7 +200,7 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
       if (lane >= d) sum += other;
     }
     const uint64_t all = from_lane(sum, 63), before = sum - mine, rate = rate_of(all, a.workers, a.least);
-    if (worker == 0 && wave == 0) {
+    if (place == 0 && wave == 0) {
       uint64_t sofar = before;
       for (uint32_t i = r0; i < r1; ++i) {
         a.prefix[i] = sofar;
@@ -219,11 +234,13 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
   float scale = all->scale;
   asm volatile("" : "+s"(row_bytes), "+s"(k_bytes), "+s"(v_bytes), "+s"(pages), "+s"(page_d), "+s"(page_m), "+s"(page_shift), "+s"(page_bytes), "+s"(scale));
 
+  uint32_t bad = 0;  // something has been left out that a row may see
   for (;;) {
-    const uint32_t together = argument()->together, heads = argument()->c.heads, group = argument()->group;
+    const uint32_t together = argument()->together, cluster = argument()->cluster, heads = argument()->c.heads, group = argument()->group;
     const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * group + ROWS - 1) / ROWS, cost = steps + kSegment;
     const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
-    const uint64_t segments = (uint64_t)(heads / together) * tiles;
+    const uint32_t groups = (tiles + cluster - 1) / cluster;
+    const uint64_t segments = (uint64_t)(heads / together) * groups;
     uint64_t seg = quotient(at, cost);
     for (at -= seg * cost; seg < segments && left != 0; ++seg, at = 0) {
       // this worker's part of the segment's cost, and of its steps
@@ -235,8 +252,9 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
       const auto &t = a.t;
       const auto &c = a.c;
       const Constants table = constants(t.table + (uint64_t)r * t.blocks);
-      const uint32_t heads_before = uniform((uint32_t)quotient(seg, tiles)), tile = uniform((uint32_t)(seg - (uint64_t)heads_before * tiles));
+      const uint32_t heads_before = uniform((uint32_t)quotient(seg, groups)), tile = uniform((uint32_t)(seg - (uint64_t)heads_before * groups) * cluster + member);
       const uint32_t head = heads_before * together + wave / WR;
+      if (tile >= tiles) continue;
       const uint32_t row0 = tile * ROWS + wr * RT;
       const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
       const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
@@ -276,7 +294,7 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
       // key, in that page still, are read and not looked at. Otherwise lane l % 32 finds key l % 32, behind the last one that one again. So
       // it is with drafted keys. (No branches here: loads under a condition, of either outcome, would be waited for as if they were not there.)
       const uint32_t end_key = q.len > 0 ? (uint32_t)q.len - 1 : 0;
-      const auto pages_of = [&](uint32_t st, uint32_t (&ids)[2]) {
+      const auto pages_of = [&](uint32_t st, uint32_t (&ids)[NI]) {
         if (st >= cached) return;
         if constexpr (PAGED) {
 #pragma unroll
@@ -285,13 +303,16 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
             ids[kk] = (uint32_t)table[uniform(__umulhi(key < end_key ? key : end_key, page_m) >> page_shift)];
           }
         } else {
-          const uint32_t key = st * kStep + (lane & 31);
-          ids[0] = (uint32_t)table[divisor(c.page_tokens).of(key < end_key ? key : end_key)];
+#pragma unroll
+          for (int i = 0; i < (SHARED ? N : 1); ++i) {
+            const uint32_t key = st * kStep + (SHARED ? (i * 64 * WR + threadIdx.x) / CH : lane & 31);
+            ids[i] = (uint32_t)table[divisor(c.page_tokens).of(key < end_key ? key : end_key)];
+          }
         }
       };
-      // Lane l % 32's row as an offset in bytes from the head's first one (without PAGED), of cached and of drafted keys.
-      const auto lane_row = [&](uint32_t st, uint32_t page, uint64_t draft_stride) -> uint64_t {
-        uint32_t key = st * kStep + (lane & 31), draft = key - cached * kStep;
+      // A row of a step as an offset in bytes from the head's first one (without PAGED), of cached and of drafted keys.
+      const auto lane_row = [&](uint32_t st, uint32_t of_step, uint32_t page, uint64_t draft_stride) -> uint64_t {
+        uint32_t key = st * kStep + of_step, draft = key - cached * kStep;
         key = key < end_key ? key : end_key;
         draft = draft < (uint32_t)q.n ? draft : (uint32_t)q.n - 1;
         const uint64_t in_cache = (page < c.pages ? page : 0) * c.page_stride + divisor(c.page_tokens).rest(key) * c.token_stride;
@@ -310,8 +331,8 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
         const uint32_t row = in_cache ? key - (__umulhi(key, page_m) >> page_shift) * page_d : draft;
         return {page * page_bytes + (uint64_t)row * (in_cache ? row_bytes : draft_stride), in_cache ? 15 : end - draft};
       };
-      const auto load_keys = [&](uint32_t st, const uint32_t (&ids)[2]) {
-        const uint64_t row = PAGED ? 0 : lane_row(st, ids[0], t.k_token_stride);
+      const auto load_keys = [&](uint32_t st, const uint32_t (&ids)[NI]) {
+        const uint64_t row = PAGED ? 0 : lane_row(st, lane & 31, ids[0], t.k_token_stride);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           Global base = global(st < cached ? kc : kd);
@@ -331,8 +352,8 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
           }
         }
       };
-      const auto load_values = [&](uint32_t st, const uint32_t (&ids)[2]) {
-        const uint64_t row = PAGED ? 0 : lane_row(st, ids[0], t.v_token_stride);
+      const auto load_values = [&](uint32_t st, const uint32_t (&ids)[NI]) {
+        const uint64_t row = PAGED ? 0 : lane_row(st, lane & 31, ids[0], t.v_token_stride);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           Global half_base = global(st < cached ? vc : vd);
@@ -367,6 +388,68 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
                 for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
               }
             }
+          }
+        }
+      };
+      // SHARED: a thread's pieces of a step's keys and values. Row r has its pieces in the order that counting up to CH and an exclusive or
+      // with r give: wavefronts read 16 bytes of each of several rows, and so meet different banks.
+      const auto fetch = [&](uint32_t st, const uint32_t (&ids)[NI], Words4 (&k)[N], Words4 (&v)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          uint32_t index = i * 64 * WR + threadIdx.x;
+          asm volatile("" : "+v"(index));
+          const uint32_t row = index / CH;
+          uint32_t piece = (index % CH) ^ (row % CH);
+          if (!PAGED && piece * 8 >= (uint32_t)c.dim) piece = 0;  // queries are zero there, and outputs not written
+          Global kb = global(st < cached ? kc : kd), vb = global(st < cached ? vc : vd);
+          uint32_t ko = 16 * piece, vo = 16 * piece;
+          if constexpr (PAGED) {
+            const uint32_t kk = uniform(row >> 4), of_half = row & 15, id = kk != 0 ? ids[1] : ids[0];
+            const Half kh = half(st, (int)kk, id, k_bytes), vh = half(st, (int)kk, id, v_bytes);
+            kb += kh.row;
+            vb += vh.row;
+            ko += __umul24(of_half < kh.behind ? of_half : kh.behind, st < cached ? row_bytes : k_bytes);
+            vo += __umul24(of_half < vh.behind ? of_half : vh.behind, st < cached ? row_bytes : v_bytes);
+            asm volatile("" : "+s"(kb), "+s"(vb), "+v"(ko), "+v"(vo));
+          } else {
+            kb += lane_row(st, row, ids[i], t.k_token_stride);
+            vb += lane_row(st, row, ids[i], t.v_token_stride);
+          }
+          k[i] = load16(kb + ko);
+          v[i] = load16(vb + vo);
+        }
+      };
+      const auto put = [&](int buf, const Words4 (&k)[N], const Words4 (&v)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          tile_lds[buf][0][i * 64 * WR + threadIdx.x] = k[i];
+          tile_lds[buf][1][i * 64 * WR + threadIdx.x] = v[i];
+        }
+      };
+      // (the empty statements keep places from being worked out once and held: registers are scarcer than instructions)
+      const auto get_keys = [&](int buf) {
+        uint32_t row = n16, group = g;
+        asm volatile("" : "+v"(row), "+v"(group));
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) kf[kk][ks] = tile_lds[buf][0][(kk * 16 + row) * CH + ((ks * 4 + group) ^ (row % CH))];
+      };
+      const auto get_values = [&](int buf) {
+        uint32_t piece = n16, first_row = 4 * g;
+        asm volatile("" : "+v"(piece), "+v"(first_row));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t row = (e >> 2) * 16 + first_row + (e & 3);
+          if constexpr (E == 4) {
+            typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+            const Words2 w = reinterpret_cast<const Words2 *>(&tile_lds[buf][1][row * CH + ((piece / 2) ^ (row % CH))])[piece & 1];
+            vf[e][0] = w[0];
+            vf[e][1] = w[1];
+          } else if constexpr (E == 8) {
+            const Words4 w = tile_lds[buf][1][row * CH + (piece ^ (row % CH))];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) vf[e][y] = w[y];
           }
         }
       };
@@ -435,8 +518,7 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
 
       // Steps in which not everything is seen: the last cached keys where they are no whole step, and drafted ones. What a row does not see
       // has a weight of zero, and its value, which may be anything, must not be met by it where it is not finite: such values
-      // are left out of the product. Where a row may see one it is added afterwards.
-      uint32_t bad = 0;
+      // are left out of the product. Where a row may see one, the kernel behind this one adds it.
       const auto edge = [&](uint32_t st) {
         if ((st + 1) * kStep <= (uint32_t)q.len) return;
 #pragma unroll
@@ -474,11 +556,19 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
       // A step's keys are on their way while the one before weighs its values, its values from there on, and the pages of the one behind it
       // are asked for first of all. The last step asks for its own rows once more, which are near by then: were there a
       // condition on these loads, what is asked for before them would be waited for together with them.
+      const auto softmax = [&](uint32_t st) {
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] *= scale;
+        edge(st);
+        weights();
+      };
       uint32_t st = first;
-      {
-        uint32_t ids[2] = {0, 0}, ahead[2] = {0, 0};
-        pages_of(st, ids);
-        if (st + 1 < last) pages_of(st + 1, ahead);
+      uint32_t ids[NI] = {}, ahead[NI] = {};
+      pages_of(st, ids);
+      if (st + 1 < last) pages_of(st + 1, ahead);
+      if constexpr (!SHARED) {
         load_keys(st, ids);
         __builtin_amdgcn_sched_barrier(0);  // (loads are waited for in their order: in the loop keys come first)
         load_values(st, ids);
@@ -487,63 +577,60 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
           more = st + 1 < last;
           const uint32_t next = more ? st + 1 : st;
           if (more) {
-            ids[0] = ahead[0];
-            ids[1] = ahead[1];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) ids[i] = ahead[i];
           }
           scores();
           load_keys(next, ids);
           __builtin_amdgcn_sched_barrier(0);  // (scalar loads come back in any order: to wait for these pages is to wait for the next ones)
           if (next + 1 < last) pages_of(next + 1, ahead);
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] *= scale;
-          edge(st);
-          weights();
+          softmax(st);
           edge_values(st);
           outputs();
           load_values(next, ids);
           st = next;
         } while (more);
-      }
-      // What has been left out, by the same product on ones: how many infinities of either sign, and NaN, a row sees of every element.
-      if (bad)
-        for (st = first; st < last; ++st) {
-          if ((st + 1) * kStep <= (uint32_t)q.len) continue;
-          for (int kind = 0; kind < 3; ++kind) {
-            uint32_t ids[2] = {0, 0};
-            pages_of(st, ids);
-            load_values(st, ids);
-            const auto one = [&](uint32_t v) {
-              const bool is = kind == 2 ? (v & 0x7fff) > T::kExponent : v == (T::kExponent | (uint32_t)kind << 15);
-              return is ? T::kOne : 0u;
-            };
+      } else {
+        // The step that is worked on lies in one half of shared memory, the next one is put into the other half, those behind it are on their way
+        // in registers. One barrier a step: it says that the half to work on is full, and that the other one has been read.
+        Words4 k[DEPTH][N], v[DEPTH][N];
+        uint32_t asked = st;  // the step that `ids` are the pages of
+        const auto ask = [&](Words4 (&into_k)[N], Words4 (&into_v)[N]) {
+          fetch(asked, ids, into_k, into_v);
+          if (asked + 1 < last) {
+            ++asked;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-              for (int x = 0; x < E / 2; ++x) vf[e][x] = one(vf[e][x] & 0xffff) | one(vf[e][x] >> 16) << 16;
-            const float value = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) {
-              const uint32_t sees = sees_of(nr, st);
-              Words4 seen;
-#pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const uint32_t two = sees >> ((x >> 1) * 16 + 4 * g + (x & 1) * 2);
-                seen[x] = (two & 1 ? T::kOne : 0) | (two & 2 ? T::kOne << 16 : 0);
-              }
-#pragma unroll
-              for (int j = 0; j < E; ++j) {
-                const Floats4 count = T::mfma(turned(vf, j / 2, j & 1 ? 0x07060302 : 0x05040100), seen, Floats4{0, 0, 0, 0});
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (count[i] != 0) acc[nr][j][i] += value;
-                __builtin_amdgcn_sched_barrier(0);  // (rare: what it takes is registers, not time)
-              }
-            }
+            for (int i = 0; i < NI; ++i) ids[i] = ahead[i];
           }
+          __builtin_amdgcn_sched_barrier(0);
+          if (asked + 1 < last) pages_of(asked + 1, ahead);
+        };
+        fence();  // what the segment before has left in shared memory has been read
+        ask(k[0], v[0]);
+        put(0, k[0], v[0]);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) ask(k[d], v[d]);
+        for (bool more = true; more;) {
+#pragma unroll
+          for (int d = 0; d < (DEPTH > 1 ? DEPTH : 2); ++d)
+            if (more) {
+              fence();
+              put(d + 1 & 1, k[d % DEPTH], v[d % DEPTH]);
+              ask(k[d % DEPTH], v[d % DEPTH]);
+              __builtin_amdgcn_sched_barrier(0);  // (keys and values at once would not leave registers for what is on its way)
+              get_keys(d & 1);
+              scores();
+              __builtin_amdgcn_sched_barrier(0);
+              softmax(st);
+              __builtin_amdgcn_sched_barrier(0);
+              get_values(d & 1);
+              edge_values(st);
+              outputs();
+              ++st;
+              more = st < last;
+            }
         }
-
+      }
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) l[nr] = row_sum(l[nr]);
       {
@@ -552,7 +639,7 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
           for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
         } else {
           // a worker has at most two segments that it shares: the one it begins in, which others have begun, and the one it ends in
-          float *sums = a.sums + (((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * together * WR + wave) * (NR * Partial<DT>::kTile);
+          float *sums = a.sums + ((((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * cluster + member) * together * WR + wave) * (NR * Partial<DT>::kTile);
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
@@ -565,12 +652,42 @@ __global__ __launch_bounds__(256 * waves(DT, NR, PAGED)) __attribute__((amdgpu_w
         }
       }
     }
-    if (left == 0) return;
     at = 0;
-    do {
-      if (++r >= argument()->t.requests) return;
-      q = request(*argument(), r);
-    } while (q.n == 0);
+    q.n = 0;
+    while (left != 0 && q.n == 0 && ++r < argument()->t.requests) q = request(*argument(), r);
+    if (left == 0 || q.n == 0) {
+      if (lane == 0) argument()->flags[place * together * WR + wave] = bad;
+      return;
+    }
+  }
+}
+
+// Infinities and NaN among the values that a row sees of the last cached keys and of drafted ones are added to its result, whatever
+// else that is: it cannot matter how much of them. The first wavefront's, each of its four lanes of a row has a quarter of the elements.
+template <class T, class A>
+__device__ inline void add_left_out(const A &a, const Request &q, uint32_t r, uint32_t row, uint32_t head, int g) {
+  if (threadIdx.x >= 64) return;
+  const uint32_t token = divisor(a.by_group).of(row), q_head = head * a.group + (row - token * a.group);
+  if ((int)token >= q.n) return;
+  const uint64_t t = (uint64_t)(q.start + (int)token);
+  const int tail = q.len & ~(kStep - 1), keys = q.len - tail + q.n;
+  for (uint32_t d = g; d < a.c.dim; d += 4) {
+    float sum = 0;
+    for (int i = 0; i < keys; ++i) {
+      const uint16_t *v;
+      if (tail + i < q.len) {
+        const uint32_t block = divisor(a.c.page_tokens).of(tail + i), page = (uint32_t)a.t.table[(uint64_t)r * a.t.blocks + block];
+        v = reinterpret_cast<const uint16_t *>(a.c.v) + (page < a.c.pages ? page : 0) * a.c.page_stride +
+            (tail + i - block * a.c.page_tokens.d) * a.c.token_stride + head * a.c.head_stride;
+      } else {
+        const int j = i - (q.len - tail);
+        if (a.t.mask != nullptr ? (a.t.mask[t * a.t.mask_words + (j >> 6)] >> (j & 63) & 1) == 0 : j > (int)token) continue;
+        v = static_cast<const uint16_t *>(a.t.v) + (uint64_t)(q.start + j) * a.t.v_token_stride + head * a.t.v_head_stride;
+      }
+      if ((v[d] & T::kExponent) == T::kExponent) sum += T::to_float(v[d]);
+    }
+    uint16_t *out = static_cast<uint16_t *>(a.t.out) + t * a.t.out_token_stride + q_head * a.t.out_head_stride + d;
+    if (sum != 0) *out = T::from_float(T::to_float(*out) + sum);
   }
 }
 
@@ -588,10 +705,18 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + ROWS - 1) / ROWS;
   if (tile >= tiles || tile * ROWS + part * 16 >= (uint32_t)q.n * a.group) return;
   const uint32_t steps = steps_of(q);
-  const uint64_t rate = a.prefix[a.t.requests], begin = a.prefix[r] + ((uint64_t)(head / a.together) * tiles + tile) * (steps + kSegment) + kSegment;
+  const uint64_t rate = a.prefix[a.t.requests], groups = (tiles + a.cluster - 1) / a.cluster;
+  const uint64_t begin = a.prefix[r] + ((head / a.together) * groups + tile / a.cluster) * (steps + kSegment) + kSegment;
   const uint32_t w0 = worker_of(begin, rate), w1 = worker_of(begin + steps - 1, rate);
-  if (w0 == w1) return;
-  const auto at = [&](uint32_t w) { return a.sums + ((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.together + head % a.together) * (WR * NR) + part) * Partial<DT>::kTile; };
+  const uint32_t wave_of = head % a.together * WR + part / NR;
+  bool left_out = false;
+  for (uint32_t w = w0; w <= w1; ++w) left_out |= a.flags[(w * a.cluster + tile % a.cluster) * (a.together * WR) + wave_of] != 0;
+  const uint32_t row = tile * ROWS + part * 16 + n16;
+  if (w0 == w1) {
+    if (left_out) add_left_out<T>(a, q, r, row, head, g);
+    return;
+  }
+  const auto at = [&](uint32_t w) { return a.sums + (((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.cluster + tile % a.cluster) * a.together + head % a.together) * (WR * NR) + part) * Partial<DT>::kTile; };
   float now = -INFINITY;
   for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) now = fmaxf(now, at(w)[16 * DT + n16]);
   top[threadIdx.x >> 4][n16] = now;
@@ -619,42 +744,52 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
   for (int w = 0; w < 3; ++w)
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[j] += join[w][j][lane];
-  write_row<T, DT>(a, acc, l, now, q, tile * ROWS + part * 16 + n16, head, g);
+  write_row<T, DT>(a, acc, l, now, q, row, head, g);
+  if (left_out) add_left_out<T>(a, q, r, row, head, g);
 }
 
 struct Shape {
   int dt, nr, wr;
+  bool shared;
+  uint32_t cluster;
 };
 
-// Heads are padded to 64, 128 or 256 elements. A wavefront has up to 32 rows (16 where heads are large), beyond that workers are several
-// wavefronts.
+// Heads are padded to 64, 128 or 256 elements. Up to 32 rows (16 where heads are large) are one wavefront's; beyond that wavefronts
+// share keys and values in shared memory, and beyond 256 rows (128 of small heads) up to four workgroups the die's cache.
 Shape shape_of(uint32_t dim, uint64_t rows) {
   const int dt = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
-  if (rows <= 16) return {dt, 1, 1};
-  if (dt == 256) return {dt, 1, 4};
-  if (rows <= 32) return {dt, 2, 1};
-  if (rows <= 64) return {dt, 2, 2};
-  return {dt, 2, 4};
+  if (rows <= 16) return {dt, 1, 1, false, 1};
+  if (dt == 256) return {dt, 1, 4, false, 1};
+  if (rows <= 32) return {dt, 2, 1, false, 1};
+  if (rows <= 64) return {dt, 1, 4, true, 1};
+  if (rows <= 128 && dt == 128) return {dt, 1, 8, true, 1};
+  const int most = dt == 64 ? 4 : 8;
+  const uint64_t tiles = (rows + 32 * most - 1) / (32 * most);
+  return {dt, 2, most, true, tiles > 4 ? 4 : (uint32_t)tiles};
 }
 
-// Key heads that a worker reads: as many as divide all of them and leave room on a compute unit.
+// Key heads that a worker reads where they are not shared: as many as divide all of them and leave room on a compute unit.
 uint32_t together_of(const Shape &s, bool paged, uint32_t heads) {
-  uint32_t n = (uint32_t)(4 * waves(s.dt, s.nr, paged) / s.wr);
+  uint32_t n = s.shared ? 1 : (uint32_t)(4 * waves(s.dt, s.nr, paged, false) / s.wr);
   while (heads % n != 0) n /= 2;
   return n;
 }
 
 // As many as the chip holds, a multiple of its dies.
 uint32_t workers_of(const Shape &s, bool paged, uint32_t together, int cu_count) {
-  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged) / (s.wr * (int)together) + 7) / 8 * 8;
+  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged, s.shared) / (s.wr * (int)(together * s.cluster)) + 7) / 8 * 8;
 }
+
+// Wavefronts of all workers, at most: workers are rounded up to the dies.
+uint64_t waves_of(const Shape &s, int cu_count) { return (uint64_t)cu_count * 4 * waves(s.dt, s.nr, true, s.shared) + 256; }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
-template <class T, int DT, int NR, int WR>
+template <class T, int DT, int NR, int WR, bool SHARED>
 hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true>), dim3(a.workers), dim3(64 * WR * a.together), 0, stream, a);
-  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false>), dim3(a.workers), dim3(64 * WR * a.together), 0, stream, a);
+  const dim3 grid(a.workers * a.cluster), threads(64 * WR * a.together);
+  if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true, SHARED>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false, SHARED>), grid, threads, 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint64_t tiles = (rows + 16 * NR * WR - 1) / (16 * NR * WR) * NR * WR;
@@ -664,11 +799,15 @@ hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) 
 
 template <class T, int DT>
 hipError_t launch_rows(const Tree &a, const Shape &s, bool paged, uint64_t rows, hipStream_t stream) {
-  if (s.nr == 1 && s.wr == 1) return launch<T, DT, 1, 1>(a, paged, rows, stream);
-  if constexpr (DT == 256) return launch<T, DT, 1, 4>(a, paged, rows, stream);
-  else if (s.wr == 1) return launch<T, DT, 2, 1>(a, paged, rows, stream);
-  else if (s.wr == 2) return launch<T, DT, 2, 2>(a, paged, rows, stream);
-  else return launch<T, DT, 2, 4>(a, paged, rows, stream);
+  if (s.nr == 1 && s.wr == 1) return launch<T, DT, 1, 1, false>(a, paged, rows, stream);
+  if constexpr (DT == 256) {
+    return launch<T, DT, 1, 4, false>(a, paged, rows, stream);
+  } else {
+    if (s.wr == 1) return launch<T, DT, 2, 1, false>(a, paged, rows, stream);
+    if (s.nr == 1 && s.wr == 4) return launch<T, DT, 1, 4, true>(a, paged, rows, stream);
+    if constexpr (DT == 64) return launch<T, DT, 2, 4, true>(a, paged, rows, stream);
+    else return s.nr == 1 ? launch<T, DT, 1, 8, true>(a, paged, rows, stream) : launch<T, DT, 2, 8, true>(a, paged, rows, stream);
+  }
 }
 
 template <class T>
@@ -686,7 +825,7 @@ uint64_t rows_of(const ft_tree_call &t, uint32_t heads) {
 
 uint64_t tree_workspace(const ft_kv_cache &c, const ft_tree_call &t, int cu_count) {
   const Shape s = shape_of(c.dim, rows_of(t, c.heads));
-  return up16(((uint64_t)t.requests + 2) * 8) + ((uint64_t)cu_count * 4 * waves(s.dt, s.nr, true) + 64) * 2 * s.nr * (16 * s.dt + 32) * 4;
+  return up16(((uint64_t)t.requests + 2) * 8) + waves_of(s, cu_count) * (4 + 2ull * s.nr * (16 * s.dt + 32) * 4);
 }
 
 hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hipStream_t stream) {
@@ -697,13 +836,15 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   // strides of 24 bits in bytes
   const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && (c.token_stride | t.k_token_stride | t.v_token_stride) < 1u << 23;
   a.together = together_of(s, paged, c.heads);
+  a.cluster = s.cluster;
   a.workers = workers_of(s, paged, a.together, cu_count);
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
   a.least = kSegment + 2;
   a.scale = t.scale * kLog2e;
   a.prefix = static_cast<uint64_t *>(t.workspace);
-  a.sums = reinterpret_cast<float *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
+  a.flags = reinterpret_cast<uint32_t *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
+  a.sums = reinterpret_cast<float *>(a.flags + waves_of(s, cu_count));
   return c.type == FT_BF16 ? launch_dim<Bf16>(a, s, paged, rows, stream) : launch_dim<Fp16>(a, s, paged, rows, stream);
 }
 
