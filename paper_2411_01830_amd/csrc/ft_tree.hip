@@ -27,7 +27,6 @@ struct Tree {
   KvView c;
   ft_tree_call t;
   uint32_t group;        // query heads of a key head
-  uint32_t together;     // key heads that a worker reads, a wavefront (or WR of them) each
   uint32_t cluster;      // workgroups of a worker, which have different rows
   Divisor by_group;
   uint32_t workers, least;  // workgroups, and steps that each takes at least
@@ -114,12 +113,12 @@ __device__ inline Request request(const A &a, uint32_t r) {
 
 __device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len + (kStep - 1)) >> 5) + (uint32_t)((q.n + (kStep - 1)) >> 5); }
 
-// Work of a request: for each few key heads that are read together and each tile of `rows` rows, which are a segment, what it costs to begin with
-// and all of its steps.
+// Work of a request: for each key head and each cluster's tiles of `rows` rows, which are a segment, what it costs to begin with and all of its
+// steps.
 template <class A>
 __device__ inline uint64_t work_of(const A &a, const Request &q, uint32_t rows) {
   const uint32_t tiles = ((uint32_t)q.n * a.group + rows - 1) / rows;
-  return (uint64_t)(a.c.heads / a.together) * ((tiles + a.cluster - 1) / a.cluster) * (steps_of(q) + kSegment);
+  return (uint64_t)a.c.heads * ((tiles + a.cluster - 1) / a.cluster) * (steps_of(q) + kSegment);
 }
 
 // A worker's sums of a segment that it has a part of: [16 rows][4 elements x 64 lanes of every product], then a row's maximum and sum.
@@ -160,22 +159,20 @@ __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t by
   return out;
 }
 
-// NR: tiles of 16 rows a wavefront has. WR: wavefronts that have different rows and read the same keys. A worker is that many for each of
-// the key heads that it reads, side by side in step: where a token's heads lie next to each other, as they mostly do, memory is read
-// in longer pieces than one head's.
+// NR: tiles of 16 rows a wavefront has. WR: wavefronts of a workgroup, which have different rows and read the same keys.
 // PAGED: the head has DT elements and a page a multiple of 16 tokens, so 16 keys are read from one base address that is the same for all
 // lanes; without it every lane finds the row of one key, and hands it on to those that read it.
 // SHARED: keys and values go through shared memory, which the WR wavefronts of a workgroup fill together; several workgroups, a cluster, have
 // the rows beyond those and are next to each other on one die, where the second finds in the cache what the first has read.
 template <class T, int DT, int NR, int WR, bool PAGED, bool SHARED>
-__global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARED)) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED, SHARED), waves(DT, NR, PAGED, SHARED)))) void ft_tree_kernel(Tree) {
+__global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED, SHARED), waves(DT, NR, PAGED, SHARED)))) void ft_tree_kernel(Tree) {
   constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
   // SHARED: 16-byte pieces of a row, those of a step that a thread has, steps that are on their way besides the one in shared memory
   constexpr int CH = DT / 8, N = SHARED ? CH / (2 * WR) : 1, DEPTH = SHARED ? (NR == 1 ? 4 : 2) / N : 1, NI = SHARED && !PAGED ? N : 2;
   static_assert(!SHARED || (N >= 1 && N * 2 * WR == CH));
   __shared__ Words4 tile_lds[SHARED ? 2 : 1][2][SHARED ? 32 * CH : 1];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
-  const uint32_t wave = uniform((uint32_t)threadIdx.x >> 6), wr = wave % WR;
+  const uint32_t wave = uniform((uint32_t)threadIdx.x >> 6);
 
   // The workers next to each other go to the same die: they read the same pages for other rows.
   const uint32_t per_die = gridDim.x / 8;
@@ -236,11 +233,11 @@ __global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARE
 
   uint32_t bad = 0;  // something has been left out that a row may see
   for (;;) {
-    const uint32_t together = argument()->together, cluster = argument()->cluster, heads = argument()->c.heads, group = argument()->group;
+    const uint32_t cluster = argument()->cluster, heads = argument()->c.heads, group = argument()->group;
     const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * group + ROWS - 1) / ROWS, cost = steps + kSegment;
     const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
     const uint32_t groups = (tiles + cluster - 1) / cluster;
-    const uint64_t segments = (uint64_t)(heads / together) * groups;
+    const uint64_t segments = (uint64_t)heads * groups;
     uint64_t seg = quotient(at, cost);
     for (at -= seg * cost; seg < segments && left != 0; ++seg, at = 0) {
       // this worker's part of the segment's cost, and of its steps
@@ -252,10 +249,9 @@ __global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARE
       const auto &t = a.t;
       const auto &c = a.c;
       const Constants table = constants(t.table + (uint64_t)r * t.blocks);
-      const uint32_t heads_before = uniform((uint32_t)quotient(seg, groups)), tile = uniform((uint32_t)(seg - (uint64_t)heads_before * groups) * cluster + member);
-      const uint32_t head = heads_before * together + wave / WR;
+      const uint32_t head = uniform((uint32_t)quotient(seg, groups)), tile = uniform((uint32_t)(seg - (uint64_t)head * groups) * cluster + member);
       if (tile >= tiles) continue;
-      const uint32_t row0 = tile * ROWS + wr * RT;
+      const uint32_t row0 = tile * ROWS + wave * RT;
       const char *kc = c.k + 2 * (head * c.head_stride), *vc = c.v + 2 * (head * c.head_stride);
       const char *kd = static_cast<const char *>(t.k) + 2 * (q.start * t.k_token_stride + head * t.k_head_stride);
       const char *vd = static_cast<const char *>(t.v) + 2 * (q.start * t.v_token_stride + head * t.v_head_stride);
@@ -639,7 +635,7 @@ __global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARE
           for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
         } else {
           // a worker has at most two segments that it shares: the one it begins in, which others have begun, and the one it ends in
-          float *sums = a.sums + ((((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * cluster + member) * together * WR + wave) * (NR * Partial<DT>::kTile);
+          float *sums = a.sums + ((((uint64_t)worker * 2 + (first == 0 ? 1 : 0)) * cluster + member) * WR + wave) * (NR * Partial<DT>::kTile);
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
@@ -656,7 +652,7 @@ __global__ __launch_bounds__(SHARED ? 64 * WR : 256 * waves(DT, NR, PAGED, SHARE
     q.n = 0;
     while (left != 0 && q.n == 0 && ++r < argument()->t.requests) q = request(*argument(), r);
     if (left == 0 || q.n == 0) {
-      if (lane == 0) argument()->flags[place * together * WR + wave] = bad;
+      if (lane == 0) argument()->flags[place * WR + wave] = bad;
       return;
     }
   }
@@ -706,21 +702,23 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
   if (tile >= tiles || tile * ROWS + part * 16 >= (uint32_t)q.n * a.group) return;
   const uint32_t steps = steps_of(q);
   const uint64_t rate = a.prefix[a.t.requests], groups = (tiles + a.cluster - 1) / a.cluster;
-  const uint64_t begin = a.prefix[r] + ((head / a.together) * groups + tile / a.cluster) * (steps + kSegment) + kSegment;
+  const uint64_t begin = a.prefix[r] + ((uint64_t)head * groups + tile / a.cluster) * (steps + kSegment) + kSegment;
   const uint32_t w0 = worker_of(begin, rate), w1 = worker_of(begin + steps - 1, rate);
-  const uint32_t wave_of = head % a.together * WR + part / NR;
-  bool left_out = false;
-  for (uint32_t w = w0; w <= w1; ++w) left_out |= a.flags[(w * a.cluster + tile % a.cluster) * (a.together * WR) + wave_of] != 0;
+  const auto left_out_by = [&](uint32_t w) { return a.flags[(w * a.cluster + tile % a.cluster) * WR + part / NR] != 0; };
   const uint32_t row = tile * ROWS + part * 16 + n16;
   if (w0 == w1) {
-    if (left_out) add_left_out<T>(a, q, r, row, head, g);
+    if (left_out_by(w0)) add_left_out<T>(a, q, r, row, head, g);
     return;
   }
-  const auto at = [&](uint32_t w) { return a.sums + (((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.cluster + tile % a.cluster) * a.together + head % a.together) * (WR * NR) + part) * Partial<DT>::kTile; };
+  const auto at = [&](uint32_t w) { return a.sums + ((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.cluster + tile % a.cluster) * (WR * NR) + part) * Partial<DT>::kTile; };
   float now = -INFINITY;
-  for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) now = fmaxf(now, at(w)[16 * DT + n16]);
+  bool left_out = false;
+  for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) {
+    now = fmaxf(now, at(w)[16 * DT + n16]);
+    left_out |= left_out_by(w);
+  }
   top[threadIdx.x >> 4][n16] = now;
-  __syncthreads();
+  left_out = __syncthreads_or(left_out);
   for (int i = 0; i < 16; ++i) now = fmaxf(now, top[i][n16]);
   const float from = now == -INFINITY ? 0 : now;
   float l = 0;
@@ -768,16 +766,9 @@ Shape shape_of(uint32_t dim, uint64_t rows) {
   return {dt, 2, most, true, tiles > 4 ? 4 : (uint32_t)tiles};
 }
 
-// Key heads that a worker reads where they are not shared: as many as divide all of them and leave room on a compute unit.
-uint32_t together_of(const Shape &s, bool paged, uint32_t heads) {
-  uint32_t n = s.shared ? 1 : (uint32_t)(4 * waves(s.dt, s.nr, paged, false) / s.wr);
-  while (heads % n != 0) n /= 2;
-  return n;
-}
-
 // As many as the chip holds, a multiple of its dies.
-uint32_t workers_of(const Shape &s, bool paged, uint32_t together, int cu_count) {
-  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged, s.shared) / (s.wr * (int)(together * s.cluster)) + 7) / 8 * 8;
+uint32_t workers_of(const Shape &s, bool paged, int cu_count) {
+  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged, s.shared) / (s.wr * (int)s.cluster) + 7) / 8 * 8;
 }
 
 // Wavefronts of all workers, at most: workers are rounded up to the dies.
@@ -787,7 +778,7 @@ uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
 template <class T, int DT, int NR, int WR, bool SHARED>
 hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) {
-  const dim3 grid(a.workers * a.cluster), threads(64 * WR * a.together);
+  const dim3 grid(a.workers * a.cluster), threads(64 * WR);
   if (paged) hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, true, SHARED>), grid, threads, 0, stream, a);
   else hipLaunchKernelGGL((ft_tree_kernel<T, DT, NR, WR, false, SHARED>), grid, threads, 0, stream, a);
   const hipError_t e = hipGetLastError();
@@ -835,9 +826,8 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.t.drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
   // strides of 24 bits in bytes
   const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && (c.token_stride | t.k_token_stride | t.v_token_stride) < 1u << 23;
-  a.together = together_of(s, paged, c.heads);
   a.cluster = s.cluster;
-  a.workers = workers_of(s, paged, a.together, cu_count);
+  a.workers = workers_of(s, paged, cu_count);
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
   a.least = kSegment + 2;
