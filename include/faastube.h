@@ -817,7 +817,7 @@ int ft_adapters_resolve(ft_pool *p, const ft_adapter *adapters, uint32_t count, 
                         ft_adapter_record *records_out);
 
 /*
- * Which rows belong to which adapter: ids (device, rows entries) is a row's adapter, anything outside [0, count) none.
+ * Which rows belong to which adapter: ids (device, rows entries) is a row's adapter, anything outside [0, count) none; count <= 16384.
  * One grouping serves every projection of a step. groups: device, ft_adapters_group_bytes bytes, 16-byte aligned.
  */
 int ft_adapters_group_bytes(uint32_t rows, uint32_t count, uint64_t *bytes_out);

@@ -1,4 +1,9 @@
-// Low-rank adapters of many requests beside a shared projection.
+// Low-rank adapters of many requests beside a shared projection: out[t] = base[t] + s B (A x[t]) with the A, B and s of row t.
+//
+// Rows are put in the order of their adapters and cut into tiles of up to 64 rows of one adapter (ft_adapter_group_kernel), so that a
+// tile's products are matrix products. H^T = A X^T first, with the long axis split over workgroups and wavefronts whose sums are put
+// into the workspace; then out^T = B H^T, where the parts of H are added up, scaled and held as the sum of two numbers of 16 bits.
+// Rows without an adapter are tiles of their own that are copied.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"
@@ -8,63 +13,368 @@ namespace ft {
 
 namespace {
 
-// A wavefront per row and rank: the row's product with a row of A.
+constexpr uint32_t kTileRows = 64;
+constexpr uint32_t kGroupThreads = 1024;
+
+struct Tile {
+  int32_t adapter;  // -1: none
+  uint32_t first;   // of its rows in `order`
+  uint32_t count;
+  uint32_t _pad;
+};
+
+// What ft_adapters_group leaves for the other kernels.
+struct Groups {
+  uint32_t *tiles_there;  // a line of its own
+  Tile *tiles;
+  int32_t *order;
+};
+
+__host__ __device__ inline uint64_t most_tiles(uint32_t rows, uint32_t count) {
+  const uint64_t kinds = (uint64_t)count + 1 < rows ? (uint64_t)count + 1 : rows;
+  return rows / kTileRows + kinds;
+}
+
+__host__ __device__ inline Groups groups_at(void *p, uint32_t rows, uint32_t count) {
+  char *at = static_cast<char *>(p);
+  return {reinterpret_cast<uint32_t *>(at), reinterpret_cast<Tile *>(at + 64), reinterpret_cast<int32_t *>(at + 64 + most_tiles(rows, count) * sizeof(Tile))};
+}
+
+// A counting sort in one workgroup. Where a row comes among those of its adapter depends on the order of atomics, and nothing else does: every
+// row's result is its own column of a product.
+__global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const int32_t *__restrict__ ids, uint32_t rows, uint32_t count, Groups out) {
+  extern __shared__ uint32_t bin[];  // count + 1: rows, then where the next one goes
+  __shared__ uint32_t part[2][kGroupThreads / 64];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (uint32_t i = tid; i <= count; i += kGroupThreads) bin[i] = 0;
+  __syncthreads();
+  for (uint32_t i = tid; i < rows; i += kGroupThreads) {
+    const uint32_t id = (uint32_t)ids[i];
+    atomicAdd(&bin[id < count ? id : count], 1u);
+  }
+  uint32_t rows_before = 0, tiles_before = 0;
+  for (uint32_t i0 = 0; i0 <= count; i0 += kGroupThreads) {
+    __syncthreads();
+    const uint32_t i = i0 + tid, n = i <= count ? bin[i] : 0, tiles = (n + kTileRows - 1) / kTileRows;
+    uint32_t a = n, b = tiles;
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t x = __shfl_up(a, d), y = __shfl_up(b, d);
+      if (lane >= (uint32_t)d) {
+        a += x;
+        b += y;
+      }
+    }
+    if (lane == 63) {
+      part[0][wave] = a;
+      part[1][wave] = b;
+    }
+    __syncthreads();
+    uint32_t first = rows_before + a - n, tile = tiles_before + b - tiles;
+    for (uint32_t w = 0; w < kGroupThreads / 64; ++w) {
+      if (w < wave) {
+        first += part[0][w];
+        tile += part[1][w];
+      }
+      rows_before += part[0][w];
+      tiles_before += part[1][w];
+    }
+    if (i <= count) {
+      bin[i] = first;
+      for (uint32_t k = 0; k < tiles; ++k)
+        out.tiles[tile + k] = {i < count ? (int32_t)i : -1, first + k * kTileRows, n - k * kTileRows < kTileRows ? n - k * kTileRows : kTileRows, 0};
+    }
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < rows; i += kGroupThreads) {
+    const uint32_t id = (uint32_t)ids[i];
+    out.order[atomicAdd(&bin[id < count ? id : count], 1u)] = (int32_t)i;
+  }
+  if (tid == 0) *out.tiles_there = tiles_before;
+}
+
+struct Adapt {
+  ft_adapters_call c;
+  Groups g;
+  float *h;          // splits x rows (in their order) x pitch
+  uint32_t pitch;    // max_rank rounded up to 16
+  uint32_t splits, split;  // of the long axis: how many, elements of one (a multiple of 256)
+  uint32_t blocks;   // of 64 columns that a workgroup of the second product has
+};
+
+// 8 elements of a row from `at`, those from `end` on zero.
+__device__ inline Words4 load_to(const uint16_t *row, uint32_t at, uint32_t end) {
+  if (at + 8 <= end) return load16(row + at);
+  Words4 w{0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i)
+    if (at + i < end) w[i / 2] |= (uint32_t)row[at + i] << (i % 2 * 16);
+  return w;
+}
+
+// Tiles of 16 rows of X times tiles of 16 rows of A, over this wavefront's part of the long axis; 64 elements of it at a time.
+template <class T, int NT, int RT>
+__device__ inline void shrink(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint32_t r0, uint32_t k0, uint32_t k1, float *lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  const uint16_t *x[NT], *a[RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint32_t i = t * 16 + n16 < tile.count ? t * 16 + n16 : tile.count - 1;
+    x[t] = static_cast<const uint16_t *>(p.c.x) + (uint64_t)p.g.order[tile.first + i] * p.c.x_stride;
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const uint32_t r = r0 + t * 16 + n16;
+    a[t] = reinterpret_cast<const uint16_t *>(rec.a) + (uint64_t)(r < rank ? r : rank - 1) * p.c.width_in;
+  }
+  Floats4 acc[NT][RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int u = 0; u < RT; ++u) acc[t][u] = Floats4{0, 0, 0, 0};
+  uint32_t k = k0 + wave * 64;
+  for (; k + 64 <= k1; k += 256) {
+    Words4 xf[2][NT], af[2][RT];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int u = 0; u < RT; ++u) af[s][u] = load16(a[u] + k + s * 32 + 8 * g);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xf[s][t] = load16(x[t] + k + s * 32 + 8 * g);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int u = 0; u < RT; ++u) acc[t][u] = T::mfma(af[s][u], xf[s][t], acc[t][u]);
+  }
+  for (; k < k1; k += k % 64 == 32 ? 224 : 32) {  // what is left of the last 64, where a row may end anywhere
+    Words4 xf[NT], af[RT];
+#pragma unroll
+    for (int u = 0; u < RT; ++u) af[u] = load_to(a[u], k + 8 * g, k1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xf[t] = load_to(x[t], k + 8 * g, k1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < RT; ++u) acc[t][u] = T::mfma(af[u], xf[t], acc[t][u]);
+  }
+  Floats4 *room = reinterpret_cast<Floats4 *>(lds);
+  __syncthreads();
+  if (wave != 0)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < RT; ++u) room[((wave - 1) * NT * RT + t * RT + u) * 64 + lane] = acc[t][u];
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int u = 0; u < RT; ++u) {
+      for (int w = 0; w < 3; ++w) acc[t][u] += room[(w * NT * RT + t * RT + u) * 64 + lane];
+      const uint32_t r = r0 + u * 16 + 4 * g;
+      if (t * 16 + n16 < tile.count && r < p.pitch)
+        *reinterpret_cast<Floats4 *>(p.h + ((uint64_t)blockIdx.y * p.c.rows + tile.first + t * 16 + n16) * p.pitch + r) = acc[t][u];
+    }
+}
+
 template <class T>
-__global__ __launch_bounds__(256) void ft_adapter_shrink_kernel(ft_adapters_call c, float *h) {
-  const int32_t *ids = static_cast<const int32_t *>(c.groups);
-  const uint32_t row = blockIdx.x, lane = threadIdx.x & 63;
-  const uint32_t id = (uint32_t)ids[row];
-  if (id >= c.count) return;
-  const ft_adapter_record rec = c.records[id];
-  const uint32_t rank = rec.rank < c.max_rank ? rec.rank : c.max_rank;
-  const uint16_t *x = static_cast<const uint16_t *>(c.x) + row * c.x_stride;
-  for (uint32_t r = threadIdx.x >> 6; r < rank; r += 4) {
-    const uint16_t *a = reinterpret_cast<const uint16_t *>(rec.a) + (uint64_t)r * c.width_in;
-    float sum = 0;
-    for (uint32_t i = lane; i < c.width_in; i += 64) sum += T::to_float(x[i]) * T::to_float(a[i]);
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) h[(uint64_t)row * c.max_rank + r] = sum * rec.scale;
+__global__ __launch_bounds__(256) void ft_adapter_shrink_kernel(Adapt p) {
+  __shared__ float lds[3 * 16 * 256];
+  if (blockIdx.x >= *p.g.tiles_there) return;
+  const Tile tile = p.g.tiles[blockIdx.x];
+  if (tile.adapter < 0) return;
+  const ft_adapter_record rec = p.c.records[tile.adapter];
+  const uint32_t rank = rec.rank < p.c.max_rank ? rec.rank : p.c.max_rank;
+  const uint32_t k0 = blockIdx.y * p.split, k1 = k0 + p.split < p.c.width_in ? k0 + p.split : p.c.width_in;
+  for (uint32_t r0 = 0; r0 < rank; r0 += 64) {
+    if (tile.count <= 16) {
+      if (rank - r0 <= 16) shrink<T, 1, 1>(p, tile, rec, rank, r0, k0, k1, lds);
+      else if (rank - r0 <= 32) shrink<T, 1, 2>(p, tile, rec, rank, r0, k0, k1, lds);
+      else shrink<T, 1, 4>(p, tile, rec, rank, r0, k0, k1, lds);
+    } else {
+      if (rank - r0 <= 16) shrink<T, 4, 1>(p, tile, rec, rank, r0, k0, k1, lds);
+      else if (rank - r0 <= 32) shrink<T, 4, 2>(p, tile, rec, rank, r0, k0, k1, lds);
+      else shrink<T, 4, 4>(p, tile, rec, rank, r0, k0, k1, lds);
+    }
+  }
+}
+
+// 64 columns of a tile's rows. MFMA j has columns 4 m + j of them, m = 0 .. 15, so a lane's 16 results are 16 neighbours: its row's columns
+// 16 g + 4 i + j in acc[j][i].
+template <class T, int NT>
+__device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, const uint16_t *high, uint32_t row_pitch, const float *size) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  const uint16_t *low = high + kTileRows * row_pitch;
+  const uint32_t end = p.c.width_out, first_block = blockIdx.y * p.blocks;
+  uint64_t row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) row[t] = (uint64_t)p.g.order[tile.first + (t * 16 + n16 < tile.count ? t * 16 + n16 : tile.count - 1)];
+  for (uint32_t block = first_block + wave; block < first_block + p.blocks && block * 64 < end; block += 4) {
+    const uint32_t n0 = block * 64, mine = n0 + 16 * g;
+    const bool whole = n0 + 64 <= end;
+    Words4 base[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        base[t][x] = Words4{0, 0, 0, 0};
+        if (p.c.base != nullptr) {
+          const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride;
+          base[t][x] = whole ? load16(b + mine + 8 * x) : load_to(b, mine + 8 * x, end);
+        }
+      }
+    Floats4 acc[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[t][j] = Floats4{0, 0, 0, 0};
+    for (uint32_t r = 0; r < rank; r += 32) {
+      Words4 b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t n = n0 + 4 * n16 + j;
+        b[j] = load_to(reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(n < end ? n : end - 1) * rec.rank, r + 8 * g, rank);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t at = (t * 16 + n16) * row_pitch + r + 8 * g;
+        const Words4 hi = *reinterpret_cast<const Words4 *>(high + at), lo = *reinterpret_cast<const Words4 *>(low + at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[j], lo, acc[t][j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[j], hi, acc[t][j]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (t * 16 + n16 >= tile.count) continue;
+      const float by = size[t * 16 + n16];
+      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + mine;
+      uint32_t w[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const uint32_t two = base[t][x / 4][x % 4];
+        const float lo = T::to_float((uint16_t)two), hi = T::to_float((uint16_t)(two >> 16));
+        w[x] = T::pack(__builtin_fmaf(acc[t][x % 2 * 2][x / 2], by, lo), __builtin_fmaf(acc[t][x % 2 * 2 + 1][x / 2], by, hi));
+      }
+      if (whole) {
+        *reinterpret_cast<Loose4 *>(out) = Loose4{{w[0], w[1], w[2], w[3]}};
+        *reinterpret_cast<Loose4 *>(out + 8) = Loose4{{w[4], w[5], w[6], w[7]}};
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i)
+          if (mine + i < end) out[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+      }
+    }
   }
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void ft_adapter_expand_kernel(ft_adapters_call c, const float *h) {
-  const int32_t *ids = static_cast<const int32_t *>(c.groups);
-  const uint32_t row = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  if (n >= c.width_out) return;
-  const uint32_t id = (uint32_t)ids[row];
-  float sum = 0;
-  if (id < c.count) {
-    const ft_adapter_record rec = c.records[id];
-    const uint32_t rank = rec.rank < c.max_rank ? rec.rank : c.max_rank;
-    const uint16_t *b = reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)n * rec.rank;
-    for (uint32_t r = 0; r < rank; ++r) sum += h[(uint64_t)row * c.max_rank + r] * T::to_float(b[r]);
+__global__ __launch_bounds__(256) void ft_adapter_expand_kernel(Adapt p) {
+  extern __shared__ uint16_t halves[];  // 64 rows x (rank rounded up to 32, and 8): the high parts, then the low ones
+  __shared__ float size[kTileRows];
+  if (blockIdx.x >= *p.g.tiles_there) return;
+  const Tile tile = p.g.tiles[blockIdx.x];
+  if (tile.adapter < 0) {
+    // rows without an adapter: base as it is, or zero
+    if (p.c.out == p.c.base && p.c.out_stride == p.c.base_stride) return;
+    const uint32_t first = blockIdx.y * p.blocks * 64, end = first + p.blocks * 64 < p.c.width_out ? first + p.blocks * 64 : p.c.width_out;
+    for (uint32_t i = threadIdx.x >> 6; i < tile.count; i += 4) {
+      const uint64_t row = (uint64_t)p.g.order[tile.first + i];
+      const uint16_t *from = static_cast<const uint16_t *>(p.c.base) + row * p.c.base_stride;
+      uint16_t *to = static_cast<uint16_t *>(p.c.out) + row * p.c.out_stride;
+      for (uint32_t n = first + (threadIdx.x & 63) * 8; n < end; n += 512) {
+        const Words4 w = p.c.base == nullptr ? Words4{0, 0, 0, 0} : load_to(from, n, end);
+        if (n + 8 <= end) *reinterpret_cast<Loose4 *>(to + n) = Loose4{{w[0], w[1], w[2], w[3]}};
+        else
+          for (uint32_t k = 0; n + k < end; ++k) to[n + k] = (uint16_t)(w[k / 2] >> (k % 2 * 16));
+      }
+    }
+    return;
   }
-  if (c.base != nullptr) sum += T::to_float(static_cast<const uint16_t *>(c.base)[row * c.base_stride + n]);
-  static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum);
+  const ft_adapter_record rec = p.c.records[tile.adapter];
+  const uint32_t rank = rec.rank < p.c.max_rank ? rec.rank : p.c.max_rank, row_pitch = (rank + 31) / 32 * 32 + 8;
+  // The parts of a row of H added up, 16 lanes to a row. Each is brought to between 1 and 2 by a power of two that multiplies the result, so that
+  // the range of 16 bits neither cuts large ones off nor takes digits from small ones. (Products with NaN and infinities remain what they are.)
+  const uint32_t rows16 = (tile.count + 15) / 16 * 16;
+  for (uint32_t i = threadIdx.x >> 4; i < rows16; i += 16) {
+    const uint32_t q = threadIdx.x & 15, from = tile.first + (i < tile.count ? i : tile.count - 1);
+    const auto part = [&](uint32_t r) {
+      float sum = 0;
+      for (uint32_t s = 0; s < p.splits; ++s) sum += p.h[((uint64_t)s * p.c.rows + from) * p.pitch + r];
+      return sum;
+    };
+    float most = 0;
+    for (uint32_t r = q; r < rank; r += 16) most = fmaxf(most, fabsf(part(r)));
+    for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    int e = (int)(__float_as_uint(most) >> 23) - 127;
+    if (most == 0 || e > 126) e = 0;
+    e = e < -120 ? -120 : e;
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    if (q == 0) size[i] = __uint_as_float((uint32_t)(127 + e) << 23) * rec.scale;
+    for (uint32_t r = q; r < row_pitch; r += 16) {
+      const float v = r < rank ? part(r) * down : 0;
+      const uint16_t hi = T::from_float(v);
+      const float rest = v - T::to_float(hi);
+      halves[i * row_pitch + r] = hi;
+      halves[(kTileRows + i) * row_pitch + r] = T::from_float(fabsf(v) < INFINITY ? rest : 0);
+    }
+  }
+  __syncthreads();
+  if (tile.count <= 16) expand<T, 1>(p, tile, rec, rank, halves, row_pitch, size);
+  else expand<T, 4>(p, tile, rec, rank, halves, row_pitch, size);
+}
+
+uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+
+// Workgroups that keep the chip busy; the long axis is split until there are as many, into pieces of 256 elements and more.
+constexpr uint64_t kEnough = 512;
+
+void split_of(const ft_adapters_call &c, uint32_t *splits, uint32_t *split) {
+  const uint64_t tiles = most_tiles(c.rows, c.count), most = (c.width_in + 255) / 256;
+  uint64_t n = (kEnough + tiles - 1) / tiles;
+  n = n > most ? most : n;
+  *split = (uint32_t)up((c.width_in + n - 1) / n, 256);
+  *splits = (c.width_in + *split - 1) / *split;
 }
 
 }  // namespace
 
-uint64_t adapter_group_bytes(uint32_t rows, uint32_t) { return ((uint64_t)rows * 4 + 15) / 16 * 16; }
+uint64_t adapter_group_bytes(uint32_t rows, uint32_t count) { return 64 + up(most_tiles(rows, count) * sizeof(Tile) + (uint64_t)rows * 4, 16); }
 
-hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t, void *groups, hipStream_t stream) {
-  return hipMemcpyAsync(groups, ids, (uint64_t)rows * 4, hipMemcpyDeviceToDevice, stream);
+hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t count, void *groups, hipStream_t stream) {
+  hipLaunchKernelGGL(ft_adapter_group_kernel, dim3(1), dim3(kGroupThreads), (count + 1) * 4, stream, ids, rows, count, groups_at(groups, rows, count));
+  return hipGetLastError();
 }
 
-uint64_t adapter_workspace(const ft_adapters_call &call) { return ((uint64_t)call.rows * call.max_rank * 4 + 15) / 16 * 16; }
+uint64_t adapter_workspace(const ft_adapters_call &c) {
+  uint32_t splits, split;
+  split_of(c, &splits, &split);
+  return (uint64_t)splits * c.rows * up(c.max_rank, 16) * 4;
+}
+
+template <class T>
+hipError_t launch(const Adapt &p, hipStream_t stream) {
+  const uint32_t tiles = (uint32_t)most_tiles(p.c.rows, p.c.count), blocks = (p.c.width_out + 63) / 64;
+  hipLaunchKernelGGL(ft_adapter_shrink_kernel<T>, dim3(tiles, p.splits), dim3(256), 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(ft_adapter_expand_kernel<T>, dim3(tiles, (blocks + p.blocks - 1) / p.blocks), dim3(256), kTileRows * (up(p.c.max_rank, 32) + 8) * 4, stream, p);
+  return hipGetLastError();
+}
 
 hipError_t launch_adapters(const ft_adapters_call &call, hipStream_t stream) {
-  float *h = static_cast<float *>(call.workspace);
-  const dim3 grid(call.rows, (call.width_out + 255) / 256);
-  if (call.type == FT_BF16) {
-    hipLaunchKernelGGL(ft_adapter_shrink_kernel<Bf16>, dim3(call.rows), dim3(256), 0, stream, call, h);
-    hipLaunchKernelGGL(ft_adapter_expand_kernel<Bf16>, grid, dim3(256), 0, stream, call, h);
-  } else {
-    hipLaunchKernelGGL(ft_adapter_shrink_kernel<Fp16>, dim3(call.rows), dim3(256), 0, stream, call, h);
-    hipLaunchKernelGGL(ft_adapter_expand_kernel<Fp16>, grid, dim3(256), 0, stream, call, h);
-  }
-  return hipGetLastError();
+  Adapt p{call};
+  p.g = groups_at(const_cast<void *>(call.groups), call.rows, call.count);
+  p.h = static_cast<float *>(call.workspace);
+  p.pitch = (uint32_t)up(call.max_rank, 16);
+  split_of(call, &p.splits, &p.split);
+  // a workgroup's four wavefronts take a block at least each
+  const uint64_t blocks = (call.width_out + 63) / 64, per = blocks * most_tiles(call.rows, call.count) / (2 * kEnough);
+  p.blocks = (uint32_t)up(per < 4 ? 4 : per > 16 ? 16 : per, 4);
+  return call.type == FT_BF16 ? launch<Bf16>(p, stream) : launch<Fp16>(p, stream);
 }
 
 }  // namespace ft

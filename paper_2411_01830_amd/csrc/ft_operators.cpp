@@ -98,7 +98,7 @@ bool good_numbers(const ft_kv_cache &c, const ft_tree_call &t) {
 }
 
 bool good_numbers(const ft_adapters_call &a) {
-  if (a.type > FT_FP16 || a.count == 0 || a.count > 1u << 20 || a.width_in == 0 || a.width_out == 0 || a.rows >= 1u << 31) return false;
+  if (a.type > FT_FP16 || a.count == 0 || a.count > 1u << 14 || a.width_in == 0 || a.width_out == 0 || a.rows >= 1u << 31) return false;
   if (a.width_in >= 1u << 24 || a.width_out >= 1u << 24) return false;
   return a.max_rank >= 1 && a.max_rank <= 256;
 }
@@ -214,13 +214,13 @@ int ft_adapters_resolve(ft_pool *p, const ft_adapter *adapters, uint32_t count, 
 FT_CATCH_ALL
 
 int ft_adapters_group_bytes(uint32_t rows, uint32_t count, uint64_t *bytes_out) {
-  if (bytes_out == nullptr || rows >= 1u << 31 || count == 0 || count > 1u << 20) return FT_EINVAL;
+  if (bytes_out == nullptr || rows >= 1u << 31 || count == 0 || count > 1u << 14) return FT_EINVAL;
   *bytes_out = adapter_group_bytes(rows, count);
   return FT_OK;
 }
 
 int ft_adapters_group(ft_pool *p, const int32_t *ids, uint32_t rows, uint32_t count, void *groups, uint64_t groups_bytes, void *hip_stream) try {
-  if (p == nullptr || rows >= 1u << 31 || count == 0 || count > 1u << 20) return FT_EINVAL;
+  if (p == nullptr || rows >= 1u << 31 || count == 0 || count > 1u << 14) return FT_EINVAL;
   if (rows != 0 && !there(ids, 4)) return FT_EINVAL;
   if (!there(groups, 16) || groups_bytes < adapter_group_bytes(rows, count)) return FT_EINVAL;
   std::lock_guard<std::mutex> lock(p->mu);

@@ -318,7 +318,7 @@ class Tree:
                     w = p / torch.where(z == 0, 1.0, z)
                     want, mass = w @ seen_v, w @ seen_v.abs()
                     # a score is a sum of dim products in 24 bits, scaled and carried to powers of two: its error is a weight's relative one
-                    score = torch.where(sees, q.abs() @ seen_k.abs().t() * self.scale, 0).max(1, keepdim=True).values
+                    score = torch.where(sees, q.abs() @ seen_k.abs().t() * abs(self.scale), 0).max(1, keepdim=True).values
                     delta = (self.dim + 8) * 2.0 ** -24 * score + 2.0 ** -19
                     keys = sees.sum(1, keepdim=True)
                     bound = u * want.abs() + (1.01 * u + 2 * delta) * mass + tiny * (1 + keys * seen_v.abs().max(0).values[None]) + keys * 2.0 ** -24 * mass
@@ -612,3 +612,29 @@ def test_operators_captured_in_a_graph():
         for x, y in zip(got, want):
             assert torch.equal(x, y), i
         torch.empty(1 << 20, device="cuda").fill_(float("nan"))
+
+
+def test_as_many_adapters_as_there_may_be():
+    """16384 of them, of which a few rows have some."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    m = Memory(1 << 20)
+    at = m.alloc(2 * 4 * 64), m.alloc(2 * 4 * 96)
+    a, b = [torch.randn(n, device="cuda", generator=g).to(BF16) for n in (4 * 64, 4 * 96)]
+    m.view(at[0], BF16, 4 * 64).copy_(a)
+    m.view(at[1], BF16, 4 * 96).copy_(b)
+    adapters = ops().Adapters(m.pool, [(at[0], at[1], 4, float(1 + i % 7)) for i in range(16384)], 64, 96, BF16)
+    ids = gpu([16383, 0, -1, 16384, 5000, 16383, 77])
+    x = torch.randn(7, 64, device="cuda", generator=g).to(BF16)
+    out = ops().adapters_apply(adapters, ops().adapter_groups(adapters, ids), x)
+    scales = torch.tensor([1 + i % 7 if 0 <= i < 16384 else 0 for i in ids.tolist()], dtype=torch.float64)
+    want = scales[:, None] * ((x.double().cpu() @ a.view(4, 64).double().cpu().t()) @ b.view(96, 4).double().cpu().t())
+    # rounded once, after sums in 24 bits of which the terms are at most 64 and 4 times the result's order of magnitude
+    assert (out.double().cpu() - want).abs().max() <= 2.0 ** -8 * want.abs().max() * 1.01
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-4, 3.0])
+def test_scales_of_either_sign(scale):
+    """A scale of zero weighs all that is seen alike; a negative one turns the order of the weights round."""
+    t = Tree(lens=[70, 0, 33], news=[5, 20, 1], heads=2, group=2, dim=64, page=16, dtype=BF16)
+    t.scale = scale
+    t.check(*t.call())
