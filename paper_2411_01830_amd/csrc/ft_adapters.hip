@@ -180,7 +180,7 @@ __device__ inline void shrink(const Adapt &p, const Tile &tile, const ft_adapter
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void ft_adapter_shrink_kernel(Adapt p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_adapter_shrink_kernel(Adapt p) {
   __shared__ float lds[3 * 16 * 256];
   if (blockIdx.x >= *p.g.tiles_there) return;
   const Tile tile = p.g.tiles[blockIdx.x];
@@ -201,8 +201,8 @@ __global__ __launch_bounds__(256) void ft_adapter_shrink_kernel(Adapt p) {
   }
 }
 
-// 64 columns of a tile's rows. MFMA j has columns 4 m + j of them, m = 0 .. 15, so a lane's 16 results are 16 neighbours: its row's columns
-// 16 g + 4 i + j in acc[j][i].
+// 64 columns of a tile's rows. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours: columns
+// 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on.
 template <class T, int NT>
 __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, const uint16_t *high, uint32_t row_pitch, const float *size) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
@@ -211,20 +211,23 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
   uint64_t row[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) row[t] = (uint64_t)p.g.order[tile.first + (t * 16 + n16 < tile.count ? t * 16 + n16 : tile.count - 1)];
-  for (uint32_t block = first_block + wave; block < first_block + p.blocks && block * 64 < end; block += 4) {
-    const uint32_t n0 = block * 64, mine = n0 + 16 * g;
+  const uint32_t last_block = first_block + p.blocks < (end + 63) / 64 ? first_block + p.blocks : (end + 63) / 64;
+  const auto load_base = [&](uint32_t block, Words4 (&into)[NT][2]) {
+    const uint32_t at = block * 64 + 8 * g;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) into[t][x] = block * 64 + 64 <= end ? load16(b + at + 32 * x) : load_to(b, at + 32 * x, end);
+    }
+  };
+  Words4 base[NT][2] = {}, next[NT][2] = {};
+  if (first_block + wave >= last_block) return;
+  if (p.c.base != nullptr) load_base(first_block + wave, base);
+  for (uint32_t block = first_block + wave; block < last_block; block += 4) {
+    const uint32_t n0 = block * 64;
     const bool whole = n0 + 64 <= end;
-    Words4 base[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        base[t][x] = Words4{0, 0, 0, 0};
-        if (p.c.base != nullptr) {
-          const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride;
-          base[t][x] = whole ? load16(b + mine + 8 * x) : load_to(b, mine + 8 * x, end);
-        }
-      }
+    if (p.c.base != nullptr && block + 4 < last_block) load_base(block + 4, next);
     Floats4 acc[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -234,8 +237,14 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
       Words4 b[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t n = n0 + 4 * n16 + j;
-        b[j] = load_to(reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(n < end ? n : end - 1) * rec.rank, r + 8 * g, rank);
+        const uint32_t n = n0 + (n16 >> 1 & 1) * 32 + (n16 >> 2) * 8 + (n16 & 1) * 4 + j, k = r + 8 * g;
+        const uint16_t *row_of_b = reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(n < end ? n : end - 1) * rec.rank;
+        if (rank % 8 == 0) {
+          b[j] = Words4{0, 0, 0, 0};
+          if (k < rank) b[j] = load16(row_of_b + k);
+        } else {
+          b[j] = load_to(row_of_b, k, rank);
+        }
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -251,28 +260,34 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
     for (int t = 0; t < NT; ++t) {
       if (t * 16 + n16 >= tile.count) continue;
       const float by = size[t * 16 + n16];
-      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + mine;
-      uint32_t w[8];
+      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + n0 + 8 * g;
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const uint32_t two = base[t][x / 4][x % 4];
-        const float lo = T::to_float((uint16_t)two), hi = T::to_float((uint16_t)(two >> 16));
-        w[x] = T::pack(__builtin_fmaf(acc[t][x % 2 * 2][x / 2], by, lo), __builtin_fmaf(acc[t][x % 2 * 2 + 1][x / 2], by, hi));
-      }
-      if (whole) {
-        *reinterpret_cast<Loose4 *>(out) = Loose4{{w[0], w[1], w[2], w[3]}};
-        *reinterpret_cast<Loose4 *>(out + 8) = Loose4{{w[4], w[5], w[6], w[7]}};
-      } else {
+      for (int x = 0; x < 2; ++x) {
+        uint32_t w[4];
 #pragma unroll
-        for (uint32_t i = 0; i < 16; ++i)
-          if (mine + i < end) out[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+        for (int y = 0; y < 4; ++y) {  // elements 2 y and 2 y + 1 of 8: i = 2 x + y / 2, j = 2 (y % 2) and the next
+          const uint32_t two = base[t][x][y];
+          const float lo = T::to_float((uint16_t)two), hi = T::to_float((uint16_t)(two >> 16));
+          w[y] = T::pack(__builtin_fmaf(acc[t][y % 2 * 2][2 * x + y / 2], by, lo), __builtin_fmaf(acc[t][y % 2 * 2 + 1][2 * x + y / 2], by, hi));
+        }
+        if (whole) {
+          *reinterpret_cast<Loose4 *>(out + 32 * x) = Loose4{{w[0], w[1], w[2], w[3]}};
+        } else {
+#pragma unroll
+          for (uint32_t i = 0; i < 8; ++i)
+            if (n0 + 32 * x + 8 * g + i < end) out[32 * x + i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+        }
       }
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) base[t][x] = next[t][x];
   }
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void ft_adapter_expand_kernel(Adapt p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_adapter_expand_kernel(Adapt p) {
   extern __shared__ uint16_t halves[];  // 64 rows x (rank rounded up to 32, and 8): the high parts, then the low ones
   __shared__ float size[kTileRows];
   if (blockIdx.x >= *p.g.tiles_there) return;
@@ -301,25 +316,43 @@ __global__ __launch_bounds__(256) void ft_adapter_expand_kernel(Adapt p) {
   const uint32_t rows16 = (tile.count + 15) / 16 * 16;
   for (uint32_t i = threadIdx.x >> 4; i < rows16; i += 16) {
     const uint32_t q = threadIdx.x & 15, from = tile.first + (i < tile.count ? i : tile.count - 1);
-    const auto part = [&](uint32_t r) {
-      float sum = 0;
-      for (uint32_t s = 0; s < p.splits; ++s) sum += p.h[((uint64_t)s * p.c.rows + from) * p.pitch + r];
-      return sum;
-    };
+    Floats4 v[4];  // elements 64 k + 4 q .. + 3
     float most = 0;
-    for (uint32_t r = q; r < rank; r += 16) most = fmaxf(most, fabsf(part(r)));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = Floats4{0, 0, 0, 0};
+      const uint32_t r = 64 * k + 4 * q;
+      if (64 * k >= (int)rank) continue;
+      const float *part = p.h + (uint64_t)from * p.pitch + (r < p.pitch ? r : 0);
+#pragma unroll 8
+      for (uint32_t s = 0; s < p.splits; ++s) v[k] += *reinterpret_cast<const Floats4 *>(part + (uint64_t)s * p.c.rows * p.pitch);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (r + x >= rank) v[k][x] = 0;
+        most = fmaxf(most, fabsf(v[k][x]));
+      }
+    }
     for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
     int e = (int)(__float_as_uint(most) >> 23) - 127;
     if (most == 0 || e > 126) e = 0;
     e = e < -120 ? -120 : e;
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
     if (q == 0) size[i] = __uint_as_float((uint32_t)(127 + e) << 23) * rec.scale;
-    for (uint32_t r = q; r < row_pitch; r += 16) {
-      const float v = r < rank ? part(r) * down : 0;
-      const uint16_t hi = T::from_float(v);
-      const float rest = v - T::to_float(hi);
-      halves[i * row_pitch + r] = hi;
-      halves[(kTileRows + i) * row_pitch + r] = T::from_float(fabsf(v) < INFINITY ? rest : 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t r = 64 * k + 4 * q;
+      if (r >= row_pitch) continue;
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int x = 0; x < 4; x += 2) {
+        const float a = v[k][x] * down, b = v[k][x + 1] * down;
+        hi[x / 2] = T::pack(a, b);
+        const float ra = a - T::to_float((uint16_t)hi[x / 2]), rb = b - T::to_float((uint16_t)(hi[x / 2] >> 16));
+        lo[x / 2] = T::pack(fabsf(a) < INFINITY ? ra : 0, fabsf(b) < INFINITY ? rb : 0);
+      }
+      typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+      *reinterpret_cast<Words2 *>(&halves[i * row_pitch + r]) = Words2{hi[0], hi[1]};
+      *reinterpret_cast<Words2 *>(&halves[(kTileRows + i) * row_pitch + r]) = Words2{lo[0], lo[1]};
     }
   }
   __syncthreads();
