@@ -40,6 +40,21 @@ __host__ __device__ inline Groups groups_at(void *p, uint32_t rows, uint32_t cou
   return {reinterpret_cast<uint32_t *>(at), reinterpret_cast<Tile *>(at + 64), reinterpret_cast<int32_t *>(at + 64 + most_tiles(rows, count) * sizeof(Tile))};
 }
 
+// Adds one for every lane that takes part to its bin, and gives each where it comes among them. Neighbouring rows are mostly of one request:
+// lanes with the first one's bin add once together.
+__device__ inline uint32_t take(uint32_t *bin, uint32_t id, bool takes) {
+  const uint64_t active = __ballot(takes);
+  if (active == 0) return 0;
+  const int lane = threadIdx.x & 63, leader = __builtin_ctzll(active);
+  const bool same = takes && id == (uint32_t)__shfl((int)id, leader);
+  const uint64_t with = __ballot(same);
+  uint32_t at = 0;
+  if (lane == leader) at = atomicAdd(&bin[id], (uint32_t)__popcll(with));
+  at = (uint32_t)__shfl((int)at, leader) + (uint32_t)__popcll(with & ((1ull << lane) - 1));
+  if (takes && !same) at = atomicAdd(&bin[id], 1u);
+  return at;
+}
+
 // A counting sort in one workgroup. Where a row comes among those of its adapter depends on the order of atomics, and nothing else does: every
 // row's result is its own column of a product.
 __global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const int32_t *__restrict__ ids, uint32_t rows, uint32_t count, Groups out) {
@@ -48,9 +63,9 @@ __global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const i
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (uint32_t i = tid; i <= count; i += kGroupThreads) bin[i] = 0;
   __syncthreads();
-  for (uint32_t i = tid; i < rows; i += kGroupThreads) {
-    const uint32_t id = (uint32_t)ids[i];
-    atomicAdd(&bin[id < count ? id : count], 1u);
+  for (uint32_t i0 = 0; i0 < rows; i0 += kGroupThreads) {
+    const uint32_t i = i0 + tid, id = i < rows ? (uint32_t)ids[i] : 0;
+    take(bin, id < count ? id : count, i < rows);
   }
   uint32_t rows_before = 0, tiles_before = 0;
   for (uint32_t i0 = 0; i0 <= count; i0 += kGroupThreads) {
@@ -85,9 +100,9 @@ __global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const i
     }
   }
   __syncthreads();
-  for (uint32_t i = tid; i < rows; i += kGroupThreads) {
-    const uint32_t id = (uint32_t)ids[i];
-    out.order[atomicAdd(&bin[id < count ? id : count], 1u)] = (int32_t)i;
+  for (uint32_t i0 = 0; i0 < rows; i0 += kGroupThreads) {
+    const uint32_t i = i0 + tid, id = i < rows ? (uint32_t)ids[i] : 0, at = take(bin, id < count ? id : count, i < rows);
+    if (i < rows) out.order[at] = (int32_t)i;
   }
   if (tid == 0) *out.tiles_there = tiles_before;
 }
@@ -182,9 +197,8 @@ __device__ inline void shrink(const Adapt &p, const Tile &tile, const ft_adapter
 template <class T>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_adapter_shrink_kernel(Adapt p) {
   __shared__ float lds[3 * 16 * 256];
-  if (blockIdx.x >= *p.g.tiles_there) return;
-  const Tile tile = p.g.tiles[blockIdx.x];
-  if (tile.adapter < 0) return;
+  const Tile tile = p.g.tiles[blockIdx.x];  // (there is room for as many as the grid has, and not all of them are there)
+  if (blockIdx.x >= *p.g.tiles_there || tile.adapter < 0) return;
   const ft_adapter_record rec = p.c.records[tile.adapter];
   const uint32_t rank = rec.rank < p.c.max_rank ? rec.rank : p.c.max_rank;
   const uint32_t k0 = blockIdx.y * p.split, k1 = k0 + p.split < p.c.width_in ? k0 + p.split : p.c.width_in;
@@ -201,10 +215,58 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
+template <class T>
+__device__ inline void add_up(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *halves, uint32_t row_pitch, float *size) {
+  // The parts of a row of H added up, 16 lanes to a row. Each is brought to between 1 and 2 by a power of two that multiplies the result, so that
+  // the range of 16 bits neither cuts large ones off nor takes digits from small ones. (Products with NaN and infinities remain what they are.)
+  const uint32_t rows16 = (tile.count + 15) / 16 * 16;
+  for (uint32_t i = threadIdx.x >> 4; i < rows16; i += 16) {
+    const uint32_t q = threadIdx.x & 15, from = tile.first + (i < tile.count ? i : tile.count - 1);
+    Floats4 v[4];  // elements 64 k + 4 q .. + 3
+    float most = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = Floats4{0, 0, 0, 0};
+      const uint32_t r = 64 * k + 4 * q;
+      if (64 * k >= (int)rank) continue;
+      const float *part = p.h + (uint64_t)from * p.pitch + (r < p.pitch ? r : 0);
+#pragma unroll 8
+      for (uint32_t s = 0; s < p.splits; ++s) v[k] += *reinterpret_cast<const Floats4 *>(part + (uint64_t)s * p.c.rows * p.pitch);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (r + x >= rank) v[k][x] = 0;
+        most = fmaxf(most, fabsf(v[k][x]));
+      }
+    }
+    for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    int e = (int)(__float_as_uint(most) >> 23) - 127;
+    if (most == 0 || e > 126) e = 0;
+    e = e < -120 ? -120 : e;
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    if (q == 0) size[i] = __uint_as_float((uint32_t)(127 + e) << 23) * rec.scale;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t r = 64 * k + 4 * q;
+      if (r >= row_pitch) continue;
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int x = 0; x < 4; x += 2) {
+        const float a = v[k][x] * down, b = v[k][x + 1] * down;
+        hi[x / 2] = T::pack(a, b);
+        const float ra = a - T::to_float((uint16_t)hi[x / 2]), rb = b - T::to_float((uint16_t)(hi[x / 2] >> 16));
+        lo[x / 2] = T::pack(fabsf(a) < INFINITY ? ra : 0, fabsf(b) < INFINITY ? rb : 0);
+      }
+      typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+      *reinterpret_cast<Words2 *>(&halves[i * row_pitch + r]) = Words2{hi[0], hi[1]};
+      *reinterpret_cast<Words2 *>(&halves[(kTileRows + i) * row_pitch + r]) = Words2{lo[0], lo[1]};
+    }
+  }
+}
+
 // 64 columns of a tile's rows. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours: columns
 // 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on.
 template <class T, int NT>
-__device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, const uint16_t *high, uint32_t row_pitch, const float *size) {
+__device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *high, uint32_t row_pitch, float *size) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
   const uint16_t *low = high + kTileRows * row_pitch;
   const uint32_t end = p.c.width_out, first_block = blockIdx.y * p.blocks;
@@ -222,8 +284,9 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
     }
   };
   Words4 base[NT][2] = {}, next[NT][2] = {};
-  if (first_block + wave >= last_block) return;
-  if (p.c.base != nullptr) load_base(first_block + wave, base);
+  if (p.c.base != nullptr && first_block + wave < last_block) load_base(first_block + wave, base);
+  add_up<T>(p, tile, rec, rank, high, row_pitch, size);
+  __syncthreads();
   for (uint32_t block = first_block + wave; block < last_block; block += 4) {
     const uint32_t n0 = block * 64;
     const bool whole = n0 + 64 <= end;
@@ -290,8 +353,8 @@ template <class T>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_adapter_expand_kernel(Adapt p) {
   extern __shared__ uint16_t halves[];  // 64 rows x (rank rounded up to 32, and 8): the high parts, then the low ones
   __shared__ float size[kTileRows];
-  if (blockIdx.x >= *p.g.tiles_there) return;
   const Tile tile = p.g.tiles[blockIdx.x];
+  if (blockIdx.x >= *p.g.tiles_there) return;
   if (tile.adapter < 0) {
     // rows without an adapter: base as it is, or zero
     if (p.c.out == p.c.base && p.c.out_stride == p.c.base_stride) return;
@@ -311,51 +374,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
   const ft_adapter_record rec = p.c.records[tile.adapter];
   const uint32_t rank = rec.rank < p.c.max_rank ? rec.rank : p.c.max_rank, row_pitch = (rank + 31) / 32 * 32 + 8;
-  // The parts of a row of H added up, 16 lanes to a row. Each is brought to between 1 and 2 by a power of two that multiplies the result, so that
-  // the range of 16 bits neither cuts large ones off nor takes digits from small ones. (Products with NaN and infinities remain what they are.)
-  const uint32_t rows16 = (tile.count + 15) / 16 * 16;
-  for (uint32_t i = threadIdx.x >> 4; i < rows16; i += 16) {
-    const uint32_t q = threadIdx.x & 15, from = tile.first + (i < tile.count ? i : tile.count - 1);
-    Floats4 v[4];  // elements 64 k + 4 q .. + 3
-    float most = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = Floats4{0, 0, 0, 0};
-      const uint32_t r = 64 * k + 4 * q;
-      if (64 * k >= (int)rank) continue;
-      const float *part = p.h + (uint64_t)from * p.pitch + (r < p.pitch ? r : 0);
-#pragma unroll 8
-      for (uint32_t s = 0; s < p.splits; ++s) v[k] += *reinterpret_cast<const Floats4 *>(part + (uint64_t)s * p.c.rows * p.pitch);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (r + x >= rank) v[k][x] = 0;
-        most = fmaxf(most, fabsf(v[k][x]));
-      }
-    }
-    for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-    int e = (int)(__float_as_uint(most) >> 23) - 127;
-    if (most == 0 || e > 126) e = 0;
-    e = e < -120 ? -120 : e;
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    if (q == 0) size[i] = __uint_as_float((uint32_t)(127 + e) << 23) * rec.scale;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t r = 64 * k + 4 * q;
-      if (r >= row_pitch) continue;
-      uint32_t hi[2], lo[2];
-#pragma unroll
-      for (int x = 0; x < 4; x += 2) {
-        const float a = v[k][x] * down, b = v[k][x + 1] * down;
-        hi[x / 2] = T::pack(a, b);
-        const float ra = a - T::to_float((uint16_t)hi[x / 2]), rb = b - T::to_float((uint16_t)(hi[x / 2] >> 16));
-        lo[x / 2] = T::pack(fabsf(a) < INFINITY ? ra : 0, fabsf(b) < INFINITY ? rb : 0);
-      }
-      typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
-      *reinterpret_cast<Words2 *>(&halves[i * row_pitch + r]) = Words2{hi[0], hi[1]};
-      *reinterpret_cast<Words2 *>(&halves[(kTileRows + i) * row_pitch + r]) = Words2{lo[0], lo[1]};
-    }
-  }
-  __syncthreads();
   if (tile.count <= 16) expand<T, 1>(p, tile, rec, rank, halves, row_pitch, size);
   else expand<T, 4>(p, tile, rec, rank, halves, row_pitch, size);
 }
