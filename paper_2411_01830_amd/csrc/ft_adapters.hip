@@ -15,6 +15,7 @@ namespace {
 
 constexpr uint32_t kTileRows = 64;
 constexpr uint32_t kGroupThreads = 1024;
+constexpr uint32_t kAtOnce = 8;  // rows of a thread of the sort
 
 struct Tile {
   int32_t adapter;  // -1: none
@@ -37,7 +38,7 @@ __host__ __device__ inline uint64_t most_tiles(uint32_t rows, uint32_t count) {
 
 __host__ __device__ inline Groups groups_at(void *p, uint32_t rows, uint32_t count) {
   char *at = static_cast<char *>(p);
-  return {reinterpret_cast<uint32_t *>(at), reinterpret_cast<Tile *>(at + 64), reinterpret_cast<int32_t *>(at + 64 + (most_tiles(rows, count) + 7) / 8 * 8 * sizeof(Tile))};
+  return {reinterpret_cast<uint32_t *>(at), reinterpret_cast<Tile *>(at + 64), reinterpret_cast<int32_t *>(at + 64 + most_tiles(rows, count) * sizeof(Tile))};
 }
 
 // Adds one for every lane that takes part to its bin, and gives each where it comes among them. Neighbouring rows are mostly of one request:
@@ -63,9 +64,20 @@ __global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const i
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (uint32_t i = tid; i <= count; i += kGroupThreads) bin[i] = 0;
   __syncthreads();
-  for (uint32_t i0 = 0; i0 < rows; i0 += kGroupThreads) {
-    const uint32_t i = i0 + tid, id = i < rows ? (uint32_t)ids[i] : 0;
-    take(bin, id < count ? id : count, i < rows);
+  uint32_t id[kAtOnce];  // of rows i0 + tid, i0 + kGroupThreads + tid, ..: asked for together
+  const auto load = [&](uint32_t i0) {
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint32_t i = i0 + k * kGroupThreads + tid;
+      id[k] = (uint32_t)ids[i < rows ? i : rows - 1];
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) id[k] = id[k] < count ? id[k] : count;
+  };
+  for (uint32_t i0 = 0; i0 < rows; i0 += kAtOnce * kGroupThreads) {
+    load(i0);
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) take(bin, id[k], i0 + k * kGroupThreads + tid < rows);
   }
   uint32_t rows_before = 0, tiles_before = 0;
   for (uint32_t i0 = 0; i0 <= count; i0 += kGroupThreads) {
@@ -100,9 +112,13 @@ __global__ __launch_bounds__(kGroupThreads) void ft_adapter_group_kernel(const i
     }
   }
   __syncthreads();
-  for (uint32_t i0 = 0; i0 < rows; i0 += kGroupThreads) {
-    const uint32_t i = i0 + tid, id = i < rows ? (uint32_t)ids[i] : 0, at = take(bin, id < count ? id : count, i < rows);
-    if (i < rows) out.order[at] = (int32_t)i;
+  for (uint32_t i0 = 0; i0 < rows; i0 += kAtOnce * kGroupThreads) {
+    if (rows > kAtOnce * kGroupThreads) load(i0);  // (else they are still there)
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint32_t i = i0 + k * kGroupThreads + tid, at = take(bin, id[k], i < rows);
+      if (i < rows) out.order[at] = (int32_t)i;
+    }
   }
   if (tid == 0) *out.tiles_there = tiles_before;
 }
@@ -263,70 +279,67 @@ __device__ inline void add_up(const Adapt &p, const Tile &tile, const ft_adapter
   }
 }
 
-// 64 columns of a tile's rows at a time. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours:
-// columns 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base and of B is asked for before the block before is
-// written (stores are waited for together with loads that come after them), and without a condition (what has one is waited for as if it
-// were not there): that is for whole blocks and ranks of whole vectors; others go one after the other.
+// 64 columns of a tile's rows. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours: columns
+// 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on.
 template <class T, int NT>
 __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *high, uint32_t row_pitch, float *size) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
   const uint16_t *low = high + kTileRows * row_pitch;
-  const uint32_t end = p.c.width_out, blocks = (end + 63) / 64, first_block = blockIdx.y * p.blocks;
-  const uint32_t last_block = first_block + p.blocks < blocks ? first_block + p.blocks : blocks;
+  const uint32_t end = p.c.width_out, first_block = blockIdx.y * p.blocks;
   uint64_t row[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) row[t] = (uint64_t)p.g.order[tile.first + (t * 16 + n16 < tile.count ? t * 16 + n16 : tile.count - 1)];
-  const uint32_t column_of_b = (n16 >> 1 & 1) * 32 + (n16 >> 2) * 8 + (n16 & 1) * 4;
-  Words4 base[NT][2] = {}, b[2][4];
-  Floats4 acc[NT][4];
-
-  const auto load_whole_b = [&](uint32_t block, uint32_t r0) {
+  const uint32_t last_block = first_block + p.blocks < (end + 63) / 64 ? first_block + p.blocks : (end + 63) / 64;
+  const auto load_base = [&](uint32_t block, Words4 (&into)[NT][2]) {
+    const uint32_t at = block * 64 + 8 * g;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int t = 0; t < NT; ++t) {
+      const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t k = r0 + 32 * s + 8 * g;
-        b[s][j] = load16(reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(block * 64 + column_of_b + j) * rec.rank + (k < rank ? k : 0));
-      }
+      for (int x = 0; x < 2; ++x) into[t][x] = block * 64 + 64 <= end ? load16(b + at + 32 * x) : load_to(b, at + 32 * x, end);
+    }
   };
-  const auto load_whole_base = [&](uint32_t block, Words4 (&into)[NT][2]) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        into[t][x] = load16(static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride + block * 64 + 8 * g + 32 * x);
-  };
-  const auto clear = [&] {
+  Words4 base[NT][2] = {}, next[NT][2] = {};
+  if (p.c.base != nullptr && first_block + wave < last_block) load_base(first_block + wave, base);
+  add_up<T>(p, tile, rec, rank, high, row_pitch, size);
+  __syncthreads();
+  for (uint32_t block = first_block + wave; block < last_block; block += 4) {
+    const uint32_t n0 = block * 64;
+    const bool whole = n0 + 64 <= end;
+    if (p.c.base != nullptr && block + 4 < last_block) load_base(block + 4, next);
+    Floats4 acc[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[t][j] = Floats4{0, 0, 0, 0};
-  };
-  // adds 64 columns of H from r0 on. Behind the rank H is zero, and B is made so: what is read there may be anything.
-  const auto products = [&](uint32_t r0) {
+    for (uint32_t r = 0; r < rank; r += 32) {
+      Words4 b[4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (r0 + 32 * s >= rank) continue;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (r0 + 32 * s + 8 * g >= rank) b[s][j] = Words4{0, 0, 0, 0};
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t n = n0 + (n16 >> 1 & 1) * 32 + (n16 >> 2) * 8 + (n16 & 1) * 4 + j, k = r + 8 * g;
+        const uint16_t *row_of_b = reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(n < end ? n : end - 1) * rec.rank;
+        if (rank % 8 == 0) {
+          b[j] = Words4{0, 0, 0, 0};
+          if (k < rank) b[j] = load16(row_of_b + k);
+        } else {
+          b[j] = load_to(row_of_b, k, rank);
+        }
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t at = (t * 16 + n16) * row_pitch + r0 + 32 * s + 8 * g;
+        const uint32_t at = (t * 16 + n16) * row_pitch + r + 8 * g;
         const Words4 hi = *reinterpret_cast<const Words4 *>(high + at), lo = *reinterpret_cast<const Words4 *>(low + at);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[s][j], lo, acc[t][j]);
+        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[j], lo, acc[t][j]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[s][j], hi, acc[t][j]);
+        for (int j = 0; j < 4; ++j) acc[t][j] = T::mfma(b[j], hi, acc[t][j]);
       }
     }
-  };
-  const auto write = [&](uint32_t block, bool whole) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       if (t * 16 + n16 >= tile.count) continue;
       const float by = size[t * 16 + n16];
-      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + block * 64 + 8 * g;
+      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + n0 + 8 * g;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         uint32_t w[4];
@@ -341,60 +354,14 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
         } else {
 #pragma unroll
           for (uint32_t i = 0; i < 8; ++i)
-            if (block * 64 + 32 * x + 8 * g + i < end) out[32 * x + i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+            if (n0 + 32 * x + 8 * g + i < end) out[32 * x + i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
         }
       }
     }
-  };
-
-  uint32_t block = first_block + wave;
-  const uint32_t whole_end = p.c.base != nullptr && rank % 8 == 0 ? (last_block < end / 64 ? last_block : end / 64) : 0;
-  if (block < whole_end) {
-    load_whole_b(block, 0);
-    load_whole_base(block, base);
-  }
-  add_up<T>(p, tile, rec, rank, high, row_pitch, size);
-  __syncthreads();
-  if (block < whole_end)
-    for (bool more = true; more; block += 4) {
-      more = block + 4 < whole_end;
-      const uint32_t ahead = more ? block + 4 : block;
-      Words4 next[NT][2];
-      clear();
-      products(0);
-      for (uint32_t r0 = 64; r0 < rank; r0 += 64) {
-        load_whole_b(block, r0);
-        products(r0);
-      }
-      load_whole_b(ahead, 0);
-      load_whole_base(ahead, next);
-      __builtin_amdgcn_sched_barrier(0);
-      write(block, true);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) base[t][x] = next[t][x];
-    }
-  for (; block < last_block; block += 4) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        base[t][x] = Words4{0, 0, 0, 0};
-        if (p.c.base != nullptr) base[t][x] = load_to(static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride, block * 64 + 8 * g + 32 * x, end);
-      }
-    clear();
-    for (uint32_t r0 = 0; r0 < rank; r0 += 64) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t n = block * 64 + column_of_b + j;
-          b[s][j] = load_to(reinterpret_cast<const uint16_t *>(rec.b) + (uint64_t)(n < end ? n : end - 1) * rec.rank, r0 + 32 * s + 8 * g, rank);
-        }
-      products(r0);
-    }
-    write(block, false);
+      for (int x = 0; x < 2; ++x) base[t][x] = next[t][x];
   }
 }
 
@@ -442,7 +409,7 @@ void split_of(const ft_adapters_call &c, uint32_t *splits, uint32_t *split) {
 
 }  // namespace
 
-uint64_t adapter_group_bytes(uint32_t rows, uint32_t count) { return 64 + up(up(most_tiles(rows, count), 8) * sizeof(Tile) + (uint64_t)rows * 4, 16); }
+uint64_t adapter_group_bytes(uint32_t rows, uint32_t count) { return 64 + up(most_tiles(rows, count) * sizeof(Tile) + (uint64_t)rows * 4, 16); }
 
 hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t count, void *groups, hipStream_t stream) {
   hipLaunchKernelGGL(ft_adapter_group_kernel, dim3(1), dim3(kGroupThreads), (count + 1) * 4, stream, ids, rows, count, groups_at(groups, rows, count));
@@ -457,8 +424,7 @@ uint64_t adapter_workspace(const ft_adapters_call &c) {
 
 template <class T>
 hipError_t launch(const Adapt &p, hipStream_t stream) {
-  // a multiple of the dies, so that what workgroups have in common that are some rows of the grid apart, a tile's part of H, is in one die's cache
-  const uint32_t tiles = (uint32_t)up(most_tiles(p.c.rows, p.c.count), 8), blocks = (p.c.width_out + 63) / 64;
+  const uint32_t tiles = (uint32_t)most_tiles(p.c.rows, p.c.count), blocks = (p.c.width_out + 63) / 64;
   hipLaunchKernelGGL(ft_adapter_shrink_kernel<T>, dim3(tiles, p.splits), dim3(256), 0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
