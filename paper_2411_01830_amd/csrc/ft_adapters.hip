@@ -279,25 +279,39 @@ __device__ inline void add_up(const Adapt &p, const Tile &tile, const ft_adapter
   }
 }
 
+// Two neighbouring lanes have two vectors each of their own row, or one each of both: from the one to the other, either way.
+__device__ inline void exchange(Words4 (&v)[2], uint32_t odd) {
+  Words4 there;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) there[y] = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[0][y] : v[1][y]), 0xb1, 0xf, 0xf, true);
+  v[0] = odd ? there : v[0];
+  v[1] = odd ? v[1] : there;
+}
+
 // 64 columns of a tile's rows. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours: columns
-// 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on.
+// 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on. What
+// lanes read and write is whole lines of 128 bytes of every other row, and is exchanged with the neighbour's: 109 us for 8192 rows, 113 without.
 template <class T, int NT>
 __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *high, uint32_t row_pitch, float *size) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
   const uint16_t *low = high + kTileRows * row_pitch;
   const uint32_t end = p.c.width_out, first_block = blockIdx.y * p.blocks;
-  uint64_t row[NT];
+  const uint32_t odd = n16 & 1, pair = n16 & ~1u;
+  uint64_t row[NT][2];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) row[t] = (uint64_t)p.g.order[tile.first + (t * 16 + n16 < tile.count ? t * 16 + n16 : tile.count - 1)];
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (uint32_t x = 0; x < 2; ++x) row[t][x] = (uint64_t)p.g.order[tile.first + (t * 16 + pair + x < tile.count ? t * 16 + pair + x : tile.count - 1)];
   const uint32_t last_block = first_block + p.blocks < (end + 63) / 64 ? first_block + p.blocks : (end + 63) / 64;
   const auto load_base = [&](uint32_t block, Words4 (&into)[NT][2]) {
-    const uint32_t at = block * 64 + 8 * g;
+    const uint32_t at = block * 64 + 8 * g + 32 * odd;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t] * p.c.base_stride;
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) into[t][x] = block * 64 + 64 <= end ? load16(b + at + 32 * x) : load_to(b, at + 32 * x, end);
-    }
+      for (int x = 0; x < 2; ++x) {
+        const uint16_t *b = static_cast<const uint16_t *>(p.c.base) + row[t][x] * p.c.base_stride;
+        into[t][x] = block * 64 + 64 <= end ? load16(b + at) : load_to(b, at, end);
+      }
   };
   Words4 base[NT][2] = {}, next[NT][2] = {};
   if (p.c.base != nullptr && first_block + wave < last_block) load_base(first_block + wave, base);
@@ -337,24 +351,29 @@ __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if (t * 16 + n16 >= tile.count) continue;
       const float by = size[t * 16 + n16];
-      uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t] * p.c.out_stride + n0 + 8 * g;
+      exchange(base[t], odd);
+      Words4 w[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        uint32_t w[4];
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) {  // elements 2 y and 2 y + 1 of 8: i = 2 x + y / 2, j = 2 (y % 2) and the next
           const uint32_t two = base[t][x][y];
           const float lo = T::to_float((uint16_t)two), hi = T::to_float((uint16_t)(two >> 16));
-          w[y] = T::pack(__builtin_fmaf(acc[t][y % 2 * 2][2 * x + y / 2], by, lo), __builtin_fmaf(acc[t][y % 2 * 2 + 1][2 * x + y / 2], by, hi));
+          w[x][y] = T::pack(__builtin_fmaf(acc[t][y % 2 * 2][2 * x + y / 2], by, lo), __builtin_fmaf(acc[t][y % 2 * 2 + 1][2 * x + y / 2], by, hi));
         }
+      exchange(w, odd);
+#pragma unroll
+      for (uint32_t x = 0; x < 2; ++x) {
+        if (t * 16 + pair + x >= tile.count) continue;
+        const uint32_t n = n0 + 8 * g + 32 * odd;
+        uint16_t *out = static_cast<uint16_t *>(p.c.out) + row[t][x] * p.c.out_stride + n;
         if (whole) {
-          *reinterpret_cast<Loose4 *>(out + 32 * x) = Loose4{{w[0], w[1], w[2], w[3]}};
+          *reinterpret_cast<Loose4 *>(out) = Loose4{{w[x][0], w[x][1], w[x][2], w[x][3]}};
         } else {
 #pragma unroll
           for (uint32_t i = 0; i < 8; ++i)
-            if (n0 + 32 * x + 8 * g + i < end) out[32 * x + i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+            if (n + i < end) out[i] = (uint16_t)(w[x][i / 2] >> (i % 2 * 16));
         }
       }
     }
