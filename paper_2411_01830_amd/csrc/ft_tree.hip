@@ -30,7 +30,8 @@ struct Tree {
   uint32_t cluster;      // workgroups of a worker, which have different rows
   Divisor by_group;
   uint32_t workers, least;  // workgroups, and steps that each takes at least
-  float scale;           // of products, times log2 e
+  float scale;           // of products, times log2 e: more than 0
+  uint32_t flip;         // the signs of queries where it was less
   uint64_t *prefix;      // requests + 1: work of the requests before; the workers' rate
   uint32_t *flags;       // of every wavefront, whether it has left out values that are not finite
   float *sums;           // partial results, see Partial
@@ -168,11 +169,14 @@ template <class T, int DT, int NR, int WR, bool PAGED, bool SHARED>
 __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED, SHARED), waves(DT, NR, PAGED, SHARED)))) void ft_tree_kernel(Tree) {
   constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
   // SHARED: 16-byte pieces of a row, those of a step that a thread has, steps that are on their way besides the one in shared memory
-  constexpr int CH = DT / 8, N = SHARED ? CH / (2 * WR) : 1, DEPTH = SHARED ? (NR == 1 ? 4 : 2) / N : 1, NI = SHARED && !PAGED ? N : 2;
+  constexpr int CH = DT / 8, N = SHARED ? CH / (2 * WR) : 1, DEPTH = SHARED ? (NR == 1 ? 4 : 2) / N : 1, NI = SHARED ? N : 2;
   static_assert(!SHARED || (N >= 1 && N * 2 * WR == CH));
   __shared__ Words4 tile_lds[SHARED ? 2 : 1][2][SHARED ? 32 * CH : 1];
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const uint32_t wave = uniform((uint32_t)threadIdx.x >> 6);
+  // SHARED: where a lane's pieces of a step's first keys and values are, in bytes; those of the others are an exclusive or and a distance away
+  const uint32_t key_at = 16 * (n16 * CH + (g ^ (n16 % CH)));
+  const uint32_t value_at = E == 4 ? 16 * (4 * g * CH + ((n16 / 2) ^ (4 * g % CH))) + 8 * (n16 & 1) : 16 * (4 * g * CH + (n16 ^ (4 * g % CH)));
 
   // The workers next to each other go to the same die: they read the same pages for other rows.
   const uint32_t per_die = gridDim.x / 8;
@@ -271,6 +275,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           const int d = ks * 32 + 8 * g;
           if (PAGED || d < (int)c.dim) qf[nr][ks] = load16(p + d);
           else qf[nr][ks] = Words4{0, 0, 0, 0};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) qf[nr][ks][x] ^= a.flip;
         }
       }
       Floats4 acc[NR][E];
@@ -290,12 +296,14 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       // key, in that page still, are read and not looked at. Otherwise lane l % 32 finds key l % 32, behind the last one that one again. So
       // it is with drafted keys. (No branches here: loads under a condition, of either outcome, would be waited for as if they were not there.)
       const uint32_t end_key = q.len > 0 ? (uint32_t)q.len - 1 : 0;
+      // SHARED: which 16 of a step's keys this wavefront brings, of its i-th pieces
+      const auto half_of = [&](int i) -> uint32_t { return (i * 64 * WR + wave * 64) / CH >> 4; };
       const auto pages_of = [&](uint32_t st, uint32_t (&ids)[NI]) {
         if (st >= cached) return;
         if constexpr (PAGED) {
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            const uint32_t key = st * kStep + kk * 16;
+          for (int kk = 0; kk < NI; ++kk) {
+            const uint32_t key = st * kStep + (SHARED ? half_of(kk) : kk) * 16;
             ids[kk] = (uint32_t)table[uniform(__umulhi(key < end_key ? key : end_key, page_m) >> page_shift)];
           }
         } else {
@@ -387,65 +395,77 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           }
         }
       };
-      // SHARED: a thread's pieces of a step's keys and values. Row r has its pieces in the order that counting up to CH and an exclusive or
-      // with r give: wavefronts read 16 bytes of each of several rows, and so meet different banks.
-      const auto fetch = [&](uint32_t st, const uint32_t (&ids)[NI], Words4 (&k)[N], Words4 (&v)[N]) {
+      // SHARED: where a thread's pieces of a step's keys and values are. Row r has its pieces in the order that counting up to CH and an exclusive
+      // or with r give: wavefronts read 16 bytes of each of several rows, and so meet different banks.
+      struct Place {
+        Global k, v;
+        uint32_t k_off, v_off;
+      };
+      uint32_t lane_off[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+      for (int i = 0; i < N; ++i) {
+        const uint32_t index = i * 64 * WR + threadIdx.x, row = index / CH;
+        lane_off[i] = 16 * ((index % CH) ^ (row % CH)) + (PAGED ? __umul24(row & 15, row_bytes) : 0);
+      }
+      const auto place = [&](uint32_t st, uint32_t page, int i) -> Place {
+        const uint32_t end = (uint32_t)q.n - 1;
+        Place at;
+        if constexpr (PAGED) {
+          const uint32_t key = st * kStep + half_of(i) * 16;
+          if (st < cached) {
+            const uint32_t row = key - (__umulhi(key, page_m) >> page_shift) * page_d;
+            const uint64_t first_row = (page < pages ? page : 0) * page_bytes + (uint64_t)row * row_bytes;
+            at = {global(kc) + first_row, global(vc) + first_row, lane_off[i], lane_off[i]};
+          } else {
+            const uint32_t draft = key - cached * kStep < end ? key - cached * kStep : end, index = i * 64 * WR + threadIdx.x, row = index / CH;
+            const uint32_t of_half = (row & 15) < end - draft ? row & 15 : end - draft, piece = 16 * ((index % CH) ^ (row % CH));
+            at = {global(kd) + (uint64_t)draft * k_bytes, global(vd) + (uint64_t)draft * v_bytes, piece + __umul24(of_half, k_bytes), piece + __umul24(of_half, v_bytes)};
+          }
+          asm volatile("" : "+s"(at.k), "+s"(at.v), "+v"(at.k_off), "+v"(at.v_off));
+        } else {
           uint32_t index = i * 64 * WR + threadIdx.x;
           asm volatile("" : "+v"(index));
-          const uint32_t row = index / CH;
-          uint32_t piece = (index % CH) ^ (row % CH);
-          if (!PAGED && piece * 8 >= (uint32_t)c.dim) piece = 0;  // queries are zero there, and outputs not written
-          Global kb = global(st < cached ? kc : kd), vb = global(st < cached ? vc : vd);
-          uint32_t ko = 16 * piece, vo = 16 * piece;
-          if constexpr (PAGED) {
-            const uint32_t kk = uniform(row >> 4), of_half = row & 15, id = kk != 0 ? ids[1] : ids[0];
-            const Half kh = half(st, (int)kk, id, k_bytes), vh = half(st, (int)kk, id, v_bytes);
-            kb += kh.row;
-            vb += vh.row;
-            ko += __umul24(of_half < kh.behind ? of_half : kh.behind, st < cached ? row_bytes : k_bytes);
-            vo += __umul24(of_half < vh.behind ? of_half : vh.behind, st < cached ? row_bytes : v_bytes);
-            asm volatile("" : "+s"(kb), "+s"(vb), "+v"(ko), "+v"(vo));
-          } else {
-            kb += lane_row(st, row, ids[i], t.k_token_stride);
-            vb += lane_row(st, row, ids[i], t.v_token_stride);
-          }
-          k[i] = load16(kb + ko);
-          v[i] = load16(vb + vo);
+          at.k_off = lane_off[i] >= 2 * c.dim ? 0 : lane_off[i];  // behind the head queries are zero, and outputs not written
+          at.v_off = at.k_off;
+          at.k = global(st < cached ? kc : kd) + lane_row(st, index / CH, page, t.k_token_stride);
+          at.v = global(st < cached ? vc : vd) + lane_row(st, index / CH, page, t.v_token_stride);
         }
+        return at;
       };
-      const auto put = [&](int buf, const Words4 (&k)[N], const Words4 (&v)[N]) {
+      const auto put = [&](Words4 *to, const Words4 (&from)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          tile_lds[buf][0][i * 64 * WR + threadIdx.x] = k[i];
-          tile_lds[buf][1][i * 64 * WR + threadIdx.x] = v[i];
-        }
+        for (int i = 0; i < N; ++i) to[i * 64 * WR + threadIdx.x] = from[i];
       };
       // (the empty statements keep places from being worked out once and held: registers are scarcer than instructions)
       const auto get_keys = [&](int buf) {
-        uint32_t row = n16, group = g;
-        asm volatile("" : "+v"(row), "+v"(group));
+        uint32_t at = key_at;
+        asm volatile("" : "+v"(at));
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int ks = 0; ks < KS; ++ks) {
+          const char *p = reinterpret_cast<const char *>(tile_lds[0][0]) + (at ^ (ks * 64));
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) kf[kk][ks] = tile_lds[buf][0][(kk * 16 + row) * CH + ((ks * 4 + group) ^ (row % CH))];
+          for (int kk = 0; kk < 2; ++kk) kf[kk][ks] = *reinterpret_cast<const Words4 *>(p + buf * (int)sizeof(tile_lds[0]) + kk * 256 * CH);
+        }
       };
       const auto get_values = [&](int buf) {
-        uint32_t piece = n16, first_row = 4 * g;
-        asm volatile("" : "+v"(piece), "+v"(first_row));
+        uint32_t at = value_at;
+        asm volatile("" : "+v"(at));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t row = (e >> 2) * 16 + first_row + (e & 3);
-          if constexpr (E == 4) {
-            typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
-            const Words2 w = reinterpret_cast<const Words2 *>(&tile_lds[buf][1][row * CH + ((piece / 2) ^ (row % CH))])[piece & 1];
-            vf[e][0] = w[0];
-            vf[e][1] = w[1];
-          } else if constexpr (E == 8) {
-            const Words4 w = tile_lds[buf][1][row * CH + (piece ^ (row % CH))];
+        for (int i = 0; i < 4; ++i) {
+          const char *p = reinterpret_cast<const char *>(tile_lds[0][0]) + (at ^ (i * 16));
 #pragma unroll
-            for (int y = 0; y < 4; ++y) vf[e][y] = w[y];
+          for (int kk = 0; kk < 2; ++kk) {
+            const char *row = p + buf * (int)sizeof(tile_lds[0]) + (int)sizeof(tile_lds[0][0]) + (16 * kk + i) * 16 * CH;
+            if constexpr (E == 4) {
+              typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+              const Words2 w = *reinterpret_cast<const Words2 *>(row);
+              vf[4 * kk + i][0] = w[0];
+              vf[4 * kk + i][1] = w[1];
+            } else if constexpr (E == 8) {
+              const Words4 w = *reinterpret_cast<const Words4 *>(row);
+#pragma unroll
+              for (int y = 0; y < 4; ++y) vf[4 * kk + i][y] = w[y];
+            }
           }
         }
       };
@@ -485,8 +505,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3];
           const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-          if (__any(top > m[nr] + kSlack)) {
-            const float now = fmaxf(m[nr], row_max(top));
+          if (__any(top * scale > m[nr] + kSlack)) {
+            const float now = fmaxf(m[nr], row_max(top) * scale);
             const float shrink = now == -INFINITY ? 1 : __builtin_amdgcn_exp2f(m[nr] - now);
             m[nr] = now;
             l[nr] *= shrink;
@@ -495,7 +515,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           }
           const float from = m[nr] == -INFINITY ? 0 : m[nr];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(x[i] - from);
+          for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -from));
           l[nr] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
           p[nr] = Words4{T::pack(w[0], w[1]), T::pack(w[2], w[3]), T::pack(w[4], w[5]), T::pack(w[6], w[7])};
         }
@@ -553,10 +573,6 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       // are asked for first of all. The last step asks for its own rows once more, which are near by then: were there a
       // condition on these loads, what is asked for before them would be waited for together with them.
       const auto softmax = [&](uint32_t st) {
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[nr][i >> 2][i & 3] *= scale;
         edge(st);
         weights();
       };
@@ -592,7 +608,12 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
         Words4 k[DEPTH][N], v[DEPTH][N];
         uint32_t asked = st;  // the step that `ids` are the pages of
         const auto ask = [&](Words4 (&into_k)[N], Words4 (&into_v)[N]) {
-          fetch(asked, ids, into_k, into_v);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const Place at = place(asked, ids[i], i);
+            into_k[i] = load16(at.k + at.k_off);
+            into_v[i] = load16(at.v + at.v_off);
+          }
           if (asked + 1 < last) {
             ++asked;
 #pragma unroll
@@ -603,7 +624,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
         };
         fence();  // what the segment before has left in shared memory has been read
         ask(k[0], v[0]);
-        put(0, k[0], v[0]);
+        put(tile_lds[0][0], k[0]);
+        put(tile_lds[0][1], v[0]);
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) ask(k[d], v[d]);
         for (bool more = true; more;) {
@@ -611,7 +633,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           for (int d = 0; d < (DEPTH > 1 ? DEPTH : 2); ++d)
             if (more) {
               fence();
-              put(d + 1 & 1, k[d % DEPTH], v[d % DEPTH]);
+              put(tile_lds[d + 1 & 1][0], k[d % DEPTH]);
+              put(tile_lds[d + 1 & 1][1], v[d % DEPTH]);
               ask(k[d % DEPTH], v[d % DEPTH]);
               __builtin_amdgcn_sched_barrier(0);  // (keys and values at once would not leave registers for what is on its way)
               get_keys(d & 1);
@@ -831,7 +854,11 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
   a.least = kSegment + 2;
-  a.scale = t.scale * kLog2e;
+  // Scores are scaled within the exponent's argument, so a scale of 0 must not make NaN of what is masked: the smallest number there is
+  // does the same. Queries change their signs for one below 0, as the largest product is to be the largest score.
+  a.scale = fabsf(t.scale * kLog2e);
+  if (a.scale == 0) a.scale = 0x1p-149f;
+  a.flip = t.scale < 0 ? 0x80008000u : 0;
   a.prefix = static_cast<uint64_t *>(t.workspace);
   a.flags = reinterpret_cast<uint32_t *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
   a.sums = reinterpret_cast<float *>(a.flags + waves_of(s, cu_count));
