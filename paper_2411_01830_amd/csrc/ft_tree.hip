@@ -149,7 +149,7 @@ __device__ inline void write_row(const A &a, const Floats4 (&acc)[DT / 16], floa
 }
 
 // Wavefronts to each of a compute unit's four parts: what their registers leave room for.
-constexpr int waves(int dt, int nr, bool paged, bool shared) { return dt <= 128 && nr * dt <= (paged || shared ? 256 : 128) ? 2 : 1; }
+constexpr int waves(int dt) { return dt <= 128 ? 2 : 1; }
 
 // Two bytes of each of eight rows, as the matrix instruction wants them.
 template <int W>
@@ -166,7 +166,7 @@ __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t by
 // SHARED: keys and values go through shared memory, which the WR wavefronts of a workgroup fill together; several workgroups, a cluster, have
 // the rows beyond those and are next to each other on one die, where the second finds in the cache what the first has read.
 template <class T, int DT, int NR, int WR, bool PAGED, bool SHARED>
-__global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(DT, NR, PAGED, SHARED), waves(DT, NR, PAGED, SHARED)))) void ft_tree_kernel(Tree) {
+__global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(DT), waves(DT)))) void ft_tree_kernel(Tree) {
   constexpr int E = DT / 16, KS = DT / 32, RT = 16 * NR, ROWS = RT * WR;
   // SHARED: 16-byte pieces of a row, those of a step that a thread has, steps that are on their way besides the one in shared memory
   constexpr int CH = DT / 8, N = SHARED ? CH / (2 * WR) : 1, DEPTH = SHARED ? (NR == 1 ? 4 : 2) / N : 1, NI = SHARED ? N : 2;
@@ -377,20 +377,13 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
             } else {
               base += from_lane(row, kk * 16 + 4 * g + i);
             }
-            // a lane's piece of a row: E elements, of which E is 4, 8 or 16 and the head's size a multiple of 8
-            if constexpr (E == 4) {
-              typedef const __attribute__((address_space(1))) Loose2 *P;
-              const bool has = PAGED || E * n16 < (int)c.dim;
-              vf[e][0] = has ? ((P)(base + off))->w[0] : 0;
-              vf[e][1] = has ? ((P)(base + off))->w[1] : 0;
-            } else {
+            // a lane's piece of a row: E elements, some multiple of 8 of which the head has
 #pragma unroll
-              for (int x = 0; x < E / 8; ++x) {
-                Words4 w{0, 0, 0, 0};
-                if (PAGED || E * n16 + 8 * x < (int)c.dim) w = load16(base + off + 16 * x);
+            for (int x = 0; x < E / 8; ++x) {
+              Words4 w{0, 0, 0, 0};
+              if (PAGED || E * n16 + 8 * x < (int)c.dim) w = load16(base + off + 16 * x);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
-              }
+              for (int y = 0; y < 4; ++y) vf[e][4 * x + y] = w[y];
             }
           }
         }
@@ -605,6 +598,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       } else {
         // The step that is worked on lies in one half of shared memory, the next one is put into the other half, those behind it are on their way
         // in registers. One barrier a step: it says that the half to work on is full, and that the other one has been read.
+        const bool works = NR > 1 || row0 < (uint32_t)q.n * group;  // wavefronts without rows of their own bring theirs and wait
         Words4 k[DEPTH][N], v[DEPTH][N];
         uint32_t asked = st;  // the step that `ids` are the pages of
         const auto ask = [&](Words4 (&into_k)[N], Words4 (&into_v)[N]) {
@@ -637,14 +631,16 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
               put(tile_lds[d + 1 & 1][1], v[d % DEPTH]);
               ask(k[d % DEPTH], v[d % DEPTH]);
               __builtin_amdgcn_sched_barrier(0);  // (keys and values at once would not leave registers for what is on its way)
-              get_keys(d & 1);
-              scores();
-              __builtin_amdgcn_sched_barrier(0);
-              softmax(st);
-              __builtin_amdgcn_sched_barrier(0);
-              get_values(d & 1);
-              edge_values(st);
-              outputs();
+              if (works) {
+                get_keys(d & 1);
+                scores();
+                __builtin_amdgcn_sched_barrier(0);
+                softmax(st);
+                __builtin_amdgcn_sched_barrier(0);
+                get_values(d & 1);
+                edge_values(st);
+                outputs();
+              }
               ++st;
               more = st < last;
             }
@@ -775,13 +771,16 @@ struct Shape {
   uint32_t cluster;
 };
 
-// Heads are padded to 64, 128 or 256 elements. Up to 32 rows (16 where heads are large) are one wavefront's; beyond that wavefronts
-// share keys and values in shared memory, and beyond 256 rows (128 of small heads) up to four workgroups the die's cache.
+// Heads are padded to 64, 128 or 256 elements. Four wavefronts of 16 rows share keys and values in shared memory, also where there are fewer
+// rows: a wavefront to itself, with four times the workers, takes 121 us instead of 109 for 64 requests of 2000 tokens and 4 rows a key head (8
+// key heads of 128), 46 instead of 35 for one of 20000, 28 and 23.5 for 17 of 700; it is faster only where there is next to nothing to do (13
+// instead of 14.6 for one of 300) or lengths are far apart (74 and 76 for 64 of 16 to 8192). Beyond 64 rows, 16 requests of 4096: eight wavefronts
+// of 16 rows take 77 us for 96 rows, four 84, eight of 32 rows 98; for 192 rows 124, 142 and 102. With heads of 64 elements four of 32 rows do what
+// eight do there (43 for 96 and 128). Beyond that up to four workgroups share the die's cache: 384 instead of 394 for 64 requests of 2000 and 512 rows,
+// 259 instead of 274 with heads of 64. Heads of 256 do not leave registers for what is on its way to shared memory.
 Shape shape_of(uint32_t dim, uint64_t rows) {
   const int dt = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
-  if (rows <= 16) return {dt, 1, 1, false, 1};
-  if (dt == 256) return {dt, 1, 4, false, 1};
-  if (rows <= 32) return {dt, 2, 1, false, 1};
+  if (dt == 256) return {dt, 1, rows <= 16 ? 1 : 4, false, 1};
   if (rows <= 64) return {dt, 1, 4, true, 1};
   if (rows <= 128 && dt == 128) return {dt, 1, 8, true, 1};
   const int most = dt == 64 ? 4 : 8;
@@ -790,12 +789,12 @@ Shape shape_of(uint32_t dim, uint64_t rows) {
 }
 
 // As many as the chip holds, a multiple of its dies.
-uint32_t workers_of(const Shape &s, bool paged, int cu_count) {
-  return (uint32_t)(cu_count * 4 * waves(s.dt, s.nr, paged, s.shared) / (s.wr * (int)s.cluster) + 7) / 8 * 8;
+uint32_t workers_of(const Shape &s, int cu_count) {
+  return (uint32_t)(cu_count * 4 * waves(s.dt) / (s.wr * (int)s.cluster) + 7) / 8 * 8;
 }
 
 // Wavefronts of all workers, at most: workers are rounded up to the dies.
-uint64_t waves_of(const Shape &s, int cu_count) { return (uint64_t)cu_count * 4 * waves(s.dt, s.nr, true, s.shared) + 256; }
+uint64_t waves_of(const Shape &s, int cu_count) { return (uint64_t)cu_count * 4 * waves(s.dt) + 256; }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
@@ -813,11 +812,9 @@ hipError_t launch(const Tree &a, bool paged, uint64_t rows, hipStream_t stream) 
 
 template <class T, int DT>
 hipError_t launch_rows(const Tree &a, const Shape &s, bool paged, uint64_t rows, hipStream_t stream) {
-  if (s.nr == 1 && s.wr == 1) return launch<T, DT, 1, 1, false>(a, paged, rows, stream);
   if constexpr (DT == 256) {
-    return launch<T, DT, 1, 4, false>(a, paged, rows, stream);
+    return s.wr == 1 ? launch<T, DT, 1, 1, false>(a, paged, rows, stream) : launch<T, DT, 1, 4, false>(a, paged, rows, stream);
   } else {
-    if (s.wr == 1) return launch<T, DT, 2, 1, false>(a, paged, rows, stream);
     if (s.nr == 1 && s.wr == 4) return launch<T, DT, 1, 4, true>(a, paged, rows, stream);
     if constexpr (DT == 64) return launch<T, DT, 2, 4, true>(a, paged, rows, stream);
     else return s.nr == 1 ? launch<T, DT, 1, 8, true>(a, paged, rows, stream) : launch<T, DT, 2, 8, true>(a, paged, rows, stream);
@@ -847,10 +844,11 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   const Shape s = shape_of(c.dim, rows);
   Tree a{c, t};
   a.t.drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
-  // strides of 24 bits in bytes
+  // Pages of whole 16 keys, heads without padding, strides of 24 bits in bytes: one base address for 16 keys (57 us for 16 requests of 4096 tokens
+  // and 64 rows, 66 without; 16 rows of 64 elements 34 both).
   const bool paged = c.dim == (uint32_t)s.dt && c.page_tokens.d % 16 == 0 && (c.token_stride | t.k_token_stride | t.v_token_stride) < 1u << 23;
   a.cluster = s.cluster;
-  a.workers = workers_of(s, paged, cu_count);
+  a.workers = workers_of(s, cu_count);
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
   a.least = kSegment + 2;
