@@ -787,7 +787,9 @@ typedef struct ft_tree_call {
  *   out[t, h] = sum over s of softmax over s (scale * q[t, h] . key[s]) value[s],   lse[t, h] = log of the sum of exp
  * A row that sees nothing is 0, its lse -infinity. What a row does not see does not reach it, NaN and
  * infinities included; neither does what lies in a page behind a request's last token. One token a request is
- * plain decoding; without a mask any number of rows may be a prompt's next piece.
+ * plain decoding; without a mask any number of rows may be a prompt's next piece. Rows of no request, and those beyond
+ * `drafts`, are left as they are in out and lse. requests <= 2^24, requests times the cache's heads < 2^31. A page number
+ * that the cache does not have is read as page 0.
  * Types: products are exact, sums, softmax and lse 32 bits, weights are rounded to the tensors' type for
  * their product with the values, and the result once.
  */
