@@ -430,7 +430,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
         } else {
           uint32_t index = i * 64 * WR + threadIdx.x;
           asm volatile("" : "+v"(index));
-          at.k_off = lane_off[i] >= 2 * c.dim ? 0 : lane_off[i];  // behind the head queries are zero, and outputs not written
+          at.k_off = lane_off[i] >= 2 * c.dim ? 0 : lane_off[i];  // (what is behind the head)
           at.v_off = at.k_off;
           at.k = global(st < cached ? kc : kd) + lane_row(st, index / CH, page, t.k_token_stride);
           at.v = global(st < cached ? vc : vd) + lane_row(st, index / CH, page, t.v_token_stride);
@@ -439,7 +439,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       };
       const auto put = [&](Words4 *to, const Words4 (&from)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) to[i * 64 * WR + threadIdx.x] = from[i];
+        for (int i = 0; i < N; ++i)  // behind the head queries are zero, and keys too: what was read there may be an infinity
+          to[i * 64 * WR + threadIdx.x] = PAGED || lane_off[i] < 2 * c.dim ? from[i] : Words4{0, 0, 0, 0};
       };
       // (the empty statements keep places from being worked out once and held: registers are scarcer than instructions)
       const auto get_keys = [&](int buf) {

@@ -427,6 +427,24 @@ def test_a_key_that_some_rows_see_reaches_those_alone():
             assert torch.equal(got[i], want[i])
 
 
+@pytest.mark.parametrize("dim", [8, 64, 72, 128, 200, 256])
+@pytest.mark.parametrize("news", [3, 30, 70])
+def test_a_key_of_minus_infinity_has_no_weight(dim, news):
+    """What is finite stays so: a product of -infinity is a weight of zero, as a mask's bit is."""
+    t = Tree(lens=[70], news=[news], heads=2, group=4, dim=dim, page=8, dtype=BF16)
+    q, k, v = t.args[:3]
+    q = q.clone()
+    q[:, :, 3] = q[:, :, 3].abs() + 0.5
+    bad_k = k.clone()
+    bad_k[2, :, 3] = -float("inf")
+    hidden = t.mask.clone()
+    first = hidden if hidden.dim() == 1 else hidden[:, 0]
+    first &= ~4
+    want = ops().tree_attention(t.cache, q, k, v, *t.args[3:], mask=hidden, lse=True)
+    got = ops().tree_attention(t.cache, q, bad_k, v, *t.args[3:], mask=t.mask, lse=True)
+    assert torch.isfinite(want[0]).all() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_a_cache_whose_offsets_pass_32_bits():
     """Three pages more than 2^31 elements apart."""
     page, heads, dim, stride = 16, 2, 64, (1 << 31) + 64
