@@ -6,9 +6,9 @@
 // Rows without an adapter are tiles of their own that are copied.
 //
 // 64 rows of 32 adapters of ranks 8 to 64, 4096 to 4096, in bfloat16: 17.6 us, three launches of 3.8 (grouping), 5.7 and 7.8 us that latency bounds, for
-// 15 MB. 8192 rows of 8 adapters, 4096 to 6144: 111 us for 273 MB, 8 + 25.5 + 71; the first product reads X at 2.7 TB/s, the second reads and
-// writes 2.9 TB/s. Of the second one's time writing is 23 us, base 12, adding up the parts of H 16 and the products none: wavefronts wait for
-// memory, two workgroups to a unit. One kernel for both products takes 122 alone, as a unit then holds one workgroup of the 137; tiles of
+// 15 MB. 8192 rows of 8 adapters, 4096 to 6144: 107 us for 273 MB, 8 + 25.5 + 67; the first product reads X at 2.7 TB/s, the second reads and
+// writes 3 TB/s. Of the second one's time writing is 23 us, base 12, adding up the parts of H 16 and the products none: wavefronts wait for
+// memory, two workgroups to a unit (three, with wavefronts of 32 rows: 118). One kernel for both products takes 122 alone, as a unit then holds one workgroup of the 137; tiles of
 // 32 rows 125 for all three.
 #include <hip/hip_runtime.h>
 
@@ -297,7 +297,7 @@ __device__ inline void exchange(Words4 (&v)[2], uint32_t odd) {
 
 // 64 columns of a tile's rows. Columns are dealt to the products so that a lane's 16 results, acc[j][i], are two groups of 8 neighbours: columns
 // 8 g + 4 (i % 2) + j of the first 32 (i < 2) and of the second. A block's part of base is asked for while the block before is worked on. What
-// lanes read and write is whole lines of 128 bytes of every other row, and is exchanged with the neighbour's: 109 us for 8192 rows, 113 without.
+// lanes read and write is whole lines of 128 bytes of every other row, and is exchanged with the neighbour's: 3.5 us less for 8192 rows.
 template <class T, int NT>
 __device__ inline void expand(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *high, uint32_t row_pitch, float *size) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
@@ -465,9 +465,19 @@ hipError_t launch_adapters(const ft_adapters_call &call, hipStream_t stream) {
   p.h = static_cast<float *>(call.workspace);
   p.pitch = (uint32_t)up(call.max_rank, 16);
   split_of(call, &p.splits, &p.split);
-  // a workgroup's four wavefronts take a block at least each
-  const uint64_t blocks = (call.width_out + 63) / 64, per = blocks * most_tiles(call.rows, call.count) / (2 * kEnough);
-  p.blocks = (uint32_t)up(per < 4 ? 4 : per > 16 ? 16 : per, 4);
+  // A workgroup's four wavefronts take a block at least each, and no more where that is two rounds of kEnough workgroups at most (64 rows of 33 tiles:
+  // 17.6 us, with 8 blocks 20.5). Beyond that each has H to add up before its blocks, which costs about what four blocks do, and the last round may
+  // be all but empty (8192 rows of 6144 columns: 117 us with 8 blocks, 111 with 12, 107 with 16, 114 with 24).
+  const uint64_t blocks = (call.width_out + 63) / 64, tiles = most_tiles(call.rows, call.count);
+  const uint32_t most = tiles * ((blocks + 3) / 4) <= 2 * kEnough ? 4 : 16;
+  uint64_t least = ~0ull;
+  for (uint32_t n = 4; n <= most; n += 4) {
+    const uint64_t cost = (tiles * ((blocks + n - 1) / n) + kEnough - 1) / kEnough * (n + 4);
+    if (cost < least) {
+      least = cost;
+      p.blocks = n;
+    }
+  }
   return call.type == FT_BF16 ? launch<Bf16>(p, stream) : launch<Fp16>(p, stream);
 }
 
