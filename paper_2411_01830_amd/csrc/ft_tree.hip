@@ -13,8 +13,8 @@
 // begins and ends anywhere, and what several have of one segment is joined by a second kernel, from sums in the workspace.
 //
 // What it costs, on a card that reads 6.1 to 6.9 TB/s and multiplies 1240 TFLOP/s in bfloat16 (caches of several inputs in turn, heads of 128):
-//   one request, 2000 tokens of 8 key heads, a token          19 us: latency, 12 us until the first product is under way, and 5 of the join
-//   64 requests of 16 to 8192, a token, 276 MB                76 us, 3.6 TB/s: the same at either end, the reads between (50 us if they were still in cache)
+//   one request, 2000 tokens of 8 key heads, a token          18 us: latency, 11 us until the first product is under way, and 5 of the join
+//   64 requests of 16 to 8192, a token, 276 MB                70 us, 3.9 TB/s: the same at either end, the reads between (50 us if they were still in cache)
 //   32 of 256 to 4096, trees of 9 to 16 under 4 heads, 175 MB 57 us, 3.1 TB/s
 //   4 of 20000 to 32768, trees of 64 under 8 heads, 232 GFLOP 274 to 290 us, 800 TFLOP/s: vector instructions, 150 a step of 32 MFMA and 32 rows, which
 //     take turns with the matrix unit: of what a step takes, products are a third, reads from shared memory an eighth, exponents a tenth
@@ -29,7 +29,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;     // keys
-// What a segment costs beside its steps, in steps, when they are dealt out (64 requests of 16 to 8192 tokens: 76 us, 80 with 2, 78 with 5 and 8).
+// What a segment costs beside its steps, in steps, when they are dealt out (64 requests of 16 to 8192 tokens: 70 us, 75 with 2, 70 with 4, 71 with 6).
 constexpr uint32_t kSegment = 3;
 // How far, in powers of two, a score may pass the maximum that weights are relative to before sums are brought to a new one: weights
 // stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
@@ -661,7 +661,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       }
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) l[nr] = row_sum(l[nr]);
-      {
+      if (row0 < (uint32_t)q.n * group) {  // (it is the most of all sums that wavefronts without rows would write)
         if (first == 0 && last == steps) {
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) write_row<T, DT>(a, acc[nr], l[nr], m[nr], q, row0 + nr * 16 + n16, head, g);
@@ -787,9 +787,9 @@ struct Shape {
 };
 
 // Heads are padded to 64, 128 or 256 elements. Four wavefronts of 16 rows share keys and values in shared memory, also where there are fewer
-// rows: a wavefront to itself, with four times the workers, takes 121 us instead of 109 for 64 requests of 2000 tokens and 4 rows a key head (8
-// key heads of 128), 46 instead of 35 for one of 20000, 28 and 23.5 for 17 of 700; it is faster only where there is next to nothing to do (13
-// instead of 14.6 for one of 300) or lengths are far apart (74 and 76 for 64 of 16 to 8192). Beyond 64 rows, 16 requests of 4096: eight wavefronts
+// rows: a wavefront to itself, with four times the workers, takes 121 us instead of 105 for 64 requests of 2000 tokens and 4 rows a key head (8
+// key heads of 128), 46 instead of 33 for one of 20000, 28 and 21 for 17 of 700, 74 and 70 for 64 of 16 to 8192; it is faster only where there is next
+// to nothing to do (13 instead of 13.8 for one of 300). Beyond 64 rows, 16 requests of 4096: eight wavefronts
 // of 16 rows take 77 us for 96 rows, four 84, eight of 32 rows 98; for 192 rows 124, 142 and 102. With heads of 64 elements four of 32 rows do what
 // eight do there (43 for 96 and 128). Beyond that up to four workgroups share the die's cache: 384 instead of 394 for 64 requests of 2000 and 512 rows,
 // 259 instead of 274 with heads of 64. Heads of 256 do not leave registers for what is on its way to shared memory.
