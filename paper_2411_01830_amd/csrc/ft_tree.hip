@@ -13,7 +13,7 @@
 // begins and ends anywhere, and what several have of one segment is joined by a second kernel, from sums in the workspace.
 //
 // What it costs, on a card that reads 6.1 to 6.9 TB/s and multiplies 1240 TFLOP/s in bfloat16 (caches of several inputs in turn, heads of 128):
-//   one request, 2000 tokens of 8 key heads, a token          18 us: latency, 11 us until the first product is under way, and 5 of the join
+//   one request, 2000 tokens of 8 key heads, a token          17.5 us: latency, 10 us until the first product is under way, and 5 of the join
 //   64 requests of 16 to 8192, a token, 276 MB                70 us, 3.9 TB/s: the same at either end, the reads between (50 us if they were still in cache)
 //   32 of 256 to 4096, trees of 9 to 16 under 4 heads, 175 MB 57 us, 3.1 TB/s
 //   4 of 20000 to 32768, trees of 64 under 8 heads, 232 GFLOP 274 to 290 us, 800 TFLOP/s: vector instructions, 150 a step of 32 MFMA and 32 rows, which
@@ -866,7 +866,7 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.workers = workers_of(s, cu_count);
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
-  a.least = kSegment + 2;
+  a.least = kSegment + 1;  // (17 requests of up to 1500 tokens: 16.3 us, with a step more 17.9, with four 19.3)
   // Scores are scaled within the exponent's argument, so a scale of 0 must not make NaN of what is masked: the smallest number there is
   // does the same. Queries change their signs for one below 0, as the largest product is to be the largest score.
   a.scale = fabsf(t.scale * kLog2e);
