@@ -738,7 +738,8 @@ typedef struct ft_kv_tables {
  *   lens_out   device, requests entries: the lengths after the step
  *   state_out  device, 4 entries: pages left on the stack, pages that were missing, refused requests, 0
  * lens and state stay as they are, so a step that was refused can be tried again; lens_out and state_out may not be
- * the same memory. Sums are exact whole numbers.
+ * the same memory. Sums are exact whole numbers. Without requests only state, slots and state_out are used: all rows are
+ * of no request, and the stack is as it was (with no rows either, state_out may be NULL, and nothing is done).
  */
 int ft_kv_grow(ft_pool *p, const ft_kv_tables *t, const int32_t *starts, const uint8_t *keep, uint32_t tokens, int64_t *slots,
                int32_t *lens_out, int32_t *state_out, void *hip_stream);
@@ -746,7 +747,8 @@ int ft_kv_grow(ft_pool *p, const ft_kv_tables *t, const int32_t *starts, const u
 /*
  * The pages of all requests r with done[r] != 0 (device, requests bytes) go back on the stack, requests in ascending order,
  * a request's pages too; their lengths become 0. state_out: pages on the stack, 0, 0, 0. lens_out and state_out as above.
- * The table keeps its entries. Pages that do not fit the stack's `pages` entries are lost.
+ * The table keeps its entries. Pages that do not fit the stack's `pages` entries are lost. Without requests only state and state_out
+ * are used, and with state_out NULL nothing is done.
  */
 int ft_kv_release(ft_pool *p, const ft_kv_tables *t, const uint8_t *done, int32_t *lens_out, int32_t *state_out, void *hip_stream);
 

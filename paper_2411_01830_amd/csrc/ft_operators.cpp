@@ -76,11 +76,12 @@ int compute_units(ft_pool *p, int *out) {
   return FT_OK;
 }
 
+// Without requests the state alone is read.
 bool good_tables(const ft_kv_tables &t) {
+  if (!there(t.state, 4) || t.pages >= 1u << 31 || t.page_tokens == 0 || (uint64_t)t.pages * t.page_tokens >= 1ull << 31) return false;
   if (t.requests == 0) return true;
-  if (!there(t.lens, 4) || !there(t.table, 4) || !there(t.free_pages, 4) || !there(t.state, 4)) return false;
-  return t.blocks != 0 && t.pages != 0 && t.pages < 1u << 31 && t.page_tokens != 0 && (uint64_t)t.pages * t.page_tokens < 1ull << 31 &&
-         t.requests < 1u << 24;
+  if (!there(t.lens, 4) || !there(t.table, 4) || !there(t.free_pages, 4)) return false;
+  return t.blocks != 0 && t.pages != 0 && t.requests < 1u << 24;
 }
 
 bool good_strides(std::initializer_list<uint64_t> strides) {
@@ -109,11 +110,11 @@ extern "C" {
 
 int ft_kv_grow(ft_pool *p, const ft_kv_tables *t, const int32_t *starts, const uint8_t *keep, uint32_t tokens, int64_t *slots, int32_t *lens_out,
                int32_t *state_out, void *hip_stream) try {
-  if (p == nullptr || t == nullptr || !good_tables(*t)) return FT_EINVAL;
-  if (t->requests == 0 && tokens == 0) return FT_OK;
-  if (t->requests == 0 || !there(starts, 4) || !there(lens_out, 4) || !there(state_out, 4) || tokens >= 1u << 31) return FT_EINVAL;
-  if (tokens != 0 && !there(slots, 8)) return FT_EINVAL;
-  if (lens_out == t->lens || state_out == t->state) return FT_EINVAL;
+  if (p == nullptr || t == nullptr) return FT_EINVAL;
+  if (t->requests == 0 && tokens == 0 && state_out == nullptr) return FT_OK;
+  if (!good_tables(*t)) return FT_EINVAL;
+  if (t->requests != 0 && (!there(starts, 4) || !there(lens_out, 4) || lens_out == t->lens)) return FT_EINVAL;
+  if (!there(state_out, 4) || state_out == t->state || tokens >= 1u << 31 || (tokens != 0 && !there(slots, 8))) return FT_EINVAL;
   std::lock_guard<std::mutex> lock(p->mu);
   DeviceGuard guard(p->device);
   FT_HIP(p, launch_kv_grow(*t, starts, keep, tokens, slots, lens_out, state_out, static_cast<hipStream_t>(hip_stream)));
@@ -122,9 +123,11 @@ int ft_kv_grow(ft_pool *p, const ft_kv_tables *t, const int32_t *starts, const u
 FT_CATCH_ALL
 
 int ft_kv_release(ft_pool *p, const ft_kv_tables *t, const uint8_t *done, int32_t *lens_out, int32_t *state_out, void *hip_stream) try {
-  if (p == nullptr || t == nullptr || !good_tables(*t)) return FT_EINVAL;
-  if (t->requests == 0) return FT_OK;
-  if (done == nullptr || !there(lens_out, 4) || !there(state_out, 4) || lens_out == t->lens || state_out == t->state) return FT_EINVAL;
+  if (p == nullptr || t == nullptr) return FT_EINVAL;
+  if (t->requests == 0 && state_out == nullptr) return FT_OK;
+  if (!good_tables(*t)) return FT_EINVAL;
+  if (t->requests != 0 && (done == nullptr || !there(lens_out, 4) || lens_out == t->lens)) return FT_EINVAL;
+  if (!there(state_out, 4) || state_out == t->state) return FT_EINVAL;
   std::lock_guard<std::mutex> lock(p->mu);
   DeviceGuard guard(p->device);
   FT_HIP(p, launch_kv_release(*t, done, lens_out, state_out, static_cast<hipStream_t>(hip_stream)));

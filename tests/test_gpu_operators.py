@@ -169,6 +169,20 @@ def test_a_stack_that_is_too_short_keeps_its_size():
     assert after.tolist() == [0, 0] and state.tolist() == [3, 0, 0, 0] and stack.tolist() == [1, 2, 5]
 
 
+@pytest.mark.parametrize("tokens", [0, 1, 5000])
+def test_steps_of_no_requests_leave_the_stack_as_it_was(tokens):
+    m = Memory(SLAB)
+    nobody, none, stack, state = gpu([]), torch.zeros(0, 4, dtype=torch.int32, device="cuda"), gpu([4, 9, 2]), gpu([2, 11, 12, 13])
+    torch.full((4,), 77, dtype=torch.int32, device="cuda")             # (what a result that nobody writes may be found to hold)
+    slots, after, grown = ops().kv_grow(m.pool, nobody, gpu([0]), tokens, none, stack, state, 16)
+    assert slots.tolist() == [-1] * tokens and after.shape == (0,) and grown.tolist() == [2, 0, 0, 0]
+    after, grown = ops().kv_release(m.pool, gpu([], torch.uint8), nobody, none, stack, grown, 16)
+    assert after.shape == (0,) and grown.tolist() == [2, 0, 0, 0]
+    table = torch.full((1, 4), -1, dtype=torch.int32, device="cuda")   # the next step goes on from it
+    slots, after, grown = ops().kv_grow(m.pool, gpu([0]), gpu([0, 20]), 20, table, stack, grown, 16)
+    assert slots.tolist() == [9 * 16 + i for i in range(16)] + [4 * 16 + i for i in range(4)] and grown.tolist() == [0, 0, 0, 0]
+
+
 # ---- a cache --------------------------------------------------------------------------------------
 
 def make_cache(pages, page, heads, dim, dtype, order="token", gap=0):

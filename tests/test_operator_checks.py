@@ -148,6 +148,20 @@ def test_steps_that_are_refused(pool):
     assert code(ft.kv_release, pool, tables(requests=0), None, None, None) == 0
 
 
+def test_steps_of_no_requests_that_are_refused(pool):
+    """Their state is written all the same, so what it is read from and written to is looked at."""
+    none = tables(requests=0, lens=None, table=None, free_pages=None)
+    for other in (dict(state=None), dict(state=BASE + 2), dict(page_tokens=0), dict(pages=1 << 31), dict(pages=1 << 27)):
+        bad = tables(**{"requests": 0, "lens": None, "table": None, "free_pages": None, **other})
+        assert code(ft.kv_grow, pool, bad, None, None, 0, None, None, BASE + 64) == EINVAL, other
+        assert code(ft.kv_release, pool, bad, None, None, BASE + 64) == EINVAL, other
+    assert code(ft.kv_grow, pool, none, None, None, 3, None, None, BASE + 64) == EINVAL
+    assert code(ft.kv_grow, pool, none, None, None, 3, BASE, None, None) == EINVAL
+    for state_out in (BASE, BASE + 66):
+        assert code(ft.kv_grow, pool, none, None, None, 0, None, None, state_out) == EINVAL
+        assert code(ft.kv_release, pool, none, None, None, state_out) == EINVAL
+
+
 def test_adapters_that_are_refused(pool):
     a, b = ft.slab_alloc(pool, 2 * 16 * 512), ft.slab_alloc(pool, 2 * 16 * 256)
     good = (a, b, 16, 1.0)
