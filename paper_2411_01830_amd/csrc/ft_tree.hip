@@ -35,6 +35,12 @@ constexpr uint32_t kSegment = 3;
 // stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
 constexpr float kSlack = 8.0f;
 
+// Where a wavefront has left out values that are not finite and that a row may see: its first and its last step with such, in units of work back from
+// the end of its worker's range (0: none; the largest number stands for larger ones too).
+struct LeftOut {
+  uint32_t first, last;
+};
+
 struct Tree {
   KvView c;
   ft_tree_call t;
@@ -44,8 +50,8 @@ struct Tree {
   uint32_t workers, least;  // workgroups, and steps that each takes at least
   float scale;           // of products, times log2 e: more than 0
   uint32_t flip;         // the signs of queries where it was less
-  uint64_t *prefix;      // requests + 1: work of the requests before; the workers' rate
-  uint32_t *flags;       // of every wavefront, whether it has left out values that are not finite
+  uint64_t *prefix;      // requests + 2: work of the requests before; the workers' rate; all work
+  LeftOut *left_out;     // of every wavefront
   float *sums;           // partial results, see Partial
 };
 
@@ -163,6 +169,12 @@ __device__ inline void write_row(const A &a, const Floats4 (&acc)[DT / 16], floa
 // Wavefronts to each of a compute unit's four parts: what their registers leave room for.
 constexpr int waves(int dt) { return dt <= 128 ? 2 : 1; }
 
+// Which of two elements are infinite or NaN: their exponents of all ones carry into the places of their signs.
+template <class T>
+__device__ inline uint32_t not_finite(uint32_t v) {
+  return ((v & T::kExponent * 0x10001u) + T::kLowest * 0x10001u) & 0x80008000u;
+}
+
 // Two bytes of each of eight rows, as the matrix instruction wants them.
 template <int W>
 __device__ inline Words4 turned(const uint32_t (&v)[8][W], int word, uint32_t bytes) {
@@ -219,7 +231,10 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
         a.prefix[i] = sofar;
         sofar += r1 - r0 == 1 ? mine : work_of(a, request(a, i), ROWS);
       }
-      if (lane == 0) a.prefix[requests] = rate;
+      if (lane == 0) {
+        a.prefix[requests] = rate;
+        a.prefix[requests + 1] = all;
+      }
     }
     const uint64_t begin = begin_of(worker, rate), end = begin_of(worker + 1, rate);
     if (begin >= all) return;
@@ -247,7 +262,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
   float scale = all->scale;
   asm volatile("" : "+s"(row_bytes), "+s"(k_bytes), "+s"(v_bytes), "+s"(pages), "+s"(page_d), "+s"(page_m), "+s"(page_shift), "+s"(page_bytes), "+s"(scale));
 
-  uint32_t bad = 0;  // something has been left out that a row may see
+  LeftOut left_out{0, 0};
   for (;;) {
     const uint32_t cluster = argument()->cluster, heads = argument()->c.heads, group = argument()->group;
     const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * group + ROWS - 1) / ROWS, cost = steps + kSegment;
@@ -552,13 +567,11 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
       };
       const auto edge_values = [&](uint32_t st) {
         if ((st + 1) * kStep <= (uint32_t)q.len) return;
-        // an exponent of all ones carries into the sign's place
-        const auto odd = [](uint32_t v) { return ((v & T::kExponent * 0x10001u) + T::kLowest * 0x10001u) & 0x80008000u; };
         uint32_t any = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int x = 0; x < E / 2; ++x) any |= odd(vf[e][x]);
+          for (int x = 0; x < E / 2; ++x) any |= not_finite<T>(vf[e][x]);
         if (!__any(any != 0)) return;
         const int valid = st >= cached ? q.n - (int)(st - cached) * kStep : q.len - (int)(st * kStep);
         uint32_t seen = 0;
@@ -567,12 +580,16 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           const uint32_t may = (e >> 2) * 16 + 4 * g + (e & 3) < valid ? ~0u : 0;
 #pragma unroll
           for (int x = 0; x < E / 2; ++x) {
-            const uint32_t bit = odd(vf[e][x]) >> 15;
+            const uint32_t bit = not_finite<T>(vf[e][x]) >> 15;
             seen |= bit & may;
             vf[e][x] &= ~((bit << 16) - bit);
           }
         }
-        bad |= uniform((uint32_t)(__any(seen != 0) ? 1 : 0));
+        // (no branch here: the compiler would hold the values twice)
+        const uint64_t back = left + (last - st);
+        const uint32_t here = back >> 32 == 0 ? (uint32_t)back : ~0u, now = uniform((uint32_t)(__any(seen != 0) ? 1 : 0));
+        left_out.last = uniform(now != 0 ? here : left_out.last);
+        left_out.first = uniform(now != 0 && left_out.first == 0 ? here : left_out.first);
       };
 
       // A step's keys are on their way while the one before weighs its values, its values from there on, and the pages of the one behind it
@@ -684,39 +701,78 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
     q.n = 0;
     while (left != 0 && q.n == 0 && ++r < argument()->t.requests) q = request(*argument(), r);
     if (left == 0 || q.n == 0) {
-      if (lane == 0) argument()->flags[place * WR + wave] = bad;
+      if (lane == 0) argument()->left_out[place * WR + wave] = left_out;
       return;
     }
   }
 }
 
-// Infinities and NaN among the values that a row sees of the last cached keys and of drafted ones are added to its result, whatever
-// else that is: it cannot matter how much of them. The first wavefront's, each of its four lanes of a row has a quarter of the elements.
-template <class T, class A>
-__device__ inline void add_left_out(const A &a, const Request &q, uint32_t r, uint32_t row, uint32_t head, int g) {
-  if (threadIdx.x >= 64) return;
-  const uint32_t token = divisor(a.by_group).of(row), q_head = head * a.group + (row - token * a.group);
-  if ((int)token >= q.n) return;
-  const uint64_t t = (uint64_t)(q.start + (int)token);
-  const int tail = q.len & ~(kStep - 1), keys = q.len - tail + q.n;
-  for (uint32_t d = g; d < a.c.dim; d += 4) {
-    float sum = 0;
-    for (int i = 0; i < keys; ++i) {
-      const uint16_t *v;
-      if (tail + i < q.len) {
-        const uint32_t block = divisor(a.c.page_tokens).of(tail + i), page = (uint32_t)a.t.table[(uint64_t)r * a.t.blocks + block];
-        v = reinterpret_cast<const uint16_t *>(a.c.v) + (page < a.c.pages ? page : 0) * a.c.page_stride +
-            (tail + i - block * a.c.page_tokens.d) * a.c.token_stride + head * a.c.head_stride;
-      } else {
-        const int j = i - (q.len - tail);
-        if (a.t.mask != nullptr ? (a.t.mask[t * a.t.mask_words + (j >> 6)] >> (j & 63) & 1) == 0 : j > (int)token) continue;
-        v = static_cast<const uint16_t *>(a.t.v) + (uint64_t)(q.start + j) * a.t.v_token_stride + head * a.t.v_head_stride;
-      }
-      if ((v[d] & T::kExponent) == T::kExponent) sum += T::to_float(v[d]);
+// Infinities and NaN among the values that a row sees, of the last cached keys and of drafted ones in steps [from, to], are added to its
+// sums, whatever else these are: it cannot matter how much of them. Every fourth step to a wavefront: two lanes look at a key's values,
+// then those with any are gone through, each lane for the elements of write_row.
+template <class T, int DT, class A>
+__device__ __forceinline__ void add_left_out(const A &a, const Request &q, uint32_t r, uint32_t row, uint32_t head, uint32_t from, uint32_t to, Floats4 (&acc)[DT / 16]) {
+  constexpr int E = DT / 16;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const uint32_t cached = (uint32_t)((q.len + (kStep - 1)) >> 5), whole = (uint32_t)q.len >> 5;
+  uint32_t token = divisor(a.by_group).of(row);
+  token = token < (uint32_t)q.n ? token : (uint32_t)q.n - 1;
+  for (uint32_t st = (from < whole ? whole : from) + (threadIdx.x >> 6); st <= to; st += 4) {
+    const bool drafted = st >= cached;
+    const uint32_t first = drafted ? (st - cached) * kStep : st * kStep, end = (uint32_t)(drafted ? q.n : q.len);
+    const uint32_t key = first + (lane >> 1) < end ? first + (lane >> 1) : end - 1;
+    const uint16_t *v;
+    if (drafted) {
+      v = static_cast<const uint16_t *>(a.t.v) + ((uint64_t)q.start + key) * a.t.v_token_stride + head * a.t.v_head_stride;
+    } else {
+      const uint32_t block = divisor(a.c.page_tokens).of(key), page = (uint32_t)a.t.table[(uint64_t)r * a.t.blocks + block];
+      v = reinterpret_cast<const uint16_t *>(a.c.v) + (page < a.c.pages ? page : 0) * a.c.page_stride + (key - block * a.c.page_tokens.d) * a.c.token_stride +
+          head * a.c.head_stride;
     }
-    uint16_t *out = static_cast<uint16_t *>(a.t.out) + t * a.t.out_token_stride + q_head * a.t.out_head_stride + d;
-    if (sum != 0) *out = T::from_float(T::to_float(*out) + sum);
+    uint32_t any = 0;
+    for (uint32_t d = 8 * (lane & 1); d < a.c.dim; d += 16) {
+      const Words4 w = load16(v + d);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) any |= not_finite<T>(w[y]);
+    }
+    uint32_t sees = ~0u;
+    if (drafted && a.t.mask != nullptr) {
+      sees = reinterpret_cast<const uint32_t *>(a.t.mask)[((uint64_t)q.start + token) * 2 * a.t.mask_words + (st - cached)];
+    } else if (drafted) {
+      const int d = (int)token - (int)first;
+      sees = d < 0 ? 0 : d >= 31 ? ~0u : (2u << d) - 1;
+    }
+    for (uint64_t found = __ballot(any != 0 && first + (lane >> 1) < end); found != 0;) {
+      const int i = __builtin_ctzll(found) >> 1;
+      found &= ~(3ull << 2 * i);
+      const uint16_t *values = reinterpret_cast<const uint16_t *>(from_lane(reinterpret_cast<uintptr_t>(v), 2 * i)) + 4 * E * g;
+      const bool seen = (sees >> i & 1) != 0;
+#pragma unroll
+      for (int x = 0; x < E / 2; ++x) {
+        Words4 w{0, 0, 0, 0};
+        if (seen && 4 * E * g + 8 * x < (int)a.c.dim) w = load16(values + 8 * x);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {  // element E k + j of the lane's 4 E
+          const uint16_t bits = (uint16_t)(w[y / 2] >> (y % 2 * 16));
+          acc[(8 * x + y) % E][(8 * x + y) / E] += (bits & T::kExponent) == T::kExponent ? T::to_float(bits) : 0;
+        }
+      }
+    }
   }
+}
+
+// What add_left_out has found, on top of a result that is in place already.
+template <class T, int DT, class A>
+__device__ inline void add_to_row(const A &a, const Floats4 (&acc)[DT / 16], const Request &q, uint32_t row, uint32_t kv_head, int g) {
+  constexpr int E = DT / 16;
+  const uint32_t token = divisor(a.by_group).of(row), head = kv_head * a.group + (row - token * a.group);
+  if ((int)token >= q.n) return;
+  uint16_t *out = static_cast<uint16_t *>(a.t.out) + ((uint64_t)q.start + token) * a.t.out_token_stride + head * a.t.out_head_stride + 4 * E * g;
+#pragma unroll
+  for (int j = 0; j < E; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (acc[j][i] != 0) out[E * i + j] = T::from_float(T::to_float(out[E * i + j]) + acc[j][i]);
 }
 
 // The sums of segments that several workers share, 16 rows to a workgroup, whose wavefronts take every fourth worker's each. A kernel of its own: 5 to 8
@@ -738,27 +794,58 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
   const uint64_t rate = a.prefix[a.t.requests], groups = (tiles + a.cluster - 1) / a.cluster;
   const uint64_t begin = a.prefix[r] + ((uint64_t)head * groups + tile / a.cluster) * (steps + kSegment) + kSegment;
   const uint32_t w0 = worker_of(begin, rate), w1 = worker_of(begin + steps - 1, rate);
-  const auto left_out_by = [&](uint32_t w) { return a.flags[(w * a.cluster + tile % a.cluster) * WR + part / NR] != 0; };
+  const auto left_out_by = [&](uint32_t w) { return a.left_out[(w * a.cluster + tile % a.cluster) * WR + part / NR]; };
   const uint32_t row = tile * ROWS + part * 16 + n16;
-  if (w0 == w1) {
-    if (left_out_by(w0)) add_left_out<T>(a, q, r, row, head, g);
+  const auto at = [&](uint32_t w) { return a.sums + ((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.cluster + tile % a.cluster) * (WR * NR) + part) * Partial<DT>::kTile; };
+  float now = -INFINITY, l = 0;
+  Floats4 acc[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc[j] = Floats4{0, 0, 0, 0};
+  // of what the workers have left out, in all that they did, the steps of this segment
+  const auto with_left_out = [&] {
+    const uint64_t all = a.prefix[a.t.requests + 1];
+    uint64_t lo = ~0ull, hi = 0;
+    for (uint32_t w = w0; w <= w1; ++w) {
+      const LeftOut out = left_out_by(w);
+      const uint64_t end = begin_of(w + 1, rate) < all ? begin_of(w + 1, rate) : all;
+      if (out.first == 0) continue;
+      const uint64_t first = out.first == ~0u ? 0 : end - out.first, last = end - out.last;
+      lo = first < lo ? first : lo;
+      hi = last > hi ? last : hi;
+    }
+    lo = lo < begin ? begin : lo;
+    hi = hi < begin + steps - 1 ? hi : begin + steps - 1;
+    if (lo <= hi) add_left_out<T, DT>(a, q, r, row, head, (uint32_t)(lo - begin), (uint32_t)(hi - begin), acc);
+  };
+  // the wavefronts' sums to the first one
+  const auto gather = [&] {
+    if (g == 0) total[wave][n16] = l;
+    if (wave != 0)
+#pragma unroll
+      for (int j = 0; j < E; ++j) join[wave - 1][j][lane] = acc[j];
+    __syncthreads();
+    if (wave != 0) return;
+    l = ((total[0][n16] + total[1][n16]) + total[2][n16]) + total[3][n16];
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc[j] += join[w][j][lane];
+  };
+  if (w0 == w1) {  // the result is in place
+    if (left_out_by(w0).first == 0) return;
+    with_left_out();
+    gather();
+    if (wave == 0) add_to_row<T, DT>(a, acc, q, row, head, g);
     return;
   }
-  const auto at = [&](uint32_t w) { return a.sums + ((((uint64_t)w * 2 + (w == w0 ? 1 : 0)) * a.cluster + tile % a.cluster) * (WR * NR) + part) * Partial<DT>::kTile; };
-  float now = -INFINITY;
   bool left_out = false;
   for (uint32_t w = w0 + (threadIdx.x >> 4); w <= w1; w += 16) {
     now = fmaxf(now, at(w)[16 * DT + n16]);
-    left_out |= left_out_by(w);
+    left_out |= left_out_by(w).first != 0;
   }
   top[threadIdx.x >> 4][n16] = now;
   left_out = __syncthreads_or(left_out);
   for (int i = 0; i < 16; ++i) now = fmaxf(now, top[i][n16]);
   const float from = now == -INFINITY ? 0 : now;
-  float l = 0;
-  Floats4 acc[E];
-#pragma unroll
-  for (int j = 0; j < E; ++j) acc[j] = Floats4{0, 0, 0, 0};
   for (uint32_t w = w0 + wave; w <= w1; w += 4) {
     const float *sums = at(w);
     const float shrink = __builtin_amdgcn_exp2f(sums[16 * DT + n16] - from);
@@ -766,18 +853,9 @@ __global__ __launch_bounds__(256) void ft_tree_join_kernel(Tree) {
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[j] += reinterpret_cast<const Floats4 *>(sums)[j * 64 + lane] * shrink;
   }
-  if (g == 0) total[wave][n16] = l;
-  if (wave != 0)
-#pragma unroll
-    for (int j = 0; j < E; ++j) join[wave - 1][j][lane] = acc[j];
-  __syncthreads();
-  if (wave != 0) return;
-  l = ((total[0][n16] + total[1][n16]) + total[2][n16]) + total[3][n16];
-  for (int w = 0; w < 3; ++w)
-#pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] += join[w][j][lane];
-  write_row<T, DT>(a, acc, l, now, q, row, head, g);
-  if (left_out) add_left_out<T>(a, q, r, row, head, g);
+  if (left_out) with_left_out();
+  gather();
+  if (wave == 0) write_row<T, DT>(a, acc, l, now, q, row, head, g);
 }
 
 struct Shape {
@@ -851,7 +929,7 @@ uint64_t rows_of(const ft_tree_call &t, uint32_t heads) {
 
 uint64_t tree_workspace(const ft_kv_cache &c, const ft_tree_call &t, int cu_count) {
   const Shape s = shape_of(c.dim, rows_of(t, c.heads));
-  return up16(((uint64_t)t.requests + 2) * 8) + waves_of(s, cu_count) * (4 + 2ull * s.nr * (16 * s.dt + 32) * 4);
+  return up16(((uint64_t)t.requests + 2) * 8) + waves_of(s, cu_count) * (sizeof(LeftOut) + 2ull * s.nr * (16 * s.dt + 32) * 4);
 }
 
 hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hipStream_t stream) {
@@ -873,8 +951,8 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   if (a.scale == 0) a.scale = 0x1p-149f;
   a.flip = t.scale < 0 ? 0x80008000u : 0;
   a.prefix = static_cast<uint64_t *>(t.workspace);
-  a.flags = reinterpret_cast<uint32_t *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
-  a.sums = reinterpret_cast<float *>(a.flags + waves_of(s, cu_count));
+  a.left_out = reinterpret_cast<LeftOut *>(static_cast<char *>(t.workspace) + up16(((uint64_t)t.requests + 2) * 8));
+  a.sums = reinterpret_cast<float *>(a.left_out + waves_of(s, cu_count));
   return c.type == FT_BF16 ? launch_dim<Bf16>(a, s, paged, rows, stream) : launch_dim<Fp16>(a, s, paged, rows, stream);
 }
 

@@ -426,6 +426,61 @@ def test_a_value_that_some_rows_see_reaches_those_alone():
             assert torch.equal(row, want[i].float()), (at, i)
 
 
+@pytest.mark.parametrize("dim,page,dtype", [(256, 16, BF16), (128, 16, FP16), (72, 7, BF16), (64, 24, FP16)])
+def test_values_that_are_not_finite_in_long_pieces(dim, page, dtype):
+    """In the last cached keys and far apart in a long piece: whoever sees them has them, beside what all answer anyway."""
+    lens, news, heads, group = [50, 0, 3000, 64], [700, 300, 3, 40], 2, 2
+    t = Tree(lens=lens, news=news, heads=heads, group=group, dim=dim, page=page, dtype=dtype, mask=None)
+    q, k, v, starts = t.args[:4]
+    want, z = t.call()
+    flat = t.m.mem.view(dtype)
+    # a cached one: request, token, head, element, value; and drafted ones
+    cached, drafted = [(0, 49, 1, dim - 1, math.inf), (2, 2999, 0, 0, -math.inf), (2, 2990, 0, 7, math.nan)], \
+        [(0, 0, 0, 3, math.inf), (0, 350, 1, 5, math.nan), (0, 699, 0, dim - 2, -math.inf), (1, 299, 1, 8, math.inf), (1, 64, 1, 8, math.inf),
+         (2, 1, 0, 0, math.inf), (3, 39, 1, 4, math.inf)]
+    bad_v, hit = v.clone(), {}
+    record, table = t.cache.record, t.args[5]
+    for r, i, h, d, value in cached:
+        at = int(table[r, i // page]) * record.page_stride + i % page * record.token_stride + h * record.head_stride + d
+        flat[record.v // 2 + at] = value
+        for row in range(news[r]):
+            hit.setdefault((t.starts[r] + row, h, d), []).append(value)
+    for r, i, h, d, value in drafted:
+        bad_v[t.starts[r] + i, h, d] = value
+        for row in range(i, news[r]):
+            hit.setdefault((t.starts[r] + row, h, d), []).append(value)
+    expect = want.clone()
+    for (row, h, d), values in hit.items():
+        expect[row, h * group:(h + 1) * group, d] = sum(values)
+    got, lse = ops().tree_attention(t.cache, q, k, bad_v, *t.args[3:], mask=None, lse=True)
+    assert torch.equal(got.isnan(), expect.isnan()) and torch.equal(got.nan_to_num(0.0, 7e4, -7e4), expect.nan_to_num(0.0, 7e4, -7e4))
+    assert torch.equal(lse, z)
+
+
+def test_values_that_are_not_finite_cost_little():
+    """One NaN among the values of a long piece, and nothing else among them: neither may cost much more than the piece itself does."""
+    n, dim = 4096, 128
+    t = Tree(lens=[40], news=[n], heads=1, group=1, dim=dim, page=16, dtype=BF16, mask=None)
+    q, k, v = t.args[:3]
+    one, all_of_them = v.clone(), torch.full_like(v, math.nan)
+    one[n // 2, 0, 5] = math.nan
+
+    def took(values):
+        times = []
+        for _ in range(4):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            ops().tree_attention(t.cache, q, k, values, *t.args[3:])
+            end.record()
+            end.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+
+    clean = took(v)
+    assert took(one) < 2 * clean + 0.5, "ms"
+    assert took(all_of_them) < 2 * clean + 10, "ms"
+
+
 def test_a_key_that_some_rows_see_reaches_those_alone():
     t = Tree(lens=[70], news=[30], heads=2, group=4, dim=64, page=16, dtype=FP16)
     q, k, v = t.args[:3]
