@@ -790,7 +790,7 @@ typedef struct ft_tree_call {
  * A row that sees nothing is 0, its lse -infinity. What a row does not see does not reach it, NaN and
  * infinities included; neither does what lies in a page behind a request's last token. One token a request is
  * plain decoding; without a mask any number of rows may be a prompt's next piece. Rows of no request, and those beyond
- * `drafts`, are left as they are in out and lse. requests <= 2^24, requests times the cache's heads < 2^31. A page number
+ * `drafts`, are left as they are in out and lse. Requests times the cache's heads < 2^24. A page number
  * that the cache does not have is read as page 0.
  * Types: products are exact, sums, softmax and lse 32 bits, weights are rounded to the tensors' type for
  * their product with the values, and the result once.
@@ -835,7 +835,7 @@ typedef struct ft_adapters_call {
   const void *base;                 /* rows x width_out: the shared projection's result, or NULL: 0 */
   void *out;                        /* rows x width_out; may be base itself */
   uint64_t x_stride, base_stride, out_stride; /* of a row: >= its width, < 2^40 */
-  uint32_t rows, count, type;
+  uint32_t rows, count, type;       /* rows / 64 + count < 2^24 */
   uint32_t width_in, width_out;
   uint32_t max_rank;                /* of the records; of a larger one's factors the rows behind it are left out */
   void *workspace;                  /* ft_adapters_workspace bytes, 16-byte aligned, as for ft_tree_attention */

@@ -436,6 +436,8 @@ void split_of(const ft_adapters_call &c, uint32_t *splits, uint32_t *split) {
 
 }  // namespace
 
+uint64_t adapter_tiles(uint32_t rows, uint32_t count) { return most_tiles(rows, count); }
+
 uint64_t adapter_group_bytes(uint32_t rows, uint32_t count) { return 64 + up(most_tiles(rows, count) * sizeof(Tile) + (uint64_t)rows * 4, 16); }
 
 hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t count, void *groups, hipStream_t stream) {

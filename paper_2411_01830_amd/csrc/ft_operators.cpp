@@ -90,17 +90,22 @@ bool good_strides(std::initializer_list<uint64_t> strides) {
   return true;
 }
 
+// A grid holds less than 2^32 threads along its first axis, and 2^16 workgroups along the others.
+constexpr uint64_t kMostWorkgroups = (1ull << 32) / 256;
+
 // What of a call is wrong whatever its pointers are.
 bool good_numbers(const ft_kv_cache &c, const ft_tree_call &t) {
   if (t.drafts == 0 || t.requests > 1u << 24 || t.tokens >= 1u << 31 || t.drafts >= 1u << 31 || t.heads == 0 || t.heads % c.heads != 0) return false;
   if (t.heads > 1u << 16 || t.blocks > 1u << 31 || !std::isfinite(t.scale)) return false;
   const uint64_t drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
-  return drafts * (t.heads / c.heads) < 1u << 20 && (uint64_t)t.requests * c.heads < 1ull << 31;  // (what a launch's grid takes)
+  // the second launch has a workgroup to a request's key head, and 16 rows of them along the other axis
+  return drafts * (t.heads / c.heads) < 1u << 20 && (uint64_t)t.requests * c.heads < kMostWorkgroups;
 }
 
 bool good_numbers(const ft_adapters_call &a) {
   if (a.type > FT_FP16 || a.count == 0 || a.count > 1u << 14 || a.width_in == 0 || a.width_out == 0 || a.rows >= 1u << 31) return false;
   if (a.width_in >= 1u << 24 || a.width_out >= 1u << 24) return false;
+  if (a.rows != 0 && adapter_tiles(a.rows, a.count) >= kMostWorkgroups) return false;
   return a.max_rank >= 1 && a.max_rank <= 256;
 }
 

@@ -43,6 +43,7 @@ hipError_t launch_kv_append(const KvView &c, const void *k, const void *v, uint6
 uint64_t tree_workspace(const ft_kv_cache &c, const ft_tree_call &call, int cu_count);
 hipError_t launch_tree(const KvView &c, const ft_tree_call &call, int cu_count, hipStream_t stream);
 
+uint64_t adapter_tiles(uint32_t rows, uint32_t count);  // at most: workgroups of 256 threads along the first axis of the products' grids
 uint64_t adapter_group_bytes(uint32_t rows, uint32_t count);
 hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t count, void *groups, hipStream_t stream);
 uint64_t adapter_workspace(const ft_adapters_call &call);

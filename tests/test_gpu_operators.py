@@ -533,6 +533,18 @@ def test_a_cache_whose_offsets_pass_32_bits():
     assert torch.isfinite(want).all() and torch.equal(out, want)
 
 
+@pytest.mark.parametrize("dim", [8, 256])
+def test_as_many_drafted_rows_as_there_may_be(dim):
+    """The bound on a request's rows is a launch's; few of them are there."""
+    t = Tree(lens=[40], news=[3], heads=1, group=1, dim=dim, page=16, dtype=BF16)
+    want = ops().tree_attention(t.cache, *t.args)
+    most = (1 << 20) - 1
+    q, k, v = [torch.cat([x, x[:1].expand(most - 3, -1, -1)]) for x in t.args[:3]]
+    out = torch.full_like(q, 7.0)
+    got = ops().tree_attention(t.cache, q, k, v, *t.args[3:6], most, out=out)
+    assert torch.equal(got[:3], want) and (got[3:] == 7).all()
+
+
 def test_lengths_and_tables_that_are_wrong_stay_inside_the_cache():
     t = Tree(lens=[100, 40, 30], news=[3, 4, 5], heads=2, group=2, dim=64, page=16, dtype=BF16)
     want, _ = t.call()

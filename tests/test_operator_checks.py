@@ -109,6 +109,20 @@ def test_attention_calls_that_are_refused(pool, other):
     assert code(ft.tree_attention, pool, cache(pool), call(**other)) == EINVAL
 
 
+def test_calls_of_more_workgroups_than_a_grid_holds_are_refused(pool):
+    """The second launch has 256 threads for every request's key head, and a grid less than 2^32: refused before the first launch."""
+    c = cache(pool)
+    assert code(ft.tree_attention, pool, c, call(requests=1 << 21)) == EINVAL
+    assert code(ft.tree_workspace, pool, c, call(requests=1 << 21)) == EINVAL
+    assert code(ft.tree_workspace, pool, c, call(requests=(1 << 21) - 1)) != EINVAL
+    assert code(ft.tree_workspace, pool, c, call(heads=8, tokens=1 << 20, drafts=1 << 20)) == EINVAL
+    assert code(ft.tree_workspace, pool, c, call(heads=8, tokens=1 << 20, drafts=(1 << 20) - 1)) != EINVAL
+    for rows, want in (((1 << 30) - 384, 0), ((1 << 30) - 320, EINVAL), (1 << 30, EINVAL)):      # 64 rows of one adapter a workgroup
+        assert code(ft.adapters_workspace, pool, adapters_call(rows=rows)) == want, rows
+        if want != 0:
+            assert code(ft.adapters_apply, pool, adapters_call(rows=rows, workspace_bytes=1 << 62)) == want, rows
+
+
 def test_nothing_to_attend_is_nothing_wrong(pool):
     c = cache(pool)
     for other in (dict(tokens=0), dict(requests=0)):
