@@ -12,17 +12,14 @@ constexpr int kWaves = kThreads / 64;
 
 // Sums over the threads before this one, and all of them. Two quantities in one go: a launch of few requests is nothing but this.
 struct Sums {
-  uint64_t pages;
-  uint32_t items;
+  uint64_t pages, items;  // (requests whose rows overlap, as starts that descend make them, have more of either than 32 bits count)
 };
 
-__device__ inline Sums scan(uint64_t pages, uint32_t items, Sums *before, Sums *lds) {
+__device__ inline Sums scan(uint64_t pages, uint64_t items, Sums *before, Sums *lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t p = pages;
-  uint32_t i = items;
+  uint64_t p = pages, i = items;
   for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t q = __shfl_up(p, d);
-    const uint32_t j = __shfl_up(i, d);
+    const uint64_t q = __shfl_up(p, d), j = __shfl_up(i, d);
     if (lane >= d) {
       p += q;
       i += j;
@@ -41,7 +38,7 @@ __device__ inline Sums scan(uint64_t pages, uint32_t items, Sums *before, Sums *
 }
 
 // The request whose items [at[r], at[r + 1]) contain i: the last r with at[r] <= i that has any. at ascends; n of them are looked at.
-__device__ inline int owner(const uint32_t *at, int n, uint32_t i) {
+__device__ inline int owner(const uint64_t *at, int n, uint64_t i) {
   int lo = 0, hi = n;  // at[lo] <= i < at[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -58,7 +55,7 @@ __device__ inline uint32_t pages_of(int32_t tokens, const Divisor &page) { retur
 struct GrowLds {
   Sums wave[kWaves];
   uint64_t first[kThreads];  // pages taken by the requests before
-  uint32_t item[kThreads];   // blocks of 64 rows of the requests before
+  uint64_t item[kThreads];   // blocks of 64 rows of the requests before
   int32_t row[kThreads], count[kThreads], len[kThreads], added[kThreads];
   unsigned long long taken;
   uint32_t refused;
@@ -108,7 +105,8 @@ __global__ __launch_bounds__(kThreads) void ft_kv_grow_kernel(ft_kv_tables t, Di
           const int q = q0 + k * kWaves;
           if (q >= n) break;
           int32_t kept = __popcll(__ballot(flag[k] != 0));
-          for (int32_t i = 64 + lane; i - lane < s.count[q]; i += 64) kept += __popcll(__ballot(i < s.count[q] && keep[s.row[q] + i] != 0));
+          const uint32_t rows_of = (uint32_t)s.count[q];
+          for (uint32_t i = 64; i < rows_of; i += 64) kept += __popcll(__ballot(i + lane < rows_of && keep[s.row[q] + i + lane] != 0));
           if (lane == 0) s.added[q] = kept;
         }
       }
@@ -120,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void ft_kv_grow_kernel(ft_kv_tables t, Di
     const bool fits = mine && len >= 0 && after <= 0x7fffffff && pages_of((int32_t)after, page) <= t.blocks;
     const uint32_t have = fits ? pages_of(len, page) : 0, want = fits ? pages_of((int32_t)after, page) : 0;
     Sums before;
-    const Sums all = scan(want - have, (uint32_t)((count + 63) >> 6), &before, s.wave);
+    const Sums all = scan(want - have, ((uint32_t)count + 63) >> 6, &before, s.wave);
     const uint64_t first = asked + before.pages, end = first + (want - have);
     const bool served = fits && (want == have || end <= (uint64_t)top);
     s.first[threadIdx.x] = first;
@@ -134,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void ft_kv_grow_kernel(ft_kv_tables t, Di
     }
     asked += all.pages;
     __syncthreads();
-    for (uint32_t i = blockIdx.x * kWaves + wave; i < all.items; i += gridDim.x * kWaves) {
+    for (uint64_t i = blockIdx.x * kWaves + wave; i < all.items; i += gridDim.x * kWaves) {
       const int q = owner(s.item, kThreads, i);
       const int32_t begin = (int32_t)(i - s.item[q]) << 6, n = s.count[q], at = begin + lane, pages = s.added[q];
       const bool there = at < n;
@@ -181,7 +179,8 @@ __global__ __launch_bounds__(kThreads) void ft_kv_grow_kernel(ft_kv_tables t, Di
 struct ReleaseLds {
   Sums wave[kWaves];
   uint64_t first[kThreads];
-  uint32_t item[kThreads], count[kThreads];
+  uint64_t item[kThreads];
+  uint32_t count[kThreads];
 };
 
 // The same sum over the pages of the requests that are done, and their entries to the stack, 64 to a wavefront: 6 us for 64 of 256 requests of up to
@@ -210,9 +209,9 @@ __global__ __launch_bounds__(kThreads) void ft_kv_release_kernel(ft_kv_tables t,
     s.count[threadIdx.x] = pages;
     given += all.pages;
     __syncthreads();
-    for (uint32_t i = blockIdx.x * kWaves + wave; i < all.items; i += gridDim.x * kWaves) {
+    for (uint64_t i = blockIdx.x * kWaves + wave; i < all.items; i += gridDim.x * kWaves) {
       const int q = owner(s.item, kThreads, i);
-      const uint32_t b = ((i - s.item[q]) << 6) + lane;
+      const uint32_t b = ((uint32_t)(i - s.item[q]) << 6) + lane;
       const uint64_t to = (uint64_t)top + s.first[q] + b;
       if (b < s.count[q] && to < t.pages) t.free_pages[to] = t.table[(uint64_t)(r0 + q) * t.blocks + b];
     }

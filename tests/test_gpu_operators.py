@@ -169,6 +169,50 @@ def test_a_stack_that_is_too_short_keeps_its_size():
     assert after.tolist() == [0, 0] and state.tolist() == [3, 0, 0, 0] and stack.tolist() == [1, 2, 5]
 
 
+def grow_between_canaries(lens, starts, tokens, table, free, top, page, keep=None):
+    """A step whose results lie between other things of the same tensors: slots, lengths, state, table."""
+    m = Memory(SLAB)
+    canary = lambda n, dtype: torch.full((n + 64,), 77, dtype=dtype, device="cuda")  # noqa: E731
+    wide = canary(tokens, torch.int64), canary(len(lens), torch.int32), canary(4, torch.int32), canary(table.numel(), torch.int32)
+    slots, after, state, rows = [w[32:-32] for w in wide]
+    rows.copy_(table.flatten())
+    given = gpu(lens), gpu(free), gpu([top, 0, 0, 0]), gpu(starts)
+    tables = ft.KvTables(given[0].data_ptr(), rows.data_ptr(), given[1].data_ptr(), given[2].data_ptr(), len(lens), table.shape[1], len(free), page)
+    ft.kv_grow(m.pool, tables, given[3].data_ptr(), None if keep is None else keep.data_ptr(), tokens, slots.data_ptr(), after.data_ptr(),
+               state.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    for w in wide:
+        assert (w[:32] == 77).all() and (w[-32:] == 77).all()
+    return slots, after, state, rows.view(table.shape)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_starts_of_any_kind_write_nothing_beside_the_results(seed):
+    rng = random.Random(seed)
+    requests, tokens, page, blocks = rng.choice([1, 3, 70, 1500]), rng.choice([1, 6, 100, 3000]), rng.choice([1, 7, 16]), 5
+    starts = [rng.choice([rng.randint(-9, tokens + 9), rng.randint(0, tokens), -2 ** 31, 2 ** 31 - 1]) for _ in range(requests + 1)]
+    lens = [rng.randint(0, 2 * page) for _ in range(requests)]
+    table = torch.arange(requests * blocks, dtype=torch.int32).view(requests, blocks)
+    free = list(range(requests * blocks, requests * blocks + 400)) + [0] * 7
+    keep = torch.tensor([rng.random() < 0.5 for _ in range(tokens)], dtype=torch.uint8, device="cuda") if seed % 2 else None
+    slots, after, state, rows = grow_between_canaries(lens, starts, tokens, table, free, 400, page, keep)
+    got = slots.cpu()
+    # every row has been written, with a slot of a page that there is
+    assert ((got == -1) | (got >= 0) & (got < (requests * blocks + 400) * page)).all() and not (got == 77).all()
+    top, lacked, refused, _ = state.tolist()
+    assert 0 <= top <= 400 and 0 <= refused <= requests and lacked >= 0
+    assert all(a <= b <= blocks * page for a, b in zip(lens, after.tolist()))
+    changed = rows.cpu() != table
+    assert (rows.cpu()[changed] >= requests * blocks).all()
+
+
+def test_rows_of_overlapping_requests_that_32_bits_do_not_count():
+    """512 requests that each claim all of 2^29 + 64 rows: more than 2^32 blocks of 64."""
+    tokens = (1 << 29) + 64
+    table = torch.zeros(1024, 1, dtype=torch.int32)
+    slots, after, state, _ = grow_between_canaries([0] * 1024, [0, tokens] * 512 + [0], tokens, table, [0] * 4, 4, 16)
+    assert (slots == -1).all() and (after == 0).all() and state.tolist() == [4, 0, 512, 0]      # none of them has a table that long
+
+
 @pytest.mark.parametrize("tokens", [0, 1, 5000])
 def test_steps_of_no_requests_leave_the_stack_as_it_was(tokens):
     m = Memory(SLAB)
