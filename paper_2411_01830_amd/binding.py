@@ -184,6 +184,7 @@ def strerror(rc):
 def pool_create(dev_base, nbytes, slab_bytes, device=0):
     h = C.c_void_p()
     _check(_lib.ft_pool_create(C.byref(h), dev_base, nbytes, slab_bytes, device))
+    h.device = device
     return h
 
 

@@ -2,7 +2,7 @@
 
 A key/value cache and low-rank adapters lie in allocations of a pool (`binding.pool_create`, `binding.slab_alloc`), where
 transfers bring and move them; everything else is the caller's tensors. Each call checks what it is given, allocates
-its results and its workspace through PyTorch, and queues its kernels on the current stream. What is wrong with the
+its results and its workspace through PyTorch, and queues its kernels on the current stream of the pool's GPU, where all tensors have to lie. What is wrong with the
 arguments raises `binding.FtError` with the library's code, before anything is launched.
 
 One step of a server:
@@ -46,10 +46,14 @@ def _rows(name, t, dtype, shape, device):
         _refuse(f"{name}: rows are not contiguous")
 
 
-def _device(name, t):
-    if not isinstance(t, torch.Tensor):
-        _refuse(f"{name}: a tensor is needed")
-    return t.device
+def _device(name, t, pool):
+    """The GPU that a call's tensors have to lie on, which is the pool's."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        _refuse(f"{name}: a tensor on the GPU is needed")
+    dev = t.device
+    if dev.index != getattr(pool, "device", dev.index):  # (a handle from elsewhere than pool_create does not know)
+        _refuse(f"{name} lies on {dev}, the pool on GPU {pool.device}")
+    return dev
 
 
 def _flags(name, t, device, n):
@@ -75,8 +79,8 @@ class KvCache:
         self.record = ft.KvCacheRecord(k_off, v_off, TYPES[dtype], pages, page_tokens, heads, dim, 0, page, token, head)
 
 
-def _tables(lens, table, free, state, page_tokens):
-    dev = _device("lens", lens)
+def _tables(pool, lens, table, free, state, page_tokens):
+    dev = _device("lens", lens, pool)
     _ints("lens", lens, torch.int32, 1, dev)
     _ints("table", table, torch.int32, 2, dev)
     _ints("free", free, torch.int32, 1, dev)
@@ -89,7 +93,7 @@ def _tables(lens, table, free, state, page_tokens):
 
 def kv_grow(pool, lens, starts, tokens, table, free, state, page_tokens, keep=None):
     """Pages and slots of a step's `tokens` rows: (slots, lengths and state after the step); table gets its new entries in place."""
-    dev, tables = _tables(lens, table, free, state, page_tokens)
+    dev, tables = _tables(pool, lens, table, free, state, page_tokens)
     _ints("starts", starts, torch.int32, 1, dev)
     if starts.shape[0] != tables.requests + 1:
         _refuse("starts has one entry more than lens")
@@ -104,7 +108,7 @@ def kv_grow(pool, lens, starts, tokens, table, free, state, page_tokens, keep=No
 
 def kv_release(pool, done, lens, table, free, state, page_tokens):
     """The pages of the requests with done != 0 go back on the stack, in place: (lengths, state) after it."""
-    dev, tables = _tables(lens, table, free, state, page_tokens)
+    dev, tables = _tables(pool, lens, table, free, state, page_tokens)
     _flags("done", done, dev, tables.requests)
     lens_out, state_out = torch.empty_like(lens), torch.empty_like(state)
     ft.kv_release(pool, tables, done.data_ptr(), lens_out.data_ptr(), state_out.data_ptr(), _stream(dev.index))
@@ -113,7 +117,7 @@ def kv_release(pool, done, lens, table, free, state, page_tokens):
 
 def kv_append(cache, k, v, slots):
     """cache[slots[t]] = k[t], v[t]; rows with slot -1 are skipped."""
-    dev = _device("slots", slots)
+    dev = _device("slots", slots, cache.pool)
     _ints("slots", slots, torch.int64, 1, dev)
     shape = (slots.shape[0], cache.heads, cache.dim)
     _rows("k", k, cache.dtype, shape, dev)
@@ -127,7 +131,7 @@ def tree_attention(cache, q, k, v, starts, lens, table, drafts, mask=None, scale
     q: tokens x heads x dim; k, v: tokens x the cache's heads x dim. drafts: the most drafted tokens of one request. mask: int64 or
     uint64, a word of 64 bits a token, or several as a second dimension. scale: dim ** -0.5 by default. With lse also
     log(sum(exp)) of every row, in 32 bits."""
-    dev = _device("q", q)
+    dev = _device("q", q, cache.pool)
     if q.dim() != 3:
         _refuse("q has three dimensions")
     shape, dtype, dim = q.shape, cache.dtype, cache.dim
@@ -176,10 +180,13 @@ class Adapters:
             _refuse(f"adapters hold bfloat16 or float16, not {dtype}")
         if len(adapters) == 0:
             _refuse("there are no adapters")
+        on = torch.device("cuda", getattr(pool, "device", 0)) if device is None else torch.device(device)
+        if on.index not in (None, getattr(pool, "device", on.index)):
+            _refuse(f"the pool lies on GPU {pool.device}, not on {on}")
         records = ft.adapters_resolve(pool, [tuple(a) for a in adapters], width_in, width_out)
         self.pool, self.dtype, self.count, self.width_in, self.width_out = pool, dtype, len(adapters), width_in, width_out
         self.max_rank = max(a[2] for a in adapters)
-        self.records = torch.frombuffer(bytearray(records), dtype=torch.uint8).to("cuda" if device is None else device)
+        self.records = torch.frombuffer(bytearray(records), dtype=torch.uint8).to(on)
 
 
 class AdapterGroups:
@@ -191,7 +198,7 @@ class AdapterGroups:
 
 def adapter_groups(adapters, ids):
     """ids: int32, a row's adapter, or anything outside [0, count) for none."""
-    dev = _device("ids", ids)
+    dev = _device("ids", ids, adapters.pool)
     _ints("ids", ids, torch.int32, 1, dev)
     rows = ids.shape[0]
     need = ft.adapters_group_bytes(rows, adapters.count)
@@ -202,7 +209,7 @@ def adapter_groups(adapters, ids):
 
 def adapters_apply(adapters, groups, x, base=None, out=None):
     """base (None: 0) and every row's scale * B (A x) on top; out may be base."""
-    dev = _device("x", x)
+    dev = _device("x", x, adapters.pool)
     rows, dtype, records, memory = groups.rows, adapters.dtype, adapters.records, groups.memory
     if x.dim() != 2 or x.shape[0] != rows or groups.count != adapters.count:
         _refuse("the groups are of other rows or adapters")

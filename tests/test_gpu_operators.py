@@ -2,6 +2,7 @@
 
 Bounds come from the types alone. u is the unit roundoff of the tensors' type (bfloat16 2^-8, float16 2^-11): a result is
 rounded once, and attention's weights once more for their product with the values; sums and softmax have 24 bits."""
+import ctypes
 import math
 import random
 
@@ -710,6 +711,29 @@ def test_what_one_row_holds_does_not_reach_another():
     assert torch.isnan(got[11]).all() == has
     rows = [i for i in range(80) if i != 11]
     assert torch.equal(got[rows], want[rows])
+
+
+def test_tensors_on_another_gpu_than_the_pool_are_refused():
+    """A pool's handle that says it lies on the next GPU: each call is refused before its launch."""
+    m = Memory(1 << 20)
+    assert m.pool.device == torch.cuda.current_device()
+    other = ctypes.c_void_p(m.pool.value)
+    other.device = m.pool.device + 1
+    at = [m.alloc(2 * 4 * 16 * 64) for _ in range(2)]
+    cache = ops().KvCache(other, at[0], at[1], 4, 16, 1, 64, BF16)
+    x, ids, one = torch.zeros(1, 1, 64, dtype=BF16, device="cuda"), gpu([0]), gpu([[0]])
+    adapters = ops().Adapters(m.pool, [(at[0], at[1], 1, 1.0)], 64, 64, BF16)
+    groups, adapters.pool = ops().adapter_groups(adapters, ids), other
+    state = gpu([1, 0, 0, 0])
+    for call in (lambda: ops().kv_append(cache, x, x, gpu([0], torch.int64)),
+                 lambda: ops().tree_attention(cache, x, x, x, gpu([0, 1]), gpu([3]), one, 1),
+                 lambda: ops().kv_grow(other, gpu([3]), gpu([0, 1]), 1, one, gpu([0]), state, 16),
+                 lambda: ops().kv_release(other, gpu([1], torch.uint8), gpu([3]), one, gpu([0]), state, 16),
+                 lambda: ops().adapter_groups(adapters, ids), lambda: ops().adapters_apply(adapters, groups, x[0]),
+                 lambda: ops().Adapters(other, [(at[0], at[1], 1, 1.0)], 64, 64, BF16, device="cuda:0")):
+        with pytest.raises(ft.FtError) as refused:
+            call()
+        assert refused.value.code == -1
 
 
 # ---- streams, graphs, the step as a whole -----------------------------------------------------------
