@@ -3,7 +3,8 @@
 A key/value cache and low-rank adapters lie in allocations of a pool (`binding.pool_create`, `binding.slab_alloc`), where
 transfers bring and move them; everything else is the caller's tensors. Each call checks what it is given, allocates
 its results and its workspace through PyTorch, and queues its kernels on the current stream of the pool's GPU, where all tensors have to lie. What is wrong with the
-arguments raises `binding.FtError` with the library's code, before anything is launched.
+arguments raises `binding.FtError` with the library's code, before anything is launched. The operators serve and do not train: inputs
+that ask for a gradient are refused, as results would not lead back to them.
 
 One step of a server:
 
@@ -44,6 +45,8 @@ def _rows(name, t, dtype, shape, device):
         _refuse(f"{name}: the shape is {tuple(t.shape)}, not {tuple(shape)}")
     if t.stride(-1) != 1 and t.shape[-1] != 1 and t.numel() != 0:
         _refuse(f"{name}: rows are not contiguous")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{name} asks for a gradient, and there is none (under torch.no_grad it is not asked for)")
 
 
 def _device(name, t, pool):

@@ -736,6 +736,29 @@ def test_tensors_on_another_gpu_than_the_pool_are_refused():
         assert refused.value.code == -1
 
 
+def test_inputs_that_ask_for_a_gradient_are_refused():
+    t = Tree(lens=[40], news=[3], heads=1, group=2, dim=64, page=16, dtype=BF16)
+    a = Adapt([0, 1], [8, 16], 64, 96, BF16)
+    want, adapted = t.call()[0], a.call()
+    groups = ops().adapter_groups(a.adapters, a.gids)
+    slots = gpu([-1] * 3, torch.int64)
+    for i in range(3):
+        args = list(t.args)
+        args[i] = args[i].clone().requires_grad_()
+        with pytest.raises(ft.FtError):
+            ops().tree_attention(t.cache, *args, mask=t.mask)
+        if i > 0:
+            with pytest.raises(ft.FtError):
+                ops().kv_append(t.cache, args[1], args[2], slots)
+        with torch.no_grad():
+            assert torch.equal(ops().tree_attention(t.cache, *args, mask=t.mask, scale=t.scale), want)
+    for x, base in ((a.gx.clone().requires_grad_(), a.gb), (a.gx, a.gb.clone().requires_grad_())):
+        with pytest.raises(ft.FtError):
+            ops().adapters_apply(a.adapters, groups, x, base)
+        with torch.no_grad():
+            assert torch.equal(ops().adapters_apply(a.adapters, groups, x, base), adapted)
+
+
 # ---- streams, graphs, the step as a whole -----------------------------------------------------------
 
 def test_operators_on_a_stream_of_their_own():
