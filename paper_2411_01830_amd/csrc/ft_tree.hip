@@ -519,6 +519,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           }
       };
       Words4 p[NR];
+      uint32_t far = 0;  // a maximum is or was beyond 2^24, on either side
       const auto weights = [&] {
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
@@ -530,13 +531,25 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
             const float now = fmaxf(m[nr], row_max(top) * scale);
             const float shrink = now == -INFINITY ? 1 : __builtin_amdgcn_exp2f(m[nr] - now);
             m[nr] = now;
+            far |= uniform((uint32_t)(__any(now != -INFINITY && fabsf(now) > 0x1p24f) ? 1 : 0));
             l[nr] *= shrink;
 #pragma unroll
             for (int j = 0; j < E; ++j) acc[nr][j] *= shrink;
           }
           const float from = m[nr] == -INFINITY ? 0 : m[nr];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -from));
+          for (int i = 0; i < 8; ++i) w[i] = __builtin_fmaf(x[i], scale, -from);
+          // The maximum is a rounded score. All weights are off by the one factor that its rounding makes, which the row's sum takes out again, but
+          // from 2^24 on that may be too much for any range: there each score is rounded as the maximum was.
+          if (far != 0)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float score = x[i] * scale;
+              asm("" : "+v"(score));
+              w[i] = score - from;
+            }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
           l[nr] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
           p[nr] = Words4{T::pack(w[0], w[1]), T::pack(w[2], w[3]), T::pack(w[4], w[5]), T::pack(w[6], w[7])};
         }

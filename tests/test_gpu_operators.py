@@ -828,3 +828,38 @@ def test_scales_of_either_sign(scale):
     t = Tree(lens=[70, 0, 33], news=[5, 20, 1], heads=2, group=2, dim=64, page=16, dtype=BF16)
     t.scale = scale
     t.check(*t.call())
+
+
+@pytest.mark.parametrize("dtype,size", [(BF16, 2.0 ** 10), (BF16, 2.0 ** 20), (BF16, 2.0 ** 28), (BF16, 2.0 ** 33), (BF16, 2.0 ** 60), (BF16, -2.0 ** 100),
+                                        (FP16, 2.0 ** 15), (FP16, 2.0 ** 22), (FP16, -2.0 ** 22)])
+@pytest.mark.parametrize("lens,dim,group", [([150], 64, 1), ([150, 3, 70], 128, 4), ([120], 128, 40), ([90, 33], 256, 2), ([150], 72, 3)])
+def test_scores_of_any_size(lens, dim, group, dtype, size):
+    """Products that are whole multiples of `size`, different for all that a row sees: the largest has all of the weight."""
+    t = Tree(lens=lens, news=[3] * len(lens), heads=1, group=group, dim=dim, page=16, dtype=dtype, mask=None)
+    q, k, v, starts, _, table = t.args[:6]
+    both = (abs(size) / 2.0 ** 15, 2.0 ** 15) if dtype is FP16 and abs(size) > 2.0 ** 15 else (1.0, abs(size))   # the keys' part and the queries'
+    g = torch.Generator().manual_seed(3)
+    q.zero_()
+    k.zero_()
+    q[:, :, 5] = math.copysign(both[1], size)
+    flat, record = t.m.mem.view(dtype), t.cache.record
+    for r, n in enumerate(lens):
+        number = torch.randperm(n + 3, generator=g) - 20
+        for i in range(n):
+            at = record.k // 2 + int(table[r, i // 16]) * record.page_stride + i % 16 * record.token_stride
+            flat[at:at + dim] = 0
+            flat[at + 5] = float(number[i]) * both[0]
+        for i in range(3):
+            k[t.starts[r] + i, 0, 5] = float(number[n + i]) * both[0]
+        t.keys[r] = number
+    out, lse = t.call()
+    for r, n in enumerate(lens):
+        for i in range(3):
+            seen = t.keys[r][:n + i + 1].double() * size
+            s = int(seen.argmax())
+            want = t.values[r][s, 0] if s < n else t.v[t.starts[r] + s - n, 0]
+            row = t.starts[r] + i
+            # the weight, which may be any power of two's neighbour, is rounded once and so is the result
+            assert ((out[row].double().cpu() - want.double()).abs() <= 2 * U[dtype] * want.double().abs() + TINY[dtype]).all(), (r, i)
+            top = float(seen.max()) * t.scale
+            assert (lse[row].double().cpu() - top).abs().max() <= 2.0 ** -21 * abs(top) + 2.0 ** -20, (r, i)
