@@ -777,7 +777,7 @@ typedef struct ft_tree_call {
   uint32_t heads;        /* query heads, a multiple of the cache's: head h reads key head h / (heads / cache heads) */
   uint32_t blocks;
   uint32_t mask_words;   /* 64 * mask_words >= drafts where there is a mask */
-  float scale;           /* of the products, finite */
+  float scale;           /* of the products; finite, also as a power of two: times 1.4427 */
   uint32_t _pad;         /* ignored */
   void *workspace;       /* ft_tree_workspace bytes, 16-byte aligned, of this call alone while it runs; contents do not matter */
   uint64_t workspace_bytes;
@@ -787,7 +787,8 @@ typedef struct ft_tree_call {
  * Attention of the drafted tokens of all requests over their cached tokens, all of which each of them sees, and over each
  * other as the mask says:
  *   out[t, h] = sum over s of softmax over s (scale * q[t, h] . key[s]) value[s],   lse[t, h] = log of the sum of exp
- * A row that sees nothing is 0, its lse -infinity. What a row does not see does not reach it, NaN and
+ * A row that sees nothing is 0, its lse -infinity. Scores beyond the range of 32 bits are infinite: above it a row is NaN and its lse
+ * infinite, below it weights are 0. What a row does not see does not reach it, NaN and
  * infinities included; neither does what lies in a page behind a request's last token. One token a request is
  * plain decoding; without a mask any number of rows may be a prompt's next piece. Rows of no request, and those beyond
  * `drafts`, are left as they are in out and lse. Requests times the cache's heads < 2^24. A page number

@@ -96,7 +96,7 @@ constexpr uint64_t kMostWorkgroups = (1ull << 32) / 256;
 // What of a call is wrong whatever its pointers are.
 bool good_numbers(const ft_kv_cache &c, const ft_tree_call &t) {
   if (t.drafts == 0 || t.requests > 1u << 24 || t.tokens >= 1u << 31 || t.drafts >= 1u << 31 || t.heads == 0 || t.heads % c.heads != 0) return false;
-  if (t.heads > 1u << 16 || t.blocks > 1u << 31 || !std::isfinite(t.scale)) return false;
+  if (t.heads > 1u << 16 || t.blocks > 1u << 31 || !std::isfinite(t.scale * 1.4426951f)) return false;  // (scores are kept in powers of two)
   const uint64_t drafts = t.drafts < t.tokens ? t.drafts : t.tokens;
   // the second launch has a workgroup to a request's key head, and 16 rows of them along the other axis
   return drafts * (t.heads / c.heads) < 1u << 20 && (uint64_t)t.requests * c.heads < kMostWorkgroups;

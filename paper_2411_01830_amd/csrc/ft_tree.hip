@@ -528,7 +528,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
           for (int i = 0; i < 8; ++i) x[i] = s[nr][i >> 2][i & 3];
           const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
           if (__any(top * scale > m[nr] + kSlack)) {
-            const float now = fmaxf(m[nr], row_max(top) * scale);
+            // (at most the largest number: relative to an infinite maximum every weight would be zero, and the row one that sees nothing)
+            const float now = fminf(fmaxf(m[nr], row_max(top) * scale), __FLT_MAX__);
             const float shrink = now == -INFINITY ? 1 : __builtin_amdgcn_exp2f(m[nr] - now);
             m[nr] = now;
             far |= uniform((uint32_t)(__any(now != -INFINITY && fabsf(now) > 0x1p24f) ? 1 : 0));

@@ -830,6 +830,21 @@ def test_scales_of_either_sign(scale):
     t.check(*t.call())
 
 
+@pytest.mark.parametrize("scale", [1e38, -1e38])
+@pytest.mark.parametrize("lens,news,dim", [([70], [5], 64), ([5000, 0], [1, 40], 128), ([40], [30], 256)])
+def test_scores_beyond_32_bits_are_infinite(lens, news, dim, scale):
+    """Among some tens of products of either sign the largest score is far beyond the largest number of 32 bits: the answer is NaN, not
+    that of a row that sees nothing."""
+    t = Tree(lens=lens, news=news, heads=2, group=2, dim=dim, page=16, dtype=BF16, mask="any")
+    t.scale = scale
+    out, lse = t.call()
+    few = [t.starts[r] + i for r in range(len(lens)) for i in range(news[r]) if lens[r] + bin(t.bits[t.starts[r] + i]).count("1") >= 40]
+    none = [t.starts[r] + i for r in range(len(lens)) for i in range(news[r]) if lens[r] == 0 and t.bits[t.starts[r] + i] == 0]
+    assert len(few) > 0
+    assert out[few].isnan().all() and (lse[few] == math.inf).all()
+    assert (out[none] == 0).all() and (lse[none] == -math.inf).all()
+
+
 @pytest.mark.parametrize("dtype,size", [(BF16, 2.0 ** 10), (BF16, 2.0 ** 20), (BF16, 2.0 ** 28), (BF16, 2.0 ** 33), (BF16, 2.0 ** 60), (BF16, -2.0 ** 100),
                                         (FP16, 2.0 ** 15), (FP16, 2.0 ** 22), (FP16, -2.0 ** 22)])
 @pytest.mark.parametrize("lens,dim,group", [([150], 64, 1), ([150, 3, 70], 128, 4), ([120], 128, 40), ([90, 33], 256, 2), ([150], 72, 3)])

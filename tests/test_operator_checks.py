@@ -109,6 +109,14 @@ def test_attention_calls_that_are_refused(pool, other):
     assert code(ft.tree_attention, pool, cache(pool), call(**other)) == EINVAL
 
 
+def test_scales_that_powers_of_two_do_not_hold_are_refused(pool):
+    c = cache(pool)
+    for scale in (2.4e38, -3e38):
+        assert code(ft.tree_attention, pool, c, call(scale=scale)) == EINVAL
+        assert code(ft.tree_workspace, pool, c, call(scale=scale)) == EINVAL
+    assert code(ft.tree_workspace, pool, c, call(scale=-2.3e38)) != EINVAL
+
+
 def test_calls_of_more_workgroups_than_a_grid_holds_are_refused(pool):
     """The second launch has 256 threads for every request's key head, and a grid less than 2^32: refused before the first launch."""
     c = cache(pool)
