@@ -241,7 +241,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 template <class T>
 __device__ inline void add_up(const Adapt &p, const Tile &tile, const ft_adapter_record &rec, uint32_t rank, uint16_t *halves, uint32_t row_pitch, float *size) {
   // The parts of a row of H added up, 16 lanes to a row. Each is brought to between 1 and 2 by a power of two that multiplies the result, so that
-  // the range of 16 bits neither cuts large ones off nor takes digits from small ones. (Products with NaN and infinities remain what they are.)
+  // the range of 16 bits neither cuts large ones off nor takes digits from small ones. The high part is cut off, so that the low one has its sign, and
+  // is never zero beside it: an infinity of B has to meet two numbers of one sign, or would be NaN. (16 bits of a value, 22 in float16.)
   const uint32_t rows16 = (tile.count + 15) / 16 * 16;
   for (uint32_t i = threadIdx.x >> 4; i < rows16; i += 16) {
     const uint32_t q = threadIdx.x & 15, from = tile.first + (i < tile.count ? i : tile.count - 1);
@@ -275,9 +276,11 @@ __device__ inline void add_up(const Adapt &p, const Tile &tile, const ft_adapter
 #pragma unroll
       for (int x = 0; x < 4; x += 2) {
         const float a = v[k][x] * down, b = v[k][x + 1] * down;
-        hi[x / 2] = T::pack(a, b);
+        hi[x / 2] = T::pack_cut(a, b);
         const float ra = a - T::to_float((uint16_t)hi[x / 2]), rb = b - T::to_float((uint16_t)(hi[x / 2] >> 16));
-        lo[x / 2] = T::pack(fabsf(a) < INFINITY ? ra : 0, fabsf(b) < INFINITY ? rb : 0);
+        lo[x / 2] = T::pack(fabsf(a) == INFINITY ? 0 : ra, fabsf(b) == INFINITY ? 0 : rb);
+        if ((lo[x / 2] & 0x7fff) == 0 && a != 0) lo[x / 2] |= (hi[x / 2] & 0x8000) | T::kTiny;
+        if ((lo[x / 2] & 0x7fff0000) == 0 && b != 0) lo[x / 2] |= (hi[x / 2] & 0x80000000) | (uint32_t)T::kTiny << 16;
       }
       typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
       *reinterpret_cast<Words2 *>(&halves[i * row_pitch + r]) = Words2{hi[0], hi[1]};

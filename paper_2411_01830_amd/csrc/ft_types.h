@@ -36,6 +36,9 @@ struct Bf16 {
     typedef __bf16 V __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((F{lo, hi}), V));
   }
+  // towards zero (a NaN may become an infinity)
+  static __device__ uint32_t pack_cut(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302); }
+  static constexpr uint32_t kTiny = 0x0080;  // a number too small for any sum beside ones: here the smallest of full precision
   static constexpr uint32_t kExponent = 0x7f80, kLowest = 0x0080, kOne = 0x3f80;  // an exponent of all ones (infinite or NaN), its lowest bit
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef __bf16 V __attribute__((ext_vector_type(8)));
@@ -51,6 +54,8 @@ struct Fp16 {
     typedef _Float16 V __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((F{lo, hi}), V));
   }
+  static __device__ uint32_t pack_cut(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi)); }
+  static constexpr uint32_t kTiny = 0x0001;  // (2^-24)
   static constexpr uint32_t kExponent = 0x7c00, kLowest = 0x0400, kOne = 0x3c00;
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef _Float16 V __attribute__((ext_vector_type(8)));

@@ -713,6 +713,30 @@ def test_what_one_row_holds_does_not_reach_another():
     assert torch.equal(got[rows], want[rows])
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width_in", [(5, 64), (90, 300)])
+def test_infinities_of_a_factor_are_infinities_of_the_result(rows, width_in, dtype):
+    """An infinite element of B gives its column the sign of what it is multiplied with, be that a number of few bits or of many."""
+    a = Adapt([i % 3 for i in range(rows)], [16, 8, 40], width_in, 200, dtype)
+    a.gx[0].zero_()
+    a.gx[0, 3] = 2.0                                    # its product with A has as few bits as A's elements
+    want = a.call()
+    b = a.adapters.records.view(torch.int64).view(-1, 3)[0, 1].item() - a.m.mem.data_ptr()
+    factor = a.m.view(b, dtype, 200 * 16).view(200, 16)
+    for n, r, value in ((0, 5, math.inf), (63, 0, -math.inf), (64, 15, math.inf), (199, 7, math.inf)):
+        factor[n, r] = value
+    got = a.call()
+    for t in range(0, rows, 3):
+        h = a.gx[t].double().cpu() @ a.factors[0][0].t()
+        for n, r, value in ((0, 5, 1), (63, 0, -1), (64, 15, 1), (199, 7, 1)):
+            assert abs(float(h[r])) > 1e-6
+            assert float(got[t, n]) == math.copysign(math.inf, float(h[r]) * value), (t, n)
+    others = torch.ones(rows, 200, dtype=torch.bool, device="cuda")
+    for n in (0, 63, 64, 199):
+        others[::3, n] = False
+    assert torch.equal(got[others], want[others])
+
+
 def test_tensors_on_another_gpu_than_the_pool_are_refused():
     """A pool's handle that says it lies on the next GPU: each call is refused before its launch."""
     m = Memory(1 << 20)
