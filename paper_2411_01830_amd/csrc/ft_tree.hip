@@ -130,7 +130,8 @@ __device__ inline Request request(const A &a, uint32_t r) {
   return {s, n > (int)a.t.drafts ? (int)a.t.drafts : n, len};
 }
 
-__device__ inline uint32_t steps_of(const Request &q) { return (uint32_t)((q.len + (kStep - 1)) >> 5) + (uint32_t)((q.n + (kStep - 1)) >> 5); }
+__device__ inline uint32_t steps_for(int keys) { return ((uint32_t)keys + (kStep - 1)) >> 5; }  // (there may be 2^31 - 1 of them)
+__device__ inline uint32_t steps_of(const Request &q) { return steps_for(q.len) + steps_for(q.n); }
 
 // Work of a request: for each key head and each cluster's tiles of `rows` rows, which are a segment, what it costs to begin with and all of its
 // steps.
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
   for (;;) {
     const uint32_t cluster = argument()->cluster, heads = argument()->c.heads, group = argument()->group;
     const uint32_t steps = steps_of(q), tiles = ((uint32_t)q.n * group + ROWS - 1) / ROWS, cost = steps + kSegment;
-    const uint32_t cached = (uint32_t)((q.len + kStep - 1) >> 5);
+    const uint32_t cached = steps_for(q.len);
     const uint32_t groups = (tiles + cluster - 1) / cluster;
     const uint64_t segments = (uint64_t)heads * groups;
     uint64_t seg = quotient(at, cost);
@@ -728,7 +729,7 @@ template <class T, int DT, class A>
 __device__ __forceinline__ void add_left_out(const A &a, const Request &q, uint32_t r, uint32_t row, uint32_t head, uint32_t from, uint32_t to, Floats4 (&acc)[DT / 16]) {
   constexpr int E = DT / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4;
-  const uint32_t cached = (uint32_t)((q.len + (kStep - 1)) >> 5), whole = (uint32_t)q.len >> 5;
+  const uint32_t cached = steps_for(q.len), whole = (uint32_t)q.len >> 5;
   uint32_t token = divisor(a.by_group).of(row);
   token = token < (uint32_t)q.n ? token : (uint32_t)q.n - 1;
   for (uint32_t st = (from < whole ? whole : from) + (threadIdx.x >> 6); st <= to; st += 4) {

@@ -590,6 +590,20 @@ def test_as_many_drafted_rows_as_there_may_be(dim):
     assert torch.equal(got[:3], want) and (got[3:] == 7).all()
 
 
+def test_the_longest_cache():
+    """2^31 - 1 cached tokens, half of them twice, as a table may name a page more than once: their number goes beyond 31 bits when it is rounded up."""
+    page, dim = 1 << 30, 8
+    m = Memory(2 * (2 * page * dim) + 4 * SLAB, fill=None)
+    at = [m.alloc(2 * page * dim), m.alloc(2 * page * dim)]
+    cache = ops().KvCache(m.pool, at[0], at[1], 1, page, 1, dim, BF16)
+    m.view(at[0], BF16, page * dim).fill_(0.5)
+    m.view(at[1], BF16, page * dim).fill_(3.0)
+    q, kv = torch.zeros(2, 1, dim, dtype=BF16, device="cuda"), torch.full((2, 1, dim), 3.0, dtype=BF16, device="cuda")
+    out, lse = ops().tree_attention(cache, q, kv, kv, gpu([0, 1, 2]), gpu([2 ** 31 - 1, 31]), gpu([[0, 0], [0, 0]]), 1, lse=True)
+    assert (out == 3).all()                              # all weights are one, and whole numbers of them are exact
+    assert (lse.cpu() - torch.tensor([[31 * math.log(2)], [5 * math.log(2)]])).abs().max() < 2.0 ** -18
+
+
 def test_lengths_and_tables_that_are_wrong_stay_inside_the_cache():
     t = Tree(lens=[100, 40, 30], news=[3, 4, 5], heads=2, group=2, dim=64, page=16, dtype=BF16)
     want, _ = t.call()
