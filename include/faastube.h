@@ -834,7 +834,7 @@ typedef struct ft_adapters_call {
   const void *groups;               /* of ft_adapters_group for the same rows and count */
   const void *x;                    /* rows x width_in */
   const void *base;                 /* rows x width_out: the shared projection's result, or NULL: 0 */
-  void *out;                        /* rows x width_out; may be base itself */
+  void *out;                        /* rows x width_out; may be base itself, with its stride */
   uint64_t x_stride, base_stride, out_stride; /* of a row: >= its width, < 2^40 */
   uint32_t rows, count, type;       /* rows / 64 + count < 2^24 */
   uint32_t width_in, width_out;

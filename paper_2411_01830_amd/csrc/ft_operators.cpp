@@ -252,6 +252,7 @@ int ft_adapters_apply(ft_pool *p, const ft_adapters_call *call, void *hip_stream
   if (!there(a.records, 8) || !there(a.groups, 16) || !there(a.x, 2) || !aligned(a.base, 2) || !there(a.out, 2)) return FT_EINVAL;
   if (a.x_stride < a.width_in || a.out_stride < a.width_out || (a.base != nullptr && a.base_stride < a.width_out)) return FT_EINVAL;
   if (!good_strides({a.x_stride, a.out_stride, a.base_stride})) return FT_EINVAL;
+  if (a.out == a.base && a.out_stride != a.base_stride && a.rows > 1) return FT_EINVAL;  // a row's result would be another's base
   const uint64_t need = adapter_workspace(a);
   if (need != 0 && (!there(a.workspace, 16) || a.workspace_bytes < need)) return FT_EINVAL;
   std::lock_guard<std::mutex> lock(p->mu);

@@ -215,6 +215,12 @@ def test_adapter_calls_that_are_refused(pool, other):
     assert code(ft.adapters_apply, pool, adapters_call(**{"workspace_bytes": 1 << 40, **other})) == EINVAL
 
 
+def test_adapters_in_place_with_another_stride_are_refused(pool):
+    """A row's result would lie where another row's base is still to be read."""
+    for other in (dict(out_stride=264), dict(base_stride=300)):
+        assert code(ft.adapters_apply, pool, adapters_call(workspace_bytes=1 << 40, **other)) == EINVAL, other
+
+
 def test_groups_that_are_refused(pool):
     need = ft.adapters_group_bytes(100, 4)
     assert need >= 400
