@@ -11,9 +11,6 @@ typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 struct __attribute__((packed, aligned(2))) Loose4 {
   uint32_t w[4];
 };
-struct __attribute__((packed, aligned(2))) Loose2 {
-  uint32_t w[2];
-};
 
 // Global memory said to be that: a pointer that has been through an empty asm statement would be taken for one to anything.
 typedef const __attribute__((address_space(1))) char *Global;
@@ -39,7 +36,7 @@ struct Bf16 {
   // towards zero (a NaN may become an infinity)
   static __device__ uint32_t pack_cut(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302); }
   static constexpr uint32_t kTiny = 0x0080;  // a number too small for any sum beside ones: here the smallest of full precision
-  static constexpr uint32_t kExponent = 0x7f80, kLowest = 0x0080, kOne = 0x3f80;  // an exponent of all ones (infinite or NaN), its lowest bit
+  static constexpr uint32_t kExponent = 0x7f80, kLowest = 0x0080;  // an exponent of all ones (infinite or NaN), its lowest bit
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef __bf16 V __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
@@ -56,7 +53,7 @@ struct Fp16 {
   }
   static __device__ uint32_t pack_cut(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi)); }
   static constexpr uint32_t kTiny = 0x0001;  // (2^-24)
-  static constexpr uint32_t kExponent = 0x7c00, kLowest = 0x0400, kOne = 0x3c00;
+  static constexpr uint32_t kExponent = 0x7c00, kLowest = 0x0400;
   static __device__ Floats4 mfma(Words4 a, Words4 b, Floats4 c) {
     typedef _Float16 V __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
