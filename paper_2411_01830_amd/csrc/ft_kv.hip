@@ -15,11 +15,13 @@ struct Sums {
   uint64_t pages, items;  // (requests whose rows overlap, as starts that descend make them, have more of either than 32 bits count)
 };
 
-__device__ inline Sums scan(uint64_t pages, uint64_t items, Sums *before, Sums *lds) {
+__device__ inline Sums scan(uint64_t pages, uint32_t items, Sums *before, Sums *lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t p = pages, i = items;
+  uint64_t p = pages;
+  uint32_t i = items;  // at most 2^25 a thread, so those of a wavefront have room
   for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t q = __shfl_up(p, d), j = __shfl_up(i, d);
+    const uint64_t q = __shfl_up(p, d);
+    const uint32_t j = __shfl_up(i, d);
     if (lane >= d) {
       p += q;
       i += j;
