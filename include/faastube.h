@@ -773,7 +773,8 @@ typedef struct ft_tree_call {
   uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
   uint64_t v_token_stride, v_head_stride, out_token_stride, out_head_stride;
   uint32_t requests, tokens;
-  uint32_t drafts;       /* the most drafted tokens of one request; those beyond are not answered. Times heads per key head: < 2^20 */
+  uint32_t drafts;       /* the most drafted tokens of one request; those beyond are not answered. Times heads per key head: < 2^20. The launch
+                            is made for requests of that many: a long piece and single tokens are faster as two calls */
   uint32_t heads;        /* query heads, a multiple of the cache's: head h reads key head h / (heads / cache heads) */
   uint32_t blocks;
   uint32_t mask_words;   /* 64 * mask_words >= drafts where there is a mask */

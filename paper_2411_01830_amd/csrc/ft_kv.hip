@@ -65,7 +65,7 @@ struct GrowLds {
 
 // A prefix sum over the requests of the pages that they lack, then 64 rows to a wavefront. Every workgroup does the whole sum for
 // itself, which costs it a few microseconds of reads from the caches and saves a second launch; the rows are shared out. Latency bounds it:
-// lengths, flags, two barriers of the sum, table, slot, each waited for. 7.5 us for 64 trees of 16 with flags, 6.5 for 256 prompts
+// lengths, flags, two barriers of the sum, table, slot, each waited for. 7.6 us for 64 trees of 16 with flags, 6.7 for 256 prompts
 // of up to 512 rows.
 __global__ __launch_bounds__(kThreads) void ft_kv_grow_kernel(ft_kv_tables t, Divisor page, const int32_t *__restrict__ starts,
                                                               const uint8_t *__restrict__ keep, uint32_t tokens, int64_t *__restrict__ slots,
@@ -185,7 +185,7 @@ struct ReleaseLds {
   uint32_t count[kThreads];
 };
 
-// The same sum over the pages of the requests that are done, and their entries to the stack, 64 to a wavefront: 6 us for 64 of 256 requests of up to
+// The same sum over the pages of the requests that are done, and their entries to the stack, 64 to a wavefront: 6.2 us for 64 of 256 requests of up to
 // 4096 tokens, of which the launch and four dependent reads are nearly all.
 __global__ __launch_bounds__(kThreads) void ft_kv_release_kernel(ft_kv_tables t, Divisor page, const uint8_t *__restrict__ done,
                                                                  int32_t *__restrict__ lens_out, int32_t *__restrict__ state_out) {

@@ -16,7 +16,7 @@
 //   one request, 2000 tokens of 8 key heads, a token          17.5 us: latency, 10 us until the first product is under way, and 5 of the join
 //   64 requests of 16 to 8192, a token, 276 MB                70 us, 3.9 TB/s: the same at either end, the reads between (50 us if they were still in cache)
 //   32 of 256 to 4096, trees of 9 to 16 under 4 heads, 175 MB 57 us, 3.1 TB/s
-//   4 of 20000 to 32768, trees of 64 under 8 heads, 232 GFLOP 274 to 290 us, 800 TFLOP/s: vector instructions, 150 a step of 32 MFMA and 32 rows, which
+//   4 of 20000 to 32768, trees of 64 under 8 heads, 232 GFLOP 282 to 290 us, 810 TFLOP/s: vector instructions, 150 a step of 32 MFMA and 32 rows, which
 //     take turns with the matrix unit: of what a step takes, products are a third, reads from shared memory an eighth, exponents a tenth
 #include <hip/hip_runtime.h>
 
@@ -29,7 +29,8 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;     // keys
-// What a segment costs beside its steps, in steps, when they are dealt out (64 requests of 16 to 8192 tokens: 70 us, 75 with 2, 70 with 4, 71 with 6).
+// What a segment costs beside its steps, in steps, when they are dealt out. 64 requests of 16 to 8192 tokens: 81.5 us, 85.5 with 2, 81 with 4, 82.5 with 6;
+// 256 of 16 to 2000: 110, 117.5, 107.5, 110; 24 of 16 to 3000, 9 rows of 64 elements: 26, 28, 24.5, 24; 5 of 16 to 400: 14.6, 14.2, 15.1, 16.5.
 constexpr uint32_t kSegment = 3;
 // How far, in powers of two, a score may pass the maximum that weights are relative to before sums are brought to a new one: weights
 // stay below 2^8 and sums of them far from the end of any range, and most steps have no maximum to agree on over the lanes.
@@ -553,6 +554,8 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
 #pragma unroll
           for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
           l[nr] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+          // rounded to the matrix unit's 16 bits for the product with the values; the sum has them as they were. Against 64 bits results are off by 0.0022 of their
+          // size in bfloat16 and 0.00025 in float16, with weights of 32 bits by 0.0017 and 0.0002: most of it is the result's own rounding.
           p[nr] = Words4{T::pack(w[0], w[1]), T::pack(w[2], w[3]), T::pack(w[4], w[5]), T::pack(w[6], w[7])};
         }
       };
@@ -642,7 +645,7 @@ __global__ __launch_bounds__(64 * WR) __attribute__((amdgpu_waves_per_eu(waves(D
         } while (more);
       } else {
         // The step that is worked on lies in one half of shared memory, the next one is put into the other half, those behind it are on their way
-        // in registers. One barrier a step: it says that the half to work on is full, and that the other one has been read.
+        // in registers. (Not all of the time: as it is compiled the first `put` of every DEPTH steps waits for all loads, the last one's too.) One barrier a step: it says that the half to work on is full, and that the other one has been read.
         const bool works = NR > 1 || row0 < (uint32_t)q.n * group;  // wavefronts without rows of their own bring theirs and wait
         Words4 k[DEPTH][N], v[DEPTH][N];
         uint32_t asked = st;  // the step that `ids` are the pages of
@@ -959,7 +962,7 @@ hipError_t launch_tree(const KvView &c, const ft_tree_call &t, int cu_count, hip
   a.workers = workers_of(s, cu_count);
   a.group = t.heads / c.heads;
   a.by_group = Divisor(a.group);
-  a.least = kSegment + 1;  // (17 requests of up to 1500 tokens: 16.3 us, with a step more 17.9, with four 19.3)
+  a.least = kSegment + 1;  // (17 requests of up to 1500 tokens: 16.3 us, with a step more 17.9, with four 19.3; 5 of up to 400 14.6, with three more 16.7)
   // Scores are scaled within the exponent's argument, so a scale of 0 must not make NaN of what is masked: the smallest number there is
   // does the same. Queries change their signs for one below 0, as the largest product is to be the largest score.
   a.scale = fabsf(t.scale * kLog2e);

@@ -133,7 +133,8 @@ def tree_attention(cache, q, k, v, starts, lens, table, drafts, mask=None, scale
 
     q: tokens x heads x dim; k, v: tokens x the cache's heads x dim. drafts: the most drafted tokens of one request. mask: int64 or
     uint64, a word of 64 bits a token, or several as a second dimension. scale: dim ** -0.5 by default. With lse also
-    log(sum(exp)) of every row, in 32 bits."""
+    log(sum(exp)) of every row, in 32 bits. Rows of no request (a padded step has them) and those beyond `drafts` are not written: in `out` they
+    stay as they were, in results that are made here they hold anything."""
     dev = _device("q", q, cache.pool)
     if q.dim() != 3:
         _refuse("q has three dimensions")
@@ -193,7 +194,8 @@ class Adapters:
 
 
 class AdapterGroups:
-    """The rows of a step in the order of their adapters; for any projection of the same adapters."""
+    """The rows of a step in the order of their adapters; for any projection of the same adapters. `memory` is of the stream that they were
+    made on: another stream's calls wait for it, and memory.record_stream says so, as for any tensor."""
 
     def __init__(self, rows, count, memory):
         self.rows, self.count, self.memory = rows, count, memory

@@ -205,7 +205,7 @@ class Server:
                     mine = mine[keep[mine]]
                     new = torch.stack([kept[layer][0][mine], kept[layer][1][mine]]).float()
                     self.history[layer][r] = torch.cat([self.history[layer][r], new], dim=1)
-        got = (lens - self.lens).cpu().numpy()                        # (the one wait of a step)
+        got = (lens - self.lens).cpu().numpy()                        # (a wait; choosing by flags, above, is another)
         self.lens = lens
         self.left -= got
         over = self.left <= 0
