@@ -697,7 +697,8 @@ int ft_plain_fill(void *dst, uint64_t bytes, uint32_t word, uint32_t workgroups,
  * contiguous; no alignment beyond an element's is needed. What a call finds wrong with its arguments is
  * FT_EINVAL, a cache or an adapter that is not inside one live allocation FT_ERANGE, and then nothing is
  * launched. Lengths, tables, masks and the like lie in device memory, where no call can look at them:
- * whatever they hold, no kernel leaves the tensors it was given.
+ * whatever they hold, no kernel leaves the tensors it was given. (An adapter call's records and groups are the library's own
+ * writing and have to be that.) What a call writes may overlap nothing else that it is given, but where it says so.
  */
 
 /* element types of tensors */
