@@ -702,7 +702,7 @@ int ft_plain_fill(void *dst, uint64_t bytes, uint32_t word, uint32_t workgroups,
  */
 
 /* element types of tensors */
-enum { FT_BF16 = 0, FT_FP16 = 1 };
+enum { FT_BF16 = 0, FT_FP16 = 1, FT_FP32 = 2 /* of probabilities alone */ };
 
 /* Keys and values of `pages` pages of page_tokens tokens: element (page, token, head, d) of either lies at
  * page * page_stride + token * token_stride + head * head_stride + d behind the pool offset k or v. A token's
@@ -852,6 +852,113 @@ typedef struct ft_adapters_call {
  */
 int ft_adapters_apply(ft_pool *p, const ft_adapters_call *call, void *hip_stream);
 int ft_adapters_workspace(ft_pool *p, const ft_adapters_call *call, uint64_t *bytes_out);
+
+/* A projection's weights in the pool, in 4 bits: row n of width_out has the codes of its width_in elements two to a byte, element k in the low
+ * half of byte k / 2 where k is even, in its high half where it is odd, (width_in + 1) / 2 bytes a row without gaps. Groups of `group`
+ * neighbouring elements of a row (the last one may be shorter) have a scale and a zero in common: width_out x G of either, without gaps,
+ * where G = ceil(width_in / group). Element k of row n is scales[n][k / group] * (code - zeros[n][k / group]). */
+typedef struct ft_linear4 {
+  ft_off_t weights;
+  ft_off_t scales;     /* of `type`; a multiple of 2 */
+  ft_off_t zeros;      /* a byte each, or FT_NO_ZEROS: 8 everywhere */
+  uint32_t type;       /* FT_BF16 or FT_FP16: of the scales, of x, base and out */
+  uint32_t width_in, width_out; /* 1 .. 2^24 - 1 */
+  uint32_t group;      /* 8 or more, a multiple of 8 */
+} ft_linear4;          /* 40 bytes */
+#define FT_NO_ZEROS (~(ft_off_t)0)
+
+/* Arguments of ft_linear4_apply: device pointers but for the numbers. */
+typedef struct ft_linear4_call {
+  const void *x;       /* rows x width_in */
+  const void *base;    /* rows x width_out, or NULL: 0 */
+  void *out;           /* rows x width_out; may be base itself, with its stride */
+  uint64_t x_stride, base_stride, out_stride; /* of a row: >= its width, < 2^40 */
+  uint32_t rows;       /* < 2^20 */
+  uint32_t _pad;       /* ignored */
+  void *workspace;     /* ft_linear4_workspace bytes, 16-byte aligned, as for ft_tree_attention */
+  uint64_t workspace_bytes;
+} ft_linear4_call;     /* 72 bytes */
+
+/*
+ * Products of few rows - the tokens of a step - with weights of 4 bits:
+ *   out[t][n] = base[t][n] + sum over k of x[t][k] * scales[n][k / group] * (code[n][k] - zeros[n][k / group])
+ * Products are exact, sums 32 bits, the result is rounded once. The call reads the weights once for every 64 rows: for hundreds of rows
+ * a product with weights that were unpacked before is faster. FT_ERANGE where weights, scales or zeros are not inside one live allocation each.
+ */
+int ft_linear4_apply(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, void *hip_stream);
+/* Bytes of workspace that ft_linear4_apply asks for (host only; of the call its number of rows is read). */
+int ft_linear4_workspace(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, uint64_t *bytes_out);
+
+/* Arguments of ft_rotate_heads: device pointers but for the numbers. */
+typedef struct ft_rotate_call {
+  const void *q, *k;              /* tokens x heads x dim, tokens x kv_heads x dim; of no heads NULL will do */
+  void *q_out, *k_out;            /* the same; may be q and k themselves, with their strides */
+  const void *q_weight, *k_weight; /* dim elements, or NULL: ones (with FT_ROTATE_NORM; not read without) */
+  const int32_t *positions;       /* tokens x axes */
+  const float *freqs;             /* rot / 2 entries: the angle of a pair, in radians, at position 1 */
+  const uint8_t *axis;            /* rot / 2 entries: whose position turns a pair, entries >= axes the last one's; NULL: axis 0 */
+  uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  uint64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride; /* < 2^40; of outputs >= dim where there are several */
+  uint32_t tokens;                /* < 2^31; times heads and kv_heads together: < 2^32 */
+  uint32_t heads, kv_heads;       /* <= 65536 */
+  uint32_t dim;                   /* a multiple of 8, at most 256 */
+  uint32_t rot;                   /* elements of a head that are turned, the first ones: even, 0 .. dim */
+  uint32_t axes;                  /* 1 .. 256 */
+  uint32_t type, flags;           /* FT_BF16 or FT_FP16; FT_ROTATE_* */
+  float eps;                      /* with FT_ROTATE_NORM: finite, >= 0 */
+  uint32_t _pad;                  /* ignored */
+} ft_rotate_call;                 /* 176 bytes */
+enum {
+  FT_ROTATE_NORM = 1,       /* heads are divided by the root of the mean of their squares, plus eps, and multiplied by the weights, before */
+  FT_ROTATE_NEIGHBOURS = 2  /* pairs are the elements 2i and 2i + 1; without it i and i + rot / 2 */
+};
+
+/*
+ * The norm of every head's query and key, where it is asked for, and the rotation of their pairs by the token's position:
+ *   y = x * rsqrt(mean of x^2 over dim + eps) * weight
+ *   (y'[a], y'[b]) = (y[a] cos - y[b] sin, y[a] sin + y[b] cos) of the angle positions[t][axis[i]] * freqs[i] of pair i = (a, b)
+ * Elements behind the first `rot` are not turned. Angles are worked out in 64 bits (positions may be negative, and as far
+ * as 2^31), all else in 32; the result is rounded once. Rows whose squares 32 bits do not hold become 0, those with
+ * infinities or NaN become NaN in part or whole, other rows are not touched by them.
+ */
+int ft_rotate_heads(ft_pool *p, const ft_rotate_call *call, void *hip_stream);
+
+/* Arguments of ft_tree_verify: device pointers but for the numbers. */
+typedef struct ft_verify_call {
+  const int64_t *tokens;   /* rows: the token of each */
+  const int32_t *starts;   /* requests + 1 entries that do not descend: rows [starts[r], starts[r + 1]) are request r's */
+  const int32_t *parent;   /* rows: which of its request's rows a row hangs from, one before it; others hang from none. NULL: from the row before */
+  const void *target;      /* rows x vocab: what the model gives to each token behind a row */
+  const void *draft;       /* rows x vocab: what the tokens of the rows that hang from a row were drawn by. NULL: they were not drawn */
+  const float *accept;     /* rows: a random number from [0, 1) for each row's test; that of a request's first row is not used */
+  const float *pick;       /* requests: a random number from [0, 1) for the token behind those that stand */
+  uint8_t *keep;           /* rows: 1 where a row stands, 0 elsewhere (as ft_kv_grow reads it) */
+  int32_t *last;           /* requests: the last row that stands, -1 of a request without rows */
+  int64_t *token;          /* requests: the token behind it, -1 of a request without rows, or where its row of target has nothing above 0 */
+  uint64_t target_stride, draft_stride; /* of a row: >= vocab, < 2^40 */
+  uint32_t rows, requests; /* rows < 2^31, requests < 2^24 - 1 */
+  uint32_t drafts;         /* the most rows of one request; those beyond are taken for no row's. At most 1024, or as many as there are rows */
+  uint32_t vocab;          /* 1 .. 2^22 */
+  uint32_t type;           /* of target and draft: FT_BF16, FT_FP16 or FT_FP32 */
+  uint32_t _pad;           /* ignored */
+  void *workspace;         /* ft_verify_workspace bytes, 16-byte aligned, as for ft_tree_attention */
+  uint64_t workspace_bytes;
+} ft_verify_call;          /* 136 bytes */
+
+/*
+ * Judges the drafted tokens of all requests, so that what is kept and the token behind it are distributed as the target says. The first row of a
+ * request is known and stands. From a row that stands, with p and q its rows of target and draft, those that hang from it are tested
+ * in ascending order until one stands, with A = 0 and T = 1 at first:
+ *   drawn      row c stands if accept[c] * T * q[token c] < max(p[token c] - A q[token c], 0); otherwise A += T, then T = the sum of max(p - A q, 0)
+ *   not drawn  row c stands if accept[c] * T < p[token c], which is 0 if it fell before; otherwise T -= p[token c] (not below 0)
+ * Behind the last one that stands the token is the first one with which the sum over what is left (max(p - A q, 0); p without the tokens that
+ * fell) exceeds pick times all of it; if nothing is left, over p; if none exceeds it, the last token of which something is left.
+ * Rows of probabilities are taken as they are, as if their sum were 1; what is negative or not finite counts as 0, as does the probability of a
+ * token outside [0, vocab). Sums and comparisons are 64 bits.
+ * Several rows that were drawn behind one row are independent draws; they may be alike.
+ */
+int ft_tree_verify(ft_pool *p, const ft_verify_call *call, void *hip_stream);
+int ft_verify_workspace(ft_pool *p, const ft_verify_call *call, uint64_t *bytes_out);
 
 const char *ft_strerror(int rc);
 /* Text of the last failing HIP call on this pool ("" if none). */

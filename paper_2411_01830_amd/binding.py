@@ -22,7 +22,8 @@ EXPORTS = ["ft_pool_create", "ft_pool_grow", "ft_pool_shrink", "ft_pool_usage", 
            "ft_job_stats", "ft_job_schedule", "ft_job_log", "ft_job_log_jobs", "ft_job_progress", "ft_job_log_workgroups", "ft_job_log_units", "ft_set_tuning", "ft_plan_schedule", "ft_plan_tickets",
            "ft_plain_copy", "ft_plain_read", "ft_plain_fill", "ft_strerror", "ft_last_hip_error",
            "ft_kv_grow", "ft_kv_release", "ft_kv_append", "ft_tree_attention", "ft_tree_workspace",
-           "ft_adapters_resolve", "ft_adapters_group_bytes", "ft_adapters_group", "ft_adapters_apply", "ft_adapters_workspace"]
+           "ft_adapters_resolve", "ft_adapters_group_bytes", "ft_adapters_group", "ft_adapters_apply", "ft_adapters_workspace",
+           "ft_linear4_apply", "ft_linear4_workspace", "ft_rotate_heads", "ft_tree_verify", "ft_verify_workspace"]
 
 
 class FtError(Exception):
@@ -75,6 +76,35 @@ class AdaptersCall(C.Structure):
                [(n, C.c_uint64) for n in ("x_stride", "base_stride", "out_stride")] + \
                [(n, C.c_uint32) for n in ("rows", "count", "type", "width_in", "width_out", "max_rank")] + \
                [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class Linear4Record(C.Structure):
+    _fields_ = [("weights", C.c_uint64), ("scales", C.c_uint64), ("zeros", C.c_uint64)] + \
+               [(n, C.c_uint32) for n in ("type", "width_in", "width_out", "group")]
+
+
+class Linear4Call(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "base", "out")] + [(n, C.c_uint64) for n in ("x_stride", "base_stride", "out_stride")] + \
+               [("rows", C.c_uint32), ("_pad", C.c_uint32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class RotateCall(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "positions", "freqs", "axis")] + \
+               [(n, C.c_uint64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                          "q_out_token_stride", "q_out_head_stride", "k_out_token_stride", "k_out_head_stride")] + \
+               [(n, C.c_uint32) for n in ("tokens", "heads", "kv_heads", "dim", "rot", "axes", "type", "flags")] + \
+               [("eps", C.c_float), ("_pad", C.c_uint32)]
+
+
+class VerifyCall(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("tokens", "starts", "parent", "target", "draft", "accept", "pick", "keep", "last", "token")] + \
+               [(n, C.c_uint64) for n in ("target_stride", "draft_stride")] + \
+               [(n, C.c_uint32) for n in ("rows", "requests", "drafts", "vocab", "type", "_pad")] + \
+               [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+NO_ZEROS = (1 << 64) - 1
+ROTATE_NORM, ROTATE_NEIGHBOURS = 1, 2
 
 
 def _load():
@@ -156,6 +186,11 @@ def _load():
         "ft_adapters_group": (i32, [vp, vp, u32, u32, vp, u64, vp]),
         "ft_adapters_apply": (i32, [vp, vp, vp]),
         "ft_adapters_workspace": (i32, [vp, vp, P(u64)]),
+        "ft_linear4_apply": (i32, [vp, vp, vp, vp]),
+        "ft_linear4_workspace": (i32, [vp, vp, vp, P(u64)]),
+        "ft_rotate_heads": (i32, [vp, vp, vp]),
+        "ft_tree_verify": (i32, [vp, vp, vp]),
+        "ft_verify_workspace": (i32, [vp, vp, P(u64)]),
         "ft_strerror": (C.c_char_p, [i32]),
         "ft_last_hip_error": (C.c_char_p, [vp]),
     }
@@ -638,3 +673,27 @@ def adapters_workspace(pool, call):
 
 def adapters_apply(pool, call, stream=0):
     _check(_lib.ft_adapters_apply(pool, C.byref(call), stream), pool)
+
+
+def linear4_workspace(pool, weights, call):
+    n = C.c_uint64()
+    _check(_lib.ft_linear4_workspace(pool, C.byref(weights), C.byref(call), C.byref(n)), pool)
+    return n.value
+
+
+def linear4_apply(pool, weights, call, stream=0):
+    _check(_lib.ft_linear4_apply(pool, C.byref(weights), C.byref(call), stream), pool)
+
+
+def rotate_heads(pool, call, stream=0):
+    _check(_lib.ft_rotate_heads(pool, C.byref(call), stream), pool)
+
+
+def verify_workspace(pool, call):
+    n = C.c_uint64()
+    _check(_lib.ft_verify_workspace(pool, C.byref(call), C.byref(n)), pool)
+    return n.value
+
+
+def tree_verify(pool, call, stream=0):
+    _check(_lib.ft_tree_verify(pool, C.byref(call), stream), pool)

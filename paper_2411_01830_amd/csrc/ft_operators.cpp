@@ -109,6 +109,55 @@ bool good_numbers(const ft_adapters_call &a) {
   return a.max_rank >= 1 && a.max_rank <= 256;
 }
 
+bool good_numbers(const ft_linear4 &w) {
+  if (w.type > FT_FP16 || w.width_in == 0 || w.width_out == 0 || w.width_in >= 1u << 24 || w.width_out >= 1u << 24) return false;
+  return w.group != 0 && w.group % 8 == 0 && w.group < 1u << 31 && w.scales % 2 == 0;
+}
+
+// Called with the pool's mutex held.
+int resolve_linear4(ft_pool *p, const ft_linear4 &w, Linear4View *out) {
+  const uint32_t groups = (w.width_in + w.group - 1) / w.group, row = (w.width_in + 1) / 2;
+  const uint64_t scales = (uint64_t)w.width_out * groups;
+  out->weights = reinterpret_cast<const uint8_t *>(resolve(p, w.weights, (uint64_t)w.width_out * row));
+  out->scales = reinterpret_cast<const uint16_t *>(resolve(p, w.scales, 2 * scales));
+  out->zeros = w.zeros == FT_NO_ZEROS ? nullptr : reinterpret_cast<const uint8_t *>(resolve(p, w.zeros, scales));
+  if (out->weights == nullptr || out->scales == nullptr || (w.zeros != FT_NO_ZEROS && out->zeros == nullptr)) return FT_ERANGE;
+  out->type = w.type;
+  out->width_in = w.width_in;
+  out->width_out = w.width_out;
+  out->groups = groups;
+  out->row_bytes = row;
+  out->group = Divisor(w.group);
+  return FT_OK;
+}
+
+// A side of a rotation: queries or keys, and what becomes of them.
+bool good_side(const ft_rotate_call &r, const void *in, void *out, uint32_t heads, uint64_t in_token, uint64_t in_head, uint64_t out_token,
+               uint64_t out_head) {
+  if (heads == 0) return true;
+  if (heads > 1u << 16 || !there(in, 2) || !there(out, 2) || !good_strides({in_token, in_head, out_token, out_head})) return false;
+  const bool tokens = r.tokens > 1, several = heads > 1;
+  if ((tokens && out_token < r.dim) || (several && out_head < r.dim)) return false;
+  // in place a head's result would lie where another one is still to be read
+  return in != out || ((!tokens || in_token == out_token) && (!several || in_head == out_head));
+}
+
+bool good_call(const ft_rotate_call &r) {
+  if (r.type > FT_FP16 || r.flags > (FT_ROTATE_NORM | FT_ROTATE_NEIGHBOURS) || r.dim == 0 || r.dim > 256 || r.dim % 8 != 0) return false;
+  if (r.rot > r.dim || r.rot % 2 != 0 || r.axes == 0 || r.axes > 256 || r.tokens >= 1u << 31) return false;
+  if ((uint64_t)r.tokens * ((uint64_t)r.heads + r.kv_heads) >= 1ull << 32) return false;
+  if ((r.flags & FT_ROTATE_NORM) != 0 && (!std::isfinite(r.eps) || r.eps < 0 || !aligned(r.q_weight, 2) || !aligned(r.k_weight, 2))) return false;
+  if (r.tokens == 0) return true;
+  if (r.rot != 0 && (!there(r.positions, 4) || !there(r.freqs, 4))) return false;
+  return good_side(r, r.q, r.q_out, r.heads, r.q_token_stride, r.q_head_stride, r.q_out_token_stride, r.q_out_head_stride) &&
+         good_side(r, r.k, r.k_out, r.kv_heads, r.k_token_stride, r.k_head_stride, r.k_out_token_stride, r.k_out_head_stride);
+}
+
+bool good_numbers(const ft_verify_call &v) {
+  if (v.type > FT_FP32 || v.vocab == 0 || v.vocab > 1u << 22 || v.rows >= 1u << 31 || v.requests + 1ull >= kMostWorkgroups || v.drafts == 0) return false;
+  return (v.drafts < v.rows ? v.drafts : v.rows) <= kMostVerifyRows;
+}
+
 }  // namespace
 
 extern "C" {
@@ -258,6 +307,93 @@ int ft_adapters_apply(ft_pool *p, const ft_adapters_call *call, void *hip_stream
   std::lock_guard<std::mutex> lock(p->mu);
   DeviceGuard guard(p->device);
   FT_HIP(p, launch_adapters(a, static_cast<hipStream_t>(hip_stream)));
+  return FT_OK;
+}
+FT_CATCH_ALL
+
+int ft_linear4_workspace(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, uint64_t *bytes_out) try {
+  if (p == nullptr || w == nullptr || call == nullptr || bytes_out == nullptr || !good_numbers(*w) || call->rows >= 1u << 20) return FT_EINVAL;
+  if (call->rows == 0) {
+    *bytes_out = 0;
+    return FT_OK;
+  }
+  std::lock_guard<std::mutex> lock(p->mu);
+  int cu_count = 0;
+  const int rc = compute_units(p, &cu_count);
+  if (rc != FT_OK) return rc;
+  *bytes_out = linear4_workspace(*w, call->rows, cu_count);
+  return FT_OK;
+}
+FT_CATCH_ALL
+
+int ft_linear4_apply(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, void *hip_stream) try {
+  if (p == nullptr || w == nullptr || call == nullptr || !good_numbers(*w) || call->rows >= 1u << 20) return FT_EINVAL;
+  const ft_linear4_call &c = *call;
+  if (c.rows != 0) {
+    if (!there(c.x, 2) || !aligned(c.base, 2) || !there(c.out, 2)) return FT_EINVAL;
+    if (c.x_stride < w->width_in || c.out_stride < w->width_out || (c.base != nullptr && c.base_stride < w->width_out)) return FT_EINVAL;
+    if (!good_strides({c.x_stride, c.out_stride, c.base_stride})) return FT_EINVAL;
+    if (c.out == c.base && c.out_stride != c.base_stride && c.rows > 1) return FT_EINVAL;  // a row's result would be another's base
+  }
+  std::lock_guard<std::mutex> lock(p->mu);
+  Linear4View view;
+  int rc = resolve_linear4(p, *w, &view);
+  if (rc != FT_OK || c.rows == 0) return rc;
+  int cu_count = 0;
+  rc = compute_units(p, &cu_count);
+  if (rc != FT_OK) return rc;
+  const uint64_t need = linear4_workspace(*w, c.rows, cu_count);
+  if (need != 0 && (!there(c.workspace, 16) || c.workspace_bytes < need)) return FT_EINVAL;
+  DeviceGuard guard(p->device);
+  FT_HIP(p, launch_linear4(view, c, cu_count, static_cast<hipStream_t>(hip_stream)));
+  return FT_OK;
+}
+FT_CATCH_ALL
+
+int ft_rotate_heads(ft_pool *p, const ft_rotate_call *call, void *hip_stream) try {
+  if (p == nullptr || call == nullptr || !good_call(*call)) return FT_EINVAL;
+  if (call->tokens == 0 || call->heads + call->kv_heads == 0) return FT_OK;
+  std::lock_guard<std::mutex> lock(p->mu);
+  DeviceGuard guard(p->device);
+  FT_HIP(p, launch_rotate(*call, static_cast<hipStream_t>(hip_stream)));
+  return FT_OK;
+}
+FT_CATCH_ALL
+
+int ft_verify_workspace(ft_pool *p, const ft_verify_call *call, uint64_t *bytes_out) try {
+  if (p == nullptr || call == nullptr || bytes_out == nullptr || !good_numbers(*call)) return FT_EINVAL;
+  if (call->requests == 0) {
+    *bytes_out = 0;
+    return FT_OK;
+  }
+  std::lock_guard<std::mutex> lock(p->mu);
+  int cu_count = 0;
+  const int rc = compute_units(p, &cu_count);
+  if (rc != FT_OK) return rc;
+  *bytes_out = verify_workspace(*call, cu_count);
+  return FT_OK;
+}
+FT_CATCH_ALL
+
+int ft_tree_verify(ft_pool *p, const ft_verify_call *call, void *hip_stream) try {
+  if (p == nullptr || call == nullptr || !good_numbers(*call)) return FT_EINVAL;
+  const ft_verify_call &v = *call;
+  if (v.rows == 0 && v.requests == 0) return FT_OK;
+  if (v.rows != 0) {
+    const uintptr_t element = v.type == FT_FP32 ? 4 : 2;
+    if (!there(v.tokens, 8) || !aligned(v.parent, 4) || !there(v.target, element) || !aligned(v.draft, element) || !there(v.accept, 4)) return FT_EINVAL;
+    if (v.keep == nullptr || v.target_stride < v.vocab || (v.draft != nullptr && v.draft_stride < v.vocab)) return FT_EINVAL;
+    if (!good_strides({v.target_stride, v.draft_stride})) return FT_EINVAL;
+  }
+  if (v.requests != 0 && (!there(v.starts, 4) || !there(v.pick, 4) || !there(v.last, 4) || !there(v.token, 8))) return FT_EINVAL;
+  std::lock_guard<std::mutex> lock(p->mu);
+  int cu_count = 0;
+  const int rc = compute_units(p, &cu_count);
+  if (rc != FT_OK) return rc;
+  const uint64_t need = v.requests == 0 ? 0 : verify_workspace(v, cu_count);
+  if (need != 0 && (!there(v.workspace, 16) || v.workspace_bytes < need)) return FT_EINVAL;
+  DeviceGuard guard(p->device);
+  FT_HIP(p, launch_verify(v, cu_count, static_cast<hipStream_t>(hip_stream)));
   return FT_OK;
 }
 FT_CATCH_ALL

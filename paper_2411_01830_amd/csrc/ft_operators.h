@@ -49,4 +49,22 @@ hipError_t launch_adapter_group(const int32_t *ids, uint32_t rows, uint32_t coun
 uint64_t adapter_workspace(const ft_adapters_call &call);
 hipError_t launch_adapters(const ft_adapters_call &call, hipStream_t stream);
 
+// Weights of 4 bits with their pool offsets resolved.
+struct Linear4View {
+  const uint8_t *weights;
+  const uint16_t *scales;
+  const uint8_t *zeros;  // or null
+  uint32_t type, width_in, width_out, groups, row_bytes;
+  Divisor group;
+};
+
+uint64_t linear4_workspace(const ft_linear4 &w, uint32_t rows, int cu_count);
+hipError_t launch_linear4(const Linear4View &w, const ft_linear4_call &call, int cu_count, hipStream_t stream);
+
+hipError_t launch_rotate(const ft_rotate_call &call, hipStream_t stream);
+
+constexpr uint32_t kMostVerifyRows = 1024;  // of one request
+uint64_t verify_workspace(const ft_verify_call &call, int cu_count);
+hipError_t launch_verify(const ft_verify_call &call, int cu_count, hipStream_t stream);
+
 }  // namespace ft

@@ -1,0 +1,387 @@
+// Drafted tokens judged against the target's probabilities, and the token behind those that stand.
+//
+// Of a request's rows only those are read whole whose sum is asked for: the row that the next token comes from, and, where tokens were
+// drawn, that of every sibling which falls with another one behind it. All other tests need two numbers each, which are gathered for all of a
+// request's rows at once. A row's sum is that of chunks of 1024 tokens; the next token is looked for in their sums first, then in one chunk.
+#include <hip/hip_runtime.h>
+
+#include "ft_operators.h"
+#include "ft_types.h"
+
+namespace ft {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kChunk = 1024;  // of the vocabulary: 16 tokens to a lane
+constexpr uint32_t kMostChunks = (1u << 22) / kChunk;
+
+// A probability: what is negative, infinite or NaN counts as 0. (0x180: positive numbers, denormal ones among them.)
+__device__ inline float sane(float v) { return __builtin_amdgcn_classf(v, 0x180) ? v : 0; }
+
+struct Fp32 {
+  typedef uint32_t Bits;
+};
+template <class T>
+struct Probability {
+  typedef uint16_t Bits;
+  static __device__ float value(Bits b) { return sane(T::to_float(b)); }
+  // 8 of them, at any element's address
+  static __device__ void load8(const Bits *p, float (&out)[8]) {
+    const Words4 w = load16(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      out[2 * i] = value((uint16_t)w[i]);
+      out[2 * i + 1] = value((uint16_t)(w[i] >> 16));
+    }
+  }
+};
+template <>
+struct Probability<Fp32> {
+  typedef uint32_t Bits;
+  static __device__ float value(Bits b) { return sane(__uint_as_float(b)); }
+  static __device__ void load8(const Bits *p, float (&out)[8]) {
+    const Words4 a = load16(p), b = load16(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      out[i] = value(a[i]);
+      out[4 + i] = value(b[i]);
+    }
+  }
+};
+
+// What is left of a token's probability p where `taken` of the draft's q is gone. The product is rounded for itself.
+__device__ inline double left_of(double p, double taken, double q) {
+  const double left = __dsub_rn(p, __dmul_rn(taken, q));
+  return left > 0 ? left : 0;
+}
+
+__device__ inline double wave_sum(double v) {
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+__device__ inline int32_t clamped(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+struct Lds {
+  int32_t parent[kMostVerifyRows], token[kMostVerifyRows];  // (a token outside the vocabulary: -1)
+  float p[kMostVerifyRows], q[kMostVerifyRows], accept[kMostVerifyRows];
+  int32_t fallen[kMostVerifyRows];
+  double chunk[kMostChunks];  // sums of what is left
+  double wave[kWaves];
+  uint32_t found[kWaves];
+};
+
+// A request's way down its rows. Every wavefront of the workgroup goes it by itself, its state is the same in all lanes.
+template <class T>
+struct Walk {
+  typedef Probability<T> Pr;
+  typedef typename Pr::Bits Bits;
+  const ft_verify_call &v;
+  Lds &s;
+  int32_t first, n;  // rows of the request
+  int32_t node, cursor;  // the last row that stands; rows from here on have not been looked at
+  double taken, mass;    // A and T
+  int32_t fell;          // rows that hang from the node and fell
+  bool lacking;          // drawn: the mass is not known, as a sum over the row is due
+
+  __device__ int lane() const { return threadIdx.x & 63; }
+  __device__ const Bits *target(int32_t row) const { return static_cast<const Bits *>(v.target) + (uint64_t)(first + row) * v.target_stride; }
+  __device__ const Bits *draft(int32_t row) const { return static_cast<const Bits *>(v.draft) + (uint64_t)(first + row) * v.draft_stride; }
+
+  // the rows' own numbers to shared memory; a barrier is behind it
+  __device__ void gather() {
+    for (int32_t j = threadIdx.x; j < n; j += kThreads) {
+      int32_t parent = v.parent == nullptr ? j - 1 : v.parent[first + j];
+      if (parent < 0 || parent >= j) parent = -1;
+      const int64_t token = v.tokens[first + j];
+      const bool known = token >= 0 && token < (int64_t)v.vocab;
+      float p = 0, q = 0;
+      if (known && parent >= 0) {
+        p = Pr::value(target(parent)[token]);
+        if (v.draft != nullptr) q = Pr::value(draft(parent)[token]);
+      }
+      s.parent[j] = parent;
+      s.token[j] = known ? (int32_t)token : -1;
+      s.p[j] = p;
+      s.q[j] = q;
+      s.accept[j] = v.accept[first + j];
+    }
+    __syncthreads();
+    stand(0);
+  }
+
+  __device__ void stand(int32_t row) {
+    node = row;
+    cursor = row + 1;
+    taken = 0;
+    mass = 1;
+    fell = 0;
+    lacking = false;
+  }
+
+  // the first row from the cursor on that hangs from the node, or n
+  __device__ int32_t next() const {
+    for (int32_t j = cursor; j < n; j += 64) {
+      const uint64_t all = __ballot(j + lane() < n && s.parent[j + lane()] == node);
+      if (all != 0) return j + __builtin_ctzll(all);
+    }
+    return n;
+  }
+
+  // not drawn: whether a row before `row` has its token and hangs from the node too
+  __device__ bool before(int32_t row) const {
+    for (int32_t j = node + 1; j < row; j += 64) {
+      const int32_t i = j + lane();
+      if (__ballot(i < row && s.parent[i] == node && s.token[i] == s.token[row]) != 0) return true;
+    }
+    return false;
+  }
+
+  // Goes on until a sum is lacking (which may not be asked for: then it is the token's), or all that hang from the node fell.
+  __device__ void go() {
+    while (!lacking) {
+      const int32_t j = next();
+      cursor = j;
+      if (j >= n) return;
+      cursor = j + 1;
+      const double p = s.p[j], q = s.q[j], u = s.accept[j];
+      if (v.draft != nullptr) {
+        if (__dmul_rn(__dmul_rn(u, mass), q) < left_of(p, taken, q)) {
+          stand(j);
+        } else {
+          taken += mass;
+          ++fell;
+          lacking = true;
+        }
+      } else {
+        const double left = before(j) ? 0 : p;
+        if (__dmul_rn(u, mass) < left) {
+          stand(j);
+        } else {
+          mass = mass > left ? mass - left : 0;
+          ++fell;
+        }
+      }
+    }
+  }
+
+  // not drawn: the tokens that fell, to shared memory; how many
+  __device__ int32_t list() {
+    if (v.draft != nullptr || fell == 0) return 0;
+    int32_t count = 0;
+    for (int32_t j = node + 1; j < n; j += 64) {
+      const int32_t i = j + lane();
+      const bool one = i < n && s.parent[i] == node && s.token[i] >= 0;
+      const uint64_t all = __ballot(one);
+      if (one && threadIdx.x < 64) s.fallen[count + __popcll(all & ((1ull << lane()) - 1))] = s.token[i];
+      count += __popcll(all);
+    }
+    __syncthreads();
+    return count;
+  }
+
+  // what is left of 8 neighbouring tokens of the node's row, `at` to at + 7
+  __device__ void left8(const Bits *p, const Bits *q, uint32_t at, uint32_t drop, double (&out)[8]) const {
+    float a[8], b[8];
+    if (at + 8 <= v.vocab) {
+      Pr::load8(p + at, a);
+      if (q != nullptr) Pr::load8(q + at, b);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] = at + i < v.vocab ? Pr::value(p[at + i]) : 0;
+        b[i] = q != nullptr && at + i < v.vocab ? Pr::value(q[at + i]) : 0;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      out[i] = q != nullptr ? left_of(a[i], taken, b[i]) : a[i];
+      if (drop >> i & 1) out[i] = 0;
+    }
+  }
+
+  // which of 8 neighbouring tokens fell. (All lanes come here.)
+  __device__ uint32_t dropped(uint32_t chunk, uint32_t at, int32_t count) const {
+    uint32_t drop = 0;
+    for (int32_t j = 0; j < count; j += 64) {
+      const uint32_t token = j + lane() < count ? (uint32_t)s.fallen[j + lane()] : 0xffffffffu;
+      for (uint64_t all = __ballot(token / kChunk == chunk); all != 0; all &= all - 1) {
+        const uint32_t off = (uint32_t)__shfl((int)token, __builtin_ctzll(all)) - at;
+        if (off < 8) drop |= 1u << off;
+      }
+    }
+    return drop;
+  }
+
+  // the sum of a chunk, in all lanes of a wavefront
+  __device__ double chunk_sum(const Bits *p, const Bits *q, uint32_t chunk, int32_t count) const {
+    double sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+      const uint32_t at = chunk * kChunk + i * 512 + lane() * 8;
+      double left[8];
+      left8(p, q, at, dropped(chunk, at, count), left);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += left[e];
+    }
+    return wave_sum(sum);
+  }
+
+  __device__ uint32_t chunks() const { return (v.vocab + kChunk - 1) / kChunk; }
+
+  // the chunks' sums to shared memory
+  __device__ void sum(const Bits *q, int32_t count) {
+    const Bits *p = target(node);
+    for (uint32_t c = threadIdx.x >> 6; c < chunks(); c += kWaves) {
+      const double one = chunk_sum(p, q, c, count);
+      if (lane() == 0) s.chunk[c] = one;
+    }
+    __syncthreads();
+  }
+
+  // all chunks' sums together, the same in every wavefront
+  __device__ double total() const {
+    double mine = 0;
+    for (uint32_t c = lane(); c < chunks(); c += 64) mine += s.chunk[c];
+    return wave_sum(mine);
+  }
+
+  // The token with which the sum over what is left exceeds `limit`: a wavefront looks for its chunk, then in it.
+  __device__ int64_t choose(const Bits *q, int32_t count, double limit) const {
+    double before = 0, there = 0;  // of the chunk: what is before it
+    uint32_t chunk = 0xffffffffu, last = 0;
+    double last_before = 0;
+    for (uint32_t c0 = 0; c0 < chunks() && chunk == 0xffffffffu; c0 += 64) {
+      const uint32_t c = c0 + lane();
+      const double one = c < chunks() ? s.chunk[c] : 0;
+      double upto = one;
+      for (int d = 1; d < 64; d <<= 1) {
+        const double other = __shfl_up(upto, d);
+        if (lane() >= d) upto += other;
+      }
+      const uint64_t over = __ballot(one > 0 && before + upto > limit), some = __ballot(one > 0);
+      if (over != 0) {
+        const int at = __builtin_ctzll(over);
+        chunk = c0 + at;
+        there = before + (__shfl(upto, at) - __shfl(one, at));
+      } else if (some != 0) {
+        const int at = 63 - __builtin_clzll(some);
+        last = c0 + at;
+        last_before = before + (__shfl(upto, at) - __shfl(one, at));
+      }
+      before += __shfl(upto, 63);
+    }
+    if (chunk == 0xffffffffu) {
+      chunk = last;
+      there = last_before;
+    }
+    // 16 neighbouring tokens to a lane
+    const uint32_t at = chunk * kChunk + lane() * 16;
+    double left[2][8], sum = 0;
+    left8(target(node), q, at, dropped(chunk, at, count), left[0]);
+    left8(target(node), q, at + 8, dropped(chunk, at + 8, count), left[1]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += left[i / 8][i % 8];
+    double upto = sum;
+    for (int d = 1; d < 64; d <<= 1) {
+      const double other = __shfl_up(upto, d);
+      if (lane() >= d) upto += other;
+    }
+    double here = there + (upto - sum);
+    int over = -1, some = -1;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const double one = left[i / 8][i % 8];
+      here += one;
+      if (one > 0) {
+        some = i;
+        if (over < 0 && here > limit) over = i;
+      }
+    }
+    const uint64_t overs = __ballot(over >= 0), somes = __ballot(some >= 0);
+    const int who = overs != 0 ? __builtin_ctzll(overs) : 63 - __builtin_clzll(somes | 1);
+    return (int64_t)chunk * kChunk + who * 16 + __shfl(overs != 0 ? over : some, who);
+  }
+};
+
+// A workgroup to a request.
+template <class T>
+__global__ __launch_bounds__(kThreads) void ft_verify_kernel(ft_verify_call v) {
+  __shared__ Lds s;
+  const int32_t rows = (int32_t)v.rows;
+  if (blockIdx.x == v.requests) {  // rows of no request
+    const int32_t lo = v.requests != 0 ? clamped(v.starts[0], 0, rows) : rows, hi = v.requests != 0 ? clamped(v.starts[v.requests], lo, rows) : rows;
+    for (int64_t i = threadIdx.x; i < lo; i += kThreads) v.keep[i] = 0;
+    for (int64_t i = (int64_t)hi + threadIdx.x; i < rows; i += kThreads) v.keep[i] = 0;
+    return;
+  }
+  const uint32_t r = blockIdx.x;
+  const int32_t first = clamped(v.starts[r], 0, rows), all = clamped(v.starts[r + 1], first, rows) - first;
+  const int32_t n = (uint32_t)all > v.drafts ? (int32_t)v.drafts : all;
+  if (n == 0) {
+    if (threadIdx.x == 0) {
+      v.last[r] = -1;
+      v.token[r] = -1;
+    }
+    return;
+  }
+  Walk<T> walk{v, s, first, n};
+  walk.gather();
+  typedef typename Walk<T>::Bits Bits;
+  const Bits *q;
+  int32_t count;
+  for (;;) {
+    walk.go();
+    q = v.draft != nullptr && walk.fell != 0 ? walk.draft(walk.node) : nullptr;
+    count = walk.list();
+    walk.sum(q, count);
+    if (!walk.lacking) break;
+    walk.lacking = false;
+    walk.mass = walk.total();
+    __syncthreads();
+    if (walk.next() >= walk.n) break;
+  }
+  double sum = walk.total();
+  if (!(sum > 0)) {  // nothing is left: the target itself
+    __syncthreads();
+    q = nullptr;
+    count = 0;
+    walk.sum(q, count);
+    sum = walk.total();
+  }
+  if (threadIdx.x < 64) {
+    const int64_t token = sum > 0 ? walk.choose(q, count, __dmul_rn((double)v.pick[r], sum)) : -1;
+    if (threadIdx.x == 0) {
+      v.last[r] = first + walk.node;
+      v.token[r] = token;
+    }
+  }
+  // a row stands if it is on the way to the last one
+  __syncthreads();
+  int32_t *on = s.fallen;
+  for (int32_t j = threadIdx.x; j < n; j += kThreads) on[j] = 0;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int32_t j = walk.node; j >= 0; j = s.parent[j]) on[j] = 1;  // (parents are before their rows)
+  __syncthreads();
+  for (int32_t j = threadIdx.x; j < all; j += kThreads) v.keep[first + j] = j < n ? (uint8_t)on[j] : 0;
+}
+
+template <class T>
+void launch(const ft_verify_call &v, hipStream_t stream) {
+  hipLaunchKernelGGL(ft_verify_kernel<T>, dim3(v.requests + 1), dim3(kThreads), 0, stream, v);
+}
+
+}  // namespace
+
+uint64_t verify_workspace(const ft_verify_call &, int) { return 0; }
+
+hipError_t launch_verify(const ft_verify_call &v, int, hipStream_t stream) {
+  if (v.type == FT_FP32) launch<Fp32>(v, stream);
+  else if (v.type == FT_BF16) launch<Bf16>(v, stream);
+  else launch<Fp16>(v, stream);
+  return hipGetLastError();
+}
+
+}  // namespace ft

@@ -22,6 +22,7 @@ from . import binding as ft
 
 FT_EINVAL = -1
 TYPES = {torch.bfloat16: 0, torch.float16: 1}
+PROBABILITIES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
 def _refuse(what):
@@ -241,4 +242,163 @@ def adapters_apply(adapters, groups, x, base=None, out=None):
     return out
 
 
+
+class Linear4:
+    """A projection's weights in the pool, in 4 bits: codes two to a byte (an even element's in the low half), width_out rows of
+    (width_in + 1) // 2 bytes; a scale of `dtype` for each group of neighbouring elements of a row, width_out x ceil(width_in / group);
+    zeros likewise, a byte each (None: 8 everywhere). A weight is scale * (code - zero). Holds as long as the allocations do."""
+
+    def __init__(self, pool, weights_off, scales_off, width_in, width_out, group, dtype, zeros_off=None):
+        if dtype not in TYPES:
+            _refuse(f"scales are bfloat16 or float16, not {dtype}")
+        self.pool, self.dtype, self.width_in, self.width_out = pool, dtype, width_in, width_out
+        self.record = ft.Linear4Record(weights_off, scales_off, ft.NO_ZEROS if zeros_off is None else zeros_off, TYPES[dtype], width_in, width_out, group)
+
+
+def linear4_apply(weights, x, base=None, out=None):
+    """base (None: 0) and x's rows times the weights on top; out may be base. For the few rows of a step: weights are read once for 64 of them."""
+    dev = _device("x", x, weights.pool)
+    if x.dim() != 2:
+        _refuse("x has two dimensions")
+    rows, dtype, ni, no = x.shape[0], weights.dtype, weights.width_in, weights.width_out
+    _rows("x", x, dtype, (rows, ni), dev)
+    shape = (rows, no)
+    if base is not None:
+        _rows("base", base, dtype, shape, dev)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        _rows("out", out, dtype, shape, dev)
+    one = rows <= 1  # a single row's stride means nothing
+    call = ft.Linear4Call(x.data_ptr(), None if base is None else base.data_ptr(), out.data_ptr(), ni if one else x.stride(0),
+                          no if one or base is None else base.stride(0), no if one else out.stride(0), rows, 0, None, 0)
+    need = ft.linear4_workspace(weights.pool, weights.record, call)
+    if need:
+        work = torch.empty(need, dtype=torch.uint8, device=dev)
+        call.workspace, call.workspace_bytes = work.data_ptr(), need
+    ft.linear4_apply(weights.pool, weights.record, call, _stream(dev.index))
+    return out
+
+
+class Rotation:
+    """How positions turn the pairs of heads of `dim` elements: freqs are radians a position, one for each of the pairs (elements behind the first
+    2 * len(freqs) are not turned); axes names the axis of each pair (None: there is one axis); neighbours: pairs are elements 2i and 2i + 1,
+    without it i and i + len(freqs)."""
+
+    def __init__(self, pool, freqs, dim, axes=None, neighbours=False):
+        on = torch.device("cuda", getattr(pool, "device", 0))
+        self.pool, self.dim, self.neighbours = pool, dim, neighbours
+        pairs = len(freqs)
+        if 2 * pairs > dim:
+            _refuse(f"{pairs} pairs are more than a head of {dim} elements has")
+        self.axis, self.axes = None, 1
+        if axes is not None:
+            axes = [int(a) for a in axes]
+            if len(axes) != pairs or any(a < 0 or a > 255 for a in axes):
+                _refuse("axes has a number from 0 to 255 for every pair")
+            self.axes = max(axes, default=0) + 1
+            self.axis = torch.tensor(axes, dtype=torch.uint8).to(on)
+        self.freqs = torch.as_tensor(freqs, dtype=torch.float32).to(on).contiguous()
+        if self.freqs.dim() != 1:
+            _refuse("freqs has one dimension")
+
+
+def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=None, q_out=None, k_out=None):
+    """Queries and keys (None: queries alone) with their heads turned by the tokens' positions: (queries, keys). With eps every head is divided by
+    the root of the mean of its squares before, and multiplied by the weights (None: ones).
+
+    q: tokens x heads x dim; k: tokens x its heads x dim. positions: int32, tokens, or tokens x axes where there are several. q_out and k_out may
+    be q and k."""
+    pool, dim = rotation.pool, rotation.dim
+    dev = _device("q", q, pool)
+    dtype = q.dtype
+    if q.dim() != 3 or dtype not in TYPES:
+        _refuse("q has three dimensions of bfloat16 or float16")
+    tokens, heads, _ = shape = q.shape
+    _rows("q", q, dtype, (tokens, heads, dim), dev)
+    _ints("positions", positions, torch.int32, positions.dim(), dev)
+    dims = positions.dim()
+    if dims not in (1, 2) or positions.shape[0] != tokens or (positions.shape[1] if dims == 2 else 1) < rotation.axes:
+        _refuse("positions has a row for every token, and a column for every axis")
+    if rotation.freqs.device != dev:
+        _refuse("q lies on another GPU than the rotation")
+    flags = ft.ROTATE_NEIGHBOURS if rotation.neighbours else 0
+    if eps is not None:
+        flags |= ft.ROTATE_NORM
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                _rows(name, w, dtype, (dim,), dev)
+    elif q_weight is not None or k_weight is not None:
+        _refuse("weights belong to a norm, which asks for eps")
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        _rows("q_out", q_out, dtype, shape, dev)
+    qs, os = q.stride(), q_out.stride()
+    kv_heads, ks, kos = 0, (0, 0), (0, 0)
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            _refuse("k has three dimensions")
+        kv_heads = k.shape[1]
+        _rows("k", k, dtype, (tokens, kv_heads, dim), dev)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=dtype, device=dev)
+        else:
+            _rows("k_out", k_out, dtype, k.shape, dev)
+        ks, kos = k.stride(), k_out.stride()
+    elif k_out is not None:
+        _refuse("there are no keys for k_out")
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    call = ft.RotateCall(q.data_ptr(), at(k), q_out.data_ptr(), at(k_out), at(q_weight), at(k_weight), positions.data_ptr(), rotation.freqs.data_ptr(),
+                         at(rotation.axis), qs[0], qs[1], ks[0], ks[1], os[0], os[1], kos[0], kos[1], tokens, heads, kv_heads, dim,
+                         2 * rotation.freqs.shape[0], positions.shape[1] if dims == 2 else 1, TYPES[dtype], flags, 0.0 if eps is None else eps, 0)
+    ft.rotate_heads(pool, call, _stream(dev.index))
+    return q_out, k_out
+
+
+def tree_verify(pool, tokens, starts, drafts, target, accept, pick, draft=None, parent=None):
+    """Judges every request's drafted tokens: (keep, last, token) - flags of the rows that stand, as kv_grow takes them, and of every request
+    the last of these and the token behind it, -1 where there is none.
+
+    tokens: int64, a row's token. Rows [starts[r], starts[r + 1]) are request r's, the first of them known, `drafts` the most of one. parent: int32,
+    the row that a row hangs from, counted from its request's first (None: the row before). target: rows x vocabulary, the model's probabilities behind
+    each row; draft: those that the rows which hang from a row were drawn by (None: they were not drawn, but chosen otherwise). accept and
+    pick: float32 random numbers from [0, 1), one a row and one a request."""
+    dev = _device("tokens", tokens, pool)
+    _ints("tokens", tokens, torch.int64, 1, dev)
+    _ints("starts", starts, torch.int32, 1, dev)
+    rows, requests = tokens.shape[0], starts.shape[0] - 1
+    if requests < 0:
+        _refuse("starts has one entry more than there are requests")
+    _ints("accept", accept, torch.float32, 1, dev)
+    _ints("pick", pick, torch.float32, 1, dev)
+    if accept.shape[0] != rows or pick.shape[0] != requests:
+        _refuse("accept has an entry for every row, pick for every request")
+    if target.dim() != 2 or target.dtype not in PROBABILITIES:
+        _refuse("target has two dimensions of bfloat16, float16 or float32")
+    vocab, dtype = target.shape[1], target.dtype
+    _rows("target", target, dtype, (rows, vocab), dev)
+    if draft is not None:
+        _rows("draft", draft, dtype, (rows, vocab), dev)
+    if parent is not None:
+        _ints("parent", parent, torch.int32, 1, dev)
+        if parent.shape[0] != rows:
+            _refuse("parent has an entry for every row")
+    keep = torch.empty(rows, dtype=torch.uint8, device=dev)
+    last = torch.empty(requests, dtype=torch.int32, device=dev)
+    token = torch.empty(requests, dtype=torch.int64, device=dev)
+    one = rows <= 1
+    call = ft.VerifyCall(tokens.data_ptr(), starts.data_ptr(), None if parent is None else parent.data_ptr(), target.data_ptr(),
+                         None if draft is None else draft.data_ptr(), accept.data_ptr(), pick.data_ptr(), keep.data_ptr(), last.data_ptr(), token.data_ptr(),
+                         vocab if one else target.stride(0), vocab if one or draft is None else draft.stride(0), rows, requests, drafts, vocab,
+                         PROBABILITIES[dtype], 0, None, 0)
+    need = ft.verify_workspace(pool, call)
+    if need:
+        work = torch.empty(need, dtype=torch.uint8, device=dev)
+        call.workspace, call.workspace_bytes = work.data_ptr(), need
+    ft.tree_verify(pool, call, _stream(dev.index))
+    return keep, last, token
+
+
 assert C.sizeof(ft.KvCacheRecord) == 64 and C.sizeof(ft.KvTables) == 48 and C.sizeof(ft.TreeCall) == 184 and C.sizeof(ft.AdaptersCall) == 104
+assert C.sizeof(ft.Linear4Record) == 40 and C.sizeof(ft.Linear4Call) == 72 and C.sizeof(ft.RotateCall) == 176 and C.sizeof(ft.VerifyCall) == 136
