@@ -873,7 +873,7 @@ typedef struct ft_linear4_call {
   const void *base;    /* rows x width_out, or NULL: 0 */
   void *out;           /* rows x width_out; may be base itself, with its stride */
   uint64_t x_stride, base_stride, out_stride; /* of a row: >= its width, < 2^40 */
-  uint32_t rows;       /* < 2^20 */
+  uint32_t rows;       /* < 2^19 */
   uint32_t _pad;       /* ignored */
   void *workspace;     /* ft_linear4_workspace bytes, 16-byte aligned, as for ft_tree_attention */
   uint64_t workspace_bytes;

@@ -312,7 +312,7 @@ int ft_adapters_apply(ft_pool *p, const ft_adapters_call *call, void *hip_stream
 FT_CATCH_ALL
 
 int ft_linear4_workspace(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, uint64_t *bytes_out) try {
-  if (p == nullptr || w == nullptr || call == nullptr || bytes_out == nullptr || !good_numbers(*w) || call->rows >= 1u << 20) return FT_EINVAL;
+  if (p == nullptr || w == nullptr || call == nullptr || bytes_out == nullptr || !good_numbers(*w) || call->rows >= 1u << 19) return FT_EINVAL;
   if (call->rows == 0) {
     *bytes_out = 0;
     return FT_OK;
@@ -327,7 +327,7 @@ int ft_linear4_workspace(ft_pool *p, const ft_linear4 *w, const ft_linear4_call 
 FT_CATCH_ALL
 
 int ft_linear4_apply(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, void *hip_stream) try {
-  if (p == nullptr || w == nullptr || call == nullptr || !good_numbers(*w) || call->rows >= 1u << 20) return FT_EINVAL;
+  if (p == nullptr || w == nullptr || call == nullptr || !good_numbers(*w) || call->rows >= 1u << 19) return FT_EINVAL;
   const ft_linear4_call &c = *call;
   if (c.rows != 0) {
     if (!there(c.x, 2) || !aligned(c.base, 2) || !there(c.out, 2)) return FT_EINVAL;
