@@ -899,7 +899,7 @@ typedef struct ft_rotate_call {
   const uint8_t *axis;            /* rot / 2 entries: whose position turns a pair, entries >= axes the last one's; NULL: axis 0 */
   uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
   uint64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride; /* < 2^40; of outputs >= dim where there are several */
-  uint32_t tokens;                /* < 2^31; times heads and kv_heads together: < 2^32 */
+  uint32_t tokens;                /* < 2^24; times heads and kv_heads together: < 2^32 */
   uint32_t heads, kv_heads;       /* <= 65536 */
   uint32_t dim;                   /* a multiple of 8, at most 256 */
   uint32_t rot;                   /* elements of a head that are turned, the first ones: even, 0 .. dim */

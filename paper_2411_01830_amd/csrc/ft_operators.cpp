@@ -144,7 +144,7 @@ bool good_side(const ft_rotate_call &r, const void *in, void *out, uint32_t head
 
 bool good_call(const ft_rotate_call &r) {
   if (r.type > FT_FP16 || r.flags > (FT_ROTATE_NORM | FT_ROTATE_NEIGHBOURS) || r.dim == 0 || r.dim > 256 || r.dim % 8 != 0) return false;
-  if (r.rot > r.dim || r.rot % 2 != 0 || r.axes == 0 || r.axes > 256 || r.tokens >= 1u << 31) return false;
+  if (r.rot > r.dim || r.rot % 2 != 0 || r.axes == 0 || r.axes > 256 || r.tokens >= 1u << 24) return false;
   if ((uint64_t)r.tokens * ((uint64_t)r.heads + r.kv_heads) >= 1ull << 32) return false;
   if ((r.flags & FT_ROTATE_NORM) != 0 && (!std::isfinite(r.eps) || r.eps < 0 || !aligned(r.q_weight, 2) || !aligned(r.k_weight, 2))) return false;
   if (r.tokens == 0) return true;

@@ -1,4 +1,8 @@
 // Norms of queries and keys, head by head, and their rotation by the token's position in the same pass.
+//
+// Every element is read once and written once. A token's angles are the same for all of its heads: a workgroup works out the sines and cosines of
+// its tokens, a pair to a thread, and has them in shared memory. Then a few neighbouring lanes have a head, 16 elements each: eight pairs, or what is
+// not turned.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"
@@ -82,15 +86,199 @@ __global__ __launch_bounds__(256) void ft_rotate_any_kernel(ft_rotate_call r, Di
   }
 }
 
-}  // namespace
+constexpr uint32_t kMostPairs = 1024;  // of a workgroup's tokens
 
-hipError_t launch_rotate(const ft_rotate_call &r, hipStream_t stream) {
-  const uint64_t all = (uint64_t)r.tokens * (r.heads + r.kv_heads), wg = (all + 3) / 4;
-  const dim3 grid((uint32_t)(wg > 1u << 20 ? 1u << 20 : wg));
-  const Divisor heads(r.heads + r.kv_heads);
-  if (r.type == FT_BF16) hipLaunchKernelGGL(ft_rotate_any_kernel<Bf16>, grid, dim3(256), 0, stream, r, heads, all);
-  else hipLaunchKernelGGL(ft_rotate_any_kernel<Fp16>, grid, dim3(256), 0, stream, r, heads, all);
+struct Eight {
+  float v[8];
+};
+
+template <class T>
+__device__ inline Eight eight(Words4 w) {
+  Eight out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    out.v[2 * i] = T::to_float((uint16_t)w[i]);
+    out.v[2 * i + 1] = T::to_float((uint16_t)(w[i] >> 16));
+  }
+  return out;
+}
+
+// elements from `skip` on
+template <class T>
+__device__ inline void write(uint16_t *p, const Eight &e, uint32_t skip) {
+  Loose4 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out.w[i] = T::pack(e.v[2 * i], e.v[2 * i + 1]);
+  if (skip == 0) {
+    *reinterpret_cast<Loose4 *>(p) = out;
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (i >= skip) p[i] = (uint16_t)(out.w[i / 2] >> 16 * (i % 2));
+  }
+}
+
+// LP lanes to a head, each two runs of eight elements. Pairs of halves: the runs of a lane are the two sides of its pairs; the last one begins
+// earlier than where the one before it ends if the pairs are not a multiple of eight, and skips what that one has. So do the last ones of what is not
+// turned. Pairs of neighbours: a run has four of them.
+template <class T, int LP, bool NEIGHBOURS, bool NORM>
+__global__ __launch_bounds__(256) void ft_rotate_kernel(ft_rotate_call r, Divisor by_heads, Divisor by_pairs, uint32_t most_tokens) {
+  __shared__ float cosine[kMostPairs], sine[kMostPairs];
+  const uint32_t token0 = blockIdx.x * most_tokens, tokens = r.tokens - token0 < most_tokens ? r.tokens - token0 : most_tokens;
+  const uint32_t half = r.rot / 2, pairs = by_pairs.d;  // turned ones, and those in shared memory: with NEIGHBOURS all of a head
+  for (uint32_t i = threadIdx.x; i < tokens * pairs; i += 256) {
+    const uint32_t token = by_pairs.of(i), pair = i - token * pairs;
+    float s = 0, c = 1;
+    if (pair < half) {
+      uint32_t axis = r.axis == nullptr ? 0 : r.axis[pair];
+      if (axis >= r.axes) axis = r.axes - 1;
+      angle(r.positions[(uint64_t)(token0 + token) * r.axes + axis], r.freqs[pair], &s, &c);
+    }
+    cosine[i] = c;
+    sine[i] = s;
+  }
+
+  // what of a head this lane has
+  const uint32_t unit = threadIdx.x % LP, rest = r.dim - r.rot;
+  uint32_t begin[2], skip[2] = {0, 0}, pair[2];
+  bool there[2], turned = true;
+  if (NEIGHBOURS) {
+    const uint32_t runs = r.dim / 8, second = (runs + 1) / 2;
+    there[0] = unit < second;
+    there[1] = there[0] && unit + second < runs;
+    begin[0] = 8 * unit;
+    begin[1] = 8 * (unit + second);
+  } else {
+    const uint32_t units = (half + 7) / 8;
+    turned = unit < units;
+    if (turned) {
+      there[0] = there[1] = true;
+      begin[0] = 8 * unit + 8 <= half ? 8 * unit : half - 8;
+      begin[1] = begin[0] + half;
+      skip[0] = skip[1] = 8 * unit - begin[0];
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t at = 16 * (unit - units) + 8 * i;
+        there[i] = at < rest;
+        begin[i] = r.rot + at + 8 <= r.dim ? r.rot + at : r.dim - 8;
+        skip[i] = r.rot + at - begin[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (!there[i]) begin[i] = 0;
+    pair[i] = NEIGHBOURS ? begin[i] / 2 : turned ? begin[0] : 0;
+  }
+  Words4 q_weight[2], k_weight[2];
+  if (NORM) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t one = T::pack(1, 1);
+      q_weight[i] = r.q_weight != nullptr ? load16(static_cast<const uint16_t *>(r.q_weight) + begin[i]) : Words4{one, one, one, one};
+      k_weight[i] = r.k_weight != nullptr ? load16(static_cast<const uint16_t *>(r.k_weight) + begin[i]) : Words4{one, one, one, one};
+    }
+  }
+  __syncthreads();
+
+  for (uint32_t i = threadIdx.x / LP; i < tokens * by_heads.d; i += 256 / LP) {
+    const uint32_t token = by_heads.of(i);
+    uint32_t head = i - token * by_heads.d;
+    const bool key = head >= r.heads;
+    if (key) head -= r.heads;
+    const uint16_t *in = static_cast<const uint16_t *>(key ? r.k : r.q) + (uint64_t)(token0 + token) * (key ? r.k_token_stride : r.q_token_stride) +
+                         head * (key ? r.k_head_stride : r.q_head_stride);
+    uint16_t *out = static_cast<uint16_t *>(key ? r.k_out : r.q_out) + (uint64_t)(token0 + token) * (key ? r.k_out_token_stride : r.q_out_token_stride) +
+                    head * (key ? r.k_out_head_stride : r.q_out_head_stride);
+    Eight x[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) x[j] = eight<T>(load16(in + begin[j]));
+    if (NORM) {
+      float squares = 0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float sum = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+          if (e >= skip[j]) sum = __builtin_fmaf(x[j].v[e], x[j].v[e], sum);
+        if (there[j]) squares += sum;
+      }
+#pragma unroll
+      for (int d = LP / 2; d > 0; d >>= 1) squares += __shfl_xor(squares, d);
+      const float by = 1.0f / sqrtf(squares / (float)r.dim + r.eps);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Words4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = key ? k_weight[j][e] : q_weight[j][e];
+        const Eight weight = eight<T>(w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j].v[e] *= by * weight.v[e];
+      }
+    }
+    const float *c = cosine + token * pairs, *s = sine + token * pairs;
+    if (NEIGHBOURS) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const float a = x[j].v[2 * e], b = x[j].v[2 * e + 1], cos = c[pair[j] + e], sin = s[pair[j] + e];
+          if (pair[j] + e < half) {
+            x[j].v[2 * e] = a * cos - b * sin;
+            x[j].v[2 * e + 1] = a * sin + b * cos;
+          }
+        }
+    } else if (turned) {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const float a = x[0].v[e], b = x[1].v[e], cos = c[pair[0] + e], sin = s[pair[0] + e];
+        x[0].v[e] = a * cos - b * sin;
+        x[1].v[e] = a * sin + b * cos;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (there[j]) write<T>(out + begin[j], x[j], skip[j]);
+  }
+}
+
+template <class T, int LP, bool NEIGHBOURS, bool NORM>
+void launch(const ft_rotate_call &r, hipStream_t stream) {
+  const uint32_t pairs = NEIGHBOURS ? r.dim / 2 : r.rot / 2 == 0 ? 1 : r.rot / 2;
+  // tokens to a workgroup: several where there are many workgroups
+  uint32_t most = r.tokens / 2048;
+  most = most < 1 ? 1 : most > 8 ? 8 : most;
+  if (most * pairs > kMostPairs) most = kMostPairs / pairs;
+  hipLaunchKernelGGL((ft_rotate_kernel<T, LP, NEIGHBOURS, NORM>), dim3((r.tokens + most - 1) / most), dim3(256), 0, stream, r, Divisor(r.heads + r.kv_heads),
+                     Divisor(pairs), most);
+}
+
+template <class T, bool NEIGHBOURS, bool NORM>
+void launch(const ft_rotate_call &r, hipStream_t stream) {
+  const uint32_t lanes = NEIGHBOURS ? (r.dim / 8 + 1) / 2 : (r.rot / 2 + 7) / 8 + (r.dim - r.rot + 15) / 16;
+  if (lanes <= 4) launch<T, 4, NEIGHBOURS, NORM>(r, stream);
+  else if (lanes <= 8) launch<T, 8, NEIGHBOURS, NORM>(r, stream);
+  else if (lanes <= 16) launch<T, 16, NEIGHBOURS, NORM>(r, stream);
+  else launch<T, 32, NEIGHBOURS, NORM>(r, stream);
+}
+
+template <class T>
+hipError_t launch(const ft_rotate_call &r, hipStream_t stream) {
+  const bool neighbours = (r.flags & FT_ROTATE_NEIGHBOURS) != 0, norm = (r.flags & FT_ROTATE_NORM) != 0;
+  if (!neighbours && r.rot != 0 && r.rot < 16) {  // fewer pairs than a run of eight has
+    const uint64_t all = (uint64_t)r.tokens * (r.heads + r.kv_heads), wg = (all + 3) / 4;
+    hipLaunchKernelGGL(ft_rotate_any_kernel<T>, dim3((uint32_t)(wg > 1u << 20 ? 1u << 20 : wg)), dim3(256), 0, stream, r, Divisor(r.heads + r.kv_heads), all);
+  } else if (neighbours) {
+    norm ? launch<T, true, true>(r, stream) : launch<T, true, false>(r, stream);
+  } else {
+    norm ? launch<T, false, true>(r, stream) : launch<T, false, false>(r, stream);
+  }
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_rotate(const ft_rotate_call &r, hipStream_t stream) { return r.type == FT_BF16 ? launch<Bf16>(r, stream) : launch<Fp16>(r, stream); }
 
 }  // namespace ft
