@@ -936,7 +936,7 @@ typedef struct ft_verify_call {
   int32_t *last;           /* requests: the last row that stands, -1 of a request without rows */
   int64_t *token;          /* requests: the token behind it, -1 of a request without rows, or where its row of target has nothing above 0 */
   uint64_t target_stride, draft_stride; /* of a row: >= vocab, < 2^40 */
-  uint32_t rows, requests; /* rows < 2^31, requests < 2^24 - 1 */
+  uint32_t rows, requests; /* rows < 2^31, requests < 2^22 - 1 */
   uint32_t drafts;         /* the most rows of one request; those beyond are taken for no row's. At most 1024, or as many as there are rows */
   uint32_t vocab;          /* 1 .. 2^22 */
   uint32_t type;           /* of target and draft: FT_BF16, FT_FP16 or FT_FP32 */

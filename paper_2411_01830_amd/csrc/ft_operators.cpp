@@ -154,7 +154,7 @@ bool good_call(const ft_rotate_call &r) {
 }
 
 bool good_numbers(const ft_verify_call &v) {
-  if (v.type > FT_FP32 || v.vocab == 0 || v.vocab > 1u << 22 || v.rows >= 1u << 31 || v.requests + 1ull >= kMostWorkgroups || v.drafts == 0) return false;
+  if (v.type > FT_FP32 || v.vocab == 0 || v.vocab > 1u << 22 || v.rows >= 1u << 31 || v.requests + 1ull >= kMostWorkgroups / 4 || v.drafts == 0) return false;
   return (v.drafts < v.rows ? v.drafts : v.rows) <= kMostVerifyRows;
 }
 

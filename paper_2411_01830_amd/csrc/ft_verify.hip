@@ -12,7 +12,6 @@ namespace ft {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kChunk = 1024;  // of the vocabulary: 16 tokens to a lane
 constexpr uint32_t kMostChunks = (1u << 22) / kChunk;
 
@@ -63,22 +62,19 @@ __device__ inline double wave_sum(double v) {
 
 __device__ inline int32_t clamped(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-struct Lds {
+struct Rows {
   int32_t parent[kMostVerifyRows], token[kMostVerifyRows];  // (a token outside the vocabulary: -1)
   float p[kMostVerifyRows], q[kMostVerifyRows], accept[kMostVerifyRows];
   int32_t fallen[kMostVerifyRows];
-  double chunk[kMostChunks];  // sums of what is left
-  double wave[kWaves];
-  uint32_t found[kWaves];
 };
 
 // A request's way down its rows. Every wavefront of the workgroup goes it by itself, its state is the same in all lanes.
-template <class T>
+template <class T, int THREADS>
 struct Walk {
   typedef Probability<T> Pr;
   typedef typename Pr::Bits Bits;
   const ft_verify_call &v;
-  Lds &s;
+  Rows &s;
   int32_t first, n;  // rows of the request
   int32_t node, cursor;  // the last row that stands; rows from here on have not been looked at
   double taken, mass;    // A and T
@@ -91,7 +87,7 @@ struct Walk {
 
   // the rows' own numbers to shared memory; a barrier is behind it
   __device__ void gather() {
-    for (int32_t j = threadIdx.x; j < n; j += kThreads) {
+    for (int32_t j = threadIdx.x; j < n; j += THREADS) {
       int32_t parent = v.parent == nullptr ? j - 1 : v.parent[first + j];
       if (parent < 0 || parent >= j) parent = -1;
       const int64_t token = v.tokens[first + j];
@@ -231,30 +227,30 @@ struct Walk {
   __device__ uint32_t chunks() const { return (v.vocab + kChunk - 1) / kChunk; }
 
   // the chunks' sums to shared memory
-  __device__ void sum(const Bits *q, int32_t count) {
+  __device__ void sum(const Bits *q, int32_t count, double *chunk) const {
     const Bits *p = target(node);
-    for (uint32_t c = threadIdx.x >> 6; c < chunks(); c += kWaves) {
+    for (uint32_t c = threadIdx.x >> 6; c < chunks(); c += THREADS / 64) {
       const double one = chunk_sum(p, q, c, count);
-      if (lane() == 0) s.chunk[c] = one;
+      if (lane() == 0) chunk[c] = one;
     }
     __syncthreads();
   }
 
   // all chunks' sums together, the same in every wavefront
-  __device__ double total() const {
+  __device__ double total(const double *chunk) const {
     double mine = 0;
-    for (uint32_t c = lane(); c < chunks(); c += 64) mine += s.chunk[c];
+    for (uint32_t c = lane(); c < chunks(); c += 64) mine += chunk[c];
     return wave_sum(mine);
   }
 
   // The token with which the sum over what is left exceeds `limit`: a wavefront looks for its chunk, then in it.
-  __device__ int64_t choose(const Bits *q, int32_t count, double limit) const {
+  __device__ int64_t choose(const Bits *q, int32_t count, const double *sums, double limit) const {
     double before = 0, there = 0;  // of the chunk: what is before it
     uint32_t chunk = 0xffffffffu, last = 0;
     double last_before = 0;
     for (uint32_t c0 = 0; c0 < chunks() && chunk == 0xffffffffu; c0 += 64) {
       const uint32_t c = c0 + lane();
-      const double one = c < chunks() ? s.chunk[c] : 0;
+      const double one = c < chunks() ? sums[c] : 0;
       double upto = one;
       for (int d = 1; d < 64; d <<= 1) {
         const double other = __shfl_up(upto, d);
@@ -305,10 +301,40 @@ struct Walk {
   }
 };
 
-// A workgroup to a request.
+// The rows of request r; n of them are judged.
+__device__ inline void rows_of(const ft_verify_call &v, uint32_t r, int32_t *first, int32_t *all, int32_t *n) {
+  *first = clamped(v.starts[r], 0, (int32_t)v.rows);
+  *all = clamped(v.starts[r + 1], *first, (int32_t)v.rows) - *first;
+  *n = (uint32_t)*all > v.drafts ? (int32_t)v.drafts : *all;
+}
+
+// The chunks' sums of the first row whose sum a request asks for, several workgroups to a request: each goes the way there by itself, and has
+// `each` chunks.
 template <class T>
-__global__ __launch_bounds__(kThreads) void ft_verify_kernel(ft_verify_call v) {
-  __shared__ Lds s;
+__global__ __launch_bounds__(256) void ft_verify_sums_kernel(ft_verify_call v, uint32_t each, double *sums) {
+  __shared__ Rows s;
+  const uint32_t r = blockIdx.y;
+  int32_t first, all, n;
+  rows_of(v, r, &first, &all, &n);
+  if (n == 0) return;
+  Walk<T, 256> walk{v, s, first, n};
+  walk.gather();
+  walk.go();
+  const int32_t count = walk.list();
+  const auto *p = walk.target(walk.node), *q = v.draft != nullptr && walk.fell != 0 ? walk.draft(walk.node) : nullptr;
+  const uint32_t chunks = walk.chunks(), end = (blockIdx.x + 1) * each < chunks ? (blockIdx.x + 1) * each : chunks;
+  for (uint32_t c = blockIdx.x * each + (threadIdx.x >> 6); c < end; c += 4) {
+    const double one = walk.chunk_sum(p, q, c, count);
+    if (walk.lane() == 0) sums[(uint64_t)r * chunks + c] = one;
+  }
+}
+
+// A workgroup to a request. SUMS: those of the first row that is asked for are there.
+template <class T, bool SUMS>
+__global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const double *sums) {
+  constexpr int kThreads = 1024;
+  __shared__ Rows s;
+  __shared__ double chunk[kMostChunks];
   const int32_t rows = (int32_t)v.rows;
   if (blockIdx.x == v.requests) {  // rows of no request
     const int32_t lo = v.requests != 0 ? clamped(v.starts[0], 0, rows) : rows, hi = v.requests != 0 ? clamped(v.starts[v.requests], lo, rows) : rows;
@@ -317,8 +343,8 @@ __global__ __launch_bounds__(kThreads) void ft_verify_kernel(ft_verify_call v) {
     return;
   }
   const uint32_t r = blockIdx.x;
-  const int32_t first = clamped(v.starts[r], 0, rows), all = clamped(v.starts[r + 1], first, rows) - first;
-  const int32_t n = (uint32_t)all > v.drafts ? (int32_t)v.drafts : all;
+  int32_t first, all, n;
+  rows_of(v, r, &first, &all, &n);
   if (n == 0) {
     if (threadIdx.x == 0) {
       v.last[r] = -1;
@@ -326,32 +352,34 @@ __global__ __launch_bounds__(kThreads) void ft_verify_kernel(ft_verify_call v) {
     }
     return;
   }
-  Walk<T> walk{v, s, first, n};
+  Walk<T, kThreads> walk{v, s, first, n};
+  if (SUMS)
+    for (uint32_t c = threadIdx.x; c < walk.chunks(); c += kThreads) chunk[c] = sums[(uint64_t)r * walk.chunks() + c];
   walk.gather();
-  typedef typename Walk<T>::Bits Bits;
+  typedef typename Walk<T, kThreads>::Bits Bits;
   const Bits *q;
   int32_t count;
-  for (;;) {
+  for (bool there = SUMS;; there = false) {
     walk.go();
     q = v.draft != nullptr && walk.fell != 0 ? walk.draft(walk.node) : nullptr;
     count = walk.list();
-    walk.sum(q, count);
+    if (!there) walk.sum(q, count, chunk);
     if (!walk.lacking) break;
-    walk.lacking = false;
-    walk.mass = walk.total();
-    __syncthreads();
     if (walk.next() >= walk.n) break;
+    walk.lacking = false;
+    walk.mass = walk.total(chunk);
+    __syncthreads();
   }
-  double sum = walk.total();
+  double sum = walk.total(chunk);
   if (!(sum > 0)) {  // nothing is left: the target itself
     __syncthreads();
     q = nullptr;
     count = 0;
-    walk.sum(q, count);
-    sum = walk.total();
+    walk.sum(q, count, chunk);
+    sum = walk.total(chunk);
   }
   if (threadIdx.x < 64) {
-    const int64_t token = sum > 0 ? walk.choose(q, count, __dmul_rn((double)v.pick[r], sum)) : -1;
+    const int64_t token = sum > 0 ? walk.choose(q, count, chunk, __dmul_rn((double)v.pick[r], sum)) : -1;
     if (threadIdx.x == 0) {
       v.last[r] = first + walk.node;
       v.token[r] = token;
@@ -368,19 +396,38 @@ __global__ __launch_bounds__(kThreads) void ft_verify_kernel(ft_verify_call v) {
   for (int32_t j = threadIdx.x; j < all; j += kThreads) v.keep[first + j] = j < n ? (uint8_t)on[j] : 0;
 }
 
+// Workgroups that a request's first sum is spread over, 0: its own does it.
+uint32_t slices_of(const ft_verify_call &v, int cu_count) {
+  const uint32_t chunks = (v.vocab + kChunk - 1) / kChunk, most = (chunks + 3) / 4;
+  const uint32_t want = (uint32_t)(4 * cu_count) / v.requests;  // of four wavefronts each
+  if (chunks < 16 || want < 2) return 0;
+  return want < most ? want : most;
+}
+
 template <class T>
-void launch(const ft_verify_call &v, hipStream_t stream) {
-  hipLaunchKernelGGL(ft_verify_kernel<T>, dim3(v.requests + 1), dim3(kThreads), 0, stream, v);
+void launch(const ft_verify_call &v, int cu_count, hipStream_t stream) {
+  const uint32_t slices = v.requests == 0 || v.rows == 0 ? 0 : slices_of(v, cu_count), chunks = (v.vocab + kChunk - 1) / kChunk;
+  if (slices != 0) {
+    const uint32_t each = (chunks + slices - 1) / slices;
+    double *sums = static_cast<double *>(v.workspace);
+    hipLaunchKernelGGL(ft_verify_sums_kernel<T>, dim3((chunks + each - 1) / each, v.requests), dim3(256), 0, stream, v, each, sums);
+    hipLaunchKernelGGL((ft_verify_kernel<T, true>), dim3(v.requests + 1), dim3(1024), 0, stream, v, sums);
+  } else {
+    hipLaunchKernelGGL((ft_verify_kernel<T, false>), dim3(v.requests + 1), dim3(1024), 0, stream, v, nullptr);
+  }
 }
 
 }  // namespace
 
-uint64_t verify_workspace(const ft_verify_call &, int) { return 0; }
+uint64_t verify_workspace(const ft_verify_call &v, int cu_count) {
+  if (v.requests == 0 || v.rows == 0 || slices_of(v, cu_count) == 0) return 0;
+  return (uint64_t)v.requests * ((v.vocab + kChunk - 1) / kChunk) * sizeof(double);
+}
 
-hipError_t launch_verify(const ft_verify_call &v, int, hipStream_t stream) {
-  if (v.type == FT_FP32) launch<Fp32>(v, stream);
-  else if (v.type == FT_BF16) launch<Bf16>(v, stream);
-  else launch<Fp16>(v, stream);
+hipError_t launch_verify(const ft_verify_call &v, int cu_count, hipStream_t stream) {
+  if (v.type == FT_FP32) launch<Fp32>(v, cu_count, stream);
+  else if (v.type == FT_BF16) launch<Bf16>(v, cu_count, stream);
+  else launch<Fp16>(v, cu_count, stream);
   return hipGetLastError();
 }
 

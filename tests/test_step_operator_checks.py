@@ -134,7 +134,7 @@ def verify_call(**other):
     dict(tokens=None), dict(tokens=BASE + 4), dict(starts=None), dict(starts=BASE + 2), dict(parent=BASE + 2), dict(target=None), dict(target=BASE + 2),
     dict(draft=BASE + 2), dict(accept=None), dict(accept=BASE + 2), dict(pick=None), dict(pick=BASE + 1), dict(keep=None), dict(last=None), dict(last=BASE + 2),
     dict(token=None), dict(token=BASE + 4), dict(target_stride=999), dict(draft_stride=999), dict(target_stride=1 << 40), dict(rows=1 << 31),
-    dict(requests=(1 << 24) - 1), dict(drafts=0), dict(drafts=1025, rows=1025), dict(vocab=0), dict(vocab=(1 << 22) + 1, target_stride=1 << 23, draft_stride=1 << 23),
+    dict(requests=(1 << 22) - 1), dict(drafts=0), dict(drafts=1025, rows=1025), dict(vocab=0), dict(vocab=(1 << 22) + 1, target_stride=1 << 23, draft_stride=1 << 23),
     dict(type=3), dict(type=0, target=BASE + 1)], ids=str)
 def test_drafts_that_are_refused(pool, other):
     assert code(ft.tree_verify, pool, verify_call(**other)) == EINVAL
