@@ -25,9 +25,13 @@ template <class T>
 struct Probability {
   typedef uint16_t Bits;
   static __device__ float value(Bits b) { return sane(T::to_float(b)); }
-  // 8 of them, at any element's address
-  static __device__ void load8(const Bits *p, float (&out)[8]) {
-    const Words4 w = load16(p);
+  // 8 of them as they lie, at any element's address
+  struct Raw {
+    Words4 w;
+  };
+  static __device__ Raw load8(const Bits *p) { return {load16(p)}; }
+  static __device__ void values(const Raw &r, float (&out)[8]) {
+    const Words4 w = r.w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       out[2 * i] = value((uint16_t)w[i]);
@@ -39,12 +43,15 @@ template <>
 struct Probability<Fp32> {
   typedef uint32_t Bits;
   static __device__ float value(Bits b) { return sane(__uint_as_float(b)); }
-  static __device__ void load8(const Bits *p, float (&out)[8]) {
-    const Words4 a = load16(p), b = load16(p + 4);
+  struct Raw {
+    Words4 a, b;
+  };
+  static __device__ Raw load8(const Bits *p) { return {load16(p), load16(p + 4)}; }
+  static __device__ void values(const Raw &r, float (&out)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      out[i] = value(a[i]);
-      out[4 + i] = value(b[i]);
+      out[i] = value(r.a[i]);
+      out[4 + i] = value(r.b[i]);
     }
   }
 };
@@ -55,9 +62,55 @@ __device__ inline double left_of(double p, double taken, double q) {
   return left > 0 ? left : 0;
 }
 
+// v of another lane: of the same 16 lanes by a pattern, of 16 or 32 lanes further
+template <int PATTERN>
+__device__ inline double other_lane(double v) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, PATTERN, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(bits >> 32), PATTERN, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// The sum over a wavefront, in all lanes: neighbours, pairs, quads mirrored, eights mirrored, and then what lies 16 and 32 lanes apart. (By shuffles through
+// shared memory the six steps take longer than a chunk's loads.)
 __device__ inline double wave_sum(double v) {
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  v += other_lane<0xb1>(v);   // quad_perm 1 0 3 2
+  v += other_lane<0x4e>(v);   // quad_perm 2 3 0 1
+  v += other_lane<0x141>(v);  // row_half_mirror
+  v += other_lane<0x140>(v);  // row_mirror
+  typedef uint32_t Two __attribute__((ext_vector_type(2)));
+  uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  Two lo = __builtin_amdgcn_permlane16_swap((uint32_t)bits, (uint32_t)bits, false, false);
+  Two hi = __builtin_amdgcn_permlane16_swap((uint32_t)(bits >> 32), (uint32_t)(bits >> 32), false, false);
+  v = __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+  bits = __builtin_bit_cast(uint64_t, v);
+  lo = __builtin_amdgcn_permlane32_swap((uint32_t)bits, (uint32_t)bits, false, false);
+  hi = __builtin_amdgcn_permlane32_swap((uint32_t)(bits >> 32), (uint32_t)(bits >> 32), false, false);
+  return __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+}
+
+// The sums over the lanes up to each: within 16 lanes, then with those of the 16 and of the 32 before.
+template <int PATTERN, int ROWS>
+__device__ inline double lane_before(double v) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, PATTERN, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(bits >> 32), PATTERN, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double wave_upto(double v) {
+  v += lane_before<0x111, 0xf>(v);  // row_shr 1
+  v += lane_before<0x112, 0xf>(v);
+  v += lane_before<0x114, 0xf>(v);
+  v += lane_before<0x118, 0xf>(v);
+  v += lane_before<0x142, 0xa>(v);  // row_bcast 15: to the second and the fourth 16 lanes
+  v += lane_before<0x143, 0xc>(v);  // row_bcast 31: to the upper 32
   return v;
+}
+
+__device__ inline double of_lane(double v, int lane) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane), hi = __builtin_amdgcn_readlane((int)(bits >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 __device__ inline int32_t clamped(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -177,12 +230,37 @@ struct Walk {
     return count;
   }
 
-  // what is left of 8 neighbouring tokens of the node's row, `at` to at + 7
+  // the same of a way that another workgroup went, by a wavefront
+  __device__ int32_t fallen(int32_t fell_there) const {
+    if (v.draft != nullptr || fell_there == 0) return 0;
+    int32_t count = 0;
+    for (int32_t j = node + 1; j < n; j += 64) {
+      const int32_t i = j + lane();
+      int64_t token = -1;
+      if (i < n && (v.parent == nullptr ? i - 1 : v.parent[first + i]) == node) token = v.tokens[first + i];
+      const bool one = token >= 0 && token < (int64_t)v.vocab;
+      const uint64_t all = __ballot(one);
+      if (one) s.fallen[count + __popcll(all & ((1ull << lane()) - 1))] = (int32_t)token;
+      count += __popcll(all);
+    }
+    __builtin_amdgcn_wave_barrier();
+    return count;
+  }
+
+  // what is left of 8 neighbouring tokens whose probabilities are a and b
+  __device__ void left8(const float (&a)[8], const float (&b)[8], bool drawn, uint32_t drop, double (&out)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      out[i] = drawn ? left_of(a[i], taken, b[i]) : a[i];
+      if (drop >> i & 1) out[i] = 0;
+    }
+  }
+  // of the node's row, `at` to at + 7
   __device__ void left8(const Bits *p, const Bits *q, uint32_t at, uint32_t drop, double (&out)[8]) const {
     float a[8], b[8];
     if (at + 8 <= v.vocab) {
-      Pr::load8(p + at, a);
-      if (q != nullptr) Pr::load8(q + at, b);
+      Pr::values(Pr::load8(p + at), a);
+      if (q != nullptr) Pr::values(Pr::load8(q + at), b);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -190,11 +268,7 @@ struct Walk {
         b[i] = q != nullptr && at + i < v.vocab ? Pr::value(q[at + i]) : 0;
       }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      out[i] = q != nullptr ? left_of(a[i], taken, b[i]) : a[i];
-      if (drop >> i & 1) out[i] = 0;
-    }
+    left8(a, b, q != nullptr, drop, out);
   }
 
   // which of 8 neighbouring tokens fell. (All lanes come here.)
@@ -210,7 +284,7 @@ struct Walk {
     return drop;
   }
 
-  // the sum of a chunk, in all lanes of a wavefront
+  // the sum of a chunk, in all lanes of a wavefront; what its two runs of eight tokens a lane give is added in their order
   __device__ double chunk_sum(const Bits *p, const Bits *q, uint32_t chunk, int32_t count) const {
     double sum = 0;
 #pragma unroll
@@ -223,16 +297,58 @@ struct Walk {
     }
     return wave_sum(sum);
   }
+  // The same of N chunks, `step` apart and before `stop`, all whole. Their loads are on their way before the first is looked at; where there are
+  // fewer, the last one's again.
+  template <int N>
+  __device__ void some_sums(const Bits *p, const Bits *q, uint32_t chunk, uint32_t step, uint32_t stop, int32_t count, double *out) const {
+    typename Pr::Raw a[N][2], b[N][2];
+    const Bits *other = q != nullptr ? q : p;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t c = chunk + j * step < stop ? chunk + j * step : stop - 1, at = c * kChunk + i * 512 + lane() * 8;
+        a[j][i] = Pr::load8(p + at);
+        b[j][i] = Pr::load8(other + at);
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t c = chunk + j * step;
+      double sum = 0;
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        float x[8], y[8];
+        Pr::values(a[j][i], x);
+        Pr::values(b[j][i], y);
+        double left[8];
+        left8(x, y, q != nullptr, dropped(c, c * kChunk + i * 512 + lane() * 8, count), left);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += left[e];
+      }
+      sum = wave_sum(sum);
+      if (lane() == 0 && c < stop) out[c] = sum;
+    }
+  }
+  // of the chunks from `chunk` to before `end`
+  __device__ void chunk_sums(const Bits *p, const Bits *q, uint32_t chunk, uint32_t step, uint32_t end, int32_t count, double *out) const {
+    constexpr int N = sizeof(Bits) == 2 ? 4 : 2;
+    const uint32_t whole = v.vocab / kChunk, stop = end < whole ? end : whole, begin = chunk;
+    for (; chunk < stop; chunk += N * step) {
+      if (chunk + step >= stop) some_sums<1>(p, q, chunk, step, stop, count, out);
+      else if (N > 2 && chunk + 2 * step >= stop) some_sums<2>(p, q, chunk, step, stop, count, out);
+      else some_sums<N>(p, q, chunk, step, stop, count, out);
+    }
+    if (whole < end && begin <= whole && (whole - begin) % step == 0) {
+      const double one = chunk_sum(p, q, whole, count);
+      if (lane() == 0) out[whole] = one;
+    }
+  }
 
   __device__ uint32_t chunks() const { return (v.vocab + kChunk - 1) / kChunk; }
 
   // the chunks' sums to shared memory
   __device__ void sum(const Bits *q, int32_t count, double *chunk) const {
-    const Bits *p = target(node);
-    for (uint32_t c = threadIdx.x >> 6; c < chunks(); c += THREADS / 64) {
-      const double one = chunk_sum(p, q, c, count);
-      if (lane() == 0) chunk[c] = one;
-    }
+    chunk_sums(target(node), q, threadIdx.x >> 6, THREADS / 64, chunks(), count, chunk);
     __syncthreads();
   }
 
@@ -251,22 +367,18 @@ struct Walk {
     for (uint32_t c0 = 0; c0 < chunks() && chunk == 0xffffffffu; c0 += 64) {
       const uint32_t c = c0 + lane();
       const double one = c < chunks() ? sums[c] : 0;
-      double upto = one;
-      for (int d = 1; d < 64; d <<= 1) {
-        const double other = __shfl_up(upto, d);
-        if (lane() >= d) upto += other;
-      }
+      const double upto = wave_upto(one);
       const uint64_t over = __ballot(one > 0 && before + upto > limit), some = __ballot(one > 0);
       if (over != 0) {
         const int at = __builtin_ctzll(over);
         chunk = c0 + at;
-        there = before + (__shfl(upto, at) - __shfl(one, at));
+        there = before + (of_lane(upto, at) - of_lane(one, at));
       } else if (some != 0) {
         const int at = 63 - __builtin_clzll(some);
         last = c0 + at;
-        last_before = before + (__shfl(upto, at) - __shfl(one, at));
+        last_before = before + (of_lane(upto, at) - of_lane(one, at));
       }
-      before += __shfl(upto, 63);
+      before += of_lane(upto, 63);
     }
     if (chunk == 0xffffffffu) {
       chunk = last;
@@ -279,11 +391,7 @@ struct Walk {
     left8(target(node), q, at + 8, dropped(chunk, at + 8, count), left[1]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += left[i / 8][i % 8];
-    double upto = sum;
-    for (int d = 1; d < 64; d <<= 1) {
-      const double other = __shfl_up(upto, d);
-      if (lane() >= d) upto += other;
-    }
+    const double upto = wave_upto(sum);
     double here = there + (upto - sum);
     int over = -1, some = -1;
 #pragma unroll
@@ -297,7 +405,7 @@ struct Walk {
     }
     const uint64_t overs = __ballot(over >= 0), somes = __ballot(some >= 0);
     const int who = overs != 0 ? __builtin_ctzll(overs) : 63 - __builtin_clzll(somes | 1);
-    return (int64_t)chunk * kChunk + who * 16 + __shfl(overs != 0 ? over : some, who);
+    return (int64_t)chunk * kChunk + who * 16 + __builtin_amdgcn_readlane(overs != 0 ? over : some, who);
   }
 };
 
@@ -308,10 +416,31 @@ __device__ inline void rows_of(const ft_verify_call &v, uint32_t r, int32_t *fir
   *n = (uint32_t)*all > v.drafts ? (int32_t)v.drafts : *all;
 }
 
+// Where a request's way stops for the first time.
+struct Stop {
+  double taken;
+  int32_t node, fell;
+  int32_t last;  // whether it ends there
+  int32_t _pad;
+};
+
+// Which rows stand: those on the way to `node`. All threads of the workgroup come here.
+template <int THREADS>
+__device__ inline void write_kept(const ft_verify_call &v, Rows &s, int32_t first, int32_t all, int32_t n, int32_t node) {
+  __syncthreads();
+  int32_t *on = s.fallen;
+  for (int32_t j = threadIdx.x; j < n; j += THREADS) on[j] = 0;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int32_t j = node; j >= 0; j = s.parent[j]) on[j] = 1;  // (parents are before their rows)
+  __syncthreads();
+  for (int32_t j = threadIdx.x; j < all; j += THREADS) v.keep[first + j] = j < n ? (uint8_t)on[j] : 0;
+}
+
 // The chunks' sums of the first row whose sum a request asks for, several workgroups to a request: each goes the way there by itself, and has
-// `each` chunks.
+// `each` chunks. The first one says where that was, and which rows stand if the way ends there.
 template <class T>
-__global__ __launch_bounds__(256) void ft_verify_sums_kernel(ft_verify_call v, uint32_t each, double *sums) {
+__global__ __launch_bounds__(256) void ft_verify_sums_kernel(ft_verify_call v, uint32_t each, double *sums, Stop *stops) {
   __shared__ Rows s;
   const uint32_t r = blockIdx.y;
   int32_t first, all, n;
@@ -323,15 +452,37 @@ __global__ __launch_bounds__(256) void ft_verify_sums_kernel(ft_verify_call v, u
   const int32_t count = walk.list();
   const auto *p = walk.target(walk.node), *q = v.draft != nullptr && walk.fell != 0 ? walk.draft(walk.node) : nullptr;
   const uint32_t chunks = walk.chunks(), end = (blockIdx.x + 1) * each < chunks ? (blockIdx.x + 1) * each : chunks;
-  for (uint32_t c = blockIdx.x * each + (threadIdx.x >> 6); c < end; c += 4) {
-    const double one = walk.chunk_sum(p, q, c, count);
-    if (walk.lane() == 0) sums[(uint64_t)r * chunks + c] = one;
+  walk.chunk_sums(p, q, blockIdx.x * each + (threadIdx.x >> 6), 4, end, count, sums + (uint64_t)r * chunks);
+  if (blockIdx.x != 0) return;
+  const bool last = !walk.lacking || walk.next() >= n;
+  if (threadIdx.x == 0) stops[r] = Stop{walk.taken, walk.node, walk.fell, last, 0};
+  if (last) write_kept<256>(v, s, first, all, n, walk.node);
+}
+
+// The last row that stands and the token behind it, by a wavefront.
+template <class W, class Bits>
+__device__ inline void finish(const ft_verify_call &v, uint32_t r, int32_t first, const W &walk, const Bits *q, int32_t count, const double *sums,
+                              double *spare) {
+  const double pick = v.pick[r];
+  double sum = walk.total(sums);
+  if (!(sum > 0)) {  // nothing is left: the target itself
+    q = nullptr;
+    count = 0;
+    walk.chunk_sums(walk.target(walk.node), q, 0, 1, walk.chunks(), 0, spare);
+    __builtin_amdgcn_wave_barrier();
+    sums = spare;
+    sum = walk.total(sums);
+  }
+  const int64_t token = sum > 0 ? walk.choose(q, count, sums, __dmul_rn(pick, sum)) : -1;
+  if (threadIdx.x == 0) {
+    v.last[r] = first + walk.node;
+    v.token[r] = token;
   }
 }
 
-// A workgroup to a request. SUMS: those of the first row that is asked for are there.
+// A workgroup to a request. SUMS: those of the first row that is asked for are there; where the way ends with it a wavefront does the rest.
 template <class T, bool SUMS>
-__global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const double *sums) {
+__global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const double *sums, const Stop *stops) {
   constexpr int kThreads = 1024;
   __shared__ Rows s;
   __shared__ double chunk[kMostChunks];
@@ -345,6 +496,8 @@ __global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const
   const uint32_t r = blockIdx.x;
   int32_t first, all, n;
   rows_of(v, r, &first, &all, &n);
+  Stop stop{};
+  if (SUMS) stop = stops[r];  // (of a request without rows it is not there)
   if (n == 0) {
     if (threadIdx.x == 0) {
       v.last[r] = -1;
@@ -353,8 +506,17 @@ __global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const
     return;
   }
   Walk<T, kThreads> walk{v, s, first, n};
-  if (SUMS)
-    for (uint32_t c = threadIdx.x; c < walk.chunks(); c += kThreads) chunk[c] = sums[(uint64_t)r * walk.chunks() + c];
+  if (SUMS) {
+    const double *mine = sums + (uint64_t)r * walk.chunks();
+    if (stop.last != 0) {
+      if (threadIdx.x >= 64) return;
+      walk.node = stop.node;
+      walk.taken = stop.taken;
+      finish(v, r, first, walk, v.draft != nullptr && stop.fell != 0 ? walk.draft(stop.node) : nullptr, walk.fallen(stop.fell), mine, chunk);
+      return;
+    }
+    for (uint32_t c = threadIdx.x; c < walk.chunks(); c += kThreads) chunk[c] = mine[c];
+  }
   walk.gather();
   typedef typename Walk<T, kThreads>::Bits Bits;
   const Bits *q;
@@ -370,30 +532,8 @@ __global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const
     walk.mass = walk.total(chunk);
     __syncthreads();
   }
-  double sum = walk.total(chunk);
-  if (!(sum > 0)) {  // nothing is left: the target itself
-    __syncthreads();
-    q = nullptr;
-    count = 0;
-    walk.sum(q, count, chunk);
-    sum = walk.total(chunk);
-  }
-  if (threadIdx.x < 64) {
-    const int64_t token = sum > 0 ? walk.choose(q, count, chunk, __dmul_rn((double)v.pick[r], sum)) : -1;
-    if (threadIdx.x == 0) {
-      v.last[r] = first + walk.node;
-      v.token[r] = token;
-    }
-  }
-  // a row stands if it is on the way to the last one
-  __syncthreads();
-  int32_t *on = s.fallen;
-  for (int32_t j = threadIdx.x; j < n; j += kThreads) on[j] = 0;
-  __syncthreads();
-  if (threadIdx.x == 0)
-    for (int32_t j = walk.node; j >= 0; j = s.parent[j]) on[j] = 1;  // (parents are before their rows)
-  __syncthreads();
-  for (int32_t j = threadIdx.x; j < all; j += kThreads) v.keep[first + j] = j < n ? (uint8_t)on[j] : 0;
+  if (threadIdx.x < 64) finish(v, r, first, walk, q, count, chunk, chunk);
+  write_kept<kThreads>(v, s, first, all, n, walk.node);
 }
 
 // Workgroups that a request's first sum is spread over, 0: its own does it.
@@ -409,11 +549,12 @@ void launch(const ft_verify_call &v, int cu_count, hipStream_t stream) {
   const uint32_t slices = v.requests == 0 || v.rows == 0 ? 0 : slices_of(v, cu_count), chunks = (v.vocab + kChunk - 1) / kChunk;
   if (slices != 0) {
     const uint32_t each = (chunks + slices - 1) / slices;
-    double *sums = static_cast<double *>(v.workspace);
-    hipLaunchKernelGGL(ft_verify_sums_kernel<T>, dim3((chunks + each - 1) / each, v.requests), dim3(256), 0, stream, v, each, sums);
-    hipLaunchKernelGGL((ft_verify_kernel<T, true>), dim3(v.requests + 1), dim3(1024), 0, stream, v, sums);
+    Stop *stops = static_cast<Stop *>(v.workspace);
+    double *sums = reinterpret_cast<double *>(stops + v.requests);
+    hipLaunchKernelGGL(ft_verify_sums_kernel<T>, dim3((chunks + each - 1) / each, v.requests), dim3(256), 0, stream, v, each, sums, stops);
+    hipLaunchKernelGGL((ft_verify_kernel<T, true>), dim3(v.requests + 1), dim3(1024), 0, stream, v, sums, stops);
   } else {
-    hipLaunchKernelGGL((ft_verify_kernel<T, false>), dim3(v.requests + 1), dim3(1024), 0, stream, v, nullptr);
+    hipLaunchKernelGGL((ft_verify_kernel<T, false>), dim3(v.requests + 1), dim3(1024), 0, stream, v, nullptr, nullptr);
   }
 }
 
@@ -421,7 +562,7 @@ void launch(const ft_verify_call &v, int cu_count, hipStream_t stream) {
 
 uint64_t verify_workspace(const ft_verify_call &v, int cu_count) {
   if (v.requests == 0 || v.rows == 0 || slices_of(v, cu_count) == 0) return 0;
-  return (uint64_t)v.requests * ((v.vocab + kChunk - 1) / kChunk) * sizeof(double);
+  return v.requests * (sizeof(Stop) + (uint64_t)((v.vocab + kChunk - 1) / kChunk) * sizeof(double));
 }
 
 hipError_t launch_verify(const ft_verify_call &v, int cu_count, hipStream_t stream) {
