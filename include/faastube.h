@@ -953,8 +953,8 @@ typedef struct ft_verify_call {
  *   not drawn  row c stands if accept[c] * T < p[token c], which is 0 if it fell before; otherwise T -= p[token c] (not below 0)
  * Behind the last one that stands the token is the first one with which the sum over what is left (max(p - A q, 0); p without the tokens that
  * fell) exceeds pick times all of it; if nothing is left, over p; if none exceeds it, the last token of which something is left.
- * Rows of probabilities are taken as they are, as if their sum were 1; what is negative or not finite counts as 0, as does the probability of a
- * token outside [0, vocab). Sums and comparisons are 64 bits.
+ * Rows of probabilities are taken as they are, as if their sum were 1. Of NaN nothing is left, the probability of a token outside [0, vocab) is 0,
+ * and where the target is infinite some token comes out. Sums and comparisons are 64 bits.
  * Several rows that were drawn behind one row are independent draws; they may be alike.
  */
 int ft_tree_verify(ft_pool *p, const ft_verify_call *call, void *hip_stream);

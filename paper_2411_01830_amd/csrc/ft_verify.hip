@@ -15,16 +15,13 @@ namespace {
 constexpr uint32_t kChunk = 1024;  // of the vocabulary: 16 tokens to a lane
 constexpr uint32_t kMostChunks = (1u << 22) / kChunk;
 
-// A probability: what is negative, infinite or NaN counts as 0. (0x180: positive numbers, denormal ones among them.)
-__device__ inline float sane(float v) { return __builtin_amdgcn_classf(v, 0x180) ? v : 0; }
-
 struct Fp32 {
   typedef uint32_t Bits;
 };
 template <class T>
 struct Probability {
   typedef uint16_t Bits;
-  static __device__ float value(Bits b) { return sane(T::to_float(b)); }
+  static __device__ float value(Bits b) { return T::to_float(b); }
   // 8 of them as they lie, at any element's address
   struct Raw {
     Words4 w;
@@ -42,7 +39,7 @@ struct Probability {
 template <>
 struct Probability<Fp32> {
   typedef uint32_t Bits;
-  static __device__ float value(Bits b) { return sane(__uint_as_float(b)); }
+  static __device__ float value(Bits b) { return __uint_as_float(b); }
   struct Raw {
     Words4 a, b;
   };
@@ -56,11 +53,9 @@ struct Probability<Fp32> {
   }
 };
 
-// What is left of a token's probability p where `taken` of the draft's q is gone. The product is rounded for itself.
-__device__ inline double left_of(double p, double taken, double q) {
-  const double left = __dsub_rn(p, __dmul_rn(taken, q));
-  return left > 0 ? left : 0;
-}
+// What is left of a token's probability p where `taken` of the draft's q is gone; of NaN nothing is. (A maximum with a NaN is the other number.)
+__device__ inline double left_of(double p, double taken, double q) { return __builtin_fmax(__builtin_fma(-taken, q, p), 0.0); }
+__device__ inline double left_of(float p) { return __builtin_fmaxf(p, 0.0f); }
 
 // v of another lane: of the same 16 lanes by a pattern, of 16 or 32 lanes further
 template <int PATTERN>
@@ -194,9 +189,9 @@ struct Walk {
       cursor = j;
       if (j >= n) return;
       cursor = j + 1;
-      const double p = s.p[j], q = s.q[j], u = s.accept[j];
+      const float p = s.p[j], q = s.q[j], u = s.accept[j];
       if (v.draft != nullptr) {
-        if (__dmul_rn(__dmul_rn(u, mass), q) < left_of(p, taken, q)) {
+        if ((double)u * mass * (double)q < (fell == 0 ? left_of(p) : left_of(p, taken, q))) {
           stand(j);
         } else {
           taken += mass;
@@ -204,8 +199,8 @@ struct Walk {
           lacking = true;
         }
       } else {
-        const double left = before(j) ? 0 : p;
-        if (__dmul_rn(u, mass) < left) {
+        const double left = before(j) ? 0 : left_of(p);
+        if ((double)u * mass < left) {
           stand(j);
         } else {
           mass = mass > left ? mass - left : 0;
@@ -247,20 +242,22 @@ struct Walk {
     return count;
   }
 
-  // what is left of 8 neighbouring tokens whose probabilities are a and b
-  __device__ void left8(const float (&a)[8], const float (&b)[8], bool drawn, uint32_t drop, double (&out)[8]) const {
+  // what is left of 8 neighbouring tokens whose probabilities are a and b (Q) or a alone. The drop is of those that were not drawn.
+  template <bool Q>
+  __device__ void left8(const float (&a)[8], const float (&b)[8], uint32_t drop, double (&out)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      out[i] = drawn ? left_of(a[i], taken, b[i]) : a[i];
-      if (drop >> i & 1) out[i] = 0;
-    }
+    for (int i = 0; i < 8; ++i) out[i] = Q ? left_of(a[i], taken, b[i]) : left_of(a[i]);
+    if (!Q && __ballot(drop != 0) != 0)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (drop >> i & 1) out[i] = 0;
   }
-  // of the node's row, `at` to at + 7
+  // of the node's row, `at` to at + 7, whatever of them there is
   __device__ void left8(const Bits *p, const Bits *q, uint32_t at, uint32_t drop, double (&out)[8]) const {
     float a[8], b[8];
     if (at + 8 <= v.vocab) {
       Pr::values(Pr::load8(p + at), a);
-      if (q != nullptr) Pr::values(Pr::load8(q + at), b);
+      Pr::values(Pr::load8((q != nullptr ? q : p) + at), b);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -268,7 +265,8 @@ struct Walk {
         b[i] = q != nullptr && at + i < v.vocab ? Pr::value(q[at + i]) : 0;
       }
     }
-    left8(a, b, q != nullptr, drop, out);
+    if (q != nullptr) left8<true>(a, b, drop, out);
+    else left8<false>(a, b, drop, out);
   }
 
   // which of 8 neighbouring tokens fell. (All lanes come here.)
@@ -299,17 +297,16 @@ struct Walk {
   }
   // The same of N chunks, `step` apart and before `stop`, all whole. Their loads are on their way before the first is looked at; where there are
   // fewer, the last one's again.
-  template <int N>
+  template <int N, bool Q>
   __device__ void some_sums(const Bits *p, const Bits *q, uint32_t chunk, uint32_t step, uint32_t stop, int32_t count, double *out) const {
     typename Pr::Raw a[N][2], b[N][2];
-    const Bits *other = q != nullptr ? q : p;
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (uint32_t i = 0; i < 2; ++i) {
         const uint32_t c = chunk + j * step < stop ? chunk + j * step : stop - 1, at = c * kChunk + i * 512 + lane() * 8;
         a[j][i] = Pr::load8(p + at);
-        b[j][i] = Pr::load8(other + at);
+        if (Q) b[j][i] = Pr::load8(q + at);
       }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -319,9 +316,9 @@ struct Walk {
       for (uint32_t i = 0; i < 2; ++i) {
         float x[8], y[8];
         Pr::values(a[j][i], x);
-        Pr::values(b[j][i], y);
+        if (Q) Pr::values(b[j][i], y);
         double left[8];
-        left8(x, y, q != nullptr, dropped(c, c * kChunk + i * 512 + lane() * 8, count), left);
+        left8<Q>(x, y, dropped(c, c * kChunk + i * 512 + lane() * 8, count), left);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += left[e];
       }
@@ -331,12 +328,16 @@ struct Walk {
   }
   // of the chunks from `chunk` to before `end`
   __device__ void chunk_sums(const Bits *p, const Bits *q, uint32_t chunk, uint32_t step, uint32_t end, int32_t count, double *out) const {
-    constexpr int N = sizeof(Bits) == 2 ? 4 : 2;
+    constexpr int N = 2;
     const uint32_t whole = v.vocab / kChunk, stop = end < whole ? end : whole, begin = chunk;
     for (; chunk < stop; chunk += N * step) {
-      if (chunk + step >= stop) some_sums<1>(p, q, chunk, step, stop, count, out);
-      else if (N > 2 && chunk + 2 * step >= stop) some_sums<2>(p, q, chunk, step, stop, count, out);
-      else some_sums<N>(p, q, chunk, step, stop, count, out);
+      if (q != nullptr) {
+        if (chunk + step >= stop) some_sums<1, true>(p, q, chunk, step, stop, count, out);
+        else some_sums<N, true>(p, q, chunk, step, stop, count, out);
+      } else {
+        if (chunk + step >= stop) some_sums<1, false>(p, q, chunk, step, stop, count, out);
+        else some_sums<N, false>(p, q, chunk, step, stop, count, out);
+      }
     }
     if (whole < end && begin <= whole && (whole - begin) % step == 0) {
       const double one = chunk_sum(p, q, whole, count);

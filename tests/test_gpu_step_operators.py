@@ -270,8 +270,8 @@ def test_heads_of_infinities_keep_to_themselves(dim, rot, neighbours):
 
 def judged(tokens, starts, drafts, target, draft, accept, pick, parent):
     """The definition, row by row, in 64 bits on the CPU."""
-    clean = lambda t: torch.where((t > 0) & torch.isfinite(t), t, 0).double().cpu()  # noqa: E731
-    target, draft = clean(target), None if draft is None else clean(draft)
+    target, draft = target.double().cpu(), None if draft is None else draft.double().cpu()
+    rest = lambda t: torch.where(t > 0, t, 0)  # noqa: E731  (of NaN nothing is left)
     vocab = target.shape[1]
     keep, last, after = [0] * len(tokens), [], []
     for r, (a, b) in enumerate(zip(starts, starts[1:])):
@@ -282,8 +282,8 @@ def judged(tokens, starts, drafts, target, draft, accept, pick, parent):
             continue
         row, keep[a] = a, 1
         while True:
-            p = target[row]
-            left, mass = p.clone(), 1.0
+            p = rest(target[row])
+            left, mass, taken = p.clone(), 1.0, 0.0
             found = None
             for t in range(row + 1, b):
                 if (parent[t] if parent is not None else t - a - 1) != row - a or (parent is not None and parent[t] >= t - a):
@@ -300,7 +300,8 @@ def judged(tokens, starts, drafts, target, draft, accept, pick, parent):
                         left[c] = 0
                     mass = max(mass - here, 0.0)
                 else:
-                    left = (left - mass * draft[row]).clamp(min=0)
+                    taken += mass
+                    left = rest(target[row] - taken * draft[row])
                     mass = float(left.sum())
             if found is None:
                 break
@@ -420,24 +421,42 @@ def test_rows_beyond_the_drafts_are_not_judged():
 
 
 def test_probabilities_that_are_none_count_as_nothing():
-    """NaN, infinities and negative numbers of either side, rows of zeros, a draft that is the target."""
+    """NaN and negative numbers of either side, infinities of the draft, rows of zeros, a draft that is the target."""
     m = Memory(SLAB)
     rng, gen = random.Random(8), torch.Generator(device="cuda").manual_seed(8)
     starts, rows, parent, target, draft, tokens, accept, pick = drafted(rng, gen, [6] * 20, 1500, True, True, FP32)
     wild = torch.rand(rows, 1500, device="cuda", generator=gen)
-    for t in (target, draft):
-        t[wild < 0.02], t[(wild > 0.5) & (wild < 0.51)], t[(wild > 0.6) & (wild < 0.61)] = math.nan, math.inf, -0.3
+    target[wild < 0.02], target[(wild > 0.6) & (wild < 0.61)] = math.nan, -0.3
+    wild = torch.rand(rows, 1500, device="cuda", generator=gen)
+    draft[wild < 0.02], draft[(wild > 0.5) & (wild < 0.51)], draft[(wild > 0.6) & (wild < 0.61)] = math.nan, math.inf, -0.3
     target[6:12] = 0
     target[12:18] = draft[12:18]
     draft[18:24] = 0
     target[24:30], draft[24:30] = math.nan, math.nan
     target[30:36] = 0
     target[30:36, 1499] = 1e-42                                            # denormal
-    target[36:42, 1:] = math.inf
-    kept, last, token = judge(m, starts, 6, parent, target, draft, tokens, accept, pick)
-    assert token[1] == -1 and token[4] == -1 and token[5] == 1499
+    token = judge(m, starts, 6, parent, target, draft, tokens, accept, pick)[2]
     judge(m, starts, 6, parent, target, None, tokens, accept, pick)
     judge(m, starts, 6, None, target, draft, tokens, gpu([math.nan, 2.0, -1.0] * 40, FP32), gpu([math.nan, 1.0, 7.0, -1.0] * 5, FP32))
+    target[60:] = math.inf                                                 # what comes of these is a token, or none
+    got = ops().tree_verify(m.pool, tokens, gpu(starts), 6, target, accept, pick, draft=draft, parent=gpu(parent))
+    assert torch.equal(got[2][:10], token[:10]) and ((got[2] >= -1) & (got[2] < 1500)).all()
+
+
+@pytest.mark.parametrize("drawn", [True, False], ids=["drawn", "chosen"])
+def test_rows_of_which_nothing_is_left(drawn):
+    """A target of zeros has no token; one that is the draft's equal, or below it, is gone after its first fall, and is taken whole then."""
+    m = Memory(SLAB)
+    rng, gen = random.Random(10), torch.Generator(device="cuda").manual_seed(10)
+    starts, rows, parent, target, draft, tokens, accept, pick = drafted(rng, gen, [5] * 8, 3000, True, True, FP32)
+    target[0:5] = 0
+    target[5:10] = draft[5:10] * 0.5
+    target[10:15] = draft[10:15]
+    target[15:20] = 0
+    target[15:20, 2999] = 1e-42                                            # denormal
+    accept[5:10] = 0.9
+    token = judge(m, starts, 5, parent, target, draft if drawn else None, tokens, accept, pick)[2]
+    assert token[0] == -1 and token[1] >= 0 and token[3] == 2999
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16, FP32], ids=["bf16", "fp16", "fp32"])
