@@ -32,6 +32,8 @@ def _refuse(what):
 def _ints(name, t, dtype, dims, device):
     """A contiguous tensor of whole numbers on the GPU. (What is wrong is put into words only when something is: these calls are made in
     loops that wait for them.)"""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.dim() == dims and t.is_contiguous():
+        return
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == dims and t.is_contiguous()):
         _refuse(f"{name}: a contiguous {dtype} tensor of {dims} dimensions on the GPU is needed")
     if t.device != device:
@@ -40,6 +42,8 @@ def _ints(name, t, dtype, dims, device):
 
 def _rows(name, t, dtype, shape, device):
     """A tensor of elements whose rows are contiguous."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape and t.stride(-1) == 1 and not t.requires_grad:
+        return
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.device == device):
         _refuse(f"{name}: a {dtype} tensor on {device} is needed")
     if t.shape != shape:
@@ -266,7 +270,7 @@ def linear4_apply(weights, x, base=None, out=None):
     if base is not None:
         _rows("base", base, dtype, shape, dev)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
+        out = x.new_empty(shape)
     else:
         _rows("out", out, dtype, shape, dev)
     one = rows <= 1  # a single row's stride means nothing
@@ -301,6 +305,7 @@ class Rotation:
         self.freqs = torch.as_tensor(freqs, dtype=torch.float32).to(on).contiguous()
         if self.freqs.dim() != 1:
             _refuse("freqs has one dimension")
+        self.rot, self.axis_at = 2 * pairs, None if self.axis is None else self.axis.data_ptr()
 
 
 def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=None, q_out=None, k_out=None):
@@ -309,49 +314,54 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
 
     q: tokens x heads x dim; k: tokens x its heads x dim. positions: int32, tokens, or tokens x axes where there are several. q_out and k_out may
     be q and k."""
-    pool, dim = rotation.pool, rotation.dim
+    pool, dim, freqs = rotation.pool, rotation.dim, rotation.freqs
     dev = _device("q", q, pool)
-    dtype = q.dtype
-    if q.dim() != 3 or dtype not in TYPES:
+    dtype, shape = q.dtype, q.shape
+    if len(shape) != 3 or dtype not in TYPES:
         _refuse("q has three dimensions of bfloat16 or float16")
-    tokens, heads, _ = shape = q.shape
+    tokens, heads, _ = shape
     _rows("q", q, dtype, (tokens, heads, dim), dev)
-    _ints("positions", positions, torch.int32, positions.dim(), dev)
-    dims = positions.dim()
-    if dims not in (1, 2) or positions.shape[0] != tokens or (positions.shape[1] if dims == 2 else 1) < rotation.axes:
+    at = positions.shape
+    _ints("positions", positions, torch.int32, len(at), dev)
+    axes = at[1] if len(at) == 2 else 1
+    if len(at) not in (1, 2) or at[0] != tokens or axes < rotation.axes:
         _refuse("positions has a row for every token, and a column for every axis")
-    if rotation.freqs.device != dev:
+    if freqs.device != dev:
         _refuse("q lies on another GPU than the rotation")
     flags = ft.ROTATE_NEIGHBOURS if rotation.neighbours else 0
+    q_by = k_by = None
     if eps is not None:
         flags |= ft.ROTATE_NORM
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None:
-                _rows(name, w, dtype, (dim,), dev)
+        if q_weight is not None:
+            _rows("q_weight", q_weight, dtype, (dim,), dev)
+            q_by = q_weight.data_ptr()
+        if k_weight is not None:
+            _rows("k_weight", k_weight, dtype, (dim,), dev)
+            k_by = k_weight.data_ptr()
     elif q_weight is not None or k_weight is not None:
         _refuse("weights belong to a norm, which asks for eps")
+    else:
+        eps = 0.0
     if q_out is None:
-        q_out = torch.empty(shape, dtype=dtype, device=dev)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _rows("q_out", q_out, dtype, shape, dev)
     qs, os = q.stride(), q_out.stride()
-    kv_heads, ks, kos = 0, (0, 0), (0, 0)
+    k_at, k_to, kv_heads, ks, kos = None, None, 0, (0, 0), (0, 0)
     if k is not None:
         if not isinstance(k, torch.Tensor) or k.dim() != 3:
             _refuse("k has three dimensions")
         kv_heads = k.shape[1]
         _rows("k", k, dtype, (tokens, kv_heads, dim), dev)
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=dtype, device=dev)
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         else:
             _rows("k_out", k_out, dtype, k.shape, dev)
-        ks, kos = k.stride(), k_out.stride()
+        k_at, k_to, ks, kos = k.data_ptr(), k_out.data_ptr(), k.stride(), k_out.stride()
     elif k_out is not None:
         _refuse("there are no keys for k_out")
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    call = ft.RotateCall(q.data_ptr(), at(k), q_out.data_ptr(), at(k_out), at(q_weight), at(k_weight), positions.data_ptr(), rotation.freqs.data_ptr(),
-                         at(rotation.axis), qs[0], qs[1], ks[0], ks[1], os[0], os[1], kos[0], kos[1], tokens, heads, kv_heads, dim,
-                         2 * rotation.freqs.shape[0], positions.shape[1] if dims == 2 else 1, TYPES[dtype], flags, 0.0 if eps is None else eps, 0)
+    call = ft.RotateCall(q.data_ptr(), k_at, q_out.data_ptr(), k_to, q_by, k_by, positions.data_ptr(), freqs.data_ptr(), rotation.axis_at, qs[0], qs[1],
+                         ks[0], ks[1], os[0], os[1], kos[0], kos[1], tokens, heads, kv_heads, dim, rotation.rot, axes, TYPES[dtype], flags, eps, 0)
     ft.rotate_heads(pool, call, _stream(dev.index))
     return q_out, k_out
 
@@ -384,9 +394,7 @@ def tree_verify(pool, tokens, starts, drafts, target, accept, pick, draft=None, 
         _ints("parent", parent, torch.int32, 1, dev)
         if parent.shape[0] != rows:
             _refuse("parent has an entry for every row")
-    keep = torch.empty(rows, dtype=torch.uint8, device=dev)
-    last = torch.empty(requests, dtype=torch.int32, device=dev)
-    token = torch.empty(requests, dtype=torch.int64, device=dev)
+    keep, last, token = torch.empty(rows, dtype=torch.uint8, device=dev), starts.new_empty(requests), tokens.new_empty(requests)
     one = rows <= 1
     call = ft.VerifyCall(tokens.data_ptr(), starts.data_ptr(), None if parent is None else parent.data_ptr(), target.data_ptr(),
                          None if draft is None else draft.data_ptr(), accept.data_ptr(), pick.data_ptr(), keep.data_ptr(), last.data_ptr(), token.data_ptr(),
