@@ -26,22 +26,23 @@ __device__ inline Words4 load_codes(const uint8_t *p) {
   const P q = (P)global(p);
   return Words4{q->w[0], q->w[1], q->w[2], q->w[3]};
 }
-// the same where a row may end in between: zeros behind it
-__device__ inline Words4 load_codes(const uint8_t *row, uint32_t at, uint32_t row_bytes) {
-  if (at + 16 <= row_bytes) return load_codes(row + at);
-  Words4 out{0, 0, 0, 0};
-#pragma unroll
-  for (uint32_t i = 0; i < 16; ++i)
-    if (at + i < row_bytes) out[i / 4] |= (uint32_t)row[at + i] << 8 * (i % 4);
-  return out;
+// 16 bytes without the first `bytes`, and zeros behind
+__device__ inline Words4 without(Words4 v, uint32_t bytes) {
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  if (bytes >= 8) {
+    lo = hi;
+    hi = 0;
+  }
+  if (bytes >= 16) lo = 0;
+  const uint32_t by = 8 * (bytes % 8);
+  lo = lo >> by | hi << 1 << (63 - by);
+  hi >>= by;
+  return Words4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
-__device__ inline Words4 load_elements(const uint16_t *row, uint32_t at, uint32_t width) {
-  if (at + 8 <= width) return load16(row + at);
-  Words4 out{0, 0, 0, 0};
-#pragma unroll
-  for (uint32_t i = 0; i < 8; ++i)
-    if (at + i < width) out[i / 2] |= (uint32_t)row[at + i] << 16 * (i % 2);
-  return out;
+// Bytes [at, at + 16) of `size`, 16 or more, from p: zeros behind the last one, and nothing read there.
+__device__ inline Words4 load_upto(const void *p, uint64_t at, uint64_t size) {
+  const uint64_t from = at + 16 <= size ? at : size - 16;
+  return without(load_codes(static_cast<const uint8_t *>(p) + from), at - from < 16 ? (uint32_t)(at - from) : 16);
 }
 
 // Eight codes as numbers, in the order 0, 4, 1, 5, 2, 6, 3, 7.
@@ -51,18 +52,19 @@ template <>
 struct Code<Bf16> {
   static constexpr float kMore = 128;
   static constexpr uint32_t kOnes = 0x3f803f80;
-  static __device__ Words4 numbers(uint32_t w) {
-    constexpr uint32_t mask = 0x000f000f, more = 0x43004300;
-    return Words4{(w & mask) | more, ((w >> 4) & mask) | more, ((w >> 8) & mask) | more, ((w >> 12) & mask) | more};
+  static constexpr uint32_t kMask = 0x000f000f, kExponent = 0x43004300;
+  // (the exponents come in a register: one instruction does not take two constants)
+  static __device__ Words4 numbers(uint32_t w, uint32_t more) {
+    return Words4{(w & kMask) | more, ((w >> 4) & kMask) | more, ((w >> 8) & kMask) | more, ((w >> 12) & kMask) | more};
   }
 };
 template <>
 struct Code<Fp16> {
   static constexpr float kMore = 64;
   static constexpr uint32_t kOnes = 0x3c003c00;
-  static __device__ Words4 numbers(uint32_t w) {
-    constexpr uint32_t mask = 0x00f000f0, more = 0x54005400;
-    return Words4{((w << 4) & mask) | more, (w & mask) | more, ((w >> 4) & mask) | more, ((w >> 8) & mask) | more};
+  static constexpr uint32_t kMask = 0x00f000f0, kExponent = 0x54005400;
+  static __device__ Words4 numbers(uint32_t w, uint32_t more) {
+    return Words4{((w << 4) & kMask) | more, (w & kMask) | more, ((w >> 4) & kMask) | more, ((w >> 8) & kMask) | more};
   }
 };
 
@@ -93,6 +95,8 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
                                 Floats4 (&acc)[NT][TT]) {
   const Words4 ones{Code<T>::kOnes, Code<T>::kOnes, Code<T>::kOnes, Code<T>::kOnes};
   const Floats4 nothing{0, 0, 0, 0};
+  uint32_t exponent = Code<T>::kExponent;
+  asm volatile("" : "+v"(exponent));
   Floats4 products[NT][TT], sums[TT];
   const auto add = [&](uint32_t group) {
 #pragma unroll
@@ -115,7 +119,7 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
 #pragma unroll
     for (int tt = 0; tt < TT; ++tt) a[tt] = x(tt, s);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) b[i] = Code<T>::numbers(codes[i][s]);
+    for (int i = 0; i < NT; ++i) b[i] = Code<T>::numbers(codes[i][s], exponent);
     if (SG != 0) {
 #pragma unroll
       for (int tt = 0; tt < TT; ++tt) {
@@ -146,12 +150,6 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
   }
 }
 
-template <uint32_t D>
-struct Known {
-  static constexpr uint32_t d = D;
-  static __device__ uint32_t of(uint32_t n) { return n / D; }
-};
-
 // A barrier for shared memory alone: loads from global memory stay on their way.
 __device__ inline void fence() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -163,26 +161,37 @@ __device__ inline void fence() {
 __host__ __device__ inline uint32_t scale_stride(uint32_t groups) { return 4 * ((groups + 1) / 2 | 1); }
 __host__ __device__ inline uint32_t zero_stride(uint32_t groups) { return 4 * ((groups + 3) / 4 | 1); }
 
-// Scales and zeros of rows n0 to n0 + count - 1, groups g0 to g0 + groups - 1, to shared memory.
-template <class D>  // what has `d` and of()
-__device__ inline void bring_scales(const Linear4View &w, uint32_t n0, uint32_t count, uint32_t g0, D groups, char *scales, char *zeros) {
-  for (uint32_t i = threadIdx.x; i < count * groups.d; i += blockDim.x) {
-    const uint32_t r = groups.of(i), n = n0 + r < w.width_out ? n0 + r : w.width_out - 1, j = i - r * groups.d, at = g0 + j < w.groups ? g0 + j : w.groups - 1;
-    *reinterpret_cast<uint16_t *>(scales + r * scale_stride(groups.d) + 2 * j) = w.scales[(uint64_t)n * w.groups + at];
-    if (w.zeros != nullptr) zeros[r * zero_stride(groups.d) + j] = (char)w.zeros[(uint64_t)n * w.groups + at];
+// Scales and zeros of rows n0 to n0 + ROWS - 1, groups g0 to g0 + groups - 1, to shared memory, 16 bytes a thread. (All rows' scales together are 16 bytes at least, and so are their zeros.)
+template <int ROWS, int THREADS>
+struct Scales {
+  __device__ static void bring(const Linear4View &w, uint32_t n0, uint32_t g0, uint32_t groups, char *scales, char *zeros) {
+    some(reinterpret_cast<const char *>(w.scales), 2, w, n0, g0, groups, scales, scale_stride(groups));
+    if (w.zeros != nullptr) some(reinterpret_cast<const char *>(w.zeros), 1, w, n0, g0, groups, zeros, zero_stride(groups));
   }
-}
+  __device__ static void some(const char *from, uint32_t size, const Linear4View &w, uint32_t n0, uint32_t g0, uint32_t groups, char *to, uint32_t stride) {
+    const uint32_t pieces = (groups * size + 15) / 16;  // of a row
+    const uint64_t all = (uint64_t)w.width_out * w.groups * size;
+    for (uint32_t i = threadIdx.x; i < ROWS * pieces; i += THREADS) {
+      const uint32_t r = i % ROWS, j = i / ROWS, n = n0 + r < w.width_out ? n0 + r : w.width_out - 1;
+      const Words4 v = load_upto(from, ((uint64_t)n * w.groups + g0) * size + 16 * j, all);
+      uint32_t *out = reinterpret_cast<uint32_t *>(to + r * stride + 16 * j);
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k)
+        if (16 * j + 4 * k < stride) out[k] = v[k];
+    }
+  }
+};
 
 // 16 rows of weights to a workgroup, and 16 rows of x, 2 XL of which there are. Its wavefronts have every KW-th 256 elements and add up what they
 // have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces, and turns it round in shared memory of
 // its own.
 template <class T, int SG, int XL, int KW>
-__global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c, Divisor groups) {
+__global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
   constexpr int R = 2 * XL, kDepth = XL <= 2 ? 4 : 2;
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
   extern __shared__ char scales_lds[];
-  char *zeros_lds = scales_lds + 16 * scale_stride(groups.d);
+  char *zeros_lds = scales_lds + 16 * scale_stride(w.groups);
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t n0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
   // where this lane's pieces come from, and where they go
@@ -213,13 +222,13 @@ __global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View 
   if (wave < pieces)
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) load(codes[i], x[i], wave + i * KW < pieces ? wave + i * KW : pieces - 1);
-  bring_scales(w, n0, 16, 0, groups, scales_lds, zeros_lds);
+  Scales<16, 64 * KW>::bring(w, n0, 0, w.groups, scales_lds, zeros_lds);
   __syncthreads();
   Floats4 acc[1][1] = {{Floats4{0, 0, 0, 0}}};
   // (of elements behind a row's last, which are zeros, the last group's)
-  const auto there = [&](uint32_t group) { return group < groups.d ? group : groups.d - 1; };
-  const auto scale = [&](int, uint32_t group) { return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + col * scale_stride(groups.d) + 2 * there(group))); };
-  const auto zero = [&](int, uint32_t group) { return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[col * zero_stride(groups.d) + there(group)]; };
+  const auto there = [&](uint32_t group) { return group < w.groups ? group : w.groups - 1; };
+  const auto scale = [&](int, uint32_t group) { return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + col * scale_stride(w.groups) + 2 * there(group))); };
+  const auto zero = [&](int, uint32_t group) { return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[col * zero_stride(w.groups) + there(group)]; };
   const auto use = [&](const Words4 (&my_codes)[2], const Words4 (&my_x)[XL], uint32_t piece) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) codes_lds[wave][to[i]] = my_codes[i];
@@ -244,9 +253,9 @@ __global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View 
   }
   if (pieces < all && wave == pieces % KW) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) codes[0][i] = load_codes(from[i], 128 * pieces + 16 * (lane % 8), w.row_bytes);
+    for (int i = 0; i < 2; ++i) codes[0][i] = load_upto(from[i], 128 * pieces + 16 * (lane % 8), w.row_bytes);
 #pragma unroll
-    for (int i = 0; i < XL; ++i) x[0][i] = load_elements(x_from[i], 256 * pieces + 8 * (lane % 32), w.width_in);
+    for (int i = 0; i < XL; ++i) x[0][i] = load_upto(x_from[i], 512 * pieces + 16 * (lane % 32), 2 * w.width_in);
     use(codes[0], x[0], pieces);
   }
 #pragma unroll
@@ -267,55 +276,40 @@ __global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View 
 // multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied.
 template <class T, int SG, int TT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_linear4_wide_kernel(Linear4View w, ft_linear4_call c) {
-  constexpr uint32_t NT = 2, kGroups = 64, kDepth = 3;
+  constexpr uint32_t NT = 2, kGroups = 64, kDepth = TT == 4 ? 3 : 4;  // (chunks that are on their way)
   __shared__ Words4 x_lds[2][TT * 16 * 32], codes_lds[8][NT][16 * 4];
   __shared__ char scales_lds[128 * 4 * (kGroups / 2 | 1)], zeros_lds[128 * 4 * (kGroups / 4 | 1)];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t kw = wave / 4, nw = wave % 4, n0 = blockIdx.x * 128, t0 = blockIdx.y * (16 * TT);
-  const uint8_t *from[NT];
+  // offsets in bytes from the workgroup's first row: of 128 rows of weights less than 2^30, of 64 rows of x less than 2^31
+  const uint8_t *weights = w.weights + (uint64_t)n0 * w.row_bytes;
+  const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(c.x) + t0 * c.x_stride);
+  uint32_t from[NT], x_from[TT], x_to[TT];
 #pragma unroll
   for (uint32_t i = 0; i < NT; ++i) {
-    const uint32_t r = 32 * nw + 16 * i + lane / 4, n = n0 + r < w.width_out ? n0 + r : w.width_out - 1;
-    from[i] = w.weights + (uint64_t)n * w.row_bytes + 64 * kw + 16 * (lane % 4);
+    const uint32_t r = 32 * nw + 16 * i + lane / 4;
+    from[i] = (n0 + r < w.width_out ? r : w.width_out - 1 - n0) * w.row_bytes;
   }
-  const uint32_t to = lane / 4 * 4 + (lane % 4 ^ lane / 16);
-  const uint16_t *x_from[TT];
-  uint32_t x_to[TT];
+  const uint32_t to = lane / 4 * 4 + (lane % 4 ^ lane / 16), piece = 64 * kw + 16 * (lane % 4), x_piece = 16 * (threadIdx.x % 32);
 #pragma unroll
   for (uint32_t i = 0; i < TT; ++i) {
-    const uint32_t r = 16 * i + threadIdx.x / 32, t = t0 + r < c.rows ? t0 + r : c.rows - 1;
-    x_from[i] = static_cast<const uint16_t *>(c.x) + t * c.x_stride;
+    const uint32_t r = 16 * i + threadIdx.x / 32;
+    x_from[i] = (t0 + r < c.rows ? r : c.rows - 1 - t0) * (2 * (uint32_t)c.x_stride);
     x_to[i] = r * 32 + (threadIdx.x % 32 ^ r % 16);
   }
-  const uint32_t x_piece = 8 * (threadIdx.x % 32);
-  const uint32_t whole = w.width_in / 256, all = (w.width_in + 255) / 256, last = all - 1;
-  Words4 codes[kDepth][NT], x[TT];
-  const auto load = [&](Words4 (&out)[NT], uint32_t chunk) {
-    if (chunk > last) chunk = last;
-    if (chunk < whole) {
-#pragma unroll
-      for (uint32_t i = 0; i < NT; ++i) out[i] = load_codes(from[i] + 128 * chunk);
-    } else {
-#pragma unroll
-      for (uint32_t i = 0; i < NT; ++i) {
-        const uint32_t at = 128 * chunk + 64 * kw + 16 * (lane % 4);
-        out[i] = load_codes(from[i] - (64 * kw + 16 * (lane % 4)), at, w.row_bytes);
-      }
-    }
+  const uint32_t whole = w.width_in / 256;  // and a part
+  struct Chunk {
+    Words4 codes[NT], x[TT];
   };
-  const auto load_x = [&](uint32_t chunk) {
-    if (chunk > last) chunk = last;
-    if (chunk < whole) {
+  const auto load = [&](Chunk &f, uint32_t chunk) {
+    if (chunk >= whole) chunk = whole - 1;
+    const uint8_t *codes_at = weights + 128 * chunk;
+    const char *x_at = rows + 512 * chunk;
 #pragma unroll
-      for (int i = 0; i < TT; ++i) x[i] = load16(x_from[i] + 256 * chunk + x_piece);
-    } else {
+    for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_codes(codes_at + (from[i] + piece));
 #pragma unroll
-      for (int i = 0; i < TT; ++i) x[i] = load_elements(x_from[i], 256 * chunk + x_piece, w.width_in);
-    }
+    for (int i = 0; i < TT; ++i) f.x[i] = load16(x_at + (x_from[i] + x_piece));
   };
-  load_x(0);
-#pragma unroll
-  for (uint32_t i = 0; i < kDepth; ++i) load(codes[i], i);
   Floats4 acc[NT][TT];
 #pragma unroll
   for (uint32_t i = 0; i < NT; ++i)
@@ -323,28 +317,27 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int tt = 0; tt < TT; ++tt) acc[i][tt] = Floats4{0, 0, 0, 0};
   uint32_t g0 = 0;
   const uint32_t part = w.group.d / (256 / kGroups);  // chunks whose scales are in shared memory together
-  const auto use = [&](Words4 (&mine)[NT], uint32_t chunk) {
-    if (chunk % part == 0) {
-      fence();  // those before are no longer read
-      g0 = chunk / part * kGroups;
-      bring_scales(w, n0, 128, g0, Known<kGroups>(), scales_lds, zeros_lds);
-    }
-    Words4 *here = x_lds[chunk & 1];
+  const auto scales_of = [&](uint32_t chunk) {
+    if (chunk % part != 0) return;
+    fence();  // those before are no longer read
+    g0 = chunk / part * kGroups;
+    Scales<128, 512>::bring(w, n0, g0, kGroups, scales_lds, zeros_lds);
+  };
+  const auto put = [&](const Chunk &f, uint32_t chunk) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i) here[x_to[i]] = in_order(x[i]);
-    load_x(chunk + 1);
+    for (int i = 0; i < TT; ++i) x_lds[chunk & 1][x_to[i]] = in_order(f.x[i]);
 #pragma unroll
-    for (uint32_t i = 0; i < NT; ++i) codes_lds[wave][i][to] = mine[i];
-    load(mine, chunk + kDepth);
+    for (uint32_t i = 0; i < NT; ++i) codes_lds[wave][i][to] = f.codes[i];
+  };
+  const auto use = [&](uint32_t chunk) {
     fence();
-    const uint32_t k0 = 256 * chunk + kBlock * kw;
-    if (k0 >= w.width_in) return;
+    const Words4 *here = x_lds[chunk & 1];
     const uint32_t r = 32 * nw + col;
     Words4 turn[NT];
 #pragma unroll
     for (uint32_t i = 0; i < NT; ++i) turn[i] = codes_lds[wave][i][col * 4 + (g ^ col / 4)];
     multiply<T, SG, NT, TT>(
-        w, turn, k0, g, [&](int tt, int s) { return here[(16 * tt + col) * 32 + (16 * kw + element<SG>(g, s) / 8 ^ col)]; },
+        w, turn, 256 * chunk + kBlock * kw, g, [&](int tt, int s) { return here[(16 * tt + col) * 32 + (16 * kw + element<SG>(g, s) / 8 ^ col)]; },
         [&](int i, uint32_t group) {
           return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + (r + 16 * i) * scale_stride(kGroups) + 2 * (group - g0)));
         },
@@ -353,10 +346,30 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         },
         acc);
   };
-  for (uint32_t chunk = 0; chunk < all; chunk += kDepth) {
+  if (whole != 0) {
+    Chunk f[kDepth];
 #pragma unroll
-    for (uint32_t i = 0; i < kDepth; ++i)
-      if (chunk + i < all) use(codes[i], chunk + i);
+    for (uint32_t i = 0; i < kDepth; ++i) load(f[i], i);
+    for (uint32_t chunk = 0; chunk < whole; chunk += kDepth) {
+#pragma unroll
+      for (uint32_t i = 0; i < kDepth; ++i) {
+        if (chunk + i >= whole) break;
+        scales_of(chunk + i);
+        put(f[i], chunk + i);
+        load(f[i], chunk + i + kDepth);
+        use(chunk + i);
+      }
+    }
+  }
+  if (256 * whole < w.width_in) {
+    scales_of(whole);
+    Chunk f;
+#pragma unroll
+    for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_upto(weights + from[i], 128 * whole + piece, w.row_bytes);
+#pragma unroll
+    for (int i = 0; i < TT; ++i) f.x[i] = load_upto(rows + x_from[i], 512 * whole + x_piece, 2 * w.width_in);
+    put(f, whole);
+    use(whole);
   }
   // the two halves of the sums
   fence();
@@ -431,8 +444,7 @@ namespace {
 template <class T, int SG, int XL>
 void launch_narrow(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
   const dim3 grid((w.width_out + 15) / 16, (c.rows + 15) / 16);
-  hipLaunchKernelGGL((ft_linear4_narrow_kernel<T, SG, XL, 8>), grid, dim3(512), 16 * (scale_stride(w.groups) + zero_stride(w.groups)), stream, w, c,
-                     Divisor(w.groups));
+  hipLaunchKernelGGL((ft_linear4_narrow_kernel<T, SG, XL, 8>), grid, dim3(512), 16 * (scale_stride(w.groups) + zero_stride(w.groups)), stream, w, c);
 }
 
 template <class T, int SG, int TT>
@@ -443,7 +455,9 @@ void launch_wide(const Linear4View &w, const ft_linear4_call &c, hipStream_t str
 
 template <class T, int SG>
 void launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
-  if (c.rows > 32) launch_wide<T, SG, 4>(w, c, stream);
+  const bool far = c.rows > 1 && c.x_stride >= 1u << 24;  // offsets of 32 bits would not reach
+  if (far) launch_narrow<T, SG, 8>(w, c, stream);
+  else if (c.rows > 32) launch_wide<T, SG, 4>(w, c, stream);
   else if (c.rows > 16) launch_wide<T, SG, 2>(w, c, stream);
   else if (w.width_out >= 16384) launch_wide<T, SG, 1>(w, c, stream);
   else if (c.rows > 8) launch_narrow<T, SG, 8>(w, c, stream);
@@ -454,7 +468,7 @@ void launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) 
 template <class T>
 hipError_t launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
   const uint32_t group = w.group.d;
-  if (group < 32 || w.groups > kMostGroups) {
+  if (group < 32 || w.groups > kMostGroups || w.width_in < 32 || (uint64_t)w.width_out * w.groups < 16) {  // (loads are of 16 bytes)
     const uint32_t parts = (c.rows + 7) / 8;
     hipLaunchKernelGGL(ft_linear4_any_kernel<T>, dim3((w.width_out + 3) / 4, parts < 1024 ? parts : 1024), dim3(256), 0, stream, w, c);
   } else if (group % 128 == 0) {
