@@ -98,16 +98,35 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
   uint32_t exponent = Code<T>::kExponent;
   asm volatile("" : "+v"(exponent));
   Floats4 products[NT][TT], sums[TT];
-  const auto add = [&](uint32_t group) {
+  const auto add = [&](const float (&by)[NT], const float (&more)[NT]) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const float by = scale(i, group), more = -by * (Code<T>::kMore + zero(i, group));
 #pragma unroll
       for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][tt][j] = __builtin_fmaf(by, products[i][tt][j], __builtin_fmaf(more, sums[tt][j], acc[i][tt][j]));
+        for (int j = 0; j < 4; ++j) acc[i][tt][j] = __builtin_fmaf(by[i], products[i][tt][j], __builtin_fmaf(more[i], sums[tt][j], acc[i][tt][j]));
     }
   };
+  // all that comes from shared memory is asked for before the first product, where it fits the registers
+  constexpr bool ahead = TT <= 2;
+  Words4 early[ahead ? 4 : 1][TT];
+  if (ahead)
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt) early[ahead ? s : 0][tt] = x(tt, s);
+  const auto factors = [&](uint32_t group, float (&by)[NT], float (&more)[NT]) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      by[i] = scale(i, group);
+      more[i] = -by[i] * (Code<T>::kMore + zero(i, group));
+    }
+  };
+  constexpr int G = SG == 0 ? 1 : SG;
+  float by[G][NT], more[G][NT];
+  if (SG != 0)
+#pragma unroll
+    for (int j = 0; j < G; ++j) factors(w.group.of(k0 + 128 / G * j), by[j], more[j]);
   if (SG != 1)
 #pragma unroll
     for (int i = 0; i < NT; ++i) codes[i] = turned(codes[i]);
@@ -117,7 +136,7 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
     const uint32_t k = k0 + 32 * s;
     Words4 a[TT], b[NT];
 #pragma unroll
-    for (int tt = 0; tt < TT; ++tt) a[tt] = x(tt, s);
+    for (int tt = 0; tt < TT; ++tt) a[tt] = ahead ? early[ahead ? s : 0][tt] : x(tt, s);
 #pragma unroll
     for (int i = 0; i < NT; ++i) b[i] = Code<T>::numbers(codes[i][s], exponent);
     if (SG != 0) {
@@ -127,10 +146,13 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
 #pragma unroll
         for (int i = 0; i < NT; ++i) products[i][tt] = T::mfma(a[tt], b[i], s % each == 0 ? nothing : products[i][tt]);
       }
-      if ((s + 1) % each == 0) add(w.group.of(k + 32 - 32 * each));
+      if ((s + 1) % each == 0) add(by[s / each % G], more[s / each % G]);
     } else {
       // a lane's eight elements are in one group, and 32 in two at most
       const uint32_t first = w.group.of(k), last = w.group.of(k + 31);
+      float by2[2][NT], more2[2][NT];
+      factors(first, by2[0], more2[0]);
+      factors(last, by2[1], more2[1]);
       const bool mine = w.group.of(k + 8 * g) == first;
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
@@ -144,7 +166,7 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
 #pragma unroll
           for (int i = 0; i < NT; ++i) products[i][tt] = T::mfma(some, b[i], nothing);
         }
-        add(part == 0 ? first : last);
+        add(by2[part], more2[part]);
       }
     }
   }
@@ -161,130 +183,175 @@ __device__ inline void fence() {
 __host__ __device__ inline uint32_t scale_stride(uint32_t groups) { return 4 * ((groups + 1) / 2 | 1); }
 __host__ __device__ inline uint32_t zero_stride(uint32_t groups) { return 4 * ((groups + 3) / 4 | 1); }
 
-// Scales and zeros of rows n0 to n0 + ROWS - 1, groups g0 to g0 + groups - 1, to shared memory, 16 bytes a thread. (All rows' scales together are 16 bytes at least, and so are their zeros.)
+// Scales or zeros, `size` bytes each, of rows n0 to n0 + ROWS - 1, groups g0 to g0 + groups - 1, to shared memory: a thread asks for 16 bytes, and puts
+// them down when others are on their way; then the rest. (All rows' scales together are 16 bytes at least, and so are their zeros.)
 template <int ROWS, int THREADS>
 struct Scales {
-  __device__ static void bring(const Linear4View &w, uint32_t n0, uint32_t g0, uint32_t groups, char *scales, char *zeros) {
-    some(reinterpret_cast<const char *>(w.scales), 2, w, n0, g0, groups, scales, scale_stride(groups));
-    if (w.zeros != nullptr) some(reinterpret_cast<const char *>(w.zeros), 1, w, n0, g0, groups, zeros, zero_stride(groups));
+  const char *from;
+  uint32_t size, pieces, stride, n0, g0;
+  uint64_t all;
+  Words4 first;
+
+  __device__ Scales(const Linear4View &w, const void *at, uint32_t size, uint32_t n0, uint32_t g0, uint32_t groups, uint32_t stride)
+      : from(static_cast<const char *>(at)), size(size), pieces((groups * size + 15) / 16), stride(stride), n0(n0), g0(g0),
+        all((uint64_t)w.width_out * w.groups * size) {
+    first = piece(w, threadIdx.x < ROWS * pieces ? threadIdx.x : 0);
   }
-  __device__ static void some(const char *from, uint32_t size, const Linear4View &w, uint32_t n0, uint32_t g0, uint32_t groups, char *to, uint32_t stride) {
-    const uint32_t pieces = (groups * size + 15) / 16;  // of a row
-    const uint64_t all = (uint64_t)w.width_out * w.groups * size;
-    for (uint32_t i = threadIdx.x; i < ROWS * pieces; i += THREADS) {
-      const uint32_t r = i % ROWS, j = i / ROWS, n = n0 + r < w.width_out ? n0 + r : w.width_out - 1;
-      const Words4 v = load_upto(from, ((uint64_t)n * w.groups + g0) * size + 16 * j, all);
-      uint32_t *out = reinterpret_cast<uint32_t *>(to + r * stride + 16 * j);
+  __device__ Words4 piece(const Linear4View &w, uint32_t i) const {
+    const uint32_t r = i / pieces, j = i - r * pieces, n = n0 + r < w.width_out ? n0 + r : w.width_out - 1;
+    return load_upto(from, ((uint64_t)n * w.groups + g0) * size + 16 * j, all);
+  }
+  __device__ void put(char *to, uint32_t i, Words4 v) const {
+    const uint32_t r = i / pieces, j = i - r * pieces;
+    uint32_t *out = reinterpret_cast<uint32_t *>(to + r * stride + 16 * j);
 #pragma unroll
-      for (uint32_t k = 0; k < 4; ++k)
-        if (16 * j + 4 * k < stride) out[k] = v[k];
-    }
+    for (uint32_t k = 0; k < 4; ++k)
+      if (16 * j + 4 * k < stride) out[k] = v[k];
+  }
+  __device__ void bring(const Linear4View &w, char *to) const {
+    if (threadIdx.x < ROWS * pieces) put(to, threadIdx.x, first);
+    for (uint32_t i = threadIdx.x + THREADS; i < ROWS * pieces; i += THREADS) put(to, i, piece(w, i));
   }
 };
+
+// Eight neighbouring elements of a row of the result, or `there` of them, from 32 bits, base added.
+template <class T>
+__device__ inline void write8(const ft_linear4_call &c, uint32_t row, uint32_t n, uint32_t there, const float *sums) {
+  uint16_t *out = static_cast<uint16_t *>(c.out) + row * c.out_stride + n;
+  const uint16_t *base = static_cast<const uint16_t *>(c.base) + row * c.base_stride + n;
+  if (there >= 8) {
+    Words4 b{0, 0, 0, 0};
+    if (c.base != nullptr) b = load16(base);
+    Loose4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v.w[i] = T::pack(sums[2 * i] + T::to_float((uint16_t)b[i]), sums[2 * i + 1] + T::to_float((uint16_t)(b[i] >> 16)));
+    *reinterpret_cast<Loose4 *>(out) = v;
+  } else {
+    for (uint32_t i = 0; i < there; ++i) out[i] = T::from_float(sums[i] + (c.base != nullptr ? T::to_float(base[i]) : 0));
+  }
+}
 
 // 16 rows of weights to a workgroup, and 16 rows of x, 2 XL of which there are. Its wavefronts have every KW-th 256 elements and add up what they
 // have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces, and turns it round in shared memory of
 // its own.
 template <class T, int SG, int XL, int KW>
-__global__ __launch_bounds__(64 * KW) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
-  constexpr int R = 2 * XL, kDepth = XL <= 2 ? 4 : 2;
+__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
+  constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
   extern __shared__ char scales_lds[];
   char *zeros_lds = scales_lds + 16 * scale_stride(w.groups);
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t n0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
-  // where this lane's pieces come from, and where they go
-  const uint8_t *from[2];
-  uint32_t to[2];
+  // where this lane's pieces come from, in bytes behind the workgroup's first rows, and where they go
+  const uint8_t *weights = w.weights + (uint64_t)n0 * w.row_bytes;
+  const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(c.x) + t0 * c.x_stride);
+  uint32_t from[2], to[2], x_from[XL], x_to[XL];
 #pragma unroll
   for (uint32_t i = 0; i < 2; ++i) {
-    const uint32_t r = 8 * i + lane / 8, n = n0 + r < w.width_out ? n0 + r : w.width_out - 1;
-    from[i] = w.weights + (uint64_t)n * w.row_bytes;
+    const uint32_t r = 8 * i + lane / 8;
+    from[i] = (n0 + r < w.width_out ? r : w.width_out - 1 - n0) * w.row_bytes + 16 * (lane % 8);
     to[i] = r * 8 + (lane % 8 ^ r >> 1);
   }
-  const uint16_t *x_from[XL];
-  uint32_t x_to[XL];
 #pragma unroll
   for (uint32_t i = 0; i < XL; ++i) {
-    const uint32_t r = 2 * i + lane / 32, t = t0 + r < c.rows ? t0 + r : c.rows - 1;
-    x_from[i] = static_cast<const uint16_t *>(c.x) + t * c.x_stride;
+    const uint32_t r = 2 * i + lane / 32;
+    x_from[i] = (t0 + r < c.rows ? r : c.rows - 1 - t0) * (2 * (uint32_t)c.x_stride) + 16 * (lane % 32);
     x_to[i] = r * 32 + (lane % 32 ^ r);
   }
   const uint32_t pieces = w.width_in / 256, all = (w.width_in + 255) / 256;
+  // of the result a thread has one element at most
+  const uint32_t row = t0 + 4 * (lane / 16) + wave % 4, n = n0 + col;
+  const bool mine = wave < 4 && row < c.rows && n < w.width_out;
+  uint16_t base = 0;
+  if (mine && c.base != nullptr) base = static_cast<const uint16_t *>(c.base)[row * c.base_stride + n];
+  __builtin_amdgcn_sched_barrier(0);
+  const Scales<16, 64 * KW> scales(w, w.scales, 2, n0, 0, w.groups, scale_stride(w.groups));
+  const Scales<16, 64 * KW> zeros(w, w.zeros != nullptr ? static_cast<const void *>(w.zeros) : w.scales, 1, n0, 0, w.groups, zero_stride(w.groups));
   Words4 codes[kDepth][2], x[kDepth][XL];
   const auto load = [&](Words4 (&to_codes)[2], Words4 (&to_x)[XL], uint32_t piece) {
+    const uint8_t *codes_at = weights + 128 * piece;
+    const char *x_at = rows + 512 * piece;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) to_codes[i] = load_codes(from[i] + 128 * piece + 16 * (lane % 8));
+    for (int i = 0; i < 2; ++i) to_codes[i] = load_codes(codes_at + from[i]);
 #pragma unroll
-    for (int i = 0; i < XL; ++i) to_x[i] = load16(x_from[i] + 256 * piece + 8 * (lane % 32));
+    for (int i = 0; i < XL; ++i) to_x[i] = load16(x_at + x_from[i]);
   };
   if (wave < pieces)
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i) load(codes[i], x[i], wave + i * KW < pieces ? wave + i * KW : pieces - 1);
-  Scales<16, 64 * KW>::bring(w, n0, 0, w.groups, scales_lds, zeros_lds);
+    for (int i = 0; i < kDepth; ++i) {
+      load(codes[i], x[i], wave + i * KW < pieces ? wave + i * KW : pieces - 1);
+      __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
+    }
+  scales.bring(w, scales_lds);
+  if (w.zeros != nullptr) zeros.bring(w, zeros_lds);
   __syncthreads();
   Floats4 acc[1][1] = {{Floats4{0, 0, 0, 0}}};
   // (of elements behind a row's last, which are zeros, the last group's)
   const auto there = [&](uint32_t group) { return group < w.groups ? group : w.groups - 1; };
   const auto scale = [&](int, uint32_t group) { return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + col * scale_stride(w.groups) + 2 * there(group))); };
   const auto zero = [&](int, uint32_t group) { return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[col * zero_stride(w.groups) + there(group)]; };
-  const auto use = [&](const Words4 (&my_codes)[2], const Words4 (&my_x)[XL], uint32_t piece) {
+  const auto put = [&](const Words4 (&my_codes)[2], const Words4 (&my_x)[XL]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) codes_lds[wave][to[i]] = my_codes[i];
 #pragma unroll
     for (int i = 0; i < XL; ++i) x_lds[wave][x_to[i]] = in_order(my_x[i]);
-    const uint32_t row = col & (R - 1);
+  };
+  const auto use = [&](uint32_t piece) {
+    const uint32_t x_row = col & (R - 1);
 #pragma unroll
     for (uint32_t block = 0; block < 2; ++block) {
       const uint32_t k0 = 256 * piece + kBlock * block;
       if (k0 >= w.width_in) break;
       Words4 mine[1] = {codes_lds[wave][col * 8 + (4 * block + g ^ col >> 1)]};
-      multiply<T, SG, 1, 1>(w, mine, k0, g, [&](int, int s) { return x_lds[wave][row * 32 + (16 * block + element<SG>(g, s) / 8 ^ row)]; }, scale, zero, acc);
+      multiply<T, SG, 1, 1>(w, mine, k0, g, [&](int, int s) { return x_lds[wave][x_row * 32 + (16 * block + element<SG>(g, s) / 8 ^ x_row)]; }, scale, zero, acc);
     }
   };
-  for (uint32_t p = wave; p < pieces; p += kDepth * KW) {
+  // (Out of the loop from within: a way back to its top that leaves out the last loads would be waited for there as if they were not on their way.)
+  for (uint32_t p = wave;;) {
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i) {
-      if (p + i * KW < pieces) use(codes[i], x[i], p + i * KW);
-      const uint32_t next = p + (i + kDepth) * KW;
-      load(codes[i], x[i], next < pieces ? next : pieces - 1);
+    for (int i = 0; i < kDepth; ++i, p += KW) {
+      if (p >= pieces) goto done;
+      put(codes[i], x[i]);
+      load(codes[i], x[i], p + kDepth * KW < pieces ? p + kDepth * KW : pieces - 1);
+      use(p);
     }
   }
+done:
   if (pieces < all && wave == pieces % KW) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) codes[0][i] = load_upto(from[i], 128 * pieces + 16 * (lane % 8), w.row_bytes);
+    for (int i = 0; i < 2; ++i) codes[0][i] = load_upto(weights + (from[i] - 16 * (lane % 8)), 128 * pieces + 16 * (lane % 8), w.row_bytes);
 #pragma unroll
-    for (int i = 0; i < XL; ++i) x[0][i] = load_upto(x_from[i], 512 * pieces + 16 * (lane % 32), 2 * w.width_in);
-    use(codes[0], x[0], pieces);
+    for (int i = 0; i < XL; ++i) x[0][i] = load_upto(rows + (x_from[i] - 16 * (lane % 32)), 512 * pieces + 16 * (lane % 32), 2 * w.width_in);
+    put(codes[0], x[0]);
+    use(pieces);
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) parts[wave][j][lane] = acc[0][0][j];
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < 256; i += 64 * KW) {
-    const uint32_t l = i % 64, row = t0 + 4 * (l / 16) + i / 64, n = n0 + l % 16;
-    if (row >= c.rows || n >= w.width_out) continue;
-    float sum = 0;
+  static_assert(KW >= 4);
+  if (!mine) return;
+  float sum = 0;
 #pragma unroll
-    for (int k = 0; k < KW; ++k) sum += parts[k][i / 64][l];
-    if (c.base != nullptr) sum += T::to_float(static_cast<const uint16_t *>(c.base)[row * c.base_stride + n]);
-    static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum);
-  }
+  for (int k = 0; k < KW; ++k) sum += parts[k][wave][lane];
+  static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum + T::to_float(base));
 }
 
 // 128 rows of weights to a workgroup - 32 to a wavefront, and two wavefronts take turns along the rows -, and 16 TT rows of x, which all wavefronts
 // multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied.
-template <class T, int SG, int TT>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void ft_linear4_wide_kernel(Linear4View w, ft_linear4_call c) {
-  constexpr uint32_t NT = 2, kGroups = 64, kDepth = TT == 4 ? 3 : 4;  // (chunks that are on their way)
-  __shared__ Words4 x_lds[2][TT * 16 * 32], codes_lds[8][NT][16 * 4];
-  __shared__ char scales_lds[128 * 4 * (kGroups / 2 | 1)], zeros_lds[128 * 4 * (kGroups / 4 | 1)];
+template <class T, int SG, int TT, int NW>
+__global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) void ft_linear4_wide_kernel(Linear4View w, ft_linear4_call c) {
+  constexpr uint32_t NT = 2, kGroups = 64, kRows = 32 * NW, XP = TT * 4 / NW;
+  constexpr uint32_t kDepth = TT == 4 ? 2 : 3;  // (chunks that are on their way)
+  __shared__ Words4 x_lds[2][TT * 16 * 32], codes_lds[2 * NW][NT][16 * 4];
+  __shared__ char scales_lds[kRows * 4 * (kGroups / 2 | 1)], zeros_lds[kRows * 4 * (kGroups / 4 | 1)];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
-  const uint32_t kw = wave / 4, nw = wave % 4, n0 = blockIdx.x * 128, t0 = blockIdx.y * (16 * TT);
+  const uint32_t kw = wave / NW, nw = wave % NW, n0 = blockIdx.x * kRows, t0 = blockIdx.y * (16 * TT);
   // offsets in bytes from the workgroup's first row: of 128 rows of weights less than 2^30, of 64 rows of x less than 2^31
   const uint8_t *weights = w.weights + (uint64_t)n0 * w.row_bytes;
   const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(c.x) + t0 * c.x_stride);
-  uint32_t from[NT], x_from[TT], x_to[TT];
+  uint32_t from[NT], x_from[XP], x_to[XP];
 #pragma unroll
   for (uint32_t i = 0; i < NT; ++i) {
     const uint32_t r = 32 * nw + 16 * i + lane / 4;
@@ -292,23 +359,23 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
   const uint32_t to = lane / 4 * 4 + (lane % 4 ^ lane / 16), piece = 64 * kw + 16 * (lane % 4), x_piece = 16 * (threadIdx.x % 32);
 #pragma unroll
-  for (uint32_t i = 0; i < TT; ++i) {
-    const uint32_t r = 16 * i + threadIdx.x / 32;
+  for (uint32_t i = 0; i < XP; ++i) {
+    const uint32_t r = 4 * NW * i + threadIdx.x / 32;
     x_from[i] = (t0 + r < c.rows ? r : c.rows - 1 - t0) * (2 * (uint32_t)c.x_stride);
     x_to[i] = r * 32 + (threadIdx.x % 32 ^ r % 16);
   }
   const uint32_t whole = w.width_in / 256;  // and a part
   struct Chunk {
-    Words4 codes[NT], x[TT];
+    Words4 codes[NT], x[XP];
   };
-  const auto load = [&](Chunk &f, uint32_t chunk) {
-    if (chunk >= whole) chunk = whole - 1;
+  const auto load = [&](Chunk &f, uint32_t chunk, uint32_t end) {
+    if (chunk >= end) chunk = end - 1;
     const uint8_t *codes_at = weights + 128 * chunk;
     const char *x_at = rows + 512 * chunk;
 #pragma unroll
     for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_codes(codes_at + (from[i] + piece));
 #pragma unroll
-    for (int i = 0; i < TT; ++i) f.x[i] = load16(x_at + (x_from[i] + x_piece));
+    for (uint32_t i = 0; i < XP; ++i) f.x[i] = load16(x_at + (x_from[i] + x_piece));
   };
   Floats4 acc[NT][TT];
 #pragma unroll
@@ -317,15 +384,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int tt = 0; tt < TT; ++tt) acc[i][tt] = Floats4{0, 0, 0, 0};
   uint32_t g0 = 0;
   const uint32_t part = w.group.d / (256 / kGroups);  // chunks whose scales are in shared memory together
-  const auto scales_of = [&](uint32_t chunk) {
-    if (chunk % part != 0) return;
-    fence();  // those before are no longer read
-    g0 = chunk / part * kGroups;
-    Scales<128, 512>::bring(w, n0, g0, kGroups, scales_lds, zeros_lds);
-  };
   const auto put = [&](const Chunk &f, uint32_t chunk) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i) x_lds[chunk & 1][x_to[i]] = in_order(f.x[i]);
+    for (uint32_t i = 0; i < XP; ++i) x_lds[chunk & 1][x_to[i]] = in_order(f.x[i]);
 #pragma unroll
     for (uint32_t i = 0; i < NT; ++i) codes_lds[wave][i][to] = f.codes[i];
   };
@@ -346,57 +407,66 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         },
         acc);
   };
-  if (whole != 0) {
+  for (uint32_t begin = 0; 256 * begin < w.width_in; begin += part) {
+    if (begin != 0) fence();  // the scales before are no longer read
+    g0 = begin / part * kGroups;
+    const uint32_t end = begin + part < whole ? begin + part : whole;
     Chunk f[kDepth];
+    {
+      const Scales<kRows, 128 * NW> scales(w, w.scales, 2, n0, g0, kGroups, scale_stride(kGroups));
+      const Scales<kRows, 128 * NW> zeros(w, w.zeros != nullptr ? static_cast<const void *>(w.zeros) : w.scales, 1, n0, g0, kGroups, zero_stride(kGroups));
+      if (begin < end)
 #pragma unroll
-    for (uint32_t i = 0; i < kDepth; ++i) load(f[i], i);
-    for (uint32_t chunk = 0; chunk < whole; chunk += kDepth) {
+        for (uint32_t i = 0; i < kDepth; ++i) {
+          load(f[i], begin + i, end);
+          __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
+        }
+      scales.bring(w, scales_lds);
+      if (w.zeros != nullptr) zeros.bring(w, zeros_lds);
+    }
+    // (Out of the loop from within: a way back to its top that leaves out the last loads would be waited for there as if they were not on their way.)
+    for (uint32_t chunk = begin;;) {
 #pragma unroll
-      for (uint32_t i = 0; i < kDepth; ++i) {
-        if (chunk + i >= whole) break;
-        scales_of(chunk + i);
-        put(f[i], chunk + i);
-        load(f[i], chunk + i + kDepth);
-        use(chunk + i);
+      for (uint32_t i = 0; i < kDepth; ++i, ++chunk) {
+        if (chunk >= end) goto done;
+        put(f[i], chunk);
+        load(f[i], chunk + kDepth, end);
+        use(chunk);
       }
     }
-  }
-  if (256 * whole < w.width_in) {
-    scales_of(whole);
-    Chunk f;
+  done:
+    if (end == whole && whole < begin + part && 256 * whole < w.width_in) {
 #pragma unroll
-    for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_upto(weights + from[i], 128 * whole + piece, w.row_bytes);
+      for (uint32_t i = 0; i < NT; ++i) f[0].codes[i] = load_upto(weights + from[i], 128 * whole + piece, w.row_bytes);
 #pragma unroll
-    for (int i = 0; i < TT; ++i) f.x[i] = load_upto(rows + x_from[i], 512 * whole + x_piece, 2 * w.width_in);
-    put(f, whole);
-    use(whole);
-  }
-  // the two halves of the sums
-  fence();
-  Floats4 *parts = reinterpret_cast<Floats4 *>(x_lds);
-  static_assert(sizeof(x_lds) >= 4 * NT * TT * 64 * sizeof(Floats4));
-#pragma unroll
-  for (uint32_t i = 0; i < NT; ++i)
-#pragma unroll
-    for (int tt = 0; tt < TT; ++tt)
-      if (kw == 1) parts[((nw * NT + i) * TT + tt) * 64 + lane] = acc[i][tt];
-  fence();
-  if (kw == 1) return;
-#pragma unroll
-  for (uint32_t i = 0; i < NT; ++i) {
-    const uint32_t n = n0 + 32 * nw + 16 * i + col;
-    if (n >= w.width_out) continue;
-#pragma unroll
-    for (int tt = 0; tt < TT; ++tt) {
-      const Floats4 sum = acc[i][tt] + parts[((nw * NT + i) * TT + tt) * 64 + lane];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t row = t0 + 16 * tt + 4 * g + j;
-        if (row >= c.rows) continue;
-        const float base = c.base != nullptr ? T::to_float(static_cast<const uint16_t *>(c.base)[row * c.base_stride + n]) : 0;
-        static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum[j] + base);
-      }
+      for (uint32_t i = 0; i < XP; ++i) f[0].x[i] = load_upto(rows + x_from[i], 512 * whole + x_piece, 2 * w.width_in);
+      put(f[0], whole);
+      use(whole);
     }
+  }
+  // The two halves of the sums, and then whole rows of the result: 8 elements to a thread.
+  constexpr uint32_t kStride = kRows + 4;  // (floats)
+  float *sums = reinterpret_cast<float *>(x_lds);
+  static_assert(sizeof(x_lds) >= 16 * TT * kStride * sizeof(float));
+#pragma unroll
+  for (uint32_t half = 0; half < 2; ++half) {
+    fence();
+    if (kw != 1 - half) continue;
+#pragma unroll
+    for (uint32_t i = 0; i < NT; ++i)
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float &at = sums[(16 * tt + 4 * g + j) * kStride + 32 * nw + 16 * i + col];
+          at = half == 0 ? acc[i][tt][j] : at + acc[i][tt][j];
+        }
+  }
+  fence();
+  for (uint32_t i = threadIdx.x; i < 16 * TT * kRows / 8; i += 128 * NW) {
+    const uint32_t r = i / (kRows / 8), row = t0 + r, n = n0 + 8 * (i % (kRows / 8));
+    if (row >= c.rows || n >= w.width_out) continue;
+    write8<T>(c, row, n, w.width_out - n, sums + r * kStride + 8 * (i % (kRows / 8)));
   }
 }
 
@@ -449,15 +519,14 @@ void launch_narrow(const Linear4View &w, const ft_linear4_call &c, hipStream_t s
 
 template <class T, int SG, int TT>
 void launch_wide(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
-  const dim3 grid((w.width_out + 127) / 128, (c.rows + 16 * TT - 1) / (16 * TT));
-  hipLaunchKernelGGL((ft_linear4_wide_kernel<T, SG, TT>), grid, dim3(512), 0, stream, w, c);
+  constexpr int NW = TT == 4 ? 4 : 2;
+  const dim3 grid((w.width_out + 32 * NW - 1) / (32 * NW), (c.rows + 16 * TT - 1) / (16 * TT));
+  hipLaunchKernelGGL((ft_linear4_wide_kernel<T, SG, TT, NW>), grid, dim3(128 * NW), 0, stream, w, c);
 }
 
 template <class T, int SG>
 void launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
-  const bool far = c.rows > 1 && c.x_stride >= 1u << 24;  // offsets of 32 bits would not reach
-  if (far) launch_narrow<T, SG, 8>(w, c, stream);
-  else if (c.rows > 32) launch_wide<T, SG, 4>(w, c, stream);
+  if (c.rows > 32) launch_wide<T, SG, 4>(w, c, stream);
   else if (c.rows > 16) launch_wide<T, SG, 2>(w, c, stream);
   else if (w.width_out >= 16384) launch_wide<T, SG, 1>(w, c, stream);
   else if (c.rows > 8) launch_narrow<T, SG, 8>(w, c, stream);
@@ -468,7 +537,9 @@ void launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) 
 template <class T>
 hipError_t launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
   const uint32_t group = w.group.d;
-  if (group < 32 || w.groups > kMostGroups || w.width_in < 32 || (uint64_t)w.width_out * w.groups < 16) {  // (loads are of 16 bytes)
+  const bool far = c.rows > 1 && c.x_stride >= 1u << 24;                                     // offsets of 32 bits would not reach
+  const bool tiny = w.width_in < 32 || (uint64_t)w.width_out * w.groups < 16;              // loads are of 16 bytes
+  if (group < 32 || w.groups > kMostGroups || far || tiny) {
     const uint32_t parts = (c.rows + 7) / 8;
     hipLaunchKernelGGL(ft_linear4_any_kernel<T>, dim3((w.width_out + 3) / 4, parts < 1024 ? parts : 1024), dim3(256), 0, stream, w, c);
   } else if (group % 128 == 0) {
