@@ -107,14 +107,6 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
         for (int j = 0; j < 4; ++j) acc[i][tt][j] = __builtin_fmaf(by[i], products[i][tt][j], __builtin_fmaf(more[i], sums[tt][j], acc[i][tt][j]));
     }
   };
-  // all that comes from shared memory is asked for before the first product, where it fits the registers
-  constexpr bool ahead = TT <= 2;
-  Words4 early[ahead ? 4 : 1][TT];
-  if (ahead)
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int tt = 0; tt < TT; ++tt) early[ahead ? s : 0][tt] = x(tt, s);
   const auto factors = [&](uint32_t group, float (&by)[NT], float (&more)[NT]) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -136,7 +128,7 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
     const uint32_t k = k0 + 32 * s;
     Words4 a[TT], b[NT];
 #pragma unroll
-    for (int tt = 0; tt < TT; ++tt) a[tt] = ahead ? early[ahead ? s : 0][tt] : x(tt, s);
+    for (int tt = 0; tt < TT; ++tt) a[tt] = x(tt, s);
 #pragma unroll
     for (int i = 0; i < NT; ++i) b[i] = Code<T>::numbers(codes[i][s], exponent);
     if (SG != 0) {
@@ -236,7 +228,7 @@ __device__ inline void write8(const ft_linear4_call &c, uint32_t row, uint32_t n
 // have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces, and turns it round in shared memory of
 // its own.
 template <class T, int SG, int XL, int KW>
-__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
+__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL == 1 ? 6 : 4))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
   constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
@@ -308,17 +300,17 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4))) vo
       multiply<T, SG, 1, 1>(w, mine, k0, g, [&](int, int s) { return x_lds[wave][x_row * 32 + (16 * block + element<SG>(g, s) / 8 ^ x_row)]; }, scale, zero, acc);
     }
   };
-  // (Out of the loop from within: a way back to its top that leaves out the last loads would be waited for there as if they were not on their way.)
-  for (uint32_t p = wave;;) {
+  for (uint32_t p = wave; p < pieces; p += kDepth * KW) {
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i, p += KW) {
-      if (p >= pieces) goto done;
-      put(codes[i], x[i]);
-      load(codes[i], x[i], p + kDepth * KW < pieces ? p + kDepth * KW : pieces - 1);
-      use(p);
+    for (int i = 0; i < kDepth; ++i) {
+      if (p + i * KW < pieces) {
+        put(codes[i], x[i]);
+        use(p + i * KW);
+      }
+      const uint32_t next = p + (i + kDepth) * KW;
+      load(codes[i], x[i], next < pieces ? next : pieces - 1);
     }
   }
-done:
   if (pieces < all && wave == pieces % KW) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) codes[0][i] = load_upto(weights + (from[i] - 16 * (lane % 8)), 128 * pieces + 16 * (lane % 8), w.row_bytes);
@@ -340,17 +332,26 @@ done:
 
 // 128 rows of weights to a workgroup - 32 to a wavefront, and two wavefronts take turns along the rows -, and 16 TT rows of x, which all wavefronts
 // multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied.
+struct Wide {
+  Linear4View w;
+  ft_linear4_call c;
+  uint32_t each;   // chunks of 256 elements to a workgroup
+  float *partial;  // where several have parts of the same sums
+};
+
 template <class T, int SG, int TT, int NW>
-__global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) void ft_linear4_wide_kernel(Linear4View w, ft_linear4_call c) {
-  constexpr uint32_t NT = 2, kGroups = 64, kRows = 32 * NW, XP = TT * 4 / NW;
-  constexpr uint32_t kDepth = TT == 4 ? 2 : 3;  // (chunks that are on their way)
+__global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) void ft_linear4_wide_kernel(Wide given) {
+  const Linear4View &w = given.w;
+  const uint32_t each = given.each;
+  constexpr uint32_t NT = 2, kGroups = 66, kRows = 32 * NW, XP = TT * 4 / NW;
+  constexpr uint32_t kDepth = TT == 4 && SG == 2 ? 1 : 2;  // (chunks that are on their way: what registers hold)
   __shared__ Words4 x_lds[2][TT * 16 * 32], codes_lds[2 * NW][NT][16 * 4];
   __shared__ char scales_lds[kRows * 4 * (kGroups / 2 | 1)], zeros_lds[kRows * 4 * (kGroups / 4 | 1)];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t kw = wave / NW, nw = wave % NW, n0 = blockIdx.x * kRows, t0 = blockIdx.y * (16 * TT);
   // offsets in bytes from the workgroup's first row: of 128 rows of weights less than 2^30, of 64 rows of x less than 2^31
   const uint8_t *weights = w.weights + (uint64_t)n0 * w.row_bytes;
-  const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(c.x) + t0 * c.x_stride);
+  const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(given.c.x) + t0 * given.c.x_stride);
   uint32_t from[NT], x_from[XP], x_to[XP];
 #pragma unroll
   for (uint32_t i = 0; i < NT; ++i) {
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
   for (uint32_t i = 0; i < XP; ++i) {
     const uint32_t r = 4 * NW * i + threadIdx.x / 32;
-    x_from[i] = (t0 + r < c.rows ? r : c.rows - 1 - t0) * (2 * (uint32_t)c.x_stride);
+    x_from[i] = (t0 + r < given.c.rows ? r : given.c.rows - 1 - t0) * (2 * (uint32_t)given.c.x_stride);
     x_to[i] = r * 32 + (threadIdx.x % 32 ^ r % 16);
   }
   const uint32_t whole = w.width_in / 256;  // and a part
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (int tt = 0; tt < TT; ++tt) acc[i][tt] = Floats4{0, 0, 0, 0};
   uint32_t g0 = 0;
-  const uint32_t part = w.group.d / (256 / kGroups);  // chunks whose scales are in shared memory together
+  const uint32_t part = w.group.d / 4;  // chunks whose scales are in shared memory together: of 64 groups and parts of two more
   const auto put = [&](const Chunk &f, uint32_t chunk) {
 #pragma unroll
     for (uint32_t i = 0; i < XP; ++i) x_lds[chunk & 1][x_to[i]] = in_order(f.x[i]);
@@ -407,10 +408,12 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
         },
         acc);
   };
-  for (uint32_t begin = 0; 256 * begin < w.width_in; begin += part) {
-    if (begin != 0) fence();  // the scales before are no longer read
-    g0 = begin / part * kGroups;
-    const uint32_t end = begin + part < whole ? begin + part : whole;
+  // of the chunks a workgroup has `each`
+  const uint32_t all = (w.width_in + 255) / 256, stop = (blockIdx.z + 1) * each < all ? (blockIdx.z + 1) * each : all;
+  for (uint32_t begin = blockIdx.z * each; begin < stop; begin += part) {
+    if (begin != blockIdx.z * each) fence();  // the scales before are no longer read
+    g0 = w.group.of(256 * begin);
+    const uint32_t here = begin + part < stop ? begin + part : stop, end = here < whole ? here : whole;
     Chunk f[kDepth];
     {
       const Scales<kRows, 128 * NW> scales(w, w.scales, 2, n0, g0, kGroups, scale_stride(kGroups));
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
       }
     }
   done:
-    if (end == whole && whole < begin + part && 256 * whole < w.width_in) {
+    if (here > whole) {
 #pragma unroll
       for (uint32_t i = 0; i < NT; ++i) f[0].codes[i] = load_upto(weights + from[i], 128 * whole + piece, w.row_bytes);
 #pragma unroll
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
     }
   }
   // The two halves of the sums, and then whole rows of the result: 8 elements to a thread.
-  constexpr uint32_t kStride = kRows + 4;  // (floats)
+  constexpr uint32_t kStride = kRows + 4;  // (floats: whole 16 bytes)
   float *sums = reinterpret_cast<float *>(x_lds);
   static_assert(sizeof(x_lds) >= 16 * TT * kStride * sizeof(float));
 #pragma unroll
@@ -463,11 +466,59 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
         }
   }
   fence();
+  // (read where they are used: as registers they would have to be kept all along)
+  typedef const __attribute__((address_space(4))) Wide *Argument;
+  Argument at_end = reinterpret_cast<Argument>(reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr()));
+  asm volatile("" : "+s"(at_end));
+  ft_linear4_call c;
+  c.out = at_end->c.out;
+  c.base = at_end->c.base;
+  c.out_stride = at_end->c.out_stride;
+  c.base_stride = at_end->c.base_stride;
+  c.rows = at_end->c.rows;
+  float *partial = at_end->partial;
+  const uint32_t width = at_end->w.width_out;
   for (uint32_t i = threadIdx.x; i < 16 * TT * kRows / 8; i += 128 * NW) {
     const uint32_t r = i / (kRows / 8), row = t0 + r, n = n0 + 8 * (i % (kRows / 8));
-    if (row >= c.rows || n >= w.width_out) continue;
-    write8<T>(c, row, n, w.width_out - n, sums + r * kStride + 8 * (i % (kRows / 8)));
+    if (row >= c.rows || n >= width) continue;
+    const float *from = sums + r * kStride + 8 * (i % (kRows / 8));
+    if (partial != nullptr) {
+      float *to = partial + ((uint64_t)blockIdx.z * c.rows + row) * ((width + 7) / 8 * 8) + n;
+      *reinterpret_cast<Floats4 *>(to) = *reinterpret_cast<const Floats4 *>(from);
+      *reinterpret_cast<Floats4 *>(to + 4) = *reinterpret_cast<const Floats4 *>(from + 4);
+      continue;
+    }
+    write8<T>(c, row, n, width - n, from);
   }
+}
+
+// What several workgroups have of the same sums, in their order: eight neighbouring elements of a row of the result to a thread, which asks for four
+// workgroups' at a time. (Rows of sums are padded to eight elements.)
+template <class T>
+__global__ __launch_bounds__(256) void ft_linear4_join_kernel(ft_linear4_call c, uint32_t width, uint32_t parts, const float *partial) {
+  const uint32_t eights = (width + 7) / 8;
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, all = (uint64_t)c.rows * eights;
+  if (i >= all) return;
+  const uint32_t row = (uint32_t)(i / eights), n = 8 * (uint32_t)(i - (uint64_t)row * eights);
+  const Floats4 *from = reinterpret_cast<const Floats4 *>(partial) + 2 * i;
+  Floats4 a{0, 0, 0, 0}, b{0, 0, 0, 0};
+  for (uint32_t z = 0; z < parts; z += 4) {
+    Floats4 v[4][2];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint64_t at = 2 * all * (z + j < parts ? z + j : parts - 1);
+      v[j][0] = from[at];
+      v[j][1] = from[at + 1];
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+      if (z + j < parts) {
+        a += v[j][0];
+        b += v[j][1];
+      }
+  }
+  const float sums[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  write8<T>(c, row, n, width - n, sums);
 }
 
 // A wavefront to an output column, eight rows at a time; any widths, groups and alignment.
@@ -507,9 +558,42 @@ __global__ __launch_bounds__(256) void ft_linear4_any_kernel(Linear4View w, ft_l
 
 }  // namespace
 
-uint64_t linear4_workspace(const ft_linear4 &, uint32_t, int) { return 0; }
-
 namespace {
+
+// Which kernel multiplies, and what of it a workgroup has.
+struct Plan {
+  bool any, narrow;
+  uint32_t tiles, waves;  // wide: tiles of 16 rows of x, wavefronts along the rows of weights
+  uint32_t each, parts;   // chunks of 256 elements to a workgroup, workgroups along them
+};
+
+// Sixteen rows of weights to a workgroup and rows of x sixteen at a time, or wider tiles whose workgroups share rows of x. The wider ones, beside the
+// others: 4 rows of 4096 to 8192 12.1 and 7.6 us, of 4096 to 32768 19.8 and 25.9; 16 of 4096 to 4096 10.3 and 6.6, of 8192 to 8192 17.1 and 19.5, of 4096 to
+// 32768 20.4 and 47.9; 32 of 4096 to 1024 10.8 and 6.1, to 4096 11.8 and 11.2, to 8192 15.2 and 20.8; 64 of 4096 to 1024 14.3 and 6.2, to 4096 16.2 and 19.9.
+// One row is as fast either way at 4096 to 32768, and below that 2 to 5 us faster in the narrow ones.
+bool narrow_is_faster(uint32_t width_in, uint32_t width_out, uint32_t rows) {
+  const uint64_t work = (uint64_t)width_in * width_out * ((rows + 15) / 16);
+  return rows <= 2 || work <= (rows <= 8 ? 96ull << 20 : 40ull << 20);
+}
+
+Plan plan_of(uint32_t width_in, uint32_t width_out, uint32_t group, uint32_t rows, int cu_count) {
+  const uint64_t groups = (width_in + (uint64_t)group - 1) / group;
+  Plan p{};
+  p.any = group < 32 || groups > kMostGroups || width_in < 32 || width_out * groups < 16;  // (loads are of 16 bytes)
+  p.narrow = narrow_is_faster(width_in, width_out, rows);
+  if (p.any || p.narrow) return p;
+  p.tiles = rows > 32 ? 4 : rows > 16 ? 2 : 1;
+  p.waves = p.tiles == 4 ? 4 : 2;
+  const uint32_t chunks = (width_in + 255) / 256;
+  const uint64_t workgroups = (uint64_t)((width_out + 32 * p.waves - 1) / (32 * p.waves)) * ((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+  uint64_t parts = ((p.tiles == 4 ? 1 : 2) * cu_count) / workgroups;
+  const uint32_t most = chunks / 4;
+  if (parts > most) parts = most;
+  if (parts < 1) parts = 1;
+  p.each = (chunks + (uint32_t)parts - 1) / (uint32_t)parts;
+  p.parts = (chunks + p.each - 1) / p.each;
+  return p;
+}
 
 template <class T, int SG, int XL>
 void launch_narrow(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
@@ -517,45 +601,57 @@ void launch_narrow(const Linear4View &w, const ft_linear4_call &c, hipStream_t s
   hipLaunchKernelGGL((ft_linear4_narrow_kernel<T, SG, XL, 8>), grid, dim3(512), 16 * (scale_stride(w.groups) + zero_stride(w.groups)), stream, w, c);
 }
 
-template <class T, int SG, int TT>
-void launch_wide(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
-  constexpr int NW = TT == 4 ? 4 : 2;
-  const dim3 grid((w.width_out + 32 * NW - 1) / (32 * NW), (c.rows + 16 * TT - 1) / (16 * TT));
-  hipLaunchKernelGGL((ft_linear4_wide_kernel<T, SG, TT, NW>), grid, dim3(128 * NW), 0, stream, w, c);
+template <class T, int SG, int TT, int NW>
+void launch_wide(const Linear4View &w, const ft_linear4_call &c, const Plan &p, hipStream_t stream) {
+  const dim3 grid((w.width_out + 32 * NW - 1) / (32 * NW), (c.rows + 16 * TT - 1) / (16 * TT), p.parts);
+  float *partial = p.parts > 1 ? static_cast<float *>(c.workspace) : nullptr;
+  hipLaunchKernelGGL((ft_linear4_wide_kernel<T, SG, TT, NW>), grid, dim3(128 * NW), 0, stream, Wide{w, c, p.each, partial});
 }
 
 template <class T, int SG>
-void launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
-  if (c.rows > 32) launch_wide<T, SG, 4>(w, c, stream);
-  else if (c.rows > 16) launch_wide<T, SG, 2>(w, c, stream);
-  else if (w.width_out >= 16384) launch_wide<T, SG, 1>(w, c, stream);
-  else if (c.rows > 8) launch_narrow<T, SG, 8>(w, c, stream);
-  else if (c.rows > 2) launch_narrow<T, SG, 4>(w, c, stream);
-  else launch_narrow<T, SG, 1>(w, c, stream);
+void launch(const Linear4View &w, const ft_linear4_call &c, const Plan &p, hipStream_t stream) {
+  if (p.narrow) {
+    if (c.rows > 8) launch_narrow<T, SG, 8>(w, c, stream);
+    else if (c.rows > 2) launch_narrow<T, SG, 4>(w, c, stream);
+    else launch_narrow<T, SG, 1>(w, c, stream);
+    return;
+  }
+  if (p.tiles == 4) launch_wide<T, SG, 4, 4>(w, c, p, stream);
+  else if (p.tiles == 2) launch_wide<T, SG, 2, 2>(w, c, p, stream);
+  else launch_wide<T, SG, 1, 2>(w, c, p, stream);
+  if (p.parts > 1)
+    hipLaunchKernelGGL(ft_linear4_join_kernel<T>, dim3((uint32_t)(((uint64_t)c.rows * ((w.width_out + 7) / 8) + 255) / 256)), dim3(256), 0, stream, c,
+                       w.width_out, p.parts,
+                       static_cast<const float *>(c.workspace));
 }
 
 template <class T>
-hipError_t launch(const Linear4View &w, const ft_linear4_call &c, hipStream_t stream) {
+hipError_t launch(const Linear4View &w, const ft_linear4_call &c, int cu_count, hipStream_t stream) {
   const uint32_t group = w.group.d;
-  const bool far = c.rows > 1 && c.x_stride >= 1u << 24;                                     // offsets of 32 bits would not reach
-  const bool tiny = w.width_in < 32 || (uint64_t)w.width_out * w.groups < 16;              // loads are of 16 bytes
-  if (group < 32 || w.groups > kMostGroups || far || tiny) {
+  const Plan p = plan_of(w.width_in, w.width_out, group, c.rows, cu_count);
+  const bool far = c.rows > 1 && c.x_stride >= 1u << 24;  // offsets of 32 bits would not reach
+  if (p.any || far) {
     const uint32_t parts = (c.rows + 7) / 8;
     hipLaunchKernelGGL(ft_linear4_any_kernel<T>, dim3((w.width_out + 3) / 4, parts < 1024 ? parts : 1024), dim3(256), 0, stream, w, c);
   } else if (group % 128 == 0) {
-    launch<T, 1>(w, c, stream);
+    launch<T, 1>(w, c, p, stream);
   } else if (group == 64) {
-    launch<T, 2>(w, c, stream);
+    launch<T, 2>(w, c, p, stream);
   } else {
-    launch<T, 0>(w, c, stream);
+    launch<T, 0>(w, c, p, stream);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_linear4(const Linear4View &w, const ft_linear4_call &c, int, hipStream_t stream) {
-  return w.type == FT_BF16 ? launch<Bf16>(w, c, stream) : launch<Fp16>(w, c, stream);
+uint64_t linear4_workspace(const ft_linear4 &w, uint32_t rows, int cu_count) {
+  const Plan p = plan_of(w.width_in, w.width_out, w.group, rows, cu_count);
+  return p.parts > 1 ? (uint64_t)p.parts * rows * ((w.width_out + 7) / 8 * 8) * sizeof(float) : 0;
+}
+
+hipError_t launch_linear4(const Linear4View &w, const ft_linear4_call &c, int cu_count, hipStream_t stream) {
+  return w.type == FT_BF16 ? launch<Bf16>(w, c, cu_count, stream) : launch<Fp16>(w, c, cu_count, stream);
 }
 
 }  // namespace ft
