@@ -142,24 +142,49 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
     } else {
       // a lane's eight elements are in one group, and 32 in two at most
       const uint32_t first = w.group.of(k), last = w.group.of(k + 31);
-      float by2[2][NT], more2[2][NT];
-      factors(first, by2[0], more2[0]);
-      factors(last, by2[1], more2[1]);
       const bool mine = w.group.of(k + 8 * g) == first;
+      float by0[NT], more0[NT];
+      factors(first, by0, more0);
+      if (TT == 4) {  // (one after the other, with the same code: registers do not hold both)
+#pragma unroll 1
+        for (int part = 0; part < (first == last ? 1 : 2); ++part) {
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        if (part == 1 && first == last) break;
+          for (int tt = 0; tt < TT; ++tt) {
+            Words4 some;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) some[i] = mine == (part == 0) ? a[tt][i] : 0;
+            sums[tt] = T::mfma(some, ones, nothing);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) products[i][tt] = T::mfma(some, b[i], nothing);
+          }
+          if (part == 1) factors(last, by0, more0);
+          add(by0, more0);
+        }
+        continue;
+      }
+      if (first != last) {
+        float by1[NT], more1[NT];
+        factors(last, by1, more1);
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt) {
           Words4 some;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) some[i] = mine == (part == 0) ? a[tt][i] : 0;
+          for (int i = 0; i < 4; ++i) some[i] = mine ? 0 : a[tt][i];
           sums[tt] = T::mfma(some, ones, nothing);
 #pragma unroll
           for (int i = 0; i < NT; ++i) products[i][tt] = T::mfma(some, b[i], nothing);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[tt][i] = mine ? a[tt][i] : 0;
         }
-        add(by2[part], more2[part]);
+        add(by1, more1);
       }
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt) {
+        sums[tt] = T::mfma(a[tt], ones, nothing);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) products[i][tt] = T::mfma(a[tt], b[i], nothing);
+      }
+      add(by0, more0);
     }
   }
 }
@@ -228,7 +253,7 @@ __device__ inline void write8(const ft_linear4_call &c, uint32_t row, uint32_t n
 // have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces, and turns it round in shared memory of
 // its own.
 template <class T, int SG, int XL, int KW>
-__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL == 1 ? 6 : 4))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
+__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1 ? 4 : SG != 0 ? 6 : 5))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
   constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
