@@ -1,6 +1,6 @@
 """A serving loop on memory of the pool: what arrives from another function's host memory, and the operators that answer with it.
 
-    python -m paper_2411_01830_amd.serve [--requests 16] [--layers 4] [--steps 32] [--check]
+    python -m paper_2411_01830_amd.serve [--requests 16] [--layers 4] [--steps 32] [--rotate] [--four-bit] [--sample] [--check]
 
 A small transformer of random weights serves requests whose prompts were read elsewhere: their keys and values, and the low-rank
 adapters of the models' variants, lie in pinned host memory and are brought into the pool by the transfer engine, a function with
@@ -8,8 +8,12 @@ a weight of its own each. Every step drafts a tree of tokens for each request (w
 a level), has the model judge all of them at once, keeps the path that the model would have taken itself, and appends what was
 kept to the pages. A request that has its tokens gives its pages back, and another one takes its place.
 
---check compares every adapted projection and every attention with plain 32-bit products over a history kept beside the pages, and
-every page's owner after every step.
+--rotate gives heads their norms and positions: a row's is that of its level behind the cached tokens. --four-bit keeps the projections' weights in the
+pool, in 4 bits, brought by transfers as the adapters are. --sample draws tokens from the model's probabilities instead of taking the likeliest: the drafted
+ones are judged by random numbers, so that what is kept is distributed as if each token had been drawn by itself.
+
+--check compares every projection, rotation and attention with plain products over a history kept beside the pages, what is
+kept with the definition of judging, and every page's owner after every step.
 """
 import argparse
 import sys
@@ -29,7 +33,7 @@ UNIT = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}    # the roundoff 
 
 class Server:
     def __init__(self, requests=16, layers=4, hidden=1024, heads=16, kv_heads=4, dim=64, vocab=4096, page=16, prompt=500, answer=40, depth=4,
-                 ranks=(8, 16, 32, 12), dtype=torch.bfloat16, check=False, seed=0):
+                 ranks=(8, 16, 32, 12), dtype=torch.bfloat16, check=False, seed=0, rotate=False, four_bit=False, sample=False):
         self.requests, self.layers, self.heads, self.kv_heads, self.dim, self.vocab = requests, layers, heads, kv_heads, dim, vocab
         self.hidden, self.page, self.prompt, self.answer, self.dtype, self.check = hidden, page, prompt, answer, dtype, check
         self.rng = np.random.default_rng(seed)
@@ -37,19 +41,22 @@ class Server:
         self.random = lambda *shape, by=1.0: (torch.randn(*shape, device="cuda", generator=gen) * by).to(dtype)
         self.width = (heads + 2 * kv_heads) * dim
         self.embed = self.random(vocab, hidden)
-        self.w_qkv = [self.random(hidden, self.width, by=hidden ** -0.5) for _ in range(layers)]
-        self.w_out = [self.random(heads * dim, hidden, by=(heads * dim) ** -0.5) for _ in range(layers)]
+        self.rotate, self.four_bit, self.sample = rotate, four_bit, sample
+        if not four_bit:
+            self.w_qkv = [self.random(hidden, self.width, by=hidden ** -0.5) for _ in range(layers)]
+            self.w_out = [self.random(heads * dim, hidden, by=(heads * dim) ** -0.5) for _ in range(layers)]
 
         if not 1 <= depth <= 31:
             raise ValueError("a tree's rows have one word of the mask: 1 to 31 levels")
         # The trees of a step are the same every time: request r drafts 1 + r % depth levels of two tokens below its last one. The first of a
         # level hangs from the first of the level before; row t sees itself and what it hangs from.
         self.levels = [1 + r % depth for r in range(requests)]
-        starts, parent, mask = [0], [], []
+        starts, parent, mask, depth_of = [0], [], [], []
         for n in self.levels:
             first, at = len(parent), 0
             parent.append(-1)
             mask.append(1)
+            depth_of += [0] + [1 + i // 2 for i in range(2 * n)]
             for _ in range(n):
                 here = len(parent) - first
                 for k in range(2):
@@ -64,6 +71,9 @@ class Server:
         self.root = self.starts[:-1].long()
         self.deep = [torch.tensor([r for r, n in enumerate(self.levels) if n > level], device="cuda") for level in range(max(self.levels))]
         self.first_of = [self.root[who] + 1 + 2 * level for level, who in enumerate(self.deep)]
+        self.level_of = self._ints(depth_of)
+        first_of_request = torch.repeat_interleave(torch.tensor(starts[:-1]), torch.tensor(starts).diff())
+        self.hangs_from = torch.where(torch.tensor(parent) < 0, -1, torch.tensor(parent) - first_of_request).to(torch.int32).cuda()  # within a request
         self.request_of = torch.repeat_interleave(torch.arange(requests, device="cuda"), torch.tensor(starts, device="cuda").diff())
         self.last = torch.zeros(requests, dtype=torch.int64, device="cuda")               # the token that is to be judged next
         self.follows = torch.zeros(requests, vocab, dtype=torch.int64, device="cuda")     # what followed a token the last time
@@ -77,8 +87,12 @@ class Server:
         cache_bytes = (pages * page * row + SLAB - 1) // SLAB * SLAB
         prompt_bytes = (prompt * row * 2 * layers + SLAB - 1) // SLAB * SLAB
         self.engine = harness.GpuEngine(0)
-        self.engine.pool_create(2 * layers * cache_bytes + layers * (sum(adapter_bytes) + len(ranks) * SLAB) + prompt_bytes, SLAB, fill=None)
-        self.engine.host_arena(max(prompt_bytes, layers * sum(adapter_bytes)), fill=None)
+        weight_bytes = 0
+        if four_bit:
+            parts = [n for ni, no in ((hidden, self.width), (heads * dim, hidden)) for n in self._parts(ni, no)]
+            weight_bytes = layers * sum((n + SLAB - 1) // SLAB * SLAB for n in parts)
+        self.engine.pool_create(2 * layers * cache_bytes + layers * (sum(adapter_bytes) + len(ranks) * SLAB) + prompt_bytes + weight_bytes, SLAB, fill=None)
+        self.engine.host_arena(max(prompt_bytes, layers * sum(adapter_bytes), weight_bytes), fill=None)
         self.pool = self.engine.pool
         self.memory = self.engine.segments[0][0]
         alloc = self.engine.slab_alloc
@@ -86,6 +100,11 @@ class Server:
         self.arrived = alloc(prompt_bytes)
         self.bytes_moved = 0
         self._bring_adapters(ranks, alloc)
+        if four_bit:
+            self._bring_weights(alloc)
+        if rotate:
+            self.rotation = ops.Rotation(self.pool, [10000.0 ** (-2 * i / dim) for i in range(dim // 2)], dim)
+            self.norms = [(1 + self.random(2, dim, by=0.1)) for _ in range(layers)]
 
         self.lens = torch.zeros(requests, dtype=torch.int32, device="cuda")
         self.table = torch.zeros(requests, self.blocks, dtype=torch.int32, device="cuda")
@@ -129,6 +148,53 @@ class Server:
         self.adapters = [ops.Adapters(self.pool, kinds[i * n:i * n + n], self.hidden, self.width, self.dtype) for i in range(self.layers)]
         self.kinds = kinds
 
+    GROUP = 64
+
+    def _parts(self, width_in, width_out):
+        """Bytes of a projection's codes, scales and zeros."""
+        groups = -(-width_in // self.GROUP)
+        return width_out * ((width_in + 1) // 2), 2 * width_out * groups, width_out * groups
+
+    def _bring_weights(self, alloc):
+        """Every layer's two projections in 4 bits, random codes from host memory."""
+        moves, at, self.w_qkv, self.w_out = [], 0, [], []
+        for _ in range(self.layers):
+            for ni, no, into in ((self.hidden, self.width, self.w_qkv), (self.heads * self.dim, self.hidden, self.w_out)):
+                to = []
+                for kind, n in enumerate(self._parts(ni, no)):
+                    here = self.engine.host[at:at + n]
+                    if kind == 1:                                                 # (codes are 4.6 from their zeros, in the mean of squares)
+                        here.view(self.dtype).copy_((torch.rand(n // 2, device="cuda") + 0.5).to(self.dtype) * (0.2 * ni ** -0.5))
+                    else:
+                        here.copy_(torch.randint(256 if kind == 0 else 16, (n,), dtype=torch.uint8, device="cuda"))
+                    to.append(alloc(n))
+                    moves.append((0, at, to[-1], n))
+                    at += (n + 255) // 256 * 256
+                into.append(ops.Linear4(self.pool, to[0], to[1], ni, no, self.GROUP, self.dtype, zeros_off=to[2]))
+        self._transfer(moves, [1])
+
+    def _weights(self, w):
+        """What a projection's codes stand for, and its factors, in 64 bits."""
+        r, groups = w.record, -(-w.width_in // self.GROUP)
+        codes = self.memory[r.weights:r.weights + w.width_out * ((w.width_in + 1) // 2)].view(w.width_out, -1)
+        codes = torch.stack([codes & 15, codes >> 4], -1).flatten(1)[:, :w.width_in].double()
+        scales = self.memory[r.scales:r.scales + 2 * w.width_out * groups].view(self.dtype).view(w.width_out, groups)
+        zeros = self.memory[r.zeros:r.zeros + w.width_out * groups].view(w.width_out, groups)
+        scales, zeros = (t.double().repeat_interleave(self.GROUP, 1)[:, :w.width_in] for t in (scales, zeros))
+        return (codes - zeros) * scales, (271 + zeros) * scales
+
+    def _project(self, w, x, base=None):
+        if not self.four_bit:
+            return x @ w if base is None else base + x @ w
+        out = ops.linear4_apply(w, x, base=base)
+        if self.check:
+            product, terms = self._weights(w)
+            want = x.double() @ product.t() + (0 if base is None else base.double())
+            # one rounding, and sums in 32 bits of a group's elements whose codes count from a power of two
+            slack = 2.0 ** -24 * (self.GROUP + 64) * (x.double().abs() @ terms.t()) + (0 if base is None else 2.0 ** -23 * base.double().abs())
+            self._within("projection", out, want.float(), (1.001 * UNIT[self.dtype] * want.abs() + slack).float() + 1e-7)
+        return out
+
     def _adapter(self, layer, i):
         at, b, r, scale = self.kinds[layer * self.adapters[layer].count + i]
         a = self.memory[at:b].view(self.dtype).view(r, self.hidden)
@@ -162,24 +228,8 @@ class Server:
             tokens[self.first_of[level]] = at[self.deep[level]]
         return tokens
 
-    def step(self):
-        """One step of all requests: how many tokens each of them got."""
-        tokens = self._draft()
-        ids = self.adapter_of[self.request_of]
-        groups = ops.adapter_groups(self.adapters[0], ids)
-        x = self.embed[tokens]
-        kept = []
-        for layer in range(self.layers):
-            base = x @ self.w_qkv[layer]
-            qkv = ops.adapters_apply(self.adapters[layer], groups, x, base)
-            q, k, v = qkv.view(self.rows, -1, self.dim).split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-            o = ops.tree_attention(self.caches[layer], q, k, v, self.starts, self.lens, self.table, self.drafts, self.mask)
-            if self.check:
-                self._check_projection(layer, ids, x, base, qkv)
-                self._check_attention(layer, q, k, v, o)
-            kept.append((k, v))
-            x = x + o.reshape(self.rows, -1) @ self.w_out[layer]
-            x = (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(self.dtype)
+    def _judge(self, tokens, x):
+        """Rows that the model would have taken itself; what it takes next."""
         said = (x @ self.embed.t()).argmax(-1)                        # what follows each row
 
         # a row is kept if the row that it hangs from is, and was followed by its token
@@ -195,6 +245,48 @@ class Server:
         order = torch.where(keep, torch.arange(self.rows, device="cuda"), -1)
         end = torch.full((self.requests,), -1, device="cuda").scatter_reduce(0, self.request_of, order, "amax")
         self.last = said[end]
+        return keep
+
+    def _judge_by_chance(self, tokens, x):
+        """Rows that stand against the model's probabilities and random numbers; what was drawn behind them."""
+        logits = (x @ self.embed.t()).float()
+        target = torch.softmax(logits * (2 / logits.std(-1, keepdim=True)), -1)
+        accept, pick = torch.rand(self.rows, device="cuda"), torch.rand(self.requests, device="cuda")
+        keep, last, token = ops.tree_verify(self.pool, tokens, self.starts, self.drafts, target, accept, pick, parent=self.hangs_from)
+        if self.check:
+            self._check_judged(tokens, target, accept, pick, keep, last, token)
+        hangs = (self.parent >= 0) & (keep != 0)                      # what follows a kept row: its kept child, or what was drawn
+        self.follows[self.request_of[hangs], tokens[self.parent[hangs]]] = tokens[hangs]
+        self.follows[torch.arange(self.requests, device="cuda"), tokens[last.long()]] = token
+        self.last = token
+        return keep
+
+    def step(self):
+        """One step of all requests: how many tokens each of them got."""
+        tokens = self._draft()
+        ids = self.adapter_of[self.request_of]
+        groups = ops.adapter_groups(self.adapters[0], ids)
+        x = self.embed[tokens]
+        kept = []
+        for layer in range(self.layers):
+            base = self._project(self.w_qkv[layer], x)
+            qkv = ops.adapters_apply(self.adapters[layer], groups, x, base)
+            q, k, v = qkv.view(self.rows, -1, self.dim).split([self.heads, self.kv_heads, self.kv_heads], dim=1)
+            if self.rotate:
+                positions = self.lens[self.request_of] + self.level_of
+                given, norms = (q, k), self.norms[layer]
+                q, k = ops.rotate_heads(self.rotation, q, k, positions, q_weight=norms[0], k_weight=norms[1], eps=1e-6)
+                if self.check:
+                    for x_, y_, w_ in zip(given, (q, k), norms):
+                        self._check_rotation(x_, y_, w_, positions)
+            o = ops.tree_attention(self.caches[layer], q, k, v, self.starts, self.lens, self.table, self.drafts, self.mask)
+            if self.check:
+                self._check_projection(layer, ids, x, base, qkv)
+                self._check_attention(layer, q, k, v, o)
+            kept.append((k, v))
+            x = self._project(self.w_out[layer], o.reshape(self.rows, -1), x)
+            x = (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(self.dtype)
+        keep = self._judge_by_chance(tokens, x) if self.sample else self._judge(tokens, x)
 
         slots, lens, self.state = ops.kv_grow(self.pool, self.lens, self.starts, self.rows, self.table, self.free, self.state, self.page, keep)
         for layer in range(self.layers):
@@ -202,7 +294,7 @@ class Server:
             if self.check:
                 for r in range(self.requests):
                     mine = torch.arange(self.starts_host[r], self.starts_host[r + 1], device="cuda")
-                    mine = mine[keep[mine]]
+                    mine = mine[keep[mine] != 0]
                     new = torch.stack([kept[layer][0][mine], kept[layer][1][mine]]).float()
                     self.history[layer][r] = torch.cat([self.history[layer][r], new], dim=1)
         got = (lens - self.lens).cpu().numpy()                        # (a wait; choosing by flags, above, is another)
@@ -235,6 +327,38 @@ class Server:
             want[mine] += (scale * (h @ b.double().t())).float()
             size[mine] = (abs(scale) * (h.abs() @ b.double().abs().t())).float()
         self._within("adapters", got, want, UNIT[self.dtype] * want.abs() + 2.0 ** -14 * size + 1e-6)
+
+    def _check_rotation(self, x, got, weight, positions):
+        y = x.double()
+        y = y / (y.square().mean(-1, keepdim=True) + 1e-6).sqrt() * weight.double()
+        angle = (positions.double()[:, None] * self.rotation.freqs.double())[:, None]
+        a, b = y.split(self.dim // 2, -1)
+        want = torch.cat([a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()], -1)
+        size = (a.abs() + b.abs()).repeat(1, 1, 2)
+        self._within("rotation", got, want.float(), (1.001 * UNIT[self.dtype] * want.abs() + 20 * 2.0 ** -24 * size).float() + 1e-7)
+
+    def _check_judged(self, tokens, target, accept, pick, keep, last, token):
+        """The definition, row by row, in 64 bits."""
+        target, tokens, accept, kept = target.double().cpu(), tokens.tolist(), accept.tolist(), keep.tolist()
+        for r in range(self.requests):
+            a, b = self.starts_host[r], self.starts_host[r + 1]
+            row, stands = a, {a}
+            while True:
+                left, mass, found = target[row].clone(), 1.0, None
+                for t in (t for t in range(row + 1, b) if self.parent_host[t] == row):
+                    p = float(left[tokens[t]])
+                    if accept[t] * mass < p:
+                        found = t
+                        break
+                    left[tokens[t]], mass = 0, max(mass - p, 0.0)
+                if found is None:
+                    break
+                row = found
+                stands.add(row)
+            sums = left.cumsum(0)
+            drawn = int(torch.nonzero(sums > float(pick[r]) * float(sums[-1]))[0])
+            if stands != {t for t in range(a, b) if kept[t]} or int(last[r]) != row or int(token[r]) != drawn:
+                raise AssertionError("judged otherwise than the definition says")
 
     def _check_attention(self, layer, q, k, v, got):
         g = self.heads // self.kv_heads
@@ -277,12 +401,16 @@ def main():
     ap.add_argument("--answer", type=int, default=40, help="the tokens that a request wants")
     ap.add_argument("--depth", type=int, default=4, help="levels of the deepest tree")
     ap.add_argument("--dtype", default="bfloat16", choices=["bfloat16", "float16"])
+    ap.add_argument("--rotate", action="store_true", help="norms of heads, and positions")
+    ap.add_argument("--four-bit", action="store_true", help="weights of 4 bits, in the pool")
+    ap.add_argument("--sample", action="store_true", help="tokens drawn by the model's probabilities")
     ap.add_argument("--check", action="store_true")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         print("needs a GPU", file=sys.stderr)
         sys.exit(2)
-    server = Server(args.requests, args.layers, prompt=args.prompt, answer=args.answer, depth=args.depth, dtype=getattr(torch, args.dtype), check=args.check)
+    server = Server(args.requests, args.layers, prompt=args.prompt, answer=args.answer, depth=args.depth, dtype=getattr(torch, args.dtype), check=args.check,
+                    rotate=args.rotate, four_bit=args.four_bit, sample=args.sample)
     server.step()
     torch.cuda.synchronize()
     begin, tokens = time.perf_counter(), 0
@@ -293,7 +421,7 @@ def main():
     print(f"{args.steps} steps of {args.requests} requests, {server.rows} rows each: {tokens} tokens, {tokens / args.steps / args.requests:.2f} a request and step, "
           f"{took / args.steps * 1e3:.2f} ms a step; {server.bytes_moved / 1e6:.1f} MB brought from host memory")
     if args.check:
-        print(f"every projection, attention and page checked: at most {server.worst:.2f} of what rounding explains")
+        print(f"every projection, rotation, attention and page checked: at most {server.worst:.2f} of what rounding explains")
     server.close()
 
 

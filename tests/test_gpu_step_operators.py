@@ -95,6 +95,10 @@ LINEAR = [
     (17, 1023, 65, 32, True, False, 0), (15, 640, 48, 64, False, False, 1), (33, 896, 272, 128, True, True, 0), (64, 1536, 640, 64, False, False, 0),
     (65, 512, 96, 32, True, True, 0), (200, 768, 80, 256, True, False, 0), (7, 8192, 96, 8192, True, False, 0), (9, 520, 100, 1024, True, False, 3),
     (4, 11008, 64, 128, False, False, 0), (1, 14336, 256, 64, True, False, 0), (31, 264, 33, 24, True, True, 5), (64, 96, 2048, 32, True, False, 0),
+    # as many groups as shared memory has room for, and one more; widths and rows on either side of the rules that choose
+    (16, 32768, 20, 32, True, True, 0), (3, 32776, 20, 32, True, False, 1), (2, 33000, 40, 32, False, False, 0), (24, 5000, 3001, 40, True, True, 1),
+    (48, 4100, 2500, 96, True, False, 0), (64, 8192, 1111, 64, True, True, 0), (40, 2304, 5000, 32, False, True, 2), (12, 2100, 20001, 64, True, True, 1),
+    (130, 3333, 700, 128, True, True, 3), (17, 513, 16400, 136, True, False, 0),
 ]
 
 
