@@ -1,5 +1,6 @@
 """ctypes binding of include/faastube.h: same names, argument marshalling only."""
 import ctypes as C
+import struct
 import os
 
 import numpy as np
@@ -675,25 +676,47 @@ def adapters_apply(pool, call, stream=0):
     _check(_lib.ft_adapters_apply(pool, C.byref(call), stream), pool)
 
 
+# Calls of these are made in loops that wait for them: their records may be bytes, packed by the formats below, as well as the structures above, which
+# take twice as long to fill.
+LINEAR4_CALL = struct.Struct("3P3Q2IPQ")
+ROTATE_CALL = struct.Struct("9P8Q8IfI")
+VERIFY_CALL = struct.Struct("10P2Q6IPQ")
+assert LINEAR4_CALL.size == C.sizeof(Linear4Call) and ROTATE_CALL.size == C.sizeof(RotateCall) and VERIFY_CALL.size == C.sizeof(VerifyCall)
+
+
+def _at(record):
+    return record if type(record) is bytes else C.byref(record)
+
+
 def linear4_workspace(pool, weights, call):
     n = C.c_uint64()
-    _check(_lib.ft_linear4_workspace(pool, C.byref(weights), C.byref(call), C.byref(n)), pool)
+    rc = _lib.ft_linear4_workspace(pool, C.byref(weights), _at(call), C.byref(n))
+    if rc:
+        _check(rc, pool)
     return n.value
 
 
 def linear4_apply(pool, weights, call, stream=0):
-    _check(_lib.ft_linear4_apply(pool, C.byref(weights), C.byref(call), stream), pool)
+    rc = _lib.ft_linear4_apply(pool, C.byref(weights), _at(call), stream)
+    if rc:
+        _check(rc, pool)
 
 
 def rotate_heads(pool, call, stream=0):
-    _check(_lib.ft_rotate_heads(pool, C.byref(call), stream), pool)
+    rc = _lib.ft_rotate_heads(pool, _at(call), stream)
+    if rc:
+        _check(rc, pool)
 
 
 def verify_workspace(pool, call):
     n = C.c_uint64()
-    _check(_lib.ft_verify_workspace(pool, C.byref(call), C.byref(n)), pool)
+    rc = _lib.ft_verify_workspace(pool, _at(call), C.byref(n))
+    if rc:
+        _check(rc, pool)
     return n.value
 
 
 def tree_verify(pool, call, stream=0):
-    _check(_lib.ft_tree_verify(pool, C.byref(call), stream), pool)
+    rc = _lib.ft_tree_verify(pool, _at(call), stream)
+    if rc:
+        _check(rc, pool)

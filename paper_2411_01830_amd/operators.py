@@ -72,6 +72,7 @@ def _flags(name, t, device, n):
         _refuse(f"{name} has {n} entries")
 
 
+_linear4, _rotate, _verify = ft.LINEAR4_CALL.pack, ft.ROTATE_CALL.pack, ft.VERIFY_CALL.pack
 _stream = torch._C._cuda_getCurrentRawStream  # of a device's index: torch.cuda.current_stream without the object that holds it
 
 
@@ -261,26 +262,33 @@ class Linear4:
 
 def linear4_apply(weights, x, base=None, out=None):
     """base (None: 0) and x's rows times the weights on top; out may be base. For the few rows of a step: weights are read once for 64 of them."""
-    dev = _device("x", x, weights.pool)
-    if x.dim() != 2:
+    pool, dtype, ni, no = weights.pool, weights.dtype, weights.width_in, weights.width_out
+    dev = _device("x", x, pool)
+    given = x.shape
+    if len(given) != 2:
         _refuse("x has two dimensions")
-    rows, dtype, ni, no = x.shape[0], weights.dtype, weights.width_in, weights.width_out
+    rows = given[0]
     _rows("x", x, dtype, (rows, ni), dev)
     shape = (rows, no)
-    if base is not None:
-        _rows("base", base, dtype, shape, dev)
     if out is None:
         out = x.new_empty(shape)
     else:
         _rows("out", out, dtype, shape, dev)
-    one = rows <= 1  # a single row's stride means nothing
-    call = ft.Linear4Call(x.data_ptr(), None if base is None else base.data_ptr(), out.data_ptr(), ni if one else x.stride(0),
-                          no if one or base is None else base.stride(0), no if one else out.stride(0), rows, 0, None, 0)
-    need = ft.linear4_workspace(weights.pool, weights.record, call)
+    base_at, base_stride, x_stride, out_stride = 0, no, ni, no
+    if base is not None:
+        _rows("base", base, dtype, shape, dev)
+        base_at = base.data_ptr()
+    if rows > 1:  # (a single row's stride means nothing)
+        x_stride, out_stride = x.stride()[0], out.stride()[0]
+        if base is not None:
+            base_stride = base.stride()[0]
+    x_at, out_at = x.data_ptr(), out.data_ptr()
+    call = _linear4(x_at, base_at, out_at, x_stride, base_stride, out_stride, rows, 0, 0, 0)
+    need = ft.linear4_workspace(pool, weights.record, call)
     if need:
         work = torch.empty(need, dtype=torch.uint8, device=dev)
-        call.workspace, call.workspace_bytes = work.data_ptr(), need
-    ft.linear4_apply(weights.pool, weights.record, call, _stream(dev.index))
+        call = _linear4(x_at, base_at, out_at, x_stride, base_stride, out_stride, rows, 0, work.data_ptr(), need)
+    ft.linear4_apply(pool, weights.record, call, _stream(dev.index))
     return out
 
 
@@ -305,7 +313,7 @@ class Rotation:
         self.freqs = torch.as_tensor(freqs, dtype=torch.float32).to(on).contiguous()
         if self.freqs.dim() != 1:
             _refuse("freqs has one dimension")
-        self.rot, self.axis_at = 2 * pairs, None if self.axis is None else self.axis.data_ptr()
+        self.rot, self.axis_at = 2 * pairs, 0 if self.axis is None else self.axis.data_ptr()
 
 
 def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=None, q_out=None, k_out=None):
@@ -329,8 +337,10 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
     if freqs.device != dev:
         _refuse("q lies on another GPU than the rotation")
     flags = ft.ROTATE_NEIGHBOURS if rotation.neighbours else 0
-    q_by = k_by = None
+    q_by = k_by = 0
     if eps is not None:
+        if not 0 <= eps < 3e38:
+            _refuse("eps is a number of 32 bits, not below 0")
         flags |= ft.ROTATE_NORM
         if q_weight is not None:
             _rows("q_weight", q_weight, dtype, (dim,), dev)
@@ -347,11 +357,12 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
     else:
         _rows("q_out", q_out, dtype, shape, dev)
     qs, os = q.stride(), q_out.stride()
-    k_at, k_to, kv_heads, ks, kos = None, None, 0, (0, 0), (0, 0)
+    k_at, k_to, kv_heads, ks, kos = 0, 0, 0, (0, 0), (0, 0)
     if k is not None:
-        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        given = k.shape
+        if len(given) != 3:
             _refuse("k has three dimensions")
-        kv_heads = k.shape[1]
+        kv_heads = given[1]
         _rows("k", k, dtype, (tokens, kv_heads, dim), dev)
         if k_out is None:
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
@@ -360,8 +371,8 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
         k_at, k_to, ks, kos = k.data_ptr(), k_out.data_ptr(), k.stride(), k_out.stride()
     elif k_out is not None:
         _refuse("there are no keys for k_out")
-    call = ft.RotateCall(q.data_ptr(), k_at, q_out.data_ptr(), k_to, q_by, k_by, positions.data_ptr(), freqs.data_ptr(), rotation.axis_at, qs[0], qs[1],
-                         ks[0], ks[1], os[0], os[1], kos[0], kos[1], tokens, heads, kv_heads, dim, rotation.rot, axes, TYPES[dtype], flags, eps, 0)
+    call = _rotate(q.data_ptr(), k_at, q_out.data_ptr(), k_to, q_by, k_by, positions.data_ptr(), freqs.data_ptr(), rotation.axis_at, qs[0], qs[1], ks[0],
+                   ks[1], os[0], os[1], kos[0], kos[1], tokens, heads, kv_heads, dim, rotation.rot, axes, TYPES[dtype], flags, eps, 0)
     ft.rotate_heads(pool, call, _stream(dev.index))
     return q_out, k_out
 
@@ -380,13 +391,16 @@ def tree_verify(pool, tokens, starts, drafts, target, accept, pick, draft=None, 
     rows, requests = tokens.shape[0], starts.shape[0] - 1
     if requests < 0:
         _refuse("starts has one entry more than there are requests")
+    if not 0 < drafts < 1 << 32:
+        _refuse("drafts is the most rows of a request")
     _ints("accept", accept, torch.float32, 1, dev)
     _ints("pick", pick, torch.float32, 1, dev)
     if accept.shape[0] != rows or pick.shape[0] != requests:
         _refuse("accept has an entry for every row, pick for every request")
-    if target.dim() != 2 or target.dtype not in PROBABILITIES:
+    shape, dtype = target.shape, target.dtype
+    if len(shape) != 2 or dtype not in PROBABILITIES:
         _refuse("target has two dimensions of bfloat16, float16 or float32")
-    vocab, dtype = target.shape[1], target.dtype
+    vocab = shape[1]
     _rows("target", target, dtype, (rows, vocab), dev)
     if draft is not None:
         _rows("draft", draft, dtype, (rows, vocab), dev)
@@ -396,14 +410,14 @@ def tree_verify(pool, tokens, starts, drafts, target, accept, pick, draft=None, 
             _refuse("parent has an entry for every row")
     keep, last, token = torch.empty(rows, dtype=torch.uint8, device=dev), starts.new_empty(requests), tokens.new_empty(requests)
     one = rows <= 1
-    call = ft.VerifyCall(tokens.data_ptr(), starts.data_ptr(), None if parent is None else parent.data_ptr(), target.data_ptr(),
-                         None if draft is None else draft.data_ptr(), accept.data_ptr(), pick.data_ptr(), keep.data_ptr(), last.data_ptr(), token.data_ptr(),
-                         vocab if one else target.stride(0), vocab if one or draft is None else draft.stride(0), rows, requests, drafts, vocab,
-                         PROBABILITIES[dtype], 0, None, 0)
+    at = (tokens.data_ptr(), starts.data_ptr(), 0 if parent is None else parent.data_ptr(), target.data_ptr(), 0 if draft is None else draft.data_ptr(),
+          accept.data_ptr(), pick.data_ptr(), keep.data_ptr(), last.data_ptr(), token.data_ptr(), vocab if one else target.stride()[0],
+          vocab if one or draft is None else draft.stride()[0], rows, requests, drafts, vocab, PROBABILITIES[dtype], 0)
+    call = _verify(*at, 0, 0)
     need = ft.verify_workspace(pool, call)
     if need:
         work = torch.empty(need, dtype=torch.uint8, device=dev)
-        call.workspace, call.workspace_bytes = work.data_ptr(), need
+        call = _verify(*at, work.data_ptr(), need)
     ft.tree_verify(pool, call, _stream(dev.index))
     return keep, last, token
 

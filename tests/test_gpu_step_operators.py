@@ -555,6 +555,8 @@ def test_tensors_that_ask_for_gradients_or_lie_elsewhere_are_refused():
         lambda: ops().rotate_heads(rotation, h, None, at.long()), lambda: ops().rotate_heads(rotation, h, None, at[:1]),
         lambda: ops().rotate_heads(rotation, h, None, at, q_weight=h[0, 0]), lambda: ops().rotate_heads(rotation, h, None, at, q_weight=h[0, 0, :7], eps=0.0),
         lambda: ops().rotate_heads(rotation, h, None, at, k_out=h), lambda: ops().rotate_heads(rotation, h, None, at, eps=-1.0),
+        lambda: ops().rotate_heads(rotation, h, None, at, eps=1e300), lambda: ops().rotate_heads(rotation, h, None, at, eps=math.nan),
+        lambda: ops().tree_verify(w.m.pool, t, gpu([0, 2]), -1, p, r, r[:1]), lambda: ops().tree_verify(w.m.pool, t, gpu([0, 2]), 1 << 40, p, r, r[:1]),
         lambda: ops().rotate_heads(rotation, h, None, at, q_out=h[:1].expand(2, 1, 8)), lambda: ops().rotate_heads(rotation, h.float(), None, at),
         lambda: ops().rotate_heads(ops().Rotation(w.m.pool, [1.0] * 4, 8, axes=[0, 0, 1, 1]), h, None, at),
         lambda: ops().tree_verify(w.m.pool, t, gpu([0, 2]), 2, p, r, r[:1], draft=p.half()), lambda: ops().tree_verify(w.m.pool, t, gpu([0, 2]), 2, p, r, r),
