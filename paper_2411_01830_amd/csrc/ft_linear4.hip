@@ -416,6 +416,8 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
     for (uint32_t i = 0; i < NT; ++i) codes_lds[wave][i][to] = f.codes[i];
   };
+  // (of elements behind a row's last, which are zeros, the last group's: the next row's scale may be infinite)
+  const auto there = [&](uint32_t group) { return group < w.groups ? group : w.groups - 1; };
   const auto use = [&](uint32_t chunk) {
     fence();
     const Words4 *here = x_lds[chunk & 1];
@@ -426,10 +428,10 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
     multiply<T, SG, NT, TT>(
         w, turn, 256 * chunk + kBlock * kw, g, [&](int tt, int s) { return here[(16 * tt + col) * 32 + (16 * kw + element<SG>(g, s) / 8 ^ col)]; },
         [&](int i, uint32_t group) {
-          return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + (r + 16 * i) * scale_stride(kGroups) + 2 * (group - g0)));
+          return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + (r + 16 * i) * scale_stride(kGroups) + 2 * (there(group) - g0)));
         },
         [&](int i, uint32_t group) {
-          return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[(r + 16 * i) * zero_stride(kGroups) + (group - g0)];
+          return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[(r + 16 * i) * zero_stride(kGroups) + (there(group) - g0)];
         },
         acc);
   };

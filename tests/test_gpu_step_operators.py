@@ -68,6 +68,7 @@ class Weights:
         self.zeros = torch.randint(256 if wild else 16, (no, groups), dtype=torch.uint8, device="cuda", generator=g) if zeros else None
         self.m = Memory(no * row + 3 * no * groups + 4 * SLAB)
         at = self.m.put(self.codes, shift), self.m.put(self.scales, 2 * shift), self.m.put(self.zeros, shift) if zeros else None
+        self.scales_off = at[1]
         self.handle = ops().Linear4(self.m.pool, at[0], at[1], ni, no, group, dtype, zeros_off=at[2])
         k = torch.arange(ni, device="cuda")
         self.scale = self.scales.double()[:, k // group]
@@ -151,6 +152,24 @@ def test_rows_and_columns_of_infinities_keep_to_themselves(dtype):
     b[5, 7] = math.nan
     out = ops().linear4_apply(w.handle, x, base=b)
     assert torch.isnan(out[5, 7]) and torch.isnan(out).sum() == 1
+
+
+@pytest.mark.parametrize("rows,ni,no,group", [(1, 640, 300, 128), (9, 328, 90, 64), (16, 296, 64, 40), (2, 21, 30, 8), (20, 384, 11008, 128), (64, 640, 17000, 128),
+                                              (64, 2112, 5000, 64), (40, 1320, 16400, 40), (70, 1290, 9001, 32)])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_columns_whose_scales_are_not_finite_keep_to_themselves(rows, ni, no, group, dtype):
+    w = Weights(ni, no, group, dtype, True, 6)
+    x = torch.randn(rows, ni, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(dtype)
+    clean = ops().linear4_apply(w.handle, x)
+    scales = w.m.mem[w.scales_off:][:2 * no * w.groups].view(dtype).view(no, w.groups)
+    assert torch.equal(scales, w.scales)
+    wild = torch.arange(4, no, 5, device="cuda")                              # (the rows before and behind them are not)
+    scales[wild, 0], scales[wild[::2], 0] = math.inf, math.nan
+    out = ops().linear4_apply(w.handle, x)
+    fine = torch.ones(no, dtype=torch.bool, device="cuda")
+    fine[wild] = False
+    assert torch.equal(out[:, fine], clean[:, fine])
+    assert not torch.isfinite(out[:, wild]).any()
 
 
 def test_no_rows_have_no_products():
