@@ -4,7 +4,13 @@
 // instructions for two codes: put into the low places of a number's mantissa it is that number plus the code, 128 + code in bfloat16, 64 + code in float16,
 // exactly. What is too much is taken away behind the products, for a group of elements at once, with the zero:
 //   sum of x (code - zero) = sum of x (128 + code) - (128 + zero) sum of x,
-// where the sums of x are a product with ones. So nothing is rounded but sums, in 32 bits, and the scale is applied to a group's sum.
+// where the sums of x are a product with ones. So nothing is rounded but sums, in 32 bits, and the scale is applied to a group's sum. An infinite or NaN
+// element of x makes its row of the result NaN or infinite, as does a scale its column.
+//
+// Every weight is read once for 64 rows of x. Up to 16 rows the codes' way from memory is the bound: 8192 to 32768 takes 32 us with one row (4.4 TB/s of the
+// 5.2 that a long read reaches) and 38 with 16 (3.7); with 64 rows, 65 us, it is what a wavefront does with a code - one of two instructions, one of 32
+// in products and sums - beside loads that only half overlap with it: without the products the same kernel takes 40 us, without the loads 45 to 48. Small
+// projections are bound by a launch and by two ways to memory, one after the other - scales and codes, then sums -: 5.3 us for one row of 4096 to 4096.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"
@@ -250,10 +256,13 @@ __device__ inline void write8(const ft_linear4_call &c, uint32_t row, uint32_t n
 }
 
 // 16 rows of weights to a workgroup, and 16 rows of x, 2 XL of which there are. Its wavefronts have every KW-th 256 elements and add up what they
-// have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces, and turns it round in shared memory of
-// its own.
+// have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces - 128 bytes of eight rows of weights to an
+// instruction; as the matrix instruction has them, four pieces of 16 bytes from each of 16 rows, the loads are bound by their addresses -, and turns it
+// round in shared memory of its own, without a barrier. There are 16 rows to a workgroup, not more, so that small projections have workgroups for all
+// compute units: 256 of eight wavefronts for 4096 rows.
 template <class T, int SG, int XL, int KW>
-__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1 ? 4 : SG != 0 ? 6 : 5))) void ft_linear4_narrow_kernel(Linear4View w, ft_linear4_call c) {
+__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1 ? 4 : SG != 0 ? 6 : 5))) void ft_linear4_narrow_kernel(Linear4View w,
+                                                                                                                                   ft_linear4_call c) {
   constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
@@ -355,8 +364,12 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
   static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum + T::to_float(base));
 }
 
-// 128 rows of weights to a workgroup - 32 to a wavefront, and two wavefronts take turns along the rows -, and 16 TT rows of x, which all wavefronts
-// multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied.
+// 32 NW rows of weights to a workgroup - 32 to a wavefront, and two wavefronts take turns along the rows -, and 16 TT rows of x, which all wavefronts
+// multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied. A row of x is read by as many
+// workgroups as there are tiles along the weights: with 128 rows of weights and 64 of x that is 32 KB beside 16 KB of codes for every 256 elements, out
+// of the second-level cache. Registers, about 240, allow two wavefronts to a SIMD; what they leave alone waits for each other at the one barrier
+// of a chunk. Not faster: sums of x by one wavefront for all (65 us as before), pieces of 128 bytes of a row to an instruction, x put down while the chunk
+// before is multiplied, chunks in another order for every workgroup.
 struct Wide {
   Linear4View w;
   ft_linear4_call c;
@@ -548,7 +561,8 @@ __global__ __launch_bounds__(256) void ft_linear4_join_kernel(ft_linear4_call c,
   write8<T>(c, row, n, width - n, sums);
 }
 
-// A wavefront to an output column, eight rows at a time; any widths, groups and alignment.
+// What the others do not take: groups below 32 elements, more than 1024 of them to a row, matrices of fewer than 16 scales, rows of x whose offsets 32 bits do
+// not hold. A wavefront to an output column, eight rows at a time, a byte of codes to a lane: 129 us for 16 rows of 4096 to 4096, where the others take 7.
 template <class T>
 __global__ __launch_bounds__(256) void ft_linear4_any_kernel(Linear4View w, ft_linear4_call c) {
   const uint32_t lane = threadIdx.x & 63, n = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -609,10 +623,15 @@ Plan plan_of(uint32_t width_in, uint32_t width_out, uint32_t group, uint32_t row
   p.any = group < 32 || groups > kMostGroups || width_in < 32 || width_out * groups < 16;  // (loads are of 16 bytes)
   p.narrow = narrow_is_faster(width_in, width_out, rows);
   if (p.any || p.narrow) return p;
+  // As few tiles of x as its rows need: 16 rows of 8192 to 32768 37 us with one, 45 with two and 58 with four. With four of them 128 rows of weights to a
+  // workgroup, else 64: 64 rows 64 us and 93 with 64 rows of weights, 32 rows 51 and 48, 16 rows 45 and 37.
   p.tiles = rows > 32 ? 4 : rows > 16 ? 2 : 1;
   p.waves = p.tiles == 4 ? 4 : 2;
   const uint32_t chunks = (width_in + 255) / 256;
   const uint64_t workgroups = (uint64_t)((width_out + 32 * p.waves - 1) / (32 * p.waves)) * ((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+  // Work along the rows is shared out until every compute unit has a workgroup, or two of the smaller ones: registers have room for no more. With as many
+  // workgroups, with twice and four times as many as compute units: 64 rows of 8192 to 8192 25.5 us, 35 and 35 (46 without sharing), 32 rows 22, 20 and 26, 16
+  // rows of 8192 to 16384 27, 23 and 29. (Four chunks at least; with two or eight the times are the same.)
   uint64_t parts = ((p.tiles == 4 ? 1 : 2) * cu_count) / workgroups;
   const uint32_t most = chunks / 4;
   if (parts > most) parts = most;

@@ -334,6 +334,7 @@ int ft_linear4_apply(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *cal
     if (c.x_stride < w->width_in || c.out_stride < w->width_out || (c.base != nullptr && c.base_stride < w->width_out)) return FT_EINVAL;
     if (!good_strides({c.x_stride, c.out_stride, c.base_stride})) return FT_EINVAL;
     if (c.out == c.base && c.out_stride != c.base_stride && c.rows > 1) return FT_EINVAL;  // a row's result would be another's base
+    if (c.out == c.x) return FT_EINVAL;  // an element's result would lie where others are still to be read for
   }
   std::lock_guard<std::mutex> lock(p->mu);
   Linear4View view;

@@ -1,5 +1,5 @@
-// Launchers of the operators on pool memory (ft_kv.hip, ft_tree.hip, ft_adapters.hip), private to the library. Their callers
-// (ft_operators.cpp) have checked the arguments.
+// Launchers of the operators on pool memory (ft_kv.hip, ft_tree.hip, ft_adapters.hip, ft_linear4.hip, ft_rotate.hip, ft_verify.hip), private to the
+// library. Their callers (ft_operators.cpp) have checked the arguments.
 #pragma once
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>

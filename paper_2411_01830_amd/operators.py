@@ -303,6 +303,8 @@ class Rotation:
         pairs = len(freqs)
         if 2 * pairs > dim:
             _refuse(f"{pairs} pairs are more than a head of {dim} elements has")
+        if isinstance(freqs, torch.Tensor) and freqs.requires_grad:
+            _refuse("freqs asks for a gradient, which a rotation does not give")
         self.axis, self.axes = None, 1
         if axes is not None:
             axes = [int(a) for a in axes]

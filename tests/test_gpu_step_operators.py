@@ -204,6 +204,9 @@ ROTATE = [
     (40, 7, 7, 64, 0, 1, False, True, True, 10, 0), (11, 3, 1, 64, 30, 1, False, True, False, 5000, 0), (129, 8, 2, 128, 96, 3, False, True, True, 60000, 0),
     (4099, 4, 1, 128, 128, 1, False, True, True, 32768, 0), (513, 16, 16, 80, 40, 2, True, True, True, 2000, 8), (21, 5, 5, 24, 24, 1, False, True, True, 99, 0),
     (6, 40, 8, 128, 128, 1, True, False, False, 1 << 24, 0), (260, 3, 2, 40, 16, 1, True, True, False, 300, 0),
+    # fewer pairs than eight, and several tokens to a workgroup
+    (30, 4, 2, 256, 14, 2, False, True, True, 8000, 1), (9, 2, 1, 64, 2, 1, False, False, False, 1 << 20, 0), (5000, 1, 1, 64, 64, 1, False, True, True, 9000, 0),
+    (2061, 3, 2, 256, 256, 2, False, True, False, 40000, 0), (6001, 2, 0, 48, 40, 1, False, True, True, 6001, 3),
 ]
 
 

@@ -92,7 +92,8 @@ def test_weights_without_zeros_need_none(pool):
 
 
 @pytest.mark.parametrize("other", [dict(x=None), dict(out=None), dict(x=BASE + 1), dict(base=BASE + 1), dict(out=BASE + 1), dict(x_stride=511), dict(base_stride=499),
-                                   dict(out_stride=499), dict(x_stride=1 << 40), dict(rows=1 << 20), dict(out=BASE, base=BASE, out_stride=501)], ids=str)
+                                   dict(out_stride=499), dict(x_stride=1 << 40), dict(rows=1 << 20), dict(out=BASE, base=BASE, out_stride=501),
+                                   dict(out=BASE), dict(out=BASE, base=None, rows=1)], ids=str)
 def test_products_that_are_refused(pool, other):
     assert code(ft.linear4_apply, pool, linear(pool), linear_call(**other)) == EINVAL
 
@@ -158,6 +159,7 @@ def test_tensors_that_are_refused(pool):
     assert code(ops.Rotation, pool, [1.0] * 4, 128, [0, 1, 2]) == EINVAL
     assert code(ops.Rotation, pool, [1.0] * 4, 128, [0, 1, 2, 256]) == EINVAL
     assert code(ops.Rotation, pool, [1.0] * 4, 128, [0, 1, 2, -1]) == EINVAL
+    assert code(ops.Rotation, pool, torch.ones(4, requires_grad=True), 128) == EINVAL
     i = torch.zeros(4, dtype=torch.int32)
     p = torch.zeros(4, 10)
     assert code(ops.tree_verify, pool, i.long(), i[:2], 4, p, p[:, 0], p[:1, 0]) == EINVAL
