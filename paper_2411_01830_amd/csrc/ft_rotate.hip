@@ -108,8 +108,8 @@ __device__ inline void write(uint16_t *p, const Eight &e, uint32_t skip) {
 }
 
 // LP lanes to a head, each two runs of eight elements. Pairs of halves: the runs of a lane are the two sides of its pairs; the last one begins
-// earlier than where the one before it ends if the pairs are not a multiple of eight, and skips what that one has. So do the last ones of what is not
-// turned. Pairs of neighbours: a run has four of them.
+// earlier than where the one before it ends if the pairs are not a multiple of eight, and does not count what that one has; both write it, the
+// same. So do the last ones of what is not turned, where that is eight elements or more. Pairs of neighbours: a run has four of them.
 template <class T, int LP, bool NEIGHBOURS, bool NORM>
 __global__ __launch_bounds__(256) void ft_rotate_kernel(ft_rotate_call r, Divisor by_heads, Divisor by_pairs, uint32_t most_tokens) {
   __shared__ float cosine[kMostPairs], sine[kMostPairs];
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void ft_rotate_kernel(ft_rotate_call r, Diviso
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      if (there[j]) write<T>(out + begin[j], x[j], skip[j]);
+      if (there[j]) write<T>(out + begin[j], x[j], NEIGHBOURS || turned || rest >= 8 ? 0 : skip[j]);
   }
 }
 
