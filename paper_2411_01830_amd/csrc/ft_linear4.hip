@@ -10,7 +10,7 @@
 // Every weight is read once for 64 rows of x. Up to 16 rows the codes' way from memory is the bound: 8192 to 32768 takes 32 us with one row (4.4 TB/s of the
 // 5.2 that a long read reaches) and 38 with 16 (3.7); with 64 rows, 65 us, it is what a wavefront does with a code - one of two instructions, one of 32
 // in products and sums - beside loads that only half overlap with it: without the products the same kernel takes 40 us, without the loads 45 to 48. Small
-// projections are bound by a launch and by two ways to memory, one after the other - scales and codes, then sums -: 5.3 us for one row of 4096 to 4096.
+// projections are bound by a launch and by one way to memory behind which come products, sums and the way back: 5.2 us for one row of 4096 to 4096.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"
@@ -195,6 +195,12 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
   }
 }
 
+// An offset that stays 32 bits: widened ahead of a loop it would take two registers in it, and an addition for each load.
+__device__ inline uint32_t here32(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // A barrier for shared memory alone: loads from global memory stay on their way.
 __device__ inline void fence() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -259,11 +265,11 @@ __device__ inline void write8(const ft_linear4_call &c, uint32_t row, uint32_t n
 // have at the end. A wavefront brings what it multiplies by itself, neighbouring lanes neighbouring pieces - 128 bytes of eight rows of weights to an
 // instruction; as the matrix instruction has them, four pieces of 16 bytes from each of 16 rows, the loads are bound by their addresses -, and turns it
 // round in shared memory of its own, without a barrier. There are 16 rows to a workgroup, not more, so that small projections have workgroups for all
-// compute units: 256 of eight wavefronts for 4096 rows.
+// compute units: 256 of eight wavefronts for 4096 rows. All loads up to the first product leave together: 16 rows of 4096 to 4096 take 6.3 us, one 5.2.
 template <class T, int SG, int XL, int KW>
 __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1 ? 4 : SG != 0 ? 6 : 5))) void ft_linear4_narrow_kernel(Linear4View w,
                                                                                                                                    ft_linear4_call c) {
-  constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;
+  constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;  // (pieces on their way; of 8 rows with two: 4096 to 14336 15.5 us instead of 14.0)
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
   extern __shared__ char scales_lds[];
@@ -290,26 +296,26 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
   // of the result a thread has one element at most
   const uint32_t row = t0 + 4 * (lane / 16) + wave % 4, n = n0 + col;
   const bool mine = wave < 4 && row < c.rows && n < w.width_out;
-  uint16_t base = 0;
-  if (mine && c.base != nullptr) base = static_cast<const uint16_t *>(c.base)[row * c.base_stride + n];
+  const bool based = mine && c.base != nullptr;
+  const uint16_t base = *(based ? static_cast<const uint16_t *>(c.base) + row * c.base_stride + n : w.scales);  // (in any case: a branch would wait for it)
   __builtin_amdgcn_sched_barrier(0);
   const Scales<16, 64 * KW> scales(w, w.scales, 2, n0, 0, w.groups, scale_stride(w.groups));
   const Scales<16, 64 * KW> zeros(w, w.zeros != nullptr ? static_cast<const void *>(w.zeros) : w.scales, 1, n0, 0, w.groups, zero_stride(w.groups));
   Words4 codes[kDepth][2], x[kDepth][XL];
-  const auto load = [&](Words4 (&to_codes)[2], Words4 (&to_x)[XL], uint32_t piece) {
+  const auto load = [&](Words4 (&to_codes)[2], Words4 (&to_x)[XL], uint32_t piece, uint32_t some = ~0u) {
     const uint8_t *codes_at = weights + 128 * piece;
     const char *x_at = rows + 512 * piece;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) to_codes[i] = load_codes(codes_at + from[i]);
+    for (int i = 0; i < 2; ++i) to_codes[i] = load_codes(codes_at + here32(from[i] & some));
 #pragma unroll
-    for (int i = 0; i < XL; ++i) to_x[i] = load16(x_at + x_from[i]);
+    for (int i = 0; i < XL; ++i) to_x[i] = load16(x_at + here32(x_from[i] & some));
   };
-  if (wave < pieces)
+  // (in any case, whether this wavefront has a piece or not: behind loads that are on their way in one case only, all would be waited for)
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i) {
-      load(codes[i], x[i], wave + i * KW < pieces ? wave + i * KW : pieces - 1);
-      __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
-    }
+  for (int i = 0; i < kDepth; ++i) {
+    load(codes[i], x[i], (wave + i * KW < pieces ? wave + i * KW : pieces - 1) & (pieces != 0 ? ~0u : 0), pieces != 0 ? ~0u : 0);
+    __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
+  }
   scales.bring(w, scales_lds);
   if (w.zeros != nullptr) zeros.bring(w, zeros_lds);
   __syncthreads();
@@ -361,15 +367,16 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
   float sum = 0;
 #pragma unroll
   for (int k = 0; k < KW; ++k) sum += parts[k][wave][lane];
-  static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum + T::to_float(base));
+  static_cast<uint16_t *>(c.out)[row * c.out_stride + n] = T::from_float(sum + (based ? T::to_float(base) : 0));
 }
 
 // 32 NW rows of weights to a workgroup - 32 to a wavefront, and two wavefronts take turns along the rows -, and 16 TT rows of x, which all wavefronts
 // multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied. A row of x is read by as many
 // workgroups as there are tiles along the weights: with 128 rows of weights and 64 of x that is 32 KB beside 16 KB of codes for every 256 elements, out
 // of the second-level cache. Registers, about 240, allow two wavefronts to a SIMD; what they leave alone waits for each other at the one barrier
-// of a chunk. Not faster: sums of x by one wavefront for all (65 us as before), pieces of 128 bytes of a row to an instruction, x put down while the chunk
-// before is multiplied, chunks in another order for every workgroup.
+// of a chunk; matrix and other instructions of the two mostly take turns (2600 cycles a chunk without loads, of 1536 and 1160). Not faster: sums of x by one
+// wavefront for all, products of one tile of x while those of the one before are scaled (65 us either way, and some variants spill), pieces of 128
+// bytes of a row to an instruction, x put down while the chunk before is multiplied, chunks in another order for every workgroup.
 struct Wide {
   Linear4View w;
   ft_linear4_call c;
@@ -391,30 +398,32 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
   const uint8_t *weights = w.weights + (uint64_t)n0 * w.row_bytes;
   const char *rows = reinterpret_cast<const char *>(static_cast<const uint16_t *>(given.c.x) + t0 * given.c.x_stride);
   uint32_t from[NT], x_from[XP], x_to[XP];
+  const uint32_t piece = 64 * kw + 16 * (lane % 4), x_piece = 16 * (threadIdx.x % 32);
 #pragma unroll
   for (uint32_t i = 0; i < NT; ++i) {
     const uint32_t r = 32 * nw + 16 * i + lane / 4;
-    from[i] = (n0 + r < w.width_out ? r : w.width_out - 1 - n0) * w.row_bytes;
+    from[i] = (n0 + r < w.width_out ? r : w.width_out - 1 - n0) * w.row_bytes + piece;
   }
-  const uint32_t to = lane / 4 * 4 + (lane % 4 ^ lane / 16), piece = 64 * kw + 16 * (lane % 4), x_piece = 16 * (threadIdx.x % 32);
+  const uint32_t to = lane / 4 * 4 + (lane % 4 ^ lane / 16);
 #pragma unroll
   for (uint32_t i = 0; i < XP; ++i) {
     const uint32_t r = 4 * NW * i + threadIdx.x / 32;
-    x_from[i] = (t0 + r < given.c.rows ? r : given.c.rows - 1 - t0) * (2 * (uint32_t)given.c.x_stride);
+    x_from[i] = (t0 + r < given.c.rows ? r : given.c.rows - 1 - t0) * (2 * (uint32_t)given.c.x_stride) + x_piece;
     x_to[i] = r * 32 + (threadIdx.x % 32 ^ r % 16);
   }
   const uint32_t whole = w.width_in / 256;  // and a part
   struct Chunk {
     Words4 codes[NT], x[XP];
   };
-  const auto load = [&](Chunk &f, uint32_t chunk, uint32_t end) {
-    if (chunk >= end) chunk = end - 1;
+  // (`all`: 0 where there is no whole chunk, and what is read is not used)
+  const auto load = [&](Chunk &f, uint32_t chunk, uint32_t end, uint32_t all = ~0u) {
+    if (chunk >= end) chunk = (end - 1) & all;
     const uint8_t *codes_at = weights + 128 * chunk;
     const char *x_at = rows + 512 * chunk;
 #pragma unroll
-    for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_codes(codes_at + (from[i] + piece));
+    for (uint32_t i = 0; i < NT; ++i) f.codes[i] = load_codes(codes_at + here32(from[i] & all));
 #pragma unroll
-    for (uint32_t i = 0; i < XP; ++i) f.x[i] = load16(x_at + (x_from[i] + x_piece));
+    for (uint32_t i = 0; i < XP; ++i) f.x[i] = load16(x_at + here32(x_from[i] & all));
   };
   Floats4 acc[NT][TT];
 #pragma unroll
@@ -444,7 +453,8 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
           return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + (r + 16 * i) * scale_stride(kGroups) + 2 * (there(group) - g0)));
         },
         [&](int i, uint32_t group) {
-          return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[(r + 16 * i) * zero_stride(kGroups) + (there(group) - g0)];
+          const float zero = (float)(uint8_t)zeros_lds[(r + 16 * i) * zero_stride(kGroups) + (there(group) - g0)];
+          return w.zeros == nullptr ? 8.0f : zero;  // (read in any case, without a branch)
         },
         acc);
   };
@@ -458,33 +468,35 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
     {
       const Scales<kRows, 128 * NW> scales(w, w.scales, 2, n0, g0, kGroups, scale_stride(kGroups));
       const Scales<kRows, 128 * NW> zeros(w, w.zeros != nullptr ? static_cast<const void *>(w.zeros) : w.scales, 1, n0, g0, kGroups, zero_stride(kGroups));
-      if (begin < end)
+      // (in any case: behind loads that are on their way in one case only, all would be waited for)
 #pragma unroll
-        for (uint32_t i = 0; i < kDepth; ++i) {
-          load(f[i], begin + i, end);
-          __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
-        }
+      for (uint32_t i = 0; i < kDepth; ++i) {
+        load(f[i], begin + i, end, whole != 0 ? ~0u : 0);
+        __builtin_amdgcn_sched_barrier(0);  // (asked for in another order they would have to be waited for together)
+      }
       scales.bring(w, scales_lds);
       if (w.zeros != nullptr) zeros.bring(w, zeros_lds);
     }
-    // (Out of the loop from within: a way back to its top that leaves out the last loads would be waited for there as if they were not on their way.)
-    for (uint32_t chunk = begin;;) {
+    uint32_t chunk = begin;
+    for (; chunk + kDepth <= end; chunk += kDepth) {
 #pragma unroll
-      for (uint32_t i = 0; i < kDepth; ++i, ++chunk) {
-        if (chunk >= end) goto done;
-        put(f[i], chunk);
-        load(f[i], chunk + kDepth, end);
-        use(chunk);
+      for (uint32_t i = 0; i < kDepth; ++i) {
+        put(f[i], chunk + i);
+        load(f[i], chunk + i + kDepth, end);
+        use(chunk + i);
       }
     }
-  done:
-    if (here > whole) {
+    // one more that is there, and a part
+#pragma unroll 1
+    for (; chunk < here; ++chunk) {
+      if (chunk == whole) {
 #pragma unroll
-      for (uint32_t i = 0; i < NT; ++i) f[0].codes[i] = load_upto(weights + from[i], 128 * whole + piece, w.row_bytes);
+        for (uint32_t i = 0; i < NT; ++i) f[0].codes[i] = load_upto(weights + (from[i] - piece), 128 * whole + piece, w.row_bytes);
 #pragma unroll
-      for (uint32_t i = 0; i < XP; ++i) f[0].x[i] = load_upto(rows + x_from[i], 512 * whole + x_piece, 2 * w.width_in);
-      put(f[0], whole);
-      use(whole);
+        for (uint32_t i = 0; i < XP; ++i) f[0].x[i] = load_upto(rows + (x_from[i] - x_piece), 512 * whole + x_piece, 2 * w.width_in);
+      }
+      put(f[0], chunk);
+      use(chunk);
     }
   }
   // The two halves of the sums, and then whole rows of the result: 8 elements to a thread.
