@@ -1,6 +1,6 @@
 """The operators on memory of the pool, on PyTorch tensors.
 
-A key/value cache and low-rank adapters lie in allocations of a pool (`binding.pool_create`, `binding.slab_alloc`), where
+A key/value cache, low-rank adapters and weights of 4 bits lie in allocations of a pool (`binding.pool_create`, `binding.slab_alloc`), where
 transfers bring and move them; everything else is the caller's tensors. Each call checks what it is given, allocates
 its results and its workspace through PyTorch, and queues its kernels on the current stream of the pool's GPU, where all tensors have to lie. What is wrong with the
 arguments raises `binding.FtError` with the library's code, before anything is launched. The operators serve and do not train: inputs
@@ -9,8 +9,10 @@ that ask for a gradient are refused, as results would not lead back to them.
 One step of a server:
 
     groups = adapter_groups(adapters, ids)                            # once a step
-    qkv = adapters_apply(adapters, groups, x, x @ w.t())              # beside every projection
+    qkv = adapters_apply(adapters, groups, x, linear4_apply(w, x))    # beside every projection
+    q, k = rotate_heads(rotation, q, k, positions, q_weight, k_weight, eps)
     out = tree_attention(cache, q, k, v, starts, lens, table, drafts, mask)
+    keep, last, token = tree_verify(pool, drafted, starts, drafts, target, accept, pick, draft)       # behind the last layer
     slots, lens, state = kv_grow(pool, lens, starts, tokens, table, free, state, page_tokens, keep)   # keep: what was accepted
     kv_append(cache, k, v, slots)                                     # in every layer
 """
