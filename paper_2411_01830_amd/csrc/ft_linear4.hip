@@ -374,9 +374,11 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
 // multiply and bring to shared memory together, 256 elements at a time, the next ones while these are multiplied. A row of x is read by as many
 // workgroups as there are tiles along the weights: with 128 rows of weights and 64 of x that is 32 KB beside 16 KB of codes for every 256 elements, out
 // of the second-level cache. Registers, about 240, allow two wavefronts to a SIMD; what they leave alone waits for each other at the one barrier
-// of a chunk; matrix and other instructions of the two mostly take turns (2600 cycles a chunk without loads, of 1536 and 1160). Not faster: sums of x by one
-// wavefront for all, products of one tile of x while those of the one before are scaled (65 us either way, and some variants spill), pieces of 128
-// bytes of a row to an instruction, x put down while the chunk before is multiplied, chunks in another order for every workgroup.
+// of a chunk, and what they do adds up: of 65 us for 64 rows of 8192 to 32768, 44 are products, 8 putting down and 13 loads, 4000 cycles a chunk of which
+// matrix instructions have 1536 and others 1160. Not faster, all within 2 us of it: sums of x by one wavefront for all, what the zeros take off by one
+// more product at the end (a fifth fewer instructions), products of one tile of x while those of the one before are scaled, reads of shared
+// memory a step ahead, half of the wavefronts putting down before they multiply and half behind, one chunk on its way instead of two, pieces of 128
+// bytes of a row to an instruction, chunks in another order for every workgroup.
 struct Wide {
   Linear4View w;
   ft_linear4_call c;
