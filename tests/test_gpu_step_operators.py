@@ -100,6 +100,11 @@ LINEAR = [
     (16, 32768, 20, 32, True, True, 0), (3, 32776, 20, 32, True, False, 1), (2, 33000, 40, 32, False, False, 0), (24, 5000, 3001, 40, True, True, 1),
     (48, 4100, 2500, 96, True, False, 0), (64, 8192, 1111, 64, True, True, 0), (40, 2304, 5000, 32, False, True, 2), (12, 2100, 20001, 64, True, True, 1),
     (130, 3333, 700, 128, True, True, 3), (17, 513, 16400, 136, True, False, 0),
+    # large enough for tiles that share rows of x: of 16, 32 and 64 rows, groups of every kind, work along the rows shared out or not, rows that end anywhere
+    (16, 8192, 8200, 128, False, True, 0), (9, 6000, 8000, 64, True, False, 1), (16, 5000, 9001, 48, True, True, 2), (32, 8200, 2600, 128, True, False, 1),
+    (17, 5000, 5003, 64, True, True, 0), (20, 4400, 5100, 72, True, False, 5), (64, 8192, 2000, 128, True, True, 0), (64, 4100, 3001, 64, True, False, 1),
+    (50, 3000, 4999, 40, True, True, 3), (33, 2500, 6000, 32, False, False, 0), (64, 300, 40000, 256, True, False, 0), (64, 200, 60000, 128, True, True, 0),
+    (300, 1024, 4096, 512, True, True, 0), (48, 20000, 2100, 1024, True, False, 0), (41, 12345, 2000, 384, True, True, 1),
 ]
 
 
@@ -561,6 +566,45 @@ def test_calls_of_a_step_in_a_graph_and_on_another_stream():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(captured, step()))
         judge(w.m, starts, 8, parent, target, draft, tokens, accept, pick)
+
+
+def test_calls_with_workspaces_in_two_graphs_at_once():
+    """Products shared out along the rows and sums by many workgroups, both with workspaces: two captured steps replayed on two streams together."""
+    w = Weights(4096, 4000, 64, FP16, True, 14)
+    rng = random.Random(14)
+
+    class Step:
+        def __init__(self, seed, stream):
+            self.gen, self.stream = torch.Generator(device="cuda").manual_seed(seed), stream
+            starts, rows, parent, self.target, self.draft, self.tokens, self.accept, self.pick = drafted(rng, self.gen, [9, 1, 12, 18], 40001, True, True, BF16)
+            self.starts, self.parent, self.rows = gpu(starts), gpu(parent), rows
+            self.x = torch.randn(rows, 4096, device="cuda", generator=self.gen).to(FP16)
+
+        def run(self):
+            return (ops().linear4_apply(w.handle, self.x), *ops().tree_verify(w.m.pool, self.tokens, self.starts, 18, self.target, self.accept, self.pick,
+                                                                             draft=self.draft, parent=self.parent))
+
+    steps = [Step(1, torch.cuda.Stream()), Step(2, torch.cuda.Stream())]
+    for s in steps:
+        assert s.rows == 40
+        s.run()
+        torch.cuda.synchronize()
+        s.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(s.graph):
+            s.out = s.run()
+    for _ in range(4):
+        for s in steps:
+            s.x.copy_(torch.randn(s.rows, 4096, device="cuda", generator=s.gen))
+            s.accept.copy_(torch.rand(s.rows, device="cuda", generator=s.gen))
+        torch.cuda.synchronize()
+        for s in steps:
+            with torch.cuda.stream(s.stream):
+                s.graph.replay()
+        torch.cuda.synchronize()
+        for s in steps:
+            assert all(torch.equal(a, b) for a, b in zip(s.out, s.run()))
+    want, bound = w.product(steps[0].x)
+    within(steps[0].out[0], want, bound)
 
 
 def test_tensors_that_ask_for_gradients_or_lie_elsewhere_are_refused():
