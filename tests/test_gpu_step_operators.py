@@ -387,7 +387,7 @@ VERIFY = [
     # requests, rows of a request up to, vocabulary, tree
     (1, 1, 1, False), (1, 1, 5000, False), (1, 5, 32768, False), (3, 4, 2, True), (40, 8, 7, True), (17, 12, 1023, True), (17, 12, 1024, False), (9, 6, 1025, True),
     (64, 8, 2048, False), (5, 70, 3001, True), (2, 200, 515, True), (300, 5, 100, True), (6, 9, 70001, True), (2, 3, 262144, False), (1, 1024, 40, True),
-    (1, 16, 131072, True), (3, 0, 64, True), (30, 3, 33000, True),
+    (1, 16, 131072, True), (3, 0, 64, True), (30, 3, 33000, True), (85, 2, 32769, True), (90, 3, 34000, False),
 ]
 
 
