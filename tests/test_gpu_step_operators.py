@@ -105,6 +105,8 @@ LINEAR = [
     (17, 5000, 5003, 64, True, True, 0), (20, 4400, 5100, 72, True, False, 5), (64, 8192, 2000, 128, True, True, 0), (64, 4100, 3001, 64, True, False, 1),
     (50, 3000, 4999, 40, True, True, 3), (33, 2500, 6000, 32, False, False, 0), (64, 300, 40000, 256, True, False, 0), (64, 200, 60000, 128, True, True, 0),
     (300, 1024, 4096, 512, True, True, 0), (48, 20000, 2100, 1024, True, False, 0), (41, 12345, 2000, 384, True, True, 1),
+    (64, 1100, 32000, 128, True, True, 1), (50, 1300, 31000, 64, True, False, 0), (33, 1290, 32700, 40, False, True, 3), (128, 14000, 4000, 64, True, True, 0),
+    (256, 4096, 4000, 128, True, False, 0), (70, 1000, 4100, 256, False, False, 2),
 ]
 
 
