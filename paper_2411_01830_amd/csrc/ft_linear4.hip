@@ -325,10 +325,12 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
   const auto scale = [&](int, uint32_t group) { return T::to_float(*reinterpret_cast<const uint16_t *>(scales_lds + col * scale_stride(w.groups) + 2 * there(group))); };
   const auto zero = [&](int, uint32_t group) { return w.zeros == nullptr ? 8.0f : (float)(uint8_t)zeros_lds[col * zero_stride(w.groups) + there(group)]; };
   const auto put = [&](const Words4 (&my_codes)[2], const Words4 (&my_x)[XL]) {
+    wave_fence();  // other lanes have read what was there
 #pragma unroll
     for (int i = 0; i < 2; ++i) codes_lds[wave][to[i]] = my_codes[i];
 #pragma unroll
     for (int i = 0; i < XL; ++i) x_lds[wave][x_to[i]] = in_order(my_x[i]);
+    wave_fence();
   };
   const auto use = [&](uint32_t piece) {
     const uint32_t x_row = col & (R - 1);
@@ -435,6 +437,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
   uint32_t g0 = 0;
   const uint32_t part = w.group.d / 4;  // chunks whose scales are in shared memory together: of 64 groups and parts of two more
   const auto put = [&](const Chunk &f, uint32_t chunk) {
+    wave_fence();  // other lanes have read the codes that were there
 #pragma unroll
     for (uint32_t i = 0; i < XP; ++i) x_lds[chunk & 1][x_to[i]] = in_order(f.x[i]);
 #pragma unroll

@@ -22,6 +22,14 @@ __device__ inline Words4 load16(Global p) {
 }
 __device__ inline Words4 load16(const void *p) { return load16(global(p)); }
 
+// Where lanes of one wavefront hand each other words through shared memory: what they read and wrote there before comes before what they do behind it.
+// (No instruction: shared memory takes a wavefront's accesses in their order, and it is the compiler that may not change it. Loads from elsewhere may pass.)
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // mfma(a, b, c) = c + a b for a of 16 x 32 and b of 32 x 16: lane l holds row l % 16 of a and column l % 16 of b, of both the
 // elements 8 (l / 16) .. + 7 of the 32 (any numbering of the 32 will do, if a's and b's are the same), and of the result column l % 16, rows 4 (l / 16) .. + 3.
 struct Bf16 {
