@@ -244,7 +244,7 @@ struct Walk {
       if (one) s.fallen[count + __popcll(all & ((1ull << lane()) - 1))] = (int32_t)token;
       count += __popcll(all);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     return count;
   }
 
@@ -475,8 +475,9 @@ __device__ inline void finish(const ft_verify_call &v, uint32_t r, int32_t first
   if (!(sum > 0)) {  // nothing is left: the target itself
     q = nullptr;
     count = 0;
+    wave_fence();  // (the spare ones may be the sums themselves)
     walk.chunk_sums(walk.target(walk.node), q, 0, 1, walk.chunks(), 0, spare);
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     sums = spare;
     sum = walk.total(sums);
   }

@@ -12,6 +12,7 @@ from paper_2411_01830_amd import build
 # arrays that lanes of a wavefront share without a barrier of the workgroup, by the kernel whose they are
 SHARED = {
     "ft_linear4.hip": {"ft_linear4_narrow_kernel": ["codes_lds", "x_lds"], "ft_linear4_wide_kernel": ["codes_lds"]},
+    "ft_verify.hip": {"ft_verify_kernel": ["chunk"]},
 }
 _cache = {}
 
