@@ -272,7 +272,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(XL != 1
   constexpr int R = 2 * XL, kDepth = XL == 1 ? 2 : 1;  // (pieces on their way; of 8 rows with two: 4096 to 14336 15.5 us instead of 14.0)
   __shared__ Words4 codes_lds[KW][16 * 8], x_lds[KW][R * 32];
   __shared__ float parts[KW][4][64];
-  extern __shared__ char scales_lds[];
+  extern __shared__ __attribute__((aligned(16))) char scales_lds[];
   char *zeros_lds = scales_lds + 16 * scale_stride(w.groups);
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t n0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(128 * NW) __attribute__((amdgpu_waves_per_eu(2))) v
   constexpr uint32_t NT = 2, kGroups = 66, kRows = 32 * NW, XP = TT * 4 / NW;
   constexpr uint32_t kDepth = TT == 4 && SG == 2 ? 1 : 2;  // (chunks that are on their way: what registers hold)
   __shared__ Words4 x_lds[2][TT * 16 * 32], codes_lds[2 * NW][NT][16 * 4];
-  __shared__ char scales_lds[kRows * 4 * (kGroups / 2 | 1)], zeros_lds[kRows * 4 * (kGroups / 4 | 1)];
+  __shared__ __attribute__((aligned(16))) char scales_lds[kRows * 4 * (kGroups / 2 | 1)], zeros_lds[kRows * 4 * (kGroups / 4 | 1)];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % 16;
   const uint32_t kw = wave / NW, nw = wave % NW, n0 = blockIdx.x * kRows, t0 = blockIdx.y * (16 * TT);
   // offsets in bytes from the workgroup's first row: of 128 rows of weights less than 2^30, of 64 rows of x less than 2^31

@@ -96,3 +96,10 @@ def test_lanes_that_share_words_are_kept_in_order(tmp_path_factory, source, kern
             bad = out_of_order(name, blocks, array)
             assert not bad, (name, array, sorted(bad)[:5])
     assert seen >= 3
+
+
+def test_shared_memory_is_aligned_as_it_is_read(tmp_path_factory):
+    """Scales and zeros are bytes to the compiler and are read in words of two and four."""
+    arrays = re.findall(r"^(@\S*(?:scales|zeros)_lds\S*) = .*addrspace\(3\) global .* align (\d+)", code(tmp_path_factory, "ft_linear4.hip"), re.M)
+    assert len(arrays) > 10
+    assert [name for name, align in arrays if int(align) < 16] == []
