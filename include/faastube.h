@@ -883,7 +883,7 @@ typedef struct ft_linear4_call {
  * Products of few rows - the tokens of a step - with weights of 4 bits:
  *   out[t][n] = base[t][n] + sum over k of x[t][k] * scales[n][k / group] * (code[n][k] - zeros[n][k / group])
  * Products are exact, sums 32 bits, the result is rounded once; zeros may be any byte. A group's sum is taken as that of x * (code + 128) less that of
- * x * (zero + 128), and both have to be within 32 bits. Where an element of x is infinite or NaN its row of the result is NaN or infinite, and
+ * x * (zero + 128), and both have to be within 32 bits, as has every weight. Where an element of x is infinite or NaN its row of the result is NaN or infinite, and
  * where a scale is, its column; others are not touched by them. The call reads the weights once for every 64 rows: for hundreds of rows
  * a product with weights that were unpacked before is faster. FT_ERANGE where weights, scales or zeros are not inside one live allocation each.
  */

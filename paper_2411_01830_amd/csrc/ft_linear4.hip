@@ -4,7 +4,8 @@
 // instructions for two codes: put into the low places of a number's mantissa it is that number plus the code, 128 + code in bfloat16, 64 + code in float16,
 // exactly. What is too much is taken away behind the products, for a group of elements at once, with the zero:
 //   sum of x (code - zero) = sum of x (128 + code) - (128 + zero) sum of x,
-// where the sums of x are a product with ones. So nothing is rounded but sums, in 32 bits, and the scale is applied to a group's sum. An infinite or NaN
+// where the sums of x are a product with ones. So nothing is rounded but sums, in 32 bits, and the scale is applied to their difference (to each of them it
+// may be too much for 32 bits where a weight is not). An infinite or NaN
 // element of x makes its row of the result NaN or infinite, as does a scale its column.
 //
 // Every weight is read once for 64 rows of x. Up to 16 rows the codes' way from memory is the bound: 8192 to 32768 takes 32 us with one row (4.4 TB/s of the
@@ -110,14 +111,14 @@ __device__ inline void multiply(const Linear4View &w, Words4 (&codes)[NT], uint3
 #pragma unroll
       for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][tt][j] = __builtin_fmaf(by[i], products[i][tt][j], __builtin_fmaf(more[i], sums[tt][j], acc[i][tt][j]));
+        for (int j = 0; j < 4; ++j) acc[i][tt][j] = __builtin_fmaf(by[i], __builtin_fmaf(more[i], sums[tt][j], products[i][tt][j]), acc[i][tt][j]);
     }
   };
   const auto factors = [&](uint32_t group, float (&by)[NT], float (&more)[NT]) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       by[i] = scale(i, group);
-      more[i] = -by[i] * (Code<T>::kMore + zero(i, group));
+      more[i] = -(Code<T>::kMore + zero(i, group));
     }
   };
   constexpr int G = SG == 0 ? 1 : SG;
