@@ -297,7 +297,7 @@ def linear4_apply(weights, x, base=None, out=None):
 class Rotation:
     """How positions turn the pairs of heads of `dim` elements: freqs are radians a position, one for each of the pairs (elements behind the first
     2 * len(freqs) are not turned); axes names the axis of each pair (None: there is one axis); neighbours: pairs are elements 2i and 2i + 1,
-    without it i and i + len(freqs)."""
+    without it i and i + len(freqs). It keeps copies of both, of the stream that it was made on: another stream's calls wait for it."""
 
     def __init__(self, pool, freqs, dim, axes=None, neighbours=False):
         on = torch.device("cuda", getattr(pool, "device", 0))
@@ -314,7 +314,7 @@ class Rotation:
                 _refuse("axes has a number from 0 to 255 for every pair")
             self.axes = max(axes, default=0) + 1
             self.axis = torch.tensor(axes, dtype=torch.uint8).to(on)
-        self.freqs = torch.as_tensor(freqs, dtype=torch.float32).to(on).contiguous()
+        self.freqs = torch.as_tensor(freqs, dtype=torch.float32).to(on, copy=True).contiguous()  # (its own, whatever becomes of the caller's)
         if self.freqs.dim() != 1:
             _refuse("freqs has one dimension")
         self.rot, self.axis_at = 2 * pairs, 0 if self.axis is None else self.axis.data_ptr()
