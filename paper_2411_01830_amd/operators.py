@@ -66,7 +66,14 @@ def _device(name, t, pool):
     return dev
 
 
+def _tensor(name, t):
+    """Ahead of looking at what a tensor is like."""
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name}: a tensor on the GPU is needed")
+
+
 def _flags(name, t, device, n):
+    _tensor(name, t)
     if t.dtype is not torch.uint8 and t.dtype is not torch.bool:
         _refuse(f"{name} is uint8 or bool")
     _ints(name, t, t.dtype, 1, device)
@@ -159,6 +166,7 @@ def tree_attention(cache, q, k, v, starts, lens, table, drafts, mask=None, scale
         _refuse("starts has one entry more than lens, table a row for each")
     words, mask_at = 0, None
     if mask is not None:
+        _tensor("mask", mask)
         if mask.dtype is not torch.int64 and mask.dtype is not torch.uint64:
             _refuse("mask has words of 64 bits")
         dims = mask.dim()
@@ -333,6 +341,7 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
         _refuse("q has three dimensions of bfloat16 or float16")
     tokens, heads, _ = shape
     _rows("q", q, dtype, (tokens, heads, dim), dev)
+    _tensor("positions", positions)
     at = positions.shape
     _ints("positions", positions, torch.int32, len(at), dev)
     axes = at[1] if len(at) == 2 else 1
@@ -363,6 +372,7 @@ def rotate_heads(rotation, q, k, positions, q_weight=None, k_weight=None, eps=No
     qs, os = q.stride(), q_out.stride()
     k_at, k_to, kv_heads, ks, kos = 0, 0, 0, (0, 0), (0, 0)
     if k is not None:
+        _tensor("k", k)
         given = k.shape
         if len(given) != 3:
             _refuse("k has three dimensions")
@@ -401,6 +411,7 @@ def tree_verify(pool, tokens, starts, drafts, target, accept, pick, draft=None, 
     _ints("pick", pick, torch.float32, 1, dev)
     if accept.shape[0] != rows or pick.shape[0] != requests:
         _refuse("accept has an entry for every row, pick for every request")
+    _tensor("target", target)
     shape, dtype = target.shape, target.dtype
     if len(shape) != 2 or dtype not in PROBABILITIES:
         _refuse("target has two dimensions of bfloat16, float16 or float32")

@@ -40,3 +40,34 @@ def test_a_rotation_keeps_the_frequencies_that_it_was_given(pool, given):
     freqs.zero_()
     assert torch.equal(ops().rotate_heads(rotation, q, None, at)[0], before)
     assert not torch.equal(before, q)
+
+
+@pytest.mark.parametrize("what", [None, 3, [0, 1]], ids=str)
+def test_what_is_no_tensor_is_refused_as_everything_else_is(pool, what):
+    o = ops()
+    dtype = dict(dtype=BF16, device="cuda")
+    rotation = o.Rotation(pool, [1.0] * 4, 8)
+    weights = o.Linear4(pool, ft.slab_alloc(pool, SLAB), ft.slab_alloc(pool, SLAB), 64, 32, 32, BF16)
+    cache = o.KvCache(pool, ft.slab_alloc(pool, SLAB), ft.slab_alloc(pool, SLAB), 2, 4, 1, 64, BF16)
+    x, h, kv = torch.zeros(2, 64, **dtype), torch.zeros(2, 1, 8, **dtype), torch.zeros(2, 1, 64, **dtype)
+    two, one, table, free, state = ints(0, 2), ints(1), ints(0)[None], ints(1, 0), ints(1, 0, 0, 0)
+    t, p, r = ints(0, 1, dtype=torch.int64), torch.ones(2, 5, device="cuda"), torch.zeros(2, device="cuda")
+    calls = {
+        "x": lambda v: o.linear4_apply(weights, v), "base": lambda v: o.linear4_apply(weights, x, base=v), "out": lambda v: o.linear4_apply(weights, x, out=v),
+        "q": lambda v: o.rotate_heads(rotation, v, None, two), "k": lambda v: o.rotate_heads(rotation, h, v, two), "positions": lambda v: o.rotate_heads(rotation, h, None, v),
+        "q_weight": lambda v: o.rotate_heads(rotation, h, None, two, q_weight=v, eps=0.0), "k_weight": lambda v: o.rotate_heads(rotation, h, h, two, k_weight=v, eps=0.0),
+        "q_out": lambda v: o.rotate_heads(rotation, h, None, two, q_out=v), "k_out": lambda v: o.rotate_heads(rotation, h, h, two, k_out=v),
+        "tokens": lambda v: o.tree_verify(pool, v, two, 2, p, r, r[:1]), "starts": lambda v: o.tree_verify(pool, t, v, 2, p, r, r[:1]),
+        "target": lambda v: o.tree_verify(pool, t, two, 2, v, r, r[:1]), "accept": lambda v: o.tree_verify(pool, t, two, 2, p, v, r[:1]),
+        "pick": lambda v: o.tree_verify(pool, t, two, 2, p, r, v), "draft": lambda v: o.tree_verify(pool, t, two, 2, p, r, r[:1], draft=v),
+        "parent": lambda v: o.tree_verify(pool, t, two, 2, p, r, r[:1], parent=v),
+        "keep": lambda v: o.kv_grow(pool, one, two, 2, table, free, state, 4, keep=v), "done": lambda v: o.kv_release(pool, v, one, table, free, state, 4),
+        "mask": lambda v: o.tree_attention(cache, kv, kv, kv, two, one, table, 2, mask=v),
+    }
+    optional = {"base", "out", "k", "q_weight", "k_weight", "q_out", "k_out", "draft", "parent", "keep", "mask"}
+    for name, call in calls.items():
+        if what is None and name in optional:
+            continue
+        with pytest.raises(ft.FtError) as err:
+            call(what)
+        assert err.value.code == -1, name
