@@ -37,8 +37,8 @@ class Server:
         self.requests, self.layers, self.heads, self.kv_heads, self.dim, self.vocab = requests, layers, heads, kv_heads, dim, vocab
         self.hidden, self.page, self.prompt, self.answer, self.dtype, self.check = hidden, page, prompt, answer, dtype, check
         self.rng = np.random.default_rng(seed)
-        gen = torch.Generator(device="cuda").manual_seed(seed)
-        self.random = lambda *shape, by=1.0: (torch.randn(*shape, device="cuda", generator=gen) * by).to(dtype)
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)                       # all chance on the GPU: a run is its seed's
+        self.random = lambda *shape, by=1.0: (torch.randn(*shape, device="cuda", generator=self.gen) * by).to(dtype)
         self.width = (heads + 2 * kv_heads) * dim
         self.embed = self.random(vocab, hidden)
         self.rotate, self.four_bit, self.sample = rotate, four_bit, sample
@@ -164,9 +164,9 @@ class Server:
                 for kind, n in enumerate(self._parts(ni, no)):
                     here = self.engine.host[at:at + n]
                     if kind == 1:                                                 # (codes are 4.6 from their zeros, in the mean of squares)
-                        here.view(self.dtype).copy_((torch.rand(n // 2, device="cuda") + 0.5).to(self.dtype) * (0.2 * ni ** -0.5))
+                        here.view(self.dtype).copy_((torch.rand(n // 2, device="cuda", generator=self.gen) + 0.5).to(self.dtype) * (0.2 * ni ** -0.5))
                     else:
-                        here.copy_(torch.randint(256 if kind == 0 else 16, (n,), dtype=torch.uint8, device="cuda"))
+                        here.copy_(torch.randint(256 if kind == 0 else 16, (n,), dtype=torch.uint8, device="cuda", generator=self.gen))
                     to.append(alloc(n))
                     moves.append((0, at, to[-1], n))
                     at += (n + 255) // 256 * 256
@@ -219,7 +219,7 @@ class Server:
 
     def _draft(self):
         """The tokens of the rows: each request's last one, then what followed it before and one other, level by level."""
-        tokens = torch.randint(self.vocab, (self.rows,), device="cuda")
+        tokens = torch.randint(self.vocab, (self.rows,), device="cuda", generator=self.gen)
         at = self.last
         tokens[self.root] = at
         who = torch.arange(self.requests, device="cuda")
@@ -251,7 +251,7 @@ class Server:
         """Rows that stand against the model's probabilities and random numbers; what was drawn behind them."""
         logits = (x @ self.embed.t()).float()
         target = torch.softmax(logits * (2 / logits.std(-1, keepdim=True)), -1)
-        accept, pick = torch.rand(self.rows, device="cuda"), torch.rand(self.requests, device="cuda")
+        accept, pick = (torch.rand(n, device="cuda", generator=self.gen) for n in (self.rows, self.requests))
         keep, last, token = ops.tree_verify(self.pool, tokens, self.starts, self.drafts, target, accept, pick, parent=self.hangs_from)
         if self.check:
             self._check_judged(tokens, target, accept, pick, keep, last, token)
