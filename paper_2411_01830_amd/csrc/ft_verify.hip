@@ -544,19 +544,30 @@ __global__ __launch_bounds__(1024) void ft_verify_kernel(ft_verify_call v, const
   write_kept<kThreads>(v, s, first, all, n, walk.node);
 }
 
-// Workgroups that a request's first sum is spread over, 0: its own does it, and there is one launch. In two launches and in one, four rows a request
-// with a draft: 1 request over 131072 tokens of float32 6.9 and 12.8 us, 32 requests 11.4 and 18.2, 128 25.5 and 30.0, 256 50 and 48; 32 over 65536 of
-// bfloat16 8.0 and 10.0, 128 13.0 and 11.6; over 32768 of float32 7.0 and 7.3 for 1, 11.8 and 10.0 for 128; over 16384 6.5 and 6.4, 8.9 and 7.6.
-uint32_t slices_of(const ft_verify_call &v, int cu_count) {
-  const uint32_t chunks = (v.vocab + kChunk - 1) / kChunk, most = (chunks + 3) / 4;
-  if (chunks <= 32 || 3 * v.requests > (uint32_t)cu_count) return 0;
-  const uint32_t want = (uint32_t)(4 * cu_count) / v.requests;  // of four wavefronts each
+// Workgroups that a request's first sum is spread over, 0: its own does it, and there is one launch. What spreading saves is a workgroup's way along
+// its rows, what it costs is a launch and, with as many requests as compute units, units that wait for no one: it is done for up to a third as
+// many requests, and for up to five eighths where a request's rows have 1 MiB. In two launches and in one, us, four rows a request:
+//   with a draft     float32   32768 tokens   1:  7.0  7.3   64:  8.4  8.6    85:  9.9  9.2   128: 11.9 10.1
+//                              65536          1:  6.6  9.1   64: 12.0 12.6    85: 13.2 12.9   128: 15.8 14.4
+//                             131072          1:  7.1 12.8   64: 16.3 19.1   128: 25.7 29.4   160: 30.4 31.5   192: 36.8 36.3   256: 48.5 47.0
+//                             262144          1:  8.1 19.9   64: 26.3 46.7   128: 51.5 64.6   160: 67.2 71.8   192: 77.2 79.5   256: 98.4 93.0
+//                   bfloat16  65536          1:  7.1  9.3   64:  9.7 11.1    85: 10.6 11.3   128: 12.8 11.7
+//                             131072          1:  7.2 13.5   64: 13.2 16.1    85: 14.5 16.2   128: 17.7 17.3
+//                             262144          1:  7.7 21.3   64: 18.1 25.2   128: 27.1 29.8   160: 32.4 32.0   192: 39.1 35.8
+//   without          float32  131072          1:  7.4 13.7   64: 14.9 15.7    85: 17.9 15.8   128: 23.6 18.1
+//                             262144          1:  8.6 21.8   64: 20.5 24.4   128: 30.8 33.4   160: 38.3 42.6   192: 43.6 49.2   256: 63.9 61.6
+//                   bfloat16 131072          1:  7.9 14.5   64: 12.0 16.1    85: 14.0 16.2   128: 16.4 16.5
+uint32_t slices_of(const ft_verify_call &v, bool drawn, int cu_count) {
+  const uint32_t chunks = (v.vocab + kChunk - 1) / kChunk, most = (chunks + 3) / 4, units = (uint32_t)cu_count;
+  const uint64_t bytes = (uint64_t)v.vocab * (v.type == FT_FP32 ? 4 : 2) * (drawn ? 2 : 1);
+  if (chunks <= 32 || (bytes < 1u << 20 ? 3 * v.requests > units : 8 * v.requests > 5 * units)) return 0;
+  const uint32_t want = 4 * units / v.requests;  // of four wavefronts each
   return want < most ? want : most;
 }
 
 template <class T>
 void launch(const ft_verify_call &v, int cu_count, hipStream_t stream) {
-  const uint32_t slices = v.requests == 0 || v.rows == 0 ? 0 : slices_of(v, cu_count), chunks = (v.vocab + kChunk - 1) / kChunk;
+  const uint32_t slices = v.requests == 0 || v.rows == 0 ? 0 : slices_of(v, v.draft != nullptr, cu_count), chunks = (v.vocab + kChunk - 1) / kChunk;
   if (slices != 0) {
     const uint32_t each = (chunks + slices - 1) / slices;
     Stop *stops = static_cast<Stop *>(v.workspace);
@@ -571,7 +582,8 @@ void launch(const ft_verify_call &v, int cu_count, hipStream_t stream) {
 }  // namespace
 
 uint64_t verify_workspace(const ft_verify_call &v, int cu_count) {
-  if (v.requests == 0 || v.rows == 0 || slices_of(v, cu_count) == 0) return 0;
+  // (for either kind of call: with a draft it is spread wherever it is without)
+  if (v.requests == 0 || v.rows == 0 || slices_of(v, true, cu_count) == 0) return 0;
   return v.requests * (sizeof(Stop) + (uint64_t)((v.vocab + kChunk - 1) / kChunk) * sizeof(double));
 }
 

@@ -71,3 +71,70 @@ def test_what_is_no_tensor_is_refused_as_everything_else_is(pool, what):
         with pytest.raises(ft.FtError) as err:
             call(what)
         assert err.value.code == -1, name
+
+
+def defined(tokens, counts, target, accept, pick, draft):
+    """Chains judged by the definition, row by row, in 64 bits."""
+    keep, last, after, a = [], [], [], 0
+    for r, n in enumerate(counts):
+        row, left, keep_here = a, None, [1] + [0] * (n - 1)
+        while True:
+            p = target[row].double()
+            left = p
+            if row + 1 == a + n:
+                break
+            c = int(tokens[row + 1])
+            q = draft[row].double() if draft is not None else None
+            if float(accept[row + 1]) * (1.0 if q is None else float(q[c])) < float(p[c]):
+                row += 1
+                keep_here[row - a] = 1
+                continue
+            if q is None:
+                left = p.clone()
+                left[c] = 0
+            else:
+                left = (p - q).clamp(min=0)
+            break
+        left = left if float(left.sum()) > 0 else p
+        sums = left.cumsum(0)
+        after.append(int(torch.nonzero(sums > float(pick[r]) * float(sums[-1]))[0]))
+        keep += keep_here
+        last.append(row)
+        a += n
+    return keep, last, after
+
+
+@pytest.mark.parametrize("requests,vocab,dtype,drawn,spread", [
+    (128, 131072, FP32, True, True), (160, 131072, FP32, True, True), (161, 131072, FP32, True, False), (128, 262144, BF16, True, True), (90, 131072, FP32, False, False),
+    (90, 262144, FP32, False, True), (90, 131071, FP32, True, False), (85, 131071, FP32, True, True), (86, 65536, BF16, False, False),
+], ids=str)
+def test_first_sums_are_spread_where_rows_are_long(pool, requests, vocab, dtype, drawn, spread):
+    """Requests beyond a third of the compute units, on either side of the rule's 1 MiB a request, judged alike in one launch and in two."""
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    if units != 256:
+        pytest.skip("the counts are for 256 compute units")
+    gen = torch.Generator(device="cuda").manual_seed(requests + vocab)
+    counts = [1 + r % 3 for r in range(requests)]
+    starts = [0]
+    for n in counts:
+        starts.append(starts[-1] + n)
+    rows = starts[-1]
+    target, draft = torch.empty(rows, vocab, dtype=dtype, device="cuda"), torch.empty(rows, vocab, dtype=dtype, device="cuda")
+    for a in range(0, rows, 64):
+        logits = 3 * torch.randn(min(64, rows - a), vocab, device="cuda", generator=gen)
+        target[a:a + 64] = torch.softmax(logits, -1)
+        draft[a:a + 64] = torch.softmax(logits + 0.7 * torch.randn(logits.shape, device="cuda", generator=gen), -1)
+    tokens = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    for row in range(1, rows):                             # a row's token was drawn by the row before
+        q = draft[row - 1].float()
+        tokens[row] = (q / torch.empty_like(q).exponential_(generator=gen)).argmax()
+    accept, pick = torch.rand(rows, device="cuda", generator=gen), torch.rand(requests, device="cuda", generator=gen)
+    record = ft.VerifyCall(rows=rows, requests=requests, drafts=3, vocab=vocab, type=2 if dtype is FP32 else 0, draft=draft.data_ptr() if drawn else None,
+                           target_stride=vocab, draft_stride=vocab)
+    # (without a draft the workspace is that of a call with one, which is spread wherever the other is)
+    assert (ft.verify_workspace(pool, record) > 0) == (spread if drawn else requests <= 85 or vocab * target.element_size() * 2 >= 1 << 20)
+    got = ops().tree_verify(pool, tokens, ints(*starts), 3, target, accept, pick, draft=draft if drawn else None)
+    want = defined(tokens, counts, target, accept, pick, draft if drawn else None)
+    assert got[0].tolist() == want[0]
+    assert got[1].tolist() == want[1]
+    assert got[2].tolist() == want[2]
