@@ -884,8 +884,9 @@ typedef struct ft_linear4_call {
  *   out[t][n] = base[t][n] + sum over k of x[t][k] * scales[n][k / group] * (code[n][k] - zeros[n][k / group])
  * Products are exact, sums 32 bits, the result is rounded once; zeros may be any byte. A group's sum is taken as that of x * (code + 128) less that of
  * x * (zero + 128), and both have to be within 32 bits, as has every weight. Where an element of x is infinite or NaN its row of the result is NaN or infinite, and
- * where a scale is, its column; others are not touched by them. The call reads the weights once for every 64 rows: for hundreds of rows
- * a product with weights that were unpacked before is faster. FT_ERANGE where weights, scales or zeros are not inside one live allocation each.
+ * where a scale is, its column; others are not touched by them. The call reads the weights once for every 16 to 64 rows, by what
+ * the sizes make shortest (once for every 8 with groups below 32 elements, more than 1024 of them to a row, or rows of x 2^24 elements and more apart): for
+ * hundreds of rows a product with weights that the caller has unpacked before is faster. FT_ERANGE where weights, scales or zeros are not inside one live allocation each.
  */
 int ft_linear4_apply(ft_pool *p, const ft_linear4 *w, const ft_linear4_call *call, void *hip_stream);
 /* Bytes of workspace that ft_linear4_apply asks for (host only; of the call its number of rows is read). */
@@ -920,8 +921,9 @@ enum {
  *   y = x * rsqrt(mean of x^2 over dim + eps) * weight
  *   (y'[a], y'[b]) = (y[a] cos - y[b] sin, y[a] sin + y[b] cos) of the angle positions[t][axis[i]] * freqs[i] of pair i = (a, b)
  * Elements behind the first `rot` are not turned. Angles are worked out in 64 bits (positions may be negative, and as far
- * as 2^31), all else in 32; the result is rounded once. Rows whose squares 32 bits do not hold become 0, those with
- * infinities or NaN become NaN in part or whole, other rows are not touched by them.
+ * as 2^31), all else in 32; the result is rounded once. Squares are 32 bits too: heads for which those are too large
+ * become 0, and with an eps of 0 heads for which they are too small (elements below about 2^-48) are normed with fewer bits, down to infinities and
+ * NaN where, as of zeros, nothing is left. Heads with infinities or NaN become NaN in part or whole, others are not touched by them.
  */
 int ft_rotate_heads(ft_pool *p, const ft_rotate_call *call, void *hip_stream);
 

@@ -8,9 +8,10 @@
 // may be too much for 32 bits where a weight is not). An infinite or NaN
 // element of x makes its row of the result NaN or infinite, as does a scale its column.
 //
-// Every weight is read once for 64 rows of x. Up to 16 rows the codes' way from memory is the bound: 8192 to 32768 takes 32 us with one row (4.4 TB/s of the
-// 5.2 that a long read reaches) and 38 with 16 (3.7); with 64 rows, 65 us, it is what a wavefront does with a code - one of two instructions, one of 32
-// in products and sums - beside loads that only half overlap with it: without the products the same kernel takes 40 us, without the loads 45 to 48. Small
+// Every weight is read once for 16, 32 or 64 rows of x, by the kernel that the rule in ft_linear4_plan.h takes, or for 8 by the plain one. Up to 16 rows the codes'
+// way from memory is the bound: 8192 to 32768 takes 32 us with one row (4.4 TB/s of the 5.2 that a long read reaches) and 38 with 16 (3.7); with 64 rows, 65 us,
+// it is what a wavefront does with a code - one of two instructions, one of 32 in products and sums - beside loads that only half overlap with it: without
+// the products the same kernel takes 40 us, without the loads 52, without putting them down either 43 to 46. Small
 // projections are bound by a launch and by one way to memory behind which come products, sums and the way back: 5.2 us for one row of 4096 to 4096.
 #include <hip/hip_runtime.h>
 

@@ -8,7 +8,8 @@
 // bfloat16 with a draft, bound by instructions on 64-bit numbers, five for a token; spread over many workgroups it is bound by memory: 64 rows of 131072 tokens
 // of float32 with their draft, 67 MB, take 12 us (5.6 TB/s). So a request's first sum, which most are done with, is spread, in a launch of its own
 // (Stop is what it hands on), and those behind it are its one workgroup's: 64 chains of 4 to 8 take 17 us, 32 trees of 9 to 16 rows, with up to four sums one
-// behind the other, 27. A further launch for each of these would not be shorter: its way down the rows takes 3 to 4 us before its first load.
+// behind the other, 27. A further launch for each of these that gathers and goes down the rows again would not be shorter: that takes 3 to 4 us before its first
+// load. One that is handed where the way stopped, and its siblings' numbers, was not tried.
 #include <hip/hip_runtime.h>
 
 #include "ft_operators.h"

@@ -271,7 +271,8 @@ class Linear4:
 
 
 def linear4_apply(weights, x, base=None, out=None):
-    """base (None: 0) and x's rows times the weights on top; out may be base. For the few rows of a step: weights are read once for 64 of them."""
+    """base (None: 0) and x's rows times the weights on top; out may be base. For the few rows of a step: weights are read once for 16 to 64 of them
+    (for 8 in groups below 32 elements, or more than 1024 of them to a row)."""
     pool, dtype, ni, no = weights.pool, weights.dtype, weights.width_in, weights.width_out
     dev = _device("x", x, pool)
     given = x.shape
