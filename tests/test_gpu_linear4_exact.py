@@ -85,7 +85,7 @@ KINDS = {
     (17, 700, 100, 32): "narrow 16", (33, 600, 200, 64): "narrow 16", (16, 2000, 4096, 128): "narrow 16", (16, 3001, 2001, 64): "narrow 16", (10, 8192, 4096, 32): "narrow 16",
     (16, 9001, 2000, 32): "narrow 16", (16, 9000, 3000, 128): "narrow 16", (9, 7003, 1500, 40): "narrow 16",
     # a tile of 16 rows
-    (16, 1001, 40001, 128): "wide 1 whole 1", (16, 1001, 40001, 64): "wide 1 whole 1", (16, 3001, 40001, 32): "wide 1 whole 2", (33, 1290, 32700, 40): "wide 4 whole 1",
+    (16, 1001, 40001, 128): "wide 1 whole 1", (16, 1001, 40001, 64): "wide 1 whole 1", (16, 3001, 40001, 32): "wide 1 whole 2",
     (64, 4100, 3001, 64): "wide 1 whole 2", (16, 8192, 8200, 128): "wide 1 shared 1", (9, 6000, 8000, 64): "wide 1 shared 1", (16, 20001, 8001, 32): "wide 1 shared 3",
     (41, 12345, 2000, 384): "wide 1 shared 1", (48, 20000, 2100, 1024): "wide 1 shared 1", (3, 32768, 1000, 32): "wide 1 shared 1", (16, 5000, 9001, 48): "wide 1 shared 1",
     # two
@@ -93,6 +93,7 @@ KINDS = {
     (32, 9001, 20001, 64): "wide 2 whole 3", (32, 10001, 20001, 128): "wide 2 whole 2", (32, 8200, 2600, 128): "wide 2 shared 1", (24, 16001, 4000, 64): "wide 2 shared 1",
     (20, 4400, 5100, 72): "wide 2 shared 1", (70, 1000, 4100, 256): "wide 2 whole 1",
     # four
+    (33, 1290, 32700, 40): "wide 4 whole 1",
     (64, 1100, 32000, 128): "wide 4 whole 1", (50, 1300, 31000, 64): "wide 4 whole 1", (64, 8191, 32001, 32): "wide 4 whole 4", (64, 8191, 32001, 64): "wide 4 whole 2",
     (64, 9001, 32000, 128): "wide 4 whole 2", (50, 3001, 32000, 40): "wide 4 whole 2", (100, 20001, 1000, 128): "wide 4 shared 1", (128, 20001, 4001, 64): "wide 4 shared 2",
     (128, 20001, 4000, 32): "wide 4 shared 3", (130, 16001, 4100, 40): "wide 4 shared 4", (64, 200, 60000, 128): "wide 4 whole 1",
